@@ -106,6 +106,89 @@ memspec_status memspec_op_sample(const float* logits_dev, int32_t rows, int32_t 
                                  float temperature, const float* u_dev, int32_t* out_dev,
                                  void* stream);
 
+/* ---- sampling rules -------------------------------------------------------
+ * What a row of logits is cut down to before it is drawn from.  Weights are
+ * w_i = exp((z_i - max z) / T); the row's ids are ordered by descending logit,
+ * equal logits by ascending id; each part keeps a prefix of that order, and the
+ * shortest one counts:
+ *   top_k  the first k ids (0: all)
+ *   top_p  of those, the shortest prefix whose weights sum to at least top_p
+ *          times the sum over them (1: all)
+ *   min_p  the ids with w_i >= min_p (0: all)
+ * temperature 0: the first id of the largest logit alone.
+ * A NaN logit counts as -inf, +inf as the largest finite float; an id at -inf is
+ * never kept.  Sums and their comparisons are exact over weights that are off by
+ * at most 2^-31.8 of themselves (and 2^-44 of the largest): the same input gives the same result
+ * however the work is split.
+ * Each part is one number for all rows, or (pointer not NULL) a device array of
+ * one value per row, which the call cannot check: there a temperature that is
+ * not above 0 (NaN too) is 0, a top_k below 1 and a top_p of 1 or more or NaN
+ * are off, a top_p of 0 or less keeps one id, a min_p that is not above 0 is
+ * off, one above 1 counts as 1. */
+typedef struct memspec_filter {
+  float temperature;            /* >= 0 */
+  int32_t top_k;                /* >= 0 */
+  float top_p;                  /* in (0, 1] */
+  float min_p;                  /* in [0, 1] */
+  const float* temperature_dev; /* [rows] or NULL */
+  const int32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+} memspec_filter;
+
+/* out[r] = the smallest kept id j of row r with sum_{i<=j} w_i > u[r] sum_i w_i
+ * over the kept ids; -1 for a row without any finite logit.  With no part of the
+ * rule on this is memspec_op_sample's draw (but for roundings at a border
+ * between two ids, which here are those of the weights alone).
+ * logits_dev: row r (fp32) starts at logits_dev + r * ld, ld >= vocab; u_dev:
+ * fp32 [rows] in [0, 1).  rows in 1..65535, vocab in 1..131072.  Enqueued on
+ * `stream`; nothing is allocated.  Errors: INVALID_ARG, CUDA. */
+memspec_status memspec_op_sample_filtered(const float* logits_dev, int64_t ld, int32_t rows, int32_t vocab,
+                                          const memspec_filter* filter, const float* u_dev,
+                                          int32_t* out_dev, void* stream);
+
+/* The same cut as a mask: out[r][i] = logits[r][i] where id i is kept (as it
+ * counts: +inf as the largest finite float), else -inf.  out_dev may be
+ * logits_dev (then out_ld == ld); otherwise the two must not overlap.  Columns
+ * past vocab are not written.  Otherwise as memspec_op_sample_filtered. */
+memspec_status memspec_op_filter_logits(const float* logits_dev, int64_t ld, int32_t rows, int32_t vocab,
+                                        const memspec_filter* filter, float* out_dev, int64_t out_ld,
+                                        void* stream);
+
+/* ---- low-rank adapters beside a shared projection --------------------------
+ * The adapters of one projection, stacked: adapter a adds scale[a] * B[a] A[a]
+ * to the projection's weight.  Adapters of smaller rank occupy the first
+ * ranks[a] rows of A[a] and columns of B[a]; the rest is not used. */
+typedef struct memspec_lora {
+  const void* a_dev;          /* bf16 [n_adapters][rank][k] */
+  const void* b_dev;          /* bf16 [n_adapters][n_out][rank] */
+  const float* scales_dev;    /* fp32 [n_adapters], or NULL: 1 */
+  const int32_t* ranks_dev;   /* [n_adapters], clamped to 0..rank, or NULL: rank */
+  int32_t n_adapters;
+  int32_t rank;               /* a multiple of 8 in 8..128 */
+} memspec_lora;
+
+/* Scratch bytes of memspec_op_lora.  Errors: INVALID_ARG. */
+memspec_status memspec_op_lora_scratch_bytes(int32_t rows, int32_t n_out, int32_t k, int32_t rank,
+                                             size_t* bytes);
+
+/* y[r] = base[r] + scale[a] * B[a] (A[a] x[r]) with a = ids[r], the adapter of
+ * row r (ids_dev: int32 [rows]; an id outside 0..n_adapters-1: no adapter,
+ * y[r] = base[r]).  base_dev is typically what memspec_op_linear or
+ * memspec_op_linear_int4 gave for the same x, or NULL for 0; it may be y_dev
+ * (then ld_base == ldy), otherwise the two must not overlap.
+ * x bf16, base and y fp32; rows at strides ldx, ld_base, ldy (elements, at least
+ * a row; ldx a multiple of 8).  rows in 1..256, k a positive multiple of 8, n_out
+ * and k at most 2^24; x, A, B and scratch 16-byte aligned.  Products are of
+ * bf16 values, sums fp32; A x enters the second product with all its 24 bits.
+ * Deterministic.  scratch_dev: memspec_op_lora_scratch_bytes bytes of any
+ * content; calls that may overlap need scratches of their own.
+ * Errors: INVALID_ARG, CUDA. */
+memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x_dev, int64_t ldx,
+                               const int32_t* ids_dev, const float* base_dev, int64_t ld_base,
+                               float* y_dev, int64_t ldy, int32_t rows, int32_t n_out, int32_t k,
+                               void* scratch_dev, size_t scratch_bytes, void* stream);
+
 /* Message describing the last failed op-level call (or memspec_init) on this
  * host thread; never NULL. */
 const char* memspec_op_last_error(void);

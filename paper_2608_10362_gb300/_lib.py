@@ -84,6 +84,18 @@ class SchedStats(C.Structure):
                 ("fallback_s", C.c_double), ("policy_s", C.c_double)]
 
 
+# sampling rules and adapters (memspec_ops.h)
+class Filter(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p),
+                ("min_p_dev", C.c_void_p)]
+
+
+class Lora(C.Structure):
+    _fields_ = [("a_dev", C.c_void_p), ("b_dev", C.c_void_p), ("scales_dev", C.c_void_p),
+                ("ranks_dev", C.c_void_p), ("n_adapters", C.c_int32), ("rank", C.c_int32)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "memspec_weights_bytes": (C.c_int, [C.POINTER(ModelCfg), C.POINTER(C.c_size_t)]),
@@ -125,6 +137,15 @@ EXPORTS = {
                                          C.c_void_p, C.c_void_p]),
     "memspec_op_sample": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_void_p,
                                     C.c_void_p, C.c_void_p]),
+    "memspec_op_sample_filtered": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.POINTER(Filter),
+                                             C.c_void_p, C.c_void_p, C.c_void_p]),
+    "memspec_op_filter_logits": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.POINTER(Filter),
+                                           C.c_void_p, C.c_int64, C.c_void_p]),
+    "memspec_op_lora_scratch_bytes": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                                C.POINTER(C.c_size_t)]),
+    "memspec_op_lora": (C.c_int, [C.POINTER(Lora), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                  C.c_size_t, C.c_void_p]),
     "memspec_op_last_error": (C.c_char_p, []),
     "memspec_pack_matrix": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
                                       C.c_size_t, C.c_void_p]),

@@ -1,0 +1,113 @@
+// expfix.cuh - softmax weights as 64-bit fixed-point integers.
+//
+// weight(z) = round(2^43 * exp((z - max) / T)): off by at most 2^-44 of the largest weight
+// and, relative to itself, 2^-31.8 (2^-34.4 in the mean square).  Integers add up to the same sum in any order, so
+// thousands of threads may sum them as they come and every comparison of sums (does this
+// prefix hold p of the mass? does the running sum pass u times the total?) is exact; with
+// 32-bit floating-point sums one draw in a few hundred lands within a rounding of a border
+// between two ids (25 of 11232 in sampling.cu's kernel).  131072 weights stay below 2^61.
+//
+// exp by a table of 2^(i/256) and a cubic for the rest (the table-driven scheme of
+// P. T. P. Tang, ACM TOMS 15 (1989)): y = (z - max) log2(e) / T as an unevaluated sum of
+// two floats, n = round(256 y), y - n / 256 in [-1/512, 1/512], where 2^f - 1 is small
+// enough that 24 bits of it are 34 of the weight.  About 30 instructions, none of them
+// 64-bit floating point (2 a clock and SM here).
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace memspec {
+
+constexpr int kExpSteps = 256;
+constexpr int kExpBits = 39;       // table entries: 2^39 * 2^(i/256)
+constexpr int kWeightBits = 43;    // weight of the maximum: 2^43
+
+struct ExpTable {
+  unsigned long long v[kExpSteps];
+};
+// 2^(1/256) by eight square roots (Newton), its powers by products: 2^-45 at worst.
+constexpr double newton_sqrt(double x) {
+  double r = x;
+  for (int i = 0; i < 60; ++i) r = 0.5 * (r + x / r);
+  return r;
+}
+constexpr ExpTable make_exp_table() {
+  ExpTable t{};
+  double base = 2.0;
+  for (int i = 0; i < 8; ++i) base = newton_sqrt(base);
+  double x = 1.0;
+  for (int i = 0; i < kExpSteps; ++i) {
+    t.v[i] = static_cast<unsigned long long>(x * 549755813888.0 + 0.5);   // 2^39
+    x *= base;
+  }
+  return t;
+}
+
+// The table in device memory (kernels copy it to shared memory).
+__device__ __forceinline__ const unsigned long long* exp_table() {
+  static __device__ const ExpTable t = make_exp_table();
+  return t.v;
+}
+
+// What weight() needs of a row: the maximum and log2(e) / T in two floats.
+struct WeightScale {
+  float max, hi, lo;
+};
+__device__ __forceinline__ WeightScale weight_scale(float row_max, float temperature) {
+  // T below 1e-30 leaves the maxima alone with weight; T = inf weighs all alike
+  const double c = fmin(1.4426950408889634 / static_cast<double>(temperature), 1e30);
+  WeightScale s;
+  s.max = row_max;
+  s.hi = static_cast<float>(c);
+  s.lo = static_cast<float>(c - static_cast<double>(s.hi));
+  return s;
+}
+
+// (max - z) log2(e) / T rounded to a float: falls monotonically as z grows (each of the
+// two roundings is monotonic), inf or NaN where z is -inf.
+__device__ __forceinline__ float weight_depth(float z, const WeightScale& s) { return (s.max - z) * s.hi; }
+
+// z finite or -inf, z <= s.max.
+__device__ __forceinline__ unsigned long long weight(float z, const WeightScale& s,
+                                                     const unsigned long long* table) {
+  // max - z = d + e exactly (two-sum)
+  const float d = s.max - z;
+  const float b = d - s.max;
+  const float e = (s.max - (d - b)) - (z + b);
+  const float yh = d * s.hi;
+  if (!(yh < 44.f)) return 0;     // below 2^-44 of the maximum; z = -inf (yh inf or NaN)
+  const float yl = fmaf(d, s.hi, -yh) + fmaf(d, s.lo, e * s.hi);
+  const float n = rintf(yh * -256.f);
+  const float f = fmaf(n, -1.f / 256.f, -yh) - yl;       // exact but for the subtraction of yl
+  const float u = f * 0.693147180559945f;
+  const float p = fmaf(u * u, fmaf(u, 1.f / 6.f, 0.5f), u);   // 2^f - 1
+  const int ni = static_cast<int>(n);
+  const unsigned long long t = table[ni & (kExpSteps - 1)];
+  // both parts scaled by 2^39; |p| < 0.0015
+  const int r = __float2int_rn(static_cast<float>(static_cast<unsigned>(t >> 8)) * (p * 256.f));
+  const unsigned long long w = (t + static_cast<long long>(r)) << (kWeightBits - kExpBits);
+  const int sh = -(ni >> 8);       // 0..44
+  return (w + ((1ull << sh) >> 1)) >> sh;
+}
+
+// The float order of logits as unsigned keys (-0 as +0).
+__device__ __forceinline__ uint32_t logit_key(float z) {
+  const uint32_t b = __float_as_uint(z + 0.f);
+  return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_logit(uint32_t k) {
+  return __uint_as_float(k ^ ((k & 0x80000000u) ? 0x80000000u : 0xFFFFFFFFu));
+}
+
+// floor(f 2^64) of f in [0, 1), exact down to 2^-64; f >= 1: 2^64 - 1; f <= 0 or NaN: 0.
+__device__ __forceinline__ unsigned long long fraction64(float f) {
+  if (!(f > 0.f)) return 0;
+  if (f >= 1.f) return ~0ull;
+  const uint32_t b = __float_as_uint(f);
+  const int ex = static_cast<int>(b >> 23);               // f = m 2^(ex - 150)
+  const unsigned long long m = ex ? (b & 0x7FFFFFu) | 0x800000u : b & 0x7FFFFFu;
+  const int sh = (ex ? ex : 1) - 150 + 64;
+  return sh >= 0 ? m << sh : (sh > -64 ? m >> -sh : 0);
+}
+
+}  // namespace memspec

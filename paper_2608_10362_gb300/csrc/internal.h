@@ -260,6 +260,24 @@ struct AcceptArgs {
   uint32_t* status;
 };
 
+struct FilterArgs {         // rows of logits under sampling rules (filter.cu)
+  const float* logits;      // row r at logits + r * ld
+  long long ld;
+  int rows, vocab;
+  int rows_per_rule;        // row r follows rule r / rows_per_rule of the arrays
+  // one rule for all rows, or (non-null) device arrays of a rule's part each
+  float temperature, top_p, min_p;
+  int top_k;
+  const float* temperatures;
+  const int* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+  const float* u;           // [rows] uniforms, and the drawn ids (-1: nothing to draw), ...
+  int* out_tok;
+  float* out;               // ... or (non-null) the masked logits, row r at out + r * out_ld
+  long long out_ld;
+};
+
 // Fused draft step (draft_fused.cu): all K forward passes of a small draft and
 // their samples in one cooperative launch, one CTA per SM, grid-wide barriers
 // between the ops of a pass.  Rows: at most 2 per request (catch-up) and at most
@@ -375,6 +393,7 @@ int attn_tc_max_clusters(int hd, int qmax, int C);
 cudaError_t launch_attn_tc(const AttnArgs& a, int n_groups, cudaStream_t s, bool pdl);
 cudaError_t launch_sample(const SampleArgs& a, cudaStream_t s, bool pdl);
 cudaError_t launch_accept(const AcceptArgs& a, cudaStream_t s, bool pdl);
+cudaError_t launch_filter(const FilterArgs& a, cudaStream_t s, bool pdl);
 cudaError_t launch_rope_table(float* cos_t, float* sin_t, int max_seq, int half, float base,
                               cudaStream_t s);
 

@@ -7,6 +7,7 @@ the library reports (memspec_weights_offset), and forwards calls.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 from typing import Iterable, Mapping
@@ -358,6 +359,15 @@ def _raw_stream(x: torch.Tensor, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on_device(x: torch.Tensor):
+    """A context in which x's device is the current one: launches go to that device."""
+    dev = x.get_device()
+    return _SAME_DEVICE if dev == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
 @functools.lru_cache(maxsize=512)
 def _linear_scratch_bytes(rows: int, n_out: int, k: int) -> int:
     lib = _lib.load()
@@ -448,3 +458,171 @@ def op_sample(logits: torch.Tensor, temperature: float, u: torch.Tensor | None =
     if st:
         _check(lib, st)
     return out
+
+
+def _cuda_arg(name: str, t: torch.Tensor, dtype, shape=None, like: torch.Tensor | None = None) -> None:
+    """Refuse a tensor argument that the library would misread: the C calls see
+    addresses and sizes only."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if shape is not None and (tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous {list(shape)}, not {list(t.shape)}")
+
+
+def _rows_arg(name: str, t: torch.Tensor, dtype, like: torch.Tensor | None = None) -> int:
+    """A 2-D tensor whose rows are contiguous and do not overlap; returns the row stride."""
+    _cuda_arg(name, t, dtype, like=like)
+    if t.dim() != 2 or t.shape[0] < 1 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be 2-D and not empty, not {list(t.shape)}")
+    rows, n = t.shape
+    if max(rows, n) >= 1 << 31:
+        raise ValueError(f"{name} is too large: {list(t.shape)}")   # the library counts in 32 bits
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), n)
+    if (n > 1 and t.stride(1) != 1) or ld < n:
+        raise ValueError(f"{name}'s rows must be contiguous and not overlap (strides {t.stride()})")
+    return ld
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    span = lambda t: (t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size())
+    (a0, a1), (b0, b1) = span(a), span(b)
+    return a0 < b1 and b0 < a1
+
+
+def _used_on(stream: torch.cuda.Stream | None, *made: torch.Tensor) -> None:
+    """Tensors made here on the current stream are in use on `stream` until its work is
+    done: their memory must not be handed out again before."""
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)
+
+
+def _filter(logits: torch.Tensor, temperature, top_k, top_p, min_p) -> _lib.Filter:
+    f = _lib.Filter()
+    for name, v, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(v, torch.Tensor):
+            _cuda_arg(name, v, dtype, (logits.shape[0],), logits)
+            setattr(f, name + "_dev", v.data_ptr())
+        elif name == "top_k" and (v != int(v) or not 0 <= v < 1 << 31):
+            raise ValueError(f"top_k must be a whole number from 0 to 2^31 - 1, not {v!r}")
+        else:
+            setattr(f, name, v)
+    return f
+
+
+def op_sample_filtered(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                       out: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
+    """One id per row of logits (fp32 [rows][vocab], rows at any stride) drawn with the
+    uniform u[row] from softmax(z / temperature) after top_k, top_p and min_p, see
+    memspec_filter; -1 for a row without a finite logit.  Each part of the rule is a
+    number, or a CUDA tensor of one value per row (fp32; top_k int32)."""
+    lib = _lib.load()
+    ld = _rows_arg("logits", logits, torch.float32)
+    rows, vocab = logits.shape
+    _cuda_arg("u", u, torch.float32, (rows,), logits)
+    f = _filter(logits, temperature, top_k, top_p, min_p)
+    if out is None:
+        out = torch.empty((rows,), dtype=torch.int32, device=logits.device)
+        _used_on(stream, out)
+    else:
+        _cuda_arg("out", out, torch.int32, (rows,), logits)
+    with _on_device(logits):
+        st = lib.memspec_op_sample_filtered(logits.data_ptr(), ld, rows, vocab, C.byref(f), u.data_ptr(),
+                                            out.data_ptr(), _raw_stream(logits, stream))
+    if st:
+        _check(lib, st)
+    return out
+
+
+def op_filter_logits(logits: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                     out: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
+    """The logits with -inf at every id that the rule cuts (arguments as
+    op_sample_filtered's); `out` may be `logits` itself."""
+    lib = _lib.load()
+    ld = _rows_arg("logits", logits, torch.float32)
+    rows, vocab = logits.shape
+    f = _filter(logits, temperature, top_k, top_p, min_p)
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=torch.float32, device=logits.device)
+        _used_on(stream, out)
+    elif out is not logits:
+        _rows_arg("out", out, torch.float32, logits)
+        if out.shape != logits.shape:
+            raise ValueError(f"out must be {list(logits.shape)}, not {list(out.shape)}")
+        if _overlap(out, logits) and (out.data_ptr(), out.stride()) != (logits.data_ptr(), logits.stride()):
+            raise ValueError("out overlaps logits without being the same rows")
+    out_ld = ld if out is logits else _rows_arg("out", out, torch.float32)
+    with _on_device(logits):
+        st = lib.memspec_op_filter_logits(logits.data_ptr(), ld, rows, vocab, C.byref(f), out.data_ptr(), out_ld,
+                                          _raw_stream(logits, stream))
+    if st:
+        _check(lib, st)
+    return out
+
+
+@functools.lru_cache(maxsize=512)
+def _lora_scratch_bytes(rows: int, n_out: int, k: int, rank: int) -> int:
+    lib = _lib.load()
+    nb = C.c_size_t()
+    _check(lib, lib.memspec_op_lora_scratch_bytes(rows, n_out, k, rank, C.byref(nb)))
+    return nb.value
+
+
+def op_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, scales: torch.Tensor | None = None,
+            ranks: torch.Tensor | None = None, base: torch.Tensor | None = None, y: torch.Tensor | None = None,
+            scratch: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
+    """y = base + scales[id] * (x A[id]^T) B[id]^T, row by row with id = ids[row] (int32;
+    outside 0..n-1: no adapter).  x bf16 [rows][k], rows at any stride of 8; a bf16 [n][rank][k],
+    b bf16 [n][n_out][rank]; scales fp32 [n], ranks int32 [n]; base fp32 [rows][n_out] at
+    any row stride: what op_linear or op_linear_int4 gave for the same x (None: 0).
+    ``y`` (fp32, may be `base` itself) receives the result, else a new tensor.
+    ``scratch`` (any content) of memspec_op_lora_scratch_bytes bytes saves an allocation."""
+    lib = _lib.load()
+    ldx = _rows_arg("x", x, torch.bfloat16)
+    rows, k = x.shape
+    if a.dim() != 3 or b.dim() != 3:
+        raise ValueError("a must be [adapters][rank][k] and b [adapters][n_out][rank]")
+    n_adapters, rank = a.shape[:2]
+    n_out = b.shape[1]
+    _cuda_arg("a", a, torch.bfloat16, (n_adapters, rank, k), x)
+    _cuda_arg("b", b, torch.bfloat16, (n_adapters, n_out, rank), x)
+    _cuda_arg("ids", ids, torch.int32, (rows,), x)
+    f = _lib.Lora(a.data_ptr(), b.data_ptr(), None, None, n_adapters, rank)
+    if scales is not None:
+        _cuda_arg("scales", scales, torch.float32, (n_adapters,), x)
+        f.scales_dev = scales.data_ptr()
+    if ranks is not None:
+        _cuda_arg("ranks", ranks, torch.int32, (n_adapters,), x)
+        f.ranks_dev = ranks.data_ptr()
+    ld_base = 0
+    if base is not None:
+        ld_base = _rows_arg("base", base, torch.float32, x)
+        if base.shape != (rows, n_out):
+            raise ValueError(f"base must be {[rows, n_out]}, not {list(base.shape)}")
+    if y is None:
+        y = torch.empty((rows, n_out), dtype=torch.float32, device=x.device)
+        _used_on(stream, y)
+    ldy = _rows_arg("y", y, torch.float32, x)
+    if y.shape != (rows, n_out):
+        raise ValueError(f"y must be {[rows, n_out]}, not {list(y.shape)}")
+    if base is not None and base is not y and _overlap(base, y) and \
+            (base.data_ptr(), base.stride()) != (y.data_ptr(), y.stride()):
+        raise ValueError("y overlaps base without being the same rows")
+    nb = _lora_scratch_bytes(rows, n_out, k, rank)
+    if scratch is None:
+        scratch = torch.empty(nb, dtype=torch.uint8, device=x.device)
+        _used_on(stream, scratch)
+    elif not scratch.is_cuda or scratch.device != x.device or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be contiguous on {x.device}")
+    with _on_device(x):
+        st = lib.memspec_op_lora(C.byref(f), x.data_ptr(), ldx, ids.data_ptr(),
+                                 None if base is None else base.data_ptr(), ld_base, y.data_ptr(), ldy, rows, n_out,
+                                 k, scratch.data_ptr(), scratch.nbytes, _raw_stream(x, stream))
+    if st:
+        _check(lib, st)
+    return y
