@@ -64,66 +64,96 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Chunk c of the call: up to CH rows of one adapter.
+// The call's chunks: up to CH rows of one adapter each, numbered by their first row.
 template <int CH>
-struct Chunk {
-  int ids[kMaxLoraRows];    // -1: none
-  int leaders[kThreads / 32];
-  int row[CH];              // the chunk's rows, ascending; -1 past the last
+struct Chunks {
+  int2 table[kWarps][32];   // a warp's distinct ids (-1: none) and how many rows have each
+  int distinct[kWarps];
+  int leaders[kWarps];
+  int row[CH];              // the selected chunk's rows, ascending; -1 past the last
   int id, first;
-  bool found;
 };
-// Chunks are numbered by their first row.  All threads; false: there is no chunk c.
+// What a thread knows of row threadIdx.x.
+struct RowPlace {
+  int id;                   // -1: no adapter
+  int pos;                  // rows of the same adapter before it
+  int chunk;                // the chunk that it leads, or -1
+};
+// All threads; returns the number of chunks.  Rows of one adapter mostly stand together, so
+// a warp's 32 rows have few distinct ids and the counts of earlier warps are a short list
+// (comparing each row with all earlier ones took 1 us more of a launch over 144 rows).
 template <int CH>
-__device__ bool find_chunk(const LoraArgs& a, int c, Chunk<CH>& s) {
-  const int tid = threadIdx.x;
-  int id = -2;
+__device__ int find_chunks(const LoraArgs& a, Chunks<CH>& s, RowPlace& p) {
+  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+  const unsigned below = (1u << lane) - 1;
+  p.id = -2;
   if (tid < a.rows) {
-    id = __ldcg(a.ids + tid);
-    if (id < 0 || id >= a.n_adapters) id = -1;
+    p.id = __ldcg(a.ids + tid);
+    if (p.id < 0 || p.id >= a.n_adapters) p.id = -1;
   }
-  s.ids[tid] = id;
-  if (tid < CH) s.row[tid] = -1;
-  if (tid == 0) s.found = false;
+  p.pos = 0;
+  if (w * 32 < a.rows) {
+    const unsigned same = __match_any_sync(0xffffffffu, p.id);
+    p.pos = __popc(same & below);
+    const unsigned firsts = __ballot_sync(0xffffffffu, p.pos == 0);
+    if (p.pos == 0) s.table[w][__popc(firsts & below)] = make_int2(p.id, __popc(same));
+    if (lane == 0) s.distinct[w] = __popc(firsts);
+  }
   __syncthreads();
-  int pos = 0;              // rows of the same adapter before this one
-  const int4* v = reinterpret_cast<const int4*>(s.ids);
-  const int last = min(tid, a.rows) >> 2;
-  for (int j = 0; j <= last && j < kMaxLoraRows / 4; ++j) {
-    const int4 q = v[j];
-    pos += (q.x == id && 4 * j < tid) + (q.y == id && 4 * j + 1 < tid) + (q.z == id && 4 * j + 2 < tid) +
-           (q.w == id && 4 * j + 3 < tid);
+  bool leads = false;
+  if (w * 32 < a.rows) {
+    for (int v = 0; v < w; ++v)
+      for (int e = 0, n = s.distinct[v]; e < n; ++e) {
+        const int2 q = s.table[v][e];
+        p.pos += q.x == p.id ? q.y : 0;
+      }
+    leads = tid < a.rows && p.pos % CH == 0;
   }
-  const bool leads = tid < a.rows && pos % CH == 0;
   const unsigned mask = __ballot_sync(0xffffffffu, leads);
-  if ((tid & 31) == 0) s.leaders[tid >> 5] = __popc(mask);
+  if (lane == 0) s.leaders[w] = __popc(mask);
   __syncthreads();
-  int before = __popc(mask & ((1u << (tid & 31)) - 1));
-  for (int w = 0; w < (tid >> 5); ++w) before += s.leaders[w];
-  if (leads && before == c) {
-    s.id = id;
-    s.first = pos;
-    s.found = true;
+  int before = __popc(mask & below), all = 0;
+#pragma unroll
+  for (int v = 0; v < kWarps; ++v) {
+    if (v < w) before += s.leaders[v];
+    all += s.leaders[v];
+  }
+  p.chunk = leads ? before : -1;
+  return all;
+}
+// All threads: chunk c's id and rows.
+template <int CH>
+__device__ void select_chunk(const LoraArgs& a, const RowPlace& p, int c, Chunks<CH>& s) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid < CH) s.row[tid] = -1;
+  if (p.chunk == c) {
+    s.id = p.id;
+    s.first = p.pos;
   }
   __syncthreads();
-  if (!s.found) return false;
-  if (tid < a.rows && id == s.id && pos >= s.first && pos < s.first + CH) s.row[pos - s.first] = tid;
+  if (tid < a.rows && p.id == s.id && p.pos >= s.first && p.pos < s.first + CH) s.row[p.pos - s.first] = tid;
   __syncthreads();
-  return true;
 }
 
-// t[row][j] for a chunk of up to 16 MT rows and 8 NT of the adapter's rows.  Grid (cluster
+// t[row][j] for a chunk of up to 16 MT rows and 8 NT of the adapter's ranks.  Grid (cluster
 // of kSplits over k, chunks, groups of 8 NT ranks).
 template <int MT, int NT>
 struct ShrinkSmem {
-  static constexpr int kElems = MT * 16 * NT * 8;
-  Chunk<MT * 16> chunk;
-  float warp[kWarps][kElems];                 // a warp's sums
-  float split[kSplits][kElems / kSplits];     // this CTA's elements, from each CTA of the cluster
+  static constexpr int kFrags = MT * NT * 32;   // a lane's four sums of a 16 x 8 tile
+  Chunks<MT * 16> chunk;
+  float4 warp[kWarps][kFrags];                  // a warp's sums
+  float4 split[kSplits][kFrags / kSplits];      // this CTA's sums, from each CTA of the cluster
 };
+__device__ __forceinline__ void add4(float4& s, const float4& v) {
+  s.x += v.x;
+  s.y += v.y;
+  s.z += v.z;
+  s.w += v.w;
+}
 
 template <int MT, int NT>
-__global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant__ LoraArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_constant__ LoraArgs a) {
   extern __shared__ __align__(16) uint8_t raw[];
   typedef ShrinkSmem<MT, NT> S;
   S& sm = *reinterpret_cast<S*>(raw);
@@ -133,8 +163,10 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
   pdl_wait();
   pdl_launch_dependents();
   // the CTAs of a cluster have one chunk and one rank group: they leave together
-  const bool found = find_chunk(a, blockIdx.y, sm.chunk) && sm.chunk.id >= 0;
-  const int rank = found ? rank_of(a, sm.chunk.id) : 0;
+  RowPlace place;
+  const bool found = static_cast<int>(blockIdx.y) < find_chunks(a, sm.chunk, place);
+  if (found) select_chunk(a, place, blockIdx.y, sm.chunk);
+  const int rank = found && sm.chunk.id >= 0 ? rank_of(a, sm.chunk.id) : 0;
   if (j0 >= rank) {
     cluster_wait_acquire();
     return;
@@ -194,39 +226,55 @@ __global__ void __launch_bounds__(kThreads) shrink_kernel(const __grid_constant_
     }
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+  for (int m = 0; m < MT; ++m) {
+    if (m >= tiles) break;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        sm.warp[w][(m * 16 + (q >> 1) * 8 + g) * (NT * 8) + n * 8 + 2 * t + (q & 1)] = acc[m][n][q];
+      sm.warp[w][(m * NT + n) * 32 + lane] = make_float4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
+  }
   __syncthreads();
   cluster_wait_acquire();
-  constexpr int kOwn = S::kElems / kSplits;
-  for (int e = tid; e < S::kElems; e += kThreads) {
-    float s = 0.f;
+  const int own = tiles * NT * 32 / kSplits;
+  for (int f = tid; f < own * kSplits; f += kThreads) {
+    float4 s = sm.warp[0][f];
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) s += sm.warp[i][e];
-    st_cluster_f(mapa_shared(smem_addr(&sm.split[split][e % kOwn]), e / kOwn), s);
+    for (int i = 1; i < kWarps; ++i) add4(s, sm.warp[i][f]);
+    const int to = f / own;
+    st_cluster_f4(mapa_shared(smem_addr(&sm.split[split][f - to * own]), to), s);
   }
   cluster_arrive_release();
   cluster_wait_acquire();
-  for (int i = tid; i < kOwn; i += kThreads) {
-    float s = 0.f;
+  for (int i = tid; i < own; i += kThreads) {
+    float4 s = sm.split[0][i];
 #pragma unroll
-    for (int c = 0; c < kSplits; ++c) s += sm.split[c][i];
-    const int e = split * kOwn + i, j = j0 + e % (NT * 8), r = sm.chunk.row[e / (NT * 8)];
-    if (r >= 0 && j < a.rank) a.t[r * a.rank + j] = s;
+    for (int c = 1; c < kSplits; ++c) add4(s, sm.split[c][i]);
+    const int f = split * own + i, l = f & 31, n = (f >> 5) % NT, m = (f >> 5) / NT;
+    const int j = j0 + n * 8 + 2 * (l & 3);
+    const int r0 = sm.chunk.row[m * 16 + (l >> 2)], r1 = sm.chunk.row[m * 16 + 8 + (l >> 2)];
+    if (j >= a.rank) continue;
+    if (r0 >= 0) *reinterpret_cast<float2*>(a.t + r0 * a.rank + j) = make_float2(s.x, s.y);
+    if (r1 >= 0) *reinterpret_cast<float2*>(a.t + r1 * a.rank + j) = make_float2(s.z, s.w);
   }
 }
 
-// y for a chunk of up to 32 rows; a warp takes 32 columns at a time.  KT: steps of 16 ranks.
+// y = base + scale B t.  Work is (chunk of up to 32 rows, 32 columns) items in that order,
+// cut evenly over as many CTAs as are resident at once; a warp takes every eighth item of
+// its CTA's part of a chunk, B's columns arriving by cp.async kStages items ahead (loads
+// into registers as they were needed left half the time waiting: gate/up of 144 rows 30
+// us).  KT: steps of 16 ranks.
 constexpr int kExpandTiles = 2;
-constexpr int kColsPerWarp = 32;
+constexpr int kCols = 32;
 template <int KT>
 struct ExpandSmem {
-  Chunk<kExpandTiles * 16> chunk;
+  static constexpr int kPieces = KT * 2;           // of 8 ranks, per column
+  static constexpr int kStages = KT <= 2 ? 4 : KT == 4 ? 3 : 2;
+  uint4 b[kWarps][kStages][kCols * kPieces];
   uint4 t[kExpandTiles][KT][3][32];   // fragments of t's planes, one per lane
+  Chunks<kExpandTiles * 16> chunk;
+  float4 turn[kWarps][16][8 + 1];     // a warp's tile where rows are not 16-byte aligned (else
+                                      // not there)
+  static constexpr size_t bytes(bool vec) { return vec ? sizeof(ExpandSmem) - sizeof(turn) : sizeof(ExpandSmem); }
+  static constexpr int per_sm(bool vec) { return KT <= 4 && 2 * (bytes(vec) + 1024) <= 228 * 1024 ? 2 : 1; }
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -234,160 +282,250 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ float bf16_part(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
+// A pair of bf16 at ranks r, r + 1 without what lies past the adapter's rank (which may be
+// anything).
+__device__ __forceinline__ uint32_t within(uint32_t pair, int r, int rank) {
+  return r + 1 < rank ? pair : (r < rank ? pair & 0xffffu : 0u);
+}
+
+__device__ __forceinline__ void copy16_async(void* dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(in ? 16 : 0)
+               : "memory");
+}
 
 template <int KT>
 __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const __grid_constant__ LoraArgs a) {
-  __shared__ ExpandSmem<KT> sm;
+  typedef ExpandSmem<KT> S;
+  constexpr int kPieces = S::kPieces, kStages = S::kStages;
+  extern __shared__ __align__(16) uint8_t raw[];
+  S& sm = *reinterpret_cast<S*>(raw);
   const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   // the ids, B, base and scales may be read now: the launch before this one (shrink) lets
   // it start only after its own wait, so all that came earlier has completed
-  if (!find_chunk(a, blockIdx.y, sm.chunk)) return;
-  const int id = sm.chunk.id;
-  const int rank = id < 0 ? 0 : rank_of(a, id);
-  const float scale = id < 0 || a.scales == nullptr ? 1.f : a.scales[id];
-  const int steps = (rank + 15) / 16;
-  int tiles = 0;
+  RowPlace place;
+  const int chunks = find_chunks(a, sm.chunk, place);
+  const int cols = (a.n + kCols - 1) / kCols;
+  const long long items = static_cast<long long>(chunks) * cols;
+  long long at = items * blockIdx.x / gridDim.x;
+  const long long end = items * (blockIdx.x + 1) / gridDim.x;
+  // column of MMA column g of tile j: 8 (g / 2) + 2 j + g % 2, so that a thread's results
+  // (columns 2 t, 2 t + 1 of each tile) are columns 8 t .. 8 t + 7
+  const int bcol = 8 * (g >> 1) + (g & 1);
+  bool waited = false;
+  while (at < end) {
+    const int c = static_cast<int>(at / cols);
+    const int lo = static_cast<int>(at - static_cast<long long>(c) * cols);
+    const int hi = static_cast<int>(min(static_cast<long long>(cols), lo + (end - at)));
+    at += hi - lo;
+    select_chunk(a, place, c, sm.chunk);
+    const int id = sm.chunk.id;
+    const int rank = id < 0 ? 0 : rank_of(a, id);
+    const float scale = id < 0 || a.scales == nullptr ? 1.f : __ldcg(a.scales + id);
+    // a thread's 8 ranks of 32 (KT = 1: 4 of 16) are split over two steps
+    const int steps = KT == 1 ? (rank + 15) / 16 : (rank + 31) / 32 * 2;
+    int tiles = 0;
 #pragma unroll
-  for (int m = 0; m < kExpandTiles; ++m) tiles += sm.chunk.row[m * 16] >= 0;
-  // column of MMA column n of tile j: 8 consecutive ones per thread, or (rows that no
-  // 16-byte access fits) pairs
-  const int bcol = a.vec ? 8 * (g >> 1) + (g & 1) : g, bstep = a.vec ? 2 : 8;
-  const bf16* bw = a.b + static_cast<long long>(max(id, 0)) * a.n * a.rank + 4 * t;
-  uint2 bv[KT][4];
-  auto load_b = [&](int c0) {
+    for (int m = 0; m < kExpandTiles; ++m) tiles += sm.chunk.row[m * 16] >= 0;
+    // lane's piece of kPieces columns of an item: piece lane % kPieces, swapped by fours
+    // in odd columns so that two columns' pieces lie in different banks
+    const int piece = lane % kPieces;
+    const bf16* bp = a.b + (static_cast<long long>(max(id, 0)) * a.n + lane / kPieces) * a.rank + piece * 8;
+    auto load_b = [&](int item, int stage) {
+      const int c0 = item * kCols;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = c0 + bcol + j * bstep;
-      const bf16* p = bw + static_cast<long long>(col) * a.rank;
-#pragma unroll
-      for (int s = 0; s < KT; ++s) {
-        const int r = s * 16 + 4 * t;
-        bv[s][j] = make_uint2(0, 0);
-        if (col < a.n && r < rank) {
-          bv[s][j] = __ldcg(reinterpret_cast<const uint2*>(p + s * 16));
-          if (r + 4 > rank) {     // entries past the adapter's rank may be anything
-            if (r + 1 >= rank) bv[s][j].x &= 0xffffu;
-            if (r + 2 >= rank) bv[s][j].y = 0;
-            if (r + 3 >= rank) bv[s][j].y &= 0xffffu;
-          }
-        }
+      for (int i = 0; i < kPieces; ++i) {
+        const int col = lane / kPieces + i * (32 / kPieces);
+        const bool in = c0 + col < a.n && piece * 8 < rank;
+        copy16_async(&sm.b[w][stage][col * kPieces + (KT >= 4 ? piece ^ ((col & 1) << 2) : piece)],
+                     in ? bp + static_cast<long long>(c0 + i * (32 / kPieces)) * a.rank : a.b, in);
       }
-    }
-  };
-  float base[2][8];
-  auto load_base = [&](int m, int c0) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = sm.chunk.row[m * 16 + h * 8 + g];
-      const float* p = a.base + r * a.ld_base + c0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) base[h][i] = 0.f;
-      if (r < 0 || a.base == nullptr) continue;
-      if (a.vec) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-          if (c0 + 8 * t + 4 * q < a.n) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p + 8 * t + 4 * q));
-            base[h][4 * q] = v.x, base[h][4 * q + 1] = v.y, base[h][4 * q + 2] = v.z, base[h][4 * q + 3] = v.w;
-          }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = (i >> 1) * 8 + 2 * t + (i & 1);
-          if (c0 + c < a.n) base[h][i] = __ldcg(p + c);
-        }
-      }
-    }
-  };
-  const int stride = gridDim.x * kWarps * kColsPerWarp;
-  const int c_first = (blockIdx.x * kWarps + w) * kColsPerWarp;
-  load_b(c_first);
-  load_base(0, c_first);
-  pdl_wait();
-  pdl_launch_dependents();
-  for (int i = tid; i < tiles * steps * 32; i += kThreads) {
-    const int l = i & 31, s = (i >> 5) % steps, m = (i >> 5) / steps;
-    const int r = s * 16 + 4 * (l & 3);
-    float v[2][4] = {};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = sm.chunk.row[m * 16 + h * 8 + (l >> 2)];
-      if (row < 0 || r >= rank) continue;
-      const float4 q = __ldcg(reinterpret_cast<const float4*>(a.t + row * a.rank + r));
-      v[h][0] = q.x;
-      v[h][1] = r + 1 < rank ? q.y : 0.f;
-      v[h][2] = r + 2 < rank ? q.z : 0.f;
-      v[h][3] = r + 3 < rank ? q.w : 0.f;
-    }
-#pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      sm.t[m][s][p][l] = make_uint4(pack_bf16(v[0][0], v[0][1]), pack_bf16(v[1][0], v[1][1]),
-                                    pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][2], v[1][3]));
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[h][q] -= bf16_part(v[h][q]);
-    }
-  }
-  __syncthreads();
-  for (int c0 = c_first; c0 < a.n; c0 += stride) {
-    if (c0 != c_first) load_b(c0);
-    for (int m = 0; m < tiles; ++m) {
-      if (c0 != c_first || m > 0) load_base(m, c0);
-      float acc[4][4] = {};
-#pragma unroll
-      for (int s = 0; s < KT; ++s) {
-        if (s >= steps) break;
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-          const uint4 f = sm.t[m][s][p][lane];
-          const uint32_t fa[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) mma(acc[j], fa, bv[s][j].x, bv[s][j].y);
-        }
-      }
+    };
+    float4 base[2][2];
+    auto load_base = [&](int m, int c0) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = sm.chunk.row[m * 16 + h * 8 + g];
-        if (r < 0) continue;
-        float* y = a.y + r * a.ldy + c0;
-        float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = rank > 0 ? fmaf(scale, acc[i >> 1][h * 2 + (i & 1)], base[h][i]) : base[h][i];
+        for (int q = 0; q < 2; ++q) {
+          const int x = c0 + 8 * t + 4 * q;
+          base[h][q] = r >= 0 && x < a.n && a.base != nullptr
+                           ? __ldcg(reinterpret_cast<const float4*>(a.base + r * a.ld_base + x))
+                           : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+    };
+    const int mine = hi - lo > w ? (hi - lo - w + kWarps - 1) / kWarps : 0;   // items of this warp
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+      if (i < mine && rank > 0) load_b(lo + w + i * kWarps, i);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (a.vec && mine > 0) load_base(0, (lo + w) * kCols);
+    if (!waited) {
+      pdl_wait();
+      pdl_launch_dependents();
+      waited = true;
+    }
+    for (int i = tid; i < tiles * steps * 32; i += kThreads) {
+      const int l = i & 31, s = (i >> 5) % steps, m = (i >> 5) / steps;
+      // the ranks of a lane's fragments of step s: as they lie in its pieces of B
+      const int r = KT == 1 ? 4 * (l & 3) : (s >> 1) * 32 + 8 * (l & 3) + (s & 1) * 4;
+      float v[2][4] = {};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = sm.chunk.row[m * 16 + h * 8 + (l >> 2)];
+        if (row < 0 || r >= rank) continue;
+        const float4 q = __ldcg(reinterpret_cast<const float4*>(a.t + row * a.rank + r));
+        v[h][0] = q.x;
+        v[h][1] = r + 1 < rank ? q.y : 0.f;
+        v[h][2] = r + 2 < rank ? q.z : 0.f;
+        v[h][3] = r + 3 < rank ? q.w : 0.f;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        sm.t[m][s][p][l] = make_uint4(pack_bf16(v[0][0], v[0][1]), pack_bf16(v[1][0], v[1][1]),
+                                      pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][2], v[1][3]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[h][q] -= bf16_part(v[h][q]);
+      }
+    }
+    __syncthreads();
+    for (int i = 0; i < mine; ++i) {
+      const int c0 = (lo + w + i * kWarps) * kCols, stage = i % kStages;
+      if (i + kStages - 1 < mine && rank > 0) load_b(lo + w + (i + kStages - 1) * kWarps, (i + kStages - 1) % kStages);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      __syncwarp();
+      for (int m = 0; m < tiles; ++m) {
+        float acc[4][4] = {};
+#pragma unroll
+        for (int s2 = 0; s2 < (KT + 1) / 2; ++s2) {
+          if (2 * s2 >= steps) break;
+          uint4 bv[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int col = bcol + 2 * j;
+            const uint4* p = &sm.b[w][stage][col * kPieces];
+            if (KT == 1) {
+              const uint2 u = reinterpret_cast<const uint2*>(p)[t];
+              bv[j] = make_uint4(u.x, u.y, 0u, 0u);
+            } else {
+              bv[j] = p[KT >= 4 ? (s2 * 4 + t) ^ ((col & 1) << 2) : s2 * 4 + t];
+            }
+            if (rank & 7) {
+              const int r = KT == 1 ? 4 * t : (s2 * 4 + t) * 8;
+              bv[j].x = within(bv[j].x, r, rank);
+              bv[j].y = within(bv[j].y, r + 2, rank);
+              bv[j].z = within(bv[j].z, r + 4, rank);
+              bv[j].w = within(bv[j].w, r + 6, rank);
+            }
+          }
+#pragma unroll
+          for (int o = 0; o < (KT == 1 ? 1 : 2); ++o) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+              const uint4 f = sm.t[m][2 * s2 + o][p][lane];
+              const uint32_t fa[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma(acc[j], fa, o ? bv[j].z : bv[j].x, o ? bv[j].w : bv[j].y);
+            }
+          }
+        }
         if (a.vec) {
 #pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (c0 + 8 * t + 4 * q < a.n)
-              *reinterpret_cast<float4*>(y + 8 * t + 4 * q) = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-        } else {
+          for (int h = 0; h < 2; ++h) {
+            const int r = sm.chunk.row[m * 16 + h * 8 + g];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int c = (i >> 1) * 8 + 2 * t + (i & 1);
-            if (c0 + c < a.n) y[c] = o[i];
+            for (int q = 0; q < 2; ++q) {
+              const int x = c0 + 8 * t + 4 * q;
+              if (r < 0 || x >= a.n) continue;
+              float4 o = base[h][q];
+              if (rank > 0) {   // else the base's own bits
+                o.x = fmaf(scale, acc[2 * q][2 * h], o.x);
+                o.y = fmaf(scale, acc[2 * q][2 * h + 1], o.y);
+                o.z = fmaf(scale, acc[2 * q + 1][2 * h], o.z);
+                o.w = fmaf(scale, acc[2 * q + 1][2 * h + 1], o.w);
+              }
+              *reinterpret_cast<float4*>(a.y + r * a.ldy + x) = o;
+            }
+          }
+          // the base of what this warp does next
+          if (m + 1 < tiles)
+            load_base(m + 1, c0);
+          else if (i + 1 < mine)
+            load_base(0, c0 + kWarps * kCols);
+        } else {
+          // through shared memory: a lane per column, 128 bytes of a row at once
+          __syncwarp();
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              sm.turn[w][h * 8 + g][2 * t + q] =
+                  make_float4(acc[2 * q][2 * h], acc[2 * q][2 * h + 1], acc[2 * q + 1][2 * h], acc[2 * q + 1][2 * h + 1]);
+          __syncwarp();
+          const int x = c0 + lane;
+          if (x < a.n) {
+            for (int i4 = 0; i4 < 16; i4 += 4) {
+              float o[4];
+              int r[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                r[q] = sm.chunk.row[m * 16 + i4 + q];
+                o[q] = r[q] >= 0 && a.base != nullptr ? __ldcg(a.base + r[q] * a.ld_base + x) : 0.f;
+              }
+              if (r[0] < 0) break;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if (r[q] < 0) continue;
+                if (rank > 0) o[q] = fmaf(scale, reinterpret_cast<const float*>(&sm.turn[w][i4 + q][0])[lane], o[q]);
+                a.y[r[q] * a.ldy + x] = o[q];
+              }
+            }
           }
         }
       }
+      __syncwarp();   // the stage is read before it is filled again
     }
   }
 }
 
+// Opt a kernel in to more than 48 KB of shared memory, once per device.
+template <class Kernel>
+cudaError_t allow_smem(Kernel* kernel, size_t bytes, std::atomic<bool> (&set)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev >= 64 || !set[dev].load(std::memory_order_relaxed))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess && dev < 64) set[dev].store(true, std::memory_order_relaxed);
+  }
+  return e;
+}
+
 template <int MT, int NT>
 cudaError_t launch_shrink(const LoraArgs& a, cudaLaunchConfig_t cfg) {
-  static_assert(sizeof(ShrinkSmem<MT, NT>) <= 227 * 1024, "shared memory");
+  static_assert(sizeof(ShrinkSmem<MT, NT>) <= 113 * 1024, "shared memory for two CTAs per SM");
+  static std::atomic<bool> set[64];
   cfg.gridDim = dim3(kSplits, std::min(a.rows, a.n_adapters + 1 + a.rows / (MT * 16)), (a.rank + NT * 8 - 1) / (NT * 8));
   cfg.dynamicSmemBytes = sizeof(ShrinkSmem<MT, NT>);
-  if (sizeof(ShrinkSmem<MT, NT>) > 48 * 1024) {   // set once per device
-    static std::atomic<bool> set[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && (dev >= 64 || !set[dev].load(std::memory_order_relaxed))) {
-      e = cudaFuncSetAttribute(shrink_kernel<MT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(cfg.dynamicSmemBytes));
-      if (e == cudaSuccess && dev < 64) set[dev].store(true, std::memory_order_relaxed);
-    }
-    if (e != cudaSuccess) return e;
-  }
+  if (const cudaError_t e = allow_smem(shrink_kernel<MT, NT>, cfg.dynamicSmemBytes, set); e != cudaSuccess) return e;
   return cudaLaunchKernelEx(&cfg, shrink_kernel<MT, NT>, a);
+}
+
+template <int KT>
+cudaError_t launch_expand(const LoraArgs& a, cudaLaunchConfig_t cfg) {
+  typedef ExpandSmem<KT> S;
+  static_assert(sizeof(S) <= 227 * 1024 && S::per_sm(true) == (KT <= 4 ? 2 : 1), "shared memory");
+  static std::atomic<bool> set[64];
+  // one item per warp, or as many CTAs as are resident at once
+  const long long items = static_cast<long long>((a.n + kCols - 1) / kCols) *
+                          std::min(a.rows, a.n_adapters + 1 + a.rows / (kExpandTiles * 16));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>((items + kWarps - 1) / kWarps, 152 * S::per_sm(a.vec))));
+  cfg.dynamicSmemBytes = S::bytes(a.vec);
+  if (const cudaError_t e = allow_smem(expand_kernel<KT>, sizeof(S), set); e != cudaSuccess) return e;
+  return cudaLaunchKernelEx(&cfg, expand_kernel<KT>, a);
 }
 
 cudaError_t launch_lora(const LoraArgs& a, cudaStream_t s) {
@@ -403,16 +541,13 @@ cudaError_t launch_lora(const LoraArgs& a, cudaStream_t s) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = a.rows <= 32 ? launch_shrink<1, 2>(a, cfg) : launch_shrink<4, 4>(a, cfg);
+  const cudaError_t e = a.rows <= 32 ? launch_shrink<1, 2>(a, cfg) : launch_shrink<2, 4>(a, cfg);
   if (e != cudaSuccess) return e;
   cfg.numAttrs = 1;
-  const int chunks = std::min(a.rows, a.n_adapters + 1 + a.rows / (kExpandTiles * 16));
-  const int cols = (a.n + kWarps * kColsPerWarp - 1) / (kWarps * kColsPerWarp);
-  cfg.gridDim = dim3(std::min(cols, std::max(1, 1216 / chunks)), chunks);
-  return a.rank <= 16   ? cudaLaunchKernelEx(&cfg, expand_kernel<1>, a)
-         : a.rank <= 32 ? cudaLaunchKernelEx(&cfg, expand_kernel<2>, a)
-         : a.rank <= 64 ? cudaLaunchKernelEx(&cfg, expand_kernel<4>, a)
-                        : cudaLaunchKernelEx(&cfg, expand_kernel<8>, a);
+  return a.rank <= 16   ? launch_expand<1>(a, cfg)
+         : a.rank <= 32 ? launch_expand<2>(a, cfg)
+         : a.rank <= 64 ? launch_expand<4>(a, cfg)
+                        : launch_expand<8>(a, cfg);
 }
 
 size_t lora_scratch(int rows, int rank) { return static_cast<size_t>(rows) * rank * 4; }

@@ -303,9 +303,11 @@ __device__ __forceinline__ void cluster_arrive_release() {
 __device__ __forceinline__ void cluster_wait_acquire() {
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
-// Plain store into a cluster peer's shared memory (mapa_shared address).
-__device__ __forceinline__ void st_cluster_f(uint32_t raddr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(raddr), "f"(v) : "memory");
+// Plain 16-byte store into a cluster peer's shared memory (mapa_shared address).
+__device__ __forceinline__ void st_cluster_f4(uint32_t raddr, const float4& v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(raddr), "f"(v.x), "f"(v.y), "f"(v.z),
+               "f"(v.w)
+               : "memory");
 }
 // 16-byte store into a cluster peer's shared memory that completes 16 bytes of
 // transaction count on the peer's mbarrier `rbar` (both shared::cluster addresses).
