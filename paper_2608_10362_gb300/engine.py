@@ -7,7 +7,6 @@ the library reports (memspec_weights_offset), and forwards calls.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import functools
 from typing import Iterable, Mapping
@@ -359,13 +358,14 @@ def _raw_stream(x: torch.Tensor, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
-_SAME_DEVICE = contextlib.nullcontext()
-
-
-def _on_device(x: torch.Tensor):
-    """A context in which x's device is the current one: launches go to that device."""
-    dev = x.get_device()
-    return _SAME_DEVICE if dev == torch.cuda.current_device() else torch.cuda.device(dev)
+def _call_on(dev: int, stream, fn, *args) -> int:
+    """fn(*args, stream) with CUDA device `dev`, the tensors' own, as the current one:
+    the library launches there."""
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if dev == torch._C._cuda_getDevice():
+        return fn(*args, s)
+    with torch.cuda.device(dev):
+        return fn(*args, s)
 
 
 @functools.lru_cache(maxsize=512)
@@ -487,10 +487,12 @@ def _rows_arg(name: str, t: torch.Tensor, dtype, like: torch.Tensor | None = Non
     return ld
 
 
-def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+def _same_or_apart(name_a: str, a: torch.Tensor, name_b: str, b: torch.Tensor) -> None:
+    """Refuse two 2-D tensors that share memory without being the same rows."""
     span = lambda t: (t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size())
     (a0, a1), (b0, b1) = span(a), span(b)
-    return a0 < b1 and b0 < a1
+    if a0 < b1 and b0 < a1 and (a0, a.stride()) != (b0, b.stride()):
+        raise ValueError(f"{name_a} overlaps {name_b} without being the same rows")
 
 
 def _used_on(stream: torch.cuda.Stream | None, *made: torch.Tensor) -> None:
@@ -515,6 +517,25 @@ def _filter(logits: torch.Tensor, temperature, top_k, top_p, min_p) -> _lib.Filt
     return f
 
 
+_F32, _I32, _BF16 = torch.float32, torch.int32, torch.bfloat16
+
+
+# The wrappers below look an argument over in one expression, and only where that is not
+# satisfied go through it piece by piece for the error (a check costs 0.1 to 0.8 us, the
+# C call of two launches 5).
+def _logits_arg(logits: torch.Tensor):
+    """(rows, vocab, row stride, device) of logits."""
+    if logits.dtype is _F32 and logits.dim() == 2:
+        rows, vocab = logits.shape
+        ld, one = logits.stride()
+        if one == 1 and ld >= vocab > 0 and 0 < rows < 1 << 31 and vocab < 1 << 31:
+            dev = logits.get_device()
+            if dev >= 0:
+                return rows, vocab, ld, dev
+    ld = _rows_arg("logits", logits, _F32)
+    return *logits.shape, ld, logits.get_device()
+
+
 def op_sample_filtered(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
                        out: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
     """One id per row of logits (fp32 [rows][vocab], rows at any stride) drawn with the
@@ -522,18 +543,17 @@ def op_sample_filtered(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, t
     memspec_filter; -1 for a row without a finite logit.  Each part of the rule is a
     number, or a CUDA tensor of one value per row (fp32; top_k int32)."""
     lib = _lib.load()
-    ld = _rows_arg("logits", logits, torch.float32)
-    rows, vocab = logits.shape
-    _cuda_arg("u", u, torch.float32, (rows,), logits)
+    rows, vocab, ld, dev = _logits_arg(logits)
+    if not (u.dtype is _F32 and u.shape == (rows,) and u.get_device() == dev and u.is_contiguous()):
+        _cuda_arg("u", u, _F32, (rows,), logits)
     f = _filter(logits, temperature, top_k, top_p, min_p)
     if out is None:
-        out = torch.empty((rows,), dtype=torch.int32, device=logits.device)
+        out = torch.empty((rows,), dtype=_I32, device=logits.device)
         _used_on(stream, out)
     else:
-        _cuda_arg("out", out, torch.int32, (rows,), logits)
-    with _on_device(logits):
-        st = lib.memspec_op_sample_filtered(logits.data_ptr(), ld, rows, vocab, C.byref(f), u.data_ptr(),
-                                            out.data_ptr(), _raw_stream(logits, stream))
+        _cuda_arg("out", out, _I32, (rows,), logits)
+    st = _call_on(dev, stream, lib.memspec_op_sample_filtered, logits.data_ptr(), ld, rows, vocab, C.byref(f),
+                  u.data_ptr(), out.data_ptr())
     if st:
         _check(lib, st)
     return out
@@ -544,22 +564,21 @@ def op_filter_logits(logits: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, 
     """The logits with -inf at every id that the rule cuts (arguments as
     op_sample_filtered's); `out` may be `logits` itself."""
     lib = _lib.load()
-    ld = _rows_arg("logits", logits, torch.float32)
-    rows, vocab = logits.shape
+    rows, vocab, ld, dev = _logits_arg(logits)
     f = _filter(logits, temperature, top_k, top_p, min_p)
     if out is None:
-        out = torch.empty((rows, vocab), dtype=torch.float32, device=logits.device)
+        out = torch.empty((rows, vocab), dtype=_F32, device=logits.device)
         _used_on(stream, out)
-    elif out is not logits:
-        _rows_arg("out", out, torch.float32, logits)
+        out_ld = vocab
+    elif out is logits:
+        out_ld = ld
+    else:
+        out_ld = _rows_arg("out", out, _F32, logits)
         if out.shape != logits.shape:
             raise ValueError(f"out must be {list(logits.shape)}, not {list(out.shape)}")
-        if _overlap(out, logits) and (out.data_ptr(), out.stride()) != (logits.data_ptr(), logits.stride()):
-            raise ValueError("out overlaps logits without being the same rows")
-    out_ld = ld if out is logits else _rows_arg("out", out, torch.float32)
-    with _on_device(logits):
-        st = lib.memspec_op_filter_logits(logits.data_ptr(), ld, rows, vocab, C.byref(f), out.data_ptr(), out_ld,
-                                          _raw_stream(logits, stream))
+        _same_or_apart("out", out, "logits", logits)
+    st = _call_on(dev, stream, lib.memspec_op_filter_logits, logits.data_ptr(), ld, rows, vocab, C.byref(f),
+                  out.data_ptr(), out_ld)
     if st:
         _check(lib, st)
     return out
@@ -573,6 +592,27 @@ def _lora_scratch_bytes(rows: int, n_out: int, k: int, rank: int) -> int:
     return nb.value
 
 
+def _lora_args(x, a, b, ids, scales, ranks, base) -> None:
+    """op_lora's arguments one by one."""
+    _rows_arg("x", x, _BF16)
+    if a.dim() != 3 or b.dim() != 3:
+        raise ValueError("a must be [adapters][rank][k] and b [adapters][n_out][rank]")
+    rows, n, rank, n_out = x.shape[0], a.shape[0], a.shape[1], b.shape[1]
+    if max(a.shape) >= 1 << 31 or max(b.shape) >= 1 << 31:
+        raise ValueError("the adapters are too large")
+    _cuda_arg("a", a, _BF16, (n, rank, x.shape[1]), x)
+    _cuda_arg("b", b, _BF16, (n, n_out, rank), x)
+    _cuda_arg("ids", ids, _I32, (rows,), x)
+    if scales is not None:
+        _cuda_arg("scales", scales, _F32, (n,), x)
+    if ranks is not None:
+        _cuda_arg("ranks", ranks, _I32, (n,), x)
+    if base is not None:
+        _rows_arg("base", base, _F32, x)
+        if base.shape != (rows, n_out):
+            raise ValueError(f"base must be {[rows, n_out]}, not {list(base.shape)}")
+
+
 def op_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, scales: torch.Tensor | None = None,
             ranks: torch.Tensor | None = None, base: torch.Tensor | None = None, y: torch.Tensor | None = None,
             scratch: torch.Tensor | None = None, stream: torch.cuda.Stream | None = None) -> torch.Tensor:
@@ -583,46 +623,54 @@ def op_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor
     ``y`` (fp32, may be `base` itself) receives the result, else a new tensor.
     ``scratch`` (any content) of memspec_op_lora_scratch_bytes bytes saves an allocation."""
     lib = _lib.load()
-    ldx = _rows_arg("x", x, torch.bfloat16)
-    rows, k = x.shape
-    if a.dim() != 3 or b.dim() != 3:
-        raise ValueError("a must be [adapters][rank][k] and b [adapters][n_out][rank]")
-    n_adapters, rank = a.shape[:2]
-    n_out = b.shape[1]
-    _cuda_arg("a", a, torch.bfloat16, (n_adapters, rank, k), x)
-    _cuda_arg("b", b, torch.bfloat16, (n_adapters, n_out, rank), x)
-    _cuda_arg("ids", ids, torch.int32, (rows,), x)
-    f = _lib.Lora(a.data_ptr(), b.data_ptr(), None, None, n_adapters, rank)
-    if scales is not None:
-        _cuda_arg("scales", scales, torch.float32, (n_adapters,), x)
-        f.scales_dev = scales.data_ptr()
-    if ranks is not None:
-        _cuda_arg("ranks", ranks, torch.int32, (n_adapters,), x)
-        f.ranks_dev = ranks.data_ptr()
-    ld_base = 0
-    if base is not None:
-        ld_base = _rows_arg("base", base, torch.float32, x)
-        if base.shape != (rows, n_out):
-            raise ValueError(f"base must be {[rows, n_out]}, not {list(base.shape)}")
+    dev = x.get_device()
+    xs, sa, sb, ld_base = x.shape, a.shape, b.shape, 0
+    fits = dev >= 0 and len(xs) == 2 and len(sa) == 3 and len(sb) == 3
+    if fits:
+        rows, k = xs
+        ldx, one = x.stride()
+        n, rank, _ = sa
+        n_out = sb[1]
+        fits = (x.dtype is _BF16 and one == 1 and ldx >= k and rows <= 256 and k < 1 << 31
+                and sa == (n, rank, k) and a.dtype is _BF16 and a.get_device() == dev and a.is_contiguous()
+                and sb == (n, n_out, rank) and b.dtype is _BF16 and b.get_device() == dev and b.is_contiguous()
+                and n < 1 << 31 and n_out < 1 << 31
+                and ids.shape == (rows,) and ids.dtype is _I32 and ids.get_device() == dev and ids.is_contiguous()
+                and (scales is None or scales.shape == (n,) and scales.dtype is _F32 and scales.get_device() == dev
+                     and scales.is_contiguous())
+                and (ranks is None or ranks.shape == (n,) and ranks.dtype is _I32 and ranks.get_device() == dev
+                     and ranks.is_contiguous()))
+        if fits and base is not None:
+            ld_base, one = base.stride() if base.dim() == 2 else (0, 0)
+            fits = (base.shape == (rows, n_out) and one == 1 and ld_base >= n_out and base.dtype is _F32
+                    and base.get_device() == dev)
+    if not fits:    # refused, or a tensor of one row or column with a stride of its own
+        _lora_args(x, a, b, ids, scales, ranks, base)
+        (rows, k), (n, rank, _), n_out = xs, sa, sb[1]
+        ldx = _rows_arg("x", x, _BF16)
+        ld_base = 0 if base is None else _rows_arg("base", base, _F32)
     if y is None:
-        y = torch.empty((rows, n_out), dtype=torch.float32, device=x.device)
+        y = torch.empty((rows, n_out), dtype=_F32, device=x.device)
         _used_on(stream, y)
-    ldy = _rows_arg("y", y, torch.float32, x)
-    if y.shape != (rows, n_out):
-        raise ValueError(f"y must be {[rows, n_out]}, not {list(y.shape)}")
-    if base is not None and base is not y and _overlap(base, y) and \
-            (base.data_ptr(), base.stride()) != (y.data_ptr(), y.stride()):
-        raise ValueError("y overlaps base without being the same rows")
-    nb = _lora_scratch_bytes(rows, n_out, k, rank)
+        ldy = n_out
+    elif y is base:
+        ldy = ld_base
+    else:
+        ldy = _rows_arg("y", y, _F32, x)
+        if y.shape != (rows, n_out):
+            raise ValueError(f"y must be {[rows, n_out]}, not {list(y.shape)}")
+        if base is not None:
+            _same_or_apart("y", y, "base", base)
     if scratch is None:
-        scratch = torch.empty(nb, dtype=torch.uint8, device=x.device)
+        scratch = torch.empty(_lora_scratch_bytes(rows, n_out, k, rank), dtype=torch.uint8, device=x.device)
         _used_on(stream, scratch)
-    elif not scratch.is_cuda or scratch.device != x.device or not scratch.is_contiguous():
+    elif scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be contiguous on {x.device}")
-    with _on_device(x):
-        st = lib.memspec_op_lora(C.byref(f), x.data_ptr(), ldx, ids.data_ptr(),
-                                 None if base is None else base.data_ptr(), ld_base, y.data_ptr(), ldy, rows, n_out,
-                                 k, scratch.data_ptr(), scratch.nbytes, _raw_stream(x, stream))
+    f = _lib.Lora(a.data_ptr(), b.data_ptr(), None if scales is None else scales.data_ptr(),
+                  None if ranks is None else ranks.data_ptr(), n, rank)
+    st = _call_on(dev, stream, lib.memspec_op_lora, C.byref(f), x.data_ptr(), ldx, ids.data_ptr(),
+                  None if base is None else base.data_ptr(), ld_base, y.data_ptr(), ldy, rows, n_out, k,
+                  scratch.data_ptr(), scratch.nbytes)
     if st:
         _check(lib, st)
     return y
