@@ -7,13 +7,24 @@
 // with weight >= min_p of the largest.  So a rule's result is a cut (key, id): an id is
 // kept if its logit's key is larger, or equal and its id not above the cut's.
 //
-// One CTA per row: the cut's key by a radix search, 8 bits a pass, over counts (top-k) or
-// over sums of weights (top-p); the sums are integers, so their comparisons are exact
-// whatever the order in which the atomics add.
+// A cluster of C = 1, 2, 4 or 8 CTAs per row; each keeps its slice of the row in shared
+// memory, so that the row is read once however many passes its rule takes:
+//   1. load, maximum;
+//   2. a search per part (top-k, then top-p among what top-k left): a histogram of the
+//      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
+//      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
+//      bins through distributed shared memory to find the bin with the cut; its elements are
+//      listed and each counted against the others.  A bin with more elements than the list
+//      takes (flat rows, many equal logits) is divided by key as often as it needs;
+//      a single key, by id;
+//   3. the draw: the kept weights' sums slice by slice, then warp by warp; or the mask.
+// Every CTA of a cluster takes the same decisions from the same numbers, so no result is
+// passed back but an id among more equal logits than the list takes.
 #include <cuda_runtime.h>
 
 #include <math.h>
 
+#include <atomic>
 #include <string>
 
 #include "../../include/memspec_ops.h"
@@ -34,15 +45,45 @@ typedef unsigned long long u64;
 // NaN as -inf, +inf as the largest finite number.
 __device__ __forceinline__ float sane(float z) { return z == z ? fminf(z, kLargest) : -INFINITY; }
 
-struct Smem {
+constexpr int kMaxCluster = 8;
+constexpr int kMantissa = 4;                 // bins per octave of depth: 2^4
+constexpr int kBins = 16 << kMantissa;       // depths 2^-10 .. 2^6, clamped
+constexpr int kSupers = kBins / 32;          // groups of 32 bins
+constexpr uint32_t kList = kBins * 3 / 4;         // list entries: the pulled list and its weights take
+                                             // the histogram's place
+
+struct alignas(16) Smem {
   u64 table[kExpSteps];
-  u64 hist[256];
+  union {
+    struct {
+      uint32_t cnt[kBins], lo[kBins], hi[kBins];   // count, sum of weights in two words
+    } h;
+    struct {
+      u64 entry[kList], weight[kList];
+    } all;                                   // the cluster's list
+  };
+  union {
+    u64 list[kList];                         // this CTA's: (~key << 32) | id
+    struct {                                 // find_bin: the sums of all CTAs
+      u64 mass[kMaxCluster][32];
+      uint32_t cnt[kMaxCluster][32];
+    } p;
+  };
+  // sums of this CTA, read by the others
+  uint32_t sup_cnt[kSupers];
+  u64 sup_mass[kSupers];
+  u64 tail;
+  uint32_t n_list;
+  u64 p_tail[kMaxCluster];                   // of all CTAs
+  float peer_max[kMaxCluster];               // pushed
+  u64 peer_sum[kMaxCluster];                 // pushed
   u64 scan[kWarps];
   float wmax[kWarps];
-  u64 found_before;
-  int found;
-  int pick;
+  uint32_t tie_id;                           // pushed
+  u64 cut;
 };
+static_assert(3 * (sizeof(Smem) + 16388 * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
+static_assert(sizeof(u64) * 2 * kList <= sizeof(uint32_t) * 3 * kBins, "the list fits the histogram's place");
 
 // A row's rule, with what "off" means resolved.
 struct Rule {
@@ -59,118 +100,374 @@ __device__ __forceinline__ Rule rule_of(const FilterArgs& a, int row) {
   if (!(r.temperature > 0.f)) {   // greedy: the first id of the largest logit
     r.temperature = 1.f;
     r.top_k = 1;
+    r.top_p = 1.f;
+    r.min_p = 0.f;
   }
   return r;
 }
 
-// Exclusive scan of one u64 per thread; *total gets the sum.
-__device__ u64 block_scan(u64 v, u64* scratch, u64* total) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  u64 incl = v;
+__device__ __forceinline__ u64 warp_sum(u64 v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ u64 warp_scan(u64 v) {   // inclusive
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const u64 n = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += n;
+    const u64 n = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += n;
   }
+  return v;
+}
+__device__ u64 block_sum(u64 v, u64* scratch) {
+  v = warp_sum(v);
   __syncthreads();
-  if (lane == 31) scratch[w] = incl;
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
   __syncthreads();
-  u64 before = 0, all = 0;
-  for (int i = 0; i < kWarps; ++i) {
-    if (i < w) before += scratch[i];
-    all += scratch[i];
-  }
-  *total = all;
-  return before + incl - v;
+  u64 s = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) s += scratch[i];
+  return s;
+}
+// All threads of the cluster: what they wrote before is read after.
+__device__ __forceinline__ void cluster_sync() {
+  cluster_arrive_release();
+  cluster_wait_acquire();
 }
 
-// The smallest prefix of the row's order whose sum of val(z) reaches `need` (1 <= need <=
-// the sum over the row): its last id's key, and in *before the sum over larger keys.
-template <class Val>
-__device__ uint32_t find_key(const float* z, int V, u64 need, Val val, Smem& sm, u64* before) {
-  uint32_t prefix = 0;
-  u64 above = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += kThreads) sm.hist[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < V; i += kThreads) {
-      const float x = sane(z[i]);
-      const uint32_t key = logit_key(x);
-      if (shift < 24 && (key >> (shift + 8)) != prefix) continue;
-      const u64 v = x == -INFINITY ? 0 : val(x);
-      if (v != 0) atomicAdd(&sm.hist[(key >> shift) & 255], v);
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      u64 sum = above;
-      int d = 255;
-      while (d > 0 && sum + sm.hist[d] < need) sum += sm.hist[d--];
-      sm.found = d;
-      sm.found_before = sum;
-    }
-    __syncthreads();
-    prefix = (prefix << 8) | static_cast<uint32_t>(sm.found);
-    above = sm.found_before;
-    __syncthreads();
+// The cut after the last kept id of a row's order: (~key << 32) | id; entries up to it are kept.
+__device__ __forceinline__ u64 entry_of(uint32_t key, uint32_t id) {
+  return (static_cast<u64>(~key) << 32) | id;
+}
+
+// A CTA's slice of a row in shared memory: ids base .. base + len - 1, -inf where there is
+// none.  Element i of the slice is held by nobody in particular: passes deal float4s.
+struct Slice {
+  float* z;
+  int base, len;            // len a multiple of 4
+};
+
+struct Part {               // one search: what it looks at and for
+  bool mass;                // top-p: `need` is a fraction of the sum; else a count
+  u64 need;
+  float scale;              // depth = (max - z) * scale
+  float max, deepest;       // elements deeper than `deepest` are not the cut (only their weight counts)
+  u64 within;               // entries up to this one take part
+};
+
+__device__ __forceinline__ int bin_of(float depth) {
+  const int b = static_cast<int>(__float_as_uint(depth) >> (23 - kMantissa)) - ((127 - 10) << kMantissa);
+  return max(0, min(b, kBins - 1));
+}
+
+// A histogram's bin that holds the cut, by the same steps in every CTA of the cluster.
+struct Found {
+  int bin;
+  u64 above;                // sum (count or mass) before the bin
+  uint32_t count;           // elements in it
+  u64 need;                 // what the prefix has to reach
+  bool all;                 // the whole set does not exceed it (a count): nothing is cut
+};
+
+// After the histogram of every CTA is complete and the cluster has synchronised.
+__device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) {
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  Found f;
+  // the groups' sums of all CTAs
+  if (tid < C * kSupers) {
+    const int peer = tid / kSupers, g = tid % kSupers;
+    sm.p.cnt[peer][g] = ld_cluster_u32(mapa_shared(smem_addr(&sm.sup_cnt[g]), peer));
+    if (p.mass) sm.p.mass[peer][g] = ld_cluster_u64(mapa_shared(smem_addr(&sm.sup_mass[g]), peer));
   }
-  *before = above;
-  return prefix;
+  if (p.mass && first && tid < C) sm.p_tail[tid] = ld_cluster_u64(mapa_shared(smem_addr(&sm.tail), tid));
+  __syncthreads();
+  u64 v = 0, tail = 0;
+  if (lane < kSupers)
+    for (int c = 0; c < C; ++c) v += p.mass ? sm.p.mass[c][lane] : sm.p.cnt[c][lane];
+  u64 incl = warp_scan(v);
+  const u64 total = __shfl_sync(0xffffffffu, incl, 31);
+  if (p.mass && first) {
+    for (int c = 0; c < C; ++c) tail += sm.p_tail[c];
+    const u64 s = total + tail, part = need * s;          // the fraction times the sum, rounded up
+    need = __umul64hi(need, s) + (part != 0 ? 1 : 0);
+    if (need == 0) need = 1;
+  }
+  f.need = need;
+  f.all = !p.mass && need >= total;
+  const unsigned reach = __ballot_sync(0xffffffffu, lane < kSupers && incl >= need);
+  const int g = reach ? __ffs(reach) - 1 : kSupers - 1;
+  const u64 before = __shfl_sync(0xffffffffu, incl - v, g);
+  __syncthreads();                                        // p is read
+  if (w < C) {
+    sm.p.cnt[w][lane] = ld_cluster_u32(mapa_shared(smem_addr(&sm.h.cnt[g * 32 + lane]), w));
+    if (p.mass)
+      sm.p.mass[w][lane] = ld_cluster_u32(mapa_shared(smem_addr(&sm.h.lo[g * 32 + lane]), w)) |
+                           (static_cast<u64>(ld_cluster_u32(mapa_shared(smem_addr(&sm.h.hi[g * 32 + lane]), w))) << 32);
+  }
+  __syncthreads();
+  uint32_t n = 0;
+  v = 0;
+  for (int c = 0; c < C; ++c) {
+    n += sm.p.cnt[c][lane];
+    if (p.mass) v += sm.p.mass[c][lane];
+  }
+  if (!p.mass) v = n;
+  incl = before + warp_scan(v);
+  const unsigned hit = __ballot_sync(0xffffffffu, incl >= need);
+  const int b = hit ? __ffs(hit) - 1 : 31;
+  f.bin = g * 32 + b;
+  f.above = __shfl_sync(0xffffffffu, incl - v, b);
+  f.count = __shfl_sync(0xffffffffu, n, b);
+  return f;
+}
+
+template <class Each>
+__device__ __forceinline__ void for_slice(const Slice& s, Each each) {
+  const float4* z4 = reinterpret_cast<const float4*>(s.z);
+  for (int i = threadIdx.x; i < s.len / 4; i += kThreads) {
+    const float4 v = z4[i];
+    each(v.x, s.base + 4 * i);
+    each(v.y, s.base + 4 * i + 1);
+    each(v.z, s.base + 4 * i + 2);
+    each(v.w, s.base + 4 * i + 3);
+  }
+}
+
+__device__ __forceinline__ void add_mass(Smem& sm, int bin, u64 w) {
+  const uint32_t lo = static_cast<uint32_t>(w);
+  const uint32_t old = atomicAdd(&sm.h.lo[bin], lo);
+  const uint32_t hi = static_cast<uint32_t>(w >> 32) + (old + lo < old ? 1u : 0u);
+  if (hi != 0) atomicAdd(&sm.h.hi[bin], hi);
+}
+__device__ void clear_histogram(Smem& sm) {
+  uint32_t* h = reinterpret_cast<uint32_t*>(&sm.h);
+  for (int i = threadIdx.x; i < static_cast<int>(sizeof(sm.h) / 4); i += kThreads) h[i] = 0;
+  __syncthreads();
+}
+// The groups' sums of this CTA's histogram, then the cluster's barrier.
+__device__ void close_histogram(const Part& p, Smem& sm) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  __syncthreads();
+  for (int g = w; g < kSupers; g += kWarps) {
+    const uint32_t n = __reduce_add_sync(0xffffffffu, sm.h.cnt[g * 32 + lane]);
+    u64 m = 0;
+    if (p.mass) m = warp_sum(sm.h.lo[g * 32 + lane] | (static_cast<u64>(sm.h.hi[g * 32 + lane]) << 32));
+    if (lane == 0) {
+      sm.sup_cnt[g] = n;
+      sm.sup_mass[g] = m;
+    }
+  }
+  cluster_sync();
+}
+
+// The entry at which the prefix that p asks for ends.
+template <class Mass>
+__device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass, Smem& sm) {
+  const int tid = threadIdx.x;
+  auto depth = [&](float z) { return (p.max - z) * p.scale; };
+  auto takes_part = [&](float z, int id) {
+    return z > -INFINITY && entry_of(logit_key(z), static_cast<uint32_t>(id)) <= p.within;
+  };
+  const bool whole = p.within == ~0ull;
+  clear_histogram(sm);
+  if (tid == 0) {
+    sm.n_list = 0;
+    sm.cut = p.within;
+  }
+  u64 tail = 0;
+  for_slice(s, [&](float z, int id) {
+    if (whole ? z == -INFINITY : !takes_part(z, id)) return;
+    const float d = depth(z);
+    const u64 w = p.mass ? mass(z) : 0;
+    if (d > p.deepest) {
+      tail += w;
+      return;
+    }
+    const int b = bin_of(d);
+    atomicAdd(&sm.h.cnt[b], 1u);
+    if (p.mass) add_mass(sm, b, w);
+  });
+  if (p.mass) {
+    tail = block_sum(tail, sm.scan);
+    if (tid == 0) sm.tail = tail;
+  }
+  close_histogram(p, sm);
+  Found f = find_bin(p, true, p.need, C, sm);
+  if (f.all) {
+    cluster_sync();           // the others have read this CTA's histogram
+    return p.within;
+  }
+  const int bin = f.bin;
+  // the keys that the bin's elements can have: those of its depths with a margin
+  uint32_t k_lo = 0, k_hi = ~0u;
+  int shift = 32;
+  auto in_bin = [&](float z, int id) {
+    if (whole ? z == -INFINITY : !takes_part(z, id)) return false;
+    const float d = depth(z);
+    if (d > p.deepest || bin_of(d) != bin) return false;
+    const uint32_t k = logit_key(z);
+    return k >= k_lo && k <= k_hi;
+  };
+  auto narrow = [&] {         // to the keys of bin f.bin of the last division
+    k_hi -= static_cast<uint32_t>(f.bin) << shift;
+    if (k_hi - k_lo >= 1u << shift) k_lo = k_hi - ((1u << shift) - 1);
+  };
+  u64 above = f.above;
+  while (f.count > kList) {
+    if (shift == 32) {
+      const float a0 = bin == 0 ? 0.f : __uint_as_float(static_cast<uint32_t>(bin + ((127 - 10) << kMantissa)) << (23 - kMantissa));
+      const float a1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + ((127 - 10) << kMantissa)) << (23 - kMantissa));
+      // z = max - depth / scale, off by some units in the last place of the larger term
+      const float z1 = p.max - a0 / p.scale, z0 = p.max - a1 / p.scale;
+      const float slack = 4e-7f * (fabsf(p.max) + fabsf(z0)) + 1e-37f;
+      k_hi = bin == 0 || !(z1 + slack < p.max) ? logit_key(p.max) : logit_key(z1 + slack);
+      k_lo = bin == kBins - 1 || !(z0 - slack > -kLargest) ? logit_key(-kLargest) : logit_key(z0 - slack);
+      shift = max(0, 32 - __clz(k_hi - k_lo) - (4 + kMantissa));
+    } else {   // the next division of [k_lo, k_hi]
+      if (shift == 0) break;
+      narrow();
+      shift = max(0, shift - (4 + kMantissa));
+    }
+    cluster_sync();           // the others have read this CTA's histogram
+    clear_histogram(sm);
+    for_slice(s, [&](float z, int id) {
+      if (!in_bin(z, id)) return;
+      const int b = static_cast<int>((k_hi - logit_key(z)) >> shift);
+      atomicAdd(&sm.h.cnt[b], 1u);
+      if (p.mass) add_mass(sm, b, mass(z));
+    });
+    close_histogram(p, sm);
+    f = find_bin(p, false, f.need - above, C, sm);
+    f.need += above;
+    above += f.above;
+  }
+  if (shift < 32) narrow();
+  if (f.count > kList) {      // one key: which of its ids
+    const u64 one = p.mass ? mass(key_logit(k_hi)) : 1;
+    u64 left = (f.need - above + one - 1) / one;       // so many of them, in all CTAs
+    // the bin's counts of the CTAs are still in sm.p
+    int owner = 0;
+    while (owner < C - 1 && left > sm.p.cnt[owner][f.bin & 31]) left -= sm.p.cnt[owner++][f.bin & 31];
+    if (owner == rank) {
+      // element order is id order: contiguous parts of the slice per thread
+      const int per = (s.len + kThreads - 1) / kThreads, lo = min(tid * per, s.len), hi = min(lo + per, s.len);
+      u64 n = 0;
+      for (int i = lo; i < hi; ++i) n += in_bin(s.z[i], s.base + i);
+      const u64 incl = warp_scan(n);
+      if ((tid & 31) == 31) sm.scan[tid >> 5] = incl;
+      __syncthreads();
+      u64 before = incl - n;
+      for (int i = 0; i < (tid >> 5); ++i) before += sm.scan[i];
+      if (before < left && left <= before + n) {
+        u64 seen = before;
+        for (int i = lo; i < hi; ++i)
+          if (in_bin(s.z[i], s.base + i) && ++seen == left) {
+            for (int c = 0; c < C; ++c)
+              st_cluster_u32(mapa_shared(smem_addr(&sm.tie_id), c), static_cast<uint32_t>(s.base + i));
+            break;
+          }
+      }
+    }
+    cluster_sync();
+    const u64 cut = entry_of(k_hi, sm.tie_id);
+    __syncthreads();
+    return cut;
+  }
+  __syncthreads();            // sm.p, in the list's place, is read
+  for_slice(s, [&](float z, int id) {
+    if (!in_bin(z, id)) return;
+    const uint32_t i = atomicAdd(&sm.n_list, 1u);
+    if (i < kList) sm.list[i] = entry_of(logit_key(z), static_cast<uint32_t>(id));
+  });
+  cluster_sync();
+  // every CTA takes the whole list (the histogram's place: nobody reads that any more)
+  uint32_t off = 0;
+  for (int c = 0; c < C; ++c) {
+    const uint32_t n = min(ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), c)), kList - off);
+    for (uint32_t i = tid; i < n; i += kThreads) {
+      const u64 e = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), c));
+      sm.all.entry[off + i] = e;
+      sm.all.weight[off + i] = p.mass ? mass(key_logit(~static_cast<uint32_t>(e >> 32))) : 1;
+    }
+    off += n;
+  }
+  __syncthreads();
+  for (uint32_t i = tid; i < off; i += kThreads) {
+    const u64 e = sm.all.entry[i], own = sm.all.weight[i];
+    u64 before = above;
+    for (uint32_t j = 0; j < off; ++j)
+      if (sm.all.entry[j] < e) before += sm.all.weight[j];
+    if (before < f.need && f.need <= before + own) sm.cut = e;
+  }
+  __syncthreads();
+  const u64 cut = sm.cut;
+  cluster_sync();             // the others have read this CTA's list
+  return cut;
 }
 
 template <bool kMask>
-__global__ void __launch_bounds__(kThreads) filter_kernel(const __grid_constant__ FilterArgs a) {
-  __shared__ Smem sm;
-  const int row = blockIdx.x, tid = threadIdx.x, V = a.vocab;
+__global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_constant__ FilterArgs a, int C, int len) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  Smem& sm = *reinterpret_cast<Smem*>(raw);
+  Slice s;
+  s.z = reinterpret_cast<float*>(raw + sizeof(Smem));
+  s.len = len;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int rank = static_cast<int>(cluster_ctarank()), row = blockIdx.x / C, V = a.vocab;
+  for (int i = tid; i < kExpSteps; i += kThreads) sm.table[i] = exp_table()[i];
+  cluster_arrive_release();   // waited for before the first push
   pdl_wait();
   pdl_launch_dependents();
   const float* z = a.logits + row * a.ld;
+  // ids are shifted so that the slice's float4s are aligned in memory
+  const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) >> 2) & 3);
+  s.base = rank * len - shift;
   const Rule r = rule_of(a, row);
-  for (int i = tid; i < kExpSteps; i += kThreads) sm.table[i] = exp_table()[i];
+  // ------------------------------------------------ load, maximum
   float m = -INFINITY;
-  for (int i = tid; i < V; i += kThreads) m = fmaxf(m, sane(z[i]));
+#pragma unroll 8
+  for (int i = tid; i < len / 4; i += kThreads) {
+    const int x = s.base + 4 * i;
+    float4 v;
+    if (x >= 0 && x + 3 < V) {
+      v = __ldcg(reinterpret_cast<const float4*>(z + x));
+    } else {
+      v.x = x >= 0 && x < V ? __ldcg(z + x) : -INFINITY;
+      v.y = x + 1 >= 0 && x + 1 < V ? __ldcg(z + x + 1) : -INFINITY;
+      v.z = x + 2 >= 0 && x + 2 < V ? __ldcg(z + x + 2) : -INFINITY;
+      v.w = x + 3 >= 0 && x + 3 < V ? __ldcg(z + x + 3) : -INFINITY;
+    }
+    v.x = sane(v.x);
+    v.y = sane(v.y);
+    v.z = sane(v.z);
+    v.w = sane(v.w);
+    m = fmaxf(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), m);
+    reinterpret_cast<float4*>(s.z)[i] = v;
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if ((tid & 31) == 0) sm.wmax[tid >> 5] = m;
+  if (lane == 0) sm.wmax[w] = m;
   __syncthreads();
+#pragma unroll
   for (int i = 0; i < kWarps; ++i) m = fmaxf(m, sm.wmax[i]);
+  cluster_wait_acquire();
+  if (tid < C) st_cluster_u32(mapa_shared(smem_addr(&sm.peer_max[rank]), tid), __float_as_uint(m));
+  cluster_sync();
+  for (int c = 0; c < C; ++c) m = fmaxf(m, sm.peer_max[c]);
+  // ------------------------------------------------ the cut
   const bool empty = m == -INFINITY;
   const WeightScale ws = weight_scale(m, r.temperature);
   auto mass = [&](float x) { return weight(x, ws, sm.table); };
-  // the cut: keys above `key`, and the first `ties` ids of it
-  uint32_t key = logit_key(-kLargest);
-  u64 ties = ~0ull;
+  u64 cut = entry_of(logit_key(-kLargest), ~0u);
   if (!empty) {
-    if (r.top_k > 0 && r.top_k < V) {
-      u64 live = 0, n, before;
-      for (int i = tid; i < V; i += kThreads) live += sane(z[i]) > -INFINITY;
-      block_scan(live, sm.scan, &n);
-      if (static_cast<u64>(r.top_k) < n) {
-        key = find_key(z, V, r.top_k, [](float) { return 1ull; }, sm, &before);
-        ties = r.top_k - before;
-      }
-    }
+    if (r.top_k > 0 && r.top_k < V)
+      cut = min(cut, search(Part{false, static_cast<u64>(r.top_k), 1.f, m, INFINITY, ~0ull}, s, C, rank, mass, sm));
     if (r.top_p < 1.f) {
-      u64 mine = 0, at = 0, sum, n_at;
-      for (int i = tid; i < V; i += kThreads) {
-        const float x = sane(z[i]);
-        const uint32_t k = logit_key(x);
-        if (x > -INFINITY && k > key) mine += mass(x);
-        at += k == key;
-      }
-      block_scan(mine, sm.scan, &sum);
-      block_scan(at, sm.scan, &n_at);
-      const u64 one = mass(key_logit(key));
-      sum += (ties < n_at ? ties : n_at) * one;
-      const u64 f = fraction64(r.top_p);
-      u64 need = __umul64hi(f, sum) + (f * sum != 0 ? 1 : 0);
-      if (need == 0) need = 1;
-      u64 before;
-      const uint32_t kp = find_key(z, V, need, mass, sm, &before);
-      const u64 w = mass(key_logit(kp)), t = (need - before + w - 1) / w;
-      if (kp > key || (kp == key && t < ties)) {
-        key = kp;
-        ties = t;
-      }
+      // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
+      const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
+      const bool whole = cut == entry_of(logit_key(-kLargest), ~0u);
+      cut = min(cut, search(Part{true, fraction64(r.top_p), ws.hi, m, deepest, whole ? ~0ull : cut}, s, C, rank, mass, sm));
     }
     if (r.min_p > 0.f) {
       // the least float z with (z - max) / T >= log(min_p)
@@ -178,51 +475,93 @@ __global__ void __launch_bounds__(kThreads) filter_kernel(const __grid_constant_
                        static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
       float cf = static_cast<float>(c);
       if (static_cast<double>(cf) < c) cf = nextafterf(cf, INFINITY);
-      const uint32_t km = logit_key(fmaxf(fminf(cf, m), -kLargest));
-      if (km > key) {
-        key = km;
-        ties = ~0ull;
-      }
+      cut = min(cut, entry_of(logit_key(fmaxf(fminf(cf, m), -kLargest)), ~0u));
     }
   }
-  // the ids in order: which ties are kept, the running sum of kept weights
-  const int per = (V + kThreads - 1) / kThreads;
-  const int lo = min(tid * per, V), hi = min(lo + per, V);
-  u64 at = 0, n_at;
-  for (int i = lo; i < hi; ++i) at += logit_key(sane(z[i])) == key;
-  u64 seen = block_scan(at, sm.scan, &n_at);
-  auto kept = [&](float x, u64& seen) {
-    if (x == -INFINITY) return false;
-    const uint32_t k = logit_key(x);
-    return k > key || (k == key && seen++ < ties);
-  };
-  if (kMask) {
+  const float cut_z = key_logit(~static_cast<uint32_t>(cut >> 32));
+  const uint32_t cut_id = static_cast<uint32_t>(cut);
+  auto kept = [&](float x, int id) { return x > cut_z || (x == cut_z && static_cast<uint32_t>(id) <= cut_id); };
+  if constexpr (kMask) {
     float* out = a.out + row * a.out_ld;
-    for (int i = lo; i < hi; ++i) {
-      const float x = sane(z[i]);
-      out[i] = kept(x, seen) ? x : -INFINITY;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(out) >> 2) & 3) == static_cast<uintptr_t>(shift);
+    for (int i = tid; i < len / 4; i += kThreads) {
+      const int x = s.base + 4 * i;
+      const float4 v = reinterpret_cast<const float4*>(s.z)[i];
+      const float4 o = make_float4(kept(v.x, x) ? v.x : -INFINITY, kept(v.y, x + 1) ? v.y : -INFINITY,
+                                   kept(v.z, x + 2) ? v.z : -INFINITY, kept(v.w, x + 3) ? v.w : -INFINITY);
+      if (aligned && x >= 0 && x + 3 < V) {
+        *reinterpret_cast<float4*>(out + x) = o;
+      } else {
+        if (x >= 0 && x < V) out[x] = o.x;
+        if (x + 1 >= 0 && x + 1 < V) out[x + 1] = o.y;
+        if (x + 2 >= 0 && x + 2 < V) out[x + 2] = o.z;
+        if (x + 3 >= 0 && x + 3 < V) out[x + 3] = o.w;
+      }
     }
     return;
   }
-  u64 mine = 0, total, s2 = seen;
-  for (int i = lo; i < hi; ++i) {
-    const float x = sane(z[i]);
-    if (kept(x, s2)) mine += mass(x);
-  }
-  const u64 before = block_scan(mine, sm.scan, &total);
-  const u64 target = __umul64hi(fraction64(a.u[row]), total);
-  if (empty) {
-    if (tid == 0) a.out_tok[row] = -1;
-  } else if (before <= target && target < before + mine) {
-    u64 sum = before;
-    for (int i = lo; i < hi; ++i) {
-      const float x = sane(z[i]);
-      if (kept(x, seen)) sum += mass(x);
-      if (sum > target) {
-        a.out_tok[row] = i;
-        break;
-      }
+  // ------------------------------------------------ the draw
+  // a warp's part of the slice: whole 128-id tiles, in id order
+  const int tiles = (len + 127) / 128, per = (tiles + kWarps - 1) / kWarps;
+  const int t_lo = min(w * per, tiles), t_hi = min(t_lo + per, tiles);
+  auto tile_weights = [&](int t, u64 (&wt)[4]) {   // false: none of the tile is kept
+    const int i = t * 128 + lane * 4;
+    float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (i < len) v = *reinterpret_cast<const float4*>(s.z + i);
+    const int x = s.base + i;
+    const bool k0 = kept(v.x, x), k1 = kept(v.y, x + 1), k2 = kept(v.z, x + 2), k3 = kept(v.w, x + 3);
+    if (!__any_sync(0xffffffffu, k0 || k1 || k2 || k3)) return false;
+    wt[0] = k0 ? mass(v.x) : 0;
+    wt[1] = k1 ? mass(v.y) : 0;
+    wt[2] = k2 ? mass(v.z) : 0;
+    wt[3] = k3 ? mass(v.w) : 0;
+    return true;
+  };
+  u64 mine = 0;
+  if (!empty)
+    for (int t = t_lo; t < t_hi; ++t) {
+      u64 wt[4];
+      if (tile_weights(t, wt)) mine += wt[0] + wt[1] + wt[2] + wt[3];
     }
+  mine = warp_sum(mine);
+  __syncthreads();
+  if (lane == 0) sm.scan[w] = mine;
+  __syncthreads();
+  u64 slice = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    if (i < w) before += sm.scan[i];
+    slice += sm.scan[i];
+  }
+  if (tid < C) st_cluster_u64(mapa_shared(smem_addr(&sm.peer_sum[rank]), tid), slice);
+  cluster_sync();
+  u64 total = 0;
+  for (int c = 0; c < C; ++c) {
+    if (c < rank) before += sm.peer_sum[c];
+    total += sm.peer_sum[c];
+  }
+  if (empty) {
+    if (rank == 0 && tid == 0) a.out_tok[row] = -1;
+    return;
+  }
+  const u64 target = __umul64hi(fraction64(a.u[row]), total);
+  if (!(before <= target && target < before + mine)) return;   // another warp's
+  for (int t = t_lo; t < t_hi; ++t) {
+    u64 wt[4];
+    if (!tile_weights(t, wt)) continue;
+    const u64 own = wt[0] + wt[1] + wt[2] + wt[3];
+    const u64 incl = before + warp_scan(own);
+    const u64 end = __shfl_sync(0xffffffffu, incl, 31);
+    if (target < end) {
+      u64 sum = incl - own;
+      if (sum <= target && target < incl) {
+        int q = 0;
+        while (q < 3 && sum + wt[q] <= target) sum += wt[q++];
+        a.out_tok[row] = s.base + t * 128 + lane * 4 + q;
+      }
+      return;
+    }
+    before = end;
   }
 }
 
@@ -230,17 +569,40 @@ __global__ void __launch_bounds__(kThreads) filter_kernel(const __grid_constant_
 
 cudaError_t launch_filter(const FilterArgs& a, cudaStream_t s, bool pdl) {
   if (a.vocab > kMaxVocab) return cudaErrorInvalidValue;
+  // as many CTAs per row as its slices need, more while the launch is small
+  constexpr int kMaxSlice = 16388;           // floats: three CTAs per SM
+  int C = 1;
+  while (C < kMaxCluster &&
+         ((a.vocab + 3 + C - 1) / C > kMaxSlice - 3 || (a.rows * C * 2 <= 304 && a.vocab >= 2 * C * 2048)))
+    C *= 2;
+  const int len = ((a.vocab + 3 + C - 1) / C + 3) / 4 * 4;
+  static std::atomic<bool> set[2][64];
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.rows));
+  cfg.gridDim = dim3(static_cast<unsigned>(a.rows) * C);
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem) + static_cast<size_t>(len) * 4;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const bool mask = a.out != nullptr;
+  if (e == cudaSuccess && (dev >= 64 || !set[mask][dev].load(std::memory_order_relaxed))) {
+    const int most = static_cast<int>(sizeof(Smem) + kMaxSlice * 4);
+    e = mask ? cudaFuncSetAttribute(filter_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)
+             : cudaFuncSetAttribute(filter_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess && dev < 64) set[mask][dev].store(true, std::memory_order_relaxed);
+  }
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = pdl ? 1 : 0;
-  return a.out != nullptr ? cudaLaunchKernelEx(&cfg, filter_kernel<true>, a)
-                          : cudaLaunchKernelEx(&cfg, filter_kernel<false>, a);
+  cfg.numAttrs = pdl ? 2 : 1;
+  return mask ? cudaLaunchKernelEx(&cfg, filter_kernel<true>, a, C, len)
+              : cudaLaunchKernelEx(&cfg, filter_kernel<false>, a, C, len);
 }
 
 namespace {
