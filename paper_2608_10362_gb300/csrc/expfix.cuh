@@ -1,11 +1,12 @@
 // expfix.cuh - softmax weights as 64-bit fixed-point integers.
 //
-// weight(z) = round(2^43 * exp((z - max) / T)): off by at most 2^-44 of the largest weight
-// and, relative to itself, 2^-31.8 (2^-34.4 in the mean square).  Integers add up to the same sum in any order, so
+// weight(z) = 2^46 * exp((z - max) / T) as an odd integer: off by at most 2^-46 of the
+// largest weight and, relative to itself, 2^-32.5 (2^-34.7 in the mean square); 0 below
+// 2^-45.  Integers add up to the same sum in any order, so
 // thousands of threads may sum them as they come and every comparison of sums (does this
 // prefix hold p of the mass? does the running sum pass u times the total?) is exact; with
 // 32-bit floating-point sums one draw in a few hundred lands within a rounding of a border
-// between two ids (25 of 11232 in sampling.cu's kernel).  131072 weights stay below 2^61.
+// between two ids (25 of 11232 in sampling.cu's kernel).  131072 weights stay below 2^63 + 2^17.
 //
 // exp by a table of 2^(i/256) and a cubic for the rest (the table-driven scheme of
 // P. T. P. Tang, ACM TOMS 15 (1989)): y = (z - max) log2(e) / T as an unevaluated sum of
@@ -19,8 +20,8 @@
 namespace memspec {
 
 constexpr int kExpSteps = 256;
-constexpr int kExpBits = 39;       // table entries: 2^39 * 2^(i/256)
-constexpr int kWeightBits = 43;    // weight of the maximum: 2^43
+constexpr int kExpBits = 62;       // table entries: 2^62 * 2^(i/256)
+constexpr int kWeightBits = 46;    // weight of the maximum: 2^46
 
 struct ExpTable {
   unsigned long long v[kExpSteps];
@@ -37,7 +38,7 @@ constexpr ExpTable make_exp_table() {
   for (int i = 0; i < 8; ++i) base = newton_sqrt(base);
   double x = 1.0;
   for (int i = 0; i < kExpSteps; ++i) {
-    t.v[i] = static_cast<unsigned long long>(x * 549755813888.0 + 0.5);   // 2^39
+    t.v[i] = static_cast<unsigned long long>(x * 4611686018427387904.0);   // 2^62
     x *= base;
   }
   return t;
@@ -75,19 +76,19 @@ __device__ __forceinline__ unsigned long long weight(float z, const WeightScale&
   const float b = d - s.max;
   const float e = (s.max - (d - b)) - (z + b);
   const float yh = d * s.hi;
-  if (!(yh < 44.f)) return 0;     // below 2^-44 of the maximum; z = -inf (yh inf or NaN)
   const float yl = fmaf(d, s.hi, -yh) + fmaf(d, s.lo, e * s.hi);
-  const float n = rintf(yh * -256.f);
-  const float f = fmaf(n, -1.f / 256.f, -yh) - yl;       // exact but for the subtraction of yl
+  // n = round(-256 yh), its integer in the low bits of the sum with 1.5 * 2^23
+  const float big = fmaf(yh, -256.f, 12582912.f);
+  const int n = __float_as_int(big) - 0x4B400000;
+  const float f = fmaf(big - 12582912.f, -1.f / 256.f, -yh) - yl;   // exact but for the subtraction of yl
   const float u = f * 0.693147180559945f;
-  const float p = fmaf(u * u, fmaf(u, 1.f / 6.f, 0.5f), u);   // 2^f - 1
-  const int ni = static_cast<int>(n);
-  const unsigned long long t = table[ni & (kExpSteps - 1)];
-  // both parts scaled by 2^39; |p| < 0.0015
-  const int r = __float2int_rn(static_cast<float>(static_cast<unsigned>(t >> 8)) * (p * 256.f));
-  const unsigned long long w = (t + static_cast<long long>(r)) << (kWeightBits - kExpBits);
-  const int sh = -(ni >> 8);       // 0..44
-  return (w + ((1ull << sh) >> 1)) >> sh;
+  const float p = fmaf(u * u, fmaf(u, 1.f / 6.f, 0.5f), u);         // 2^f - 1, |p| < 0.0014
+  const unsigned long long t = table[n & (kExpSteps - 1)];          // [2^62, 2^63)
+  // t * p: the upper half of t times p in units of 2^-40, in units of 2^24
+  const long long r = static_cast<long long>(__mulhi(static_cast<int>(t >> 32), __float2int_rn(p * 1099511627776.f)));
+  const unsigned long long w = t + static_cast<unsigned long long>(r * (1ll << 24));
+  // 2 floor(x / 2) + 1 is x in the mean, so that truncation adds no drift to a long sum
+  return yh < 45.f ? (w >> (kExpBits - kWeightBits - (n >> 8))) | 1u : 0;
 }
 
 // The float order of logits as unsigned keys (-0 as +0).

@@ -9,15 +9,20 @@
 //
 // A cluster of C = 1, 2, 4 or 8 CTAs per row; each keeps its slice of the row in shared
 // memory, so that the row is read once however many passes its rule takes:
-//   1. load, maximum;
-//   2. a search per part (top-k, then top-p among what top-k left): a histogram of the
-//      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
-//      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
-//      bins through distributed shared memory to find the bin with the cut; its elements are
-//      listed and each counted against the others.  A bin with more elements than the list
-//      takes (flat rows, many equal logits) is divided by key as often as it needs;
-//      a single key, by id;
-//   3. the draw: the kept weights' sums slice by slice, then warp by warp; or the mask.
+//   1. load; the maximum, and a bound: if each CTA has j groups of threads with a logit
+//      above its bound, C j logits of the row lie above the least of the bounds;
+//   2. candidates: the logits above the bound (two or three times as many as top-k keeps, or
+//      about 250), listed by each CTA - with top-p alone also the sum of the slice's weights;
+//   3. where the candidates hold what the rule keeps, the rest is theirs alone: each is
+//      counted against the others for its place in the order, the sum of weights before it
+//      and, among the kept ones, the sum before it in id order.
+//   Else (a nucleus or top-k of hundreds, flat rows, many equal logits) a search per part: a
+//      histogram of the elements' depth below the maximum, 16 bins an octave, with counts
+//      and for top-p the weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add
+//      up each other's bins through distributed shared memory to find the bin with the cut
+//      and list its elements.  A bin with more than the list takes is divided by key
+//      as often as it needs; a single key, by id.
+//   4. the draw: the kept weights' sums slice by slice, then warp by warp; or the mask.
 // Every CTA of a cluster takes the same decisions from the same numbers, so no result is
 // passed back but an id among more equal logits than the list takes.
 #include <cuda_runtime.h>
@@ -43,47 +48,52 @@ constexpr float kLargest = 3.402823466e38f;
 typedef unsigned long long u64;
 
 // NaN as -inf, +inf as the largest finite number.
-__device__ __forceinline__ float sane(float z) { return z == z ? fminf(z, kLargest) : -INFINITY; }
+__device__ __forceinline__ float sane(float z) { return fminf(fmaxf(z, -INFINITY), kLargest); }
 
 constexpr int kMaxCluster = 8;
 constexpr int kMantissa = 4;                 // bins per octave of depth: 2^4
 constexpr int kBins = 16 << kMantissa;       // depths 2^-10 .. 2^6, clamped
 constexpr int kSupers = kBins / 32;          // groups of 32 bins
-constexpr uint32_t kList = kBins * 3 / 4;         // list entries: the pulled list and its weights take
-                                             // the histogram's place
+constexpr uint32_t kList = 192;              // list entries of a CTA
+constexpr uint32_t kAll = 384;               // of the cluster
+constexpr int kGroups = 64;                  // groups of 8 threads whose maxima give the bound
+constexpr int kMostAbove = 56;               // of them above it at most
+constexpr int kTopPAbove = 160;              // logits above the bound for top-p alone
 
 struct alignas(16) Smem {
   u64 table[kExpSteps];
   union {
     struct {
-      uint32_t cnt[kBins], lo[kBins], hi[kBins];   // count, sum of weights in two words
-    } h;
+      struct {
+        uint32_t cnt[kBins], lo[kBins], hi[kBins];   // count, sum of weights in two words
+      } h;
+      struct {                               // find_bin: the sums of all CTAs
+        u64 mass[kMaxCluster][32];
+        uint32_t cnt[kMaxCluster][32];
+      } p;
+    };
     struct {
-      u64 entry[kList], weight[kList];
+      u64 entry[kAll], weight[kAll];
     } all;                                   // the cluster's list
   };
-  union {
-    u64 list[kList];                         // this CTA's: (~key << 32) | id
-    struct {                                 // find_bin: the sums of all CTAs
-      u64 mass[kMaxCluster][32];
-      uint32_t cnt[kMaxCluster][32];
-    } p;
-  };
-  // sums of this CTA, read by the others
+  u64 list[kList];                           // this CTA's: (~key << 32) | id
+  // of this CTA, read by the others
   uint32_t sup_cnt[kSupers];
   u64 sup_mass[kSupers];
   u64 tail;
   uint32_t n_list;
+  u64 sum, list_sum;                         // weights of the slice, of the list
   u64 p_tail[kMaxCluster];                   // of all CTAs
-  float peer_max[kMaxCluster];               // pushed
+  float2 peer_max[kMaxCluster];              // pushed: maximum, bound
   u64 peer_sum[kMaxCluster];                 // pushed
   u64 scan[kWarps];
+  float group[kGroups];
   float wmax[kWarps];
   uint32_t tie_id;                           // pushed
-  u64 cut;
+  u64 cut, total;
 };
+static_assert(sizeof(u64) * 2 * kList <= sizeof(u64) * 2 * kAll, "a search's list fits the cluster's");
 static_assert(3 * (sizeof(Smem) + 16388 * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
-static_assert(sizeof(u64) * 2 * kList <= sizeof(uint32_t) * 3 * kBins, "the list fits the histogram's place");
 
 // A row's rule, with what "off" means resolved.
 struct Rule {
@@ -222,11 +232,13 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   return f;
 }
 
+// The elements of at least z_min (four at a time: some below it too).
 template <class Each>
-__device__ __forceinline__ void for_slice(const Slice& s, Each each) {
+__device__ __forceinline__ void for_slice(const Slice& s, float z_min, Each each) {
   const float4* z4 = reinterpret_cast<const float4*>(s.z);
   for (int i = threadIdx.x; i < s.len / 4; i += kThreads) {
     const float4 v = z4[i];
+    if (fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) < z_min) continue;
     each(v.x, s.base + 4 * i);
     each(v.y, s.base + 4 * i + 1);
     each(v.z, s.base + 4 * i + 2);
@@ -261,6 +273,23 @@ __device__ void close_histogram(const Part& p, Smem& sm) {
   cluster_sync();
 }
 
+// The CTAs' lists into sm.all; returns the number of entries.  All threads.
+template <class Mass>
+__device__ uint32_t pull_list(int C, bool weighted, Mass mass, Smem& sm) {
+  uint32_t off = 0;
+  for (int c = 0; c < C; ++c) {
+    const uint32_t n = min(ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), c)), min(kList, kAll - off));
+    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+      const u64 e = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), c));
+      sm.all.entry[off + i] = e;
+      sm.all.weight[off + i] = weighted ? mass(key_logit(~static_cast<uint32_t>(e >> 32))) : 1;
+    }
+    off += n;
+  }
+  __syncthreads();
+  return off;
+}
+
 // The entry at which the prefix that p asks for ends.
 template <class Mass>
 __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass, Smem& sm) {
@@ -270,13 +299,14 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
     return z > -INFINITY && entry_of(logit_key(z), static_cast<uint32_t>(id)) <= p.within;
   };
   const bool whole = p.within == ~0ull;
+  const float z_in = whole ? -kLargest : key_logit(~static_cast<uint32_t>(p.within >> 32));
   clear_histogram(sm);
   if (tid == 0) {
     sm.n_list = 0;
     sm.cut = p.within;
   }
   u64 tail = 0;
-  for_slice(s, [&](float z, int id) {
+  for_slice(s, z_in, [&](float z, int id) {
     if (whole ? z == -INFINITY : !takes_part(z, id)) return;
     const float d = depth(z);
     const u64 w = p.mass ? mass(z) : 0;
@@ -299,9 +329,19 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
     return p.within;
   }
   const int bin = f.bin;
-  // the keys that the bin's elements can have: those of its depths with a margin
-  uint32_t k_lo = 0, k_hi = ~0u;
-  int shift = 32;
+  // the keys that the bin's elements can have: those of its depths with a margin (depth is
+  // (max - z) * scale, off by some units in the last place of the larger term)
+  uint32_t k_lo, k_hi;
+  {
+    constexpr int kFirst = (127 - 10) << kMantissa;
+    const float a0 = __uint_as_float(static_cast<uint32_t>(bin + kFirst) << (23 - kMantissa));
+    const float a1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + kFirst) << (23 - kMantissa));
+    const float z1 = p.max - a0 / p.scale, z0 = p.max - a1 / p.scale;
+    const float slack = 4e-7f * (fabsf(p.max) + fabsf(z0)) + 1e-37f;
+    k_hi = bin == 0 || !(z1 + slack < p.max) ? logit_key(p.max) : logit_key(z1 + slack);
+    k_lo = bin == kBins - 1 || !(z0 - slack > -kLargest) ? logit_key(-kLargest) : logit_key(z0 - slack);
+  }
+  int shift = 32;             // keys per bin of the last division: 2^shift
   auto in_bin = [&](float z, int id) {
     if (whole ? z == -INFINITY : !takes_part(z, id)) return false;
     const float d = depth(z);
@@ -315,23 +355,16 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
   };
   u64 above = f.above;
   while (f.count > kList) {
-    if (shift == 32) {
-      const float a0 = bin == 0 ? 0.f : __uint_as_float(static_cast<uint32_t>(bin + ((127 - 10) << kMantissa)) << (23 - kMantissa));
-      const float a1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + ((127 - 10) << kMantissa)) << (23 - kMantissa));
-      // z = max - depth / scale, off by some units in the last place of the larger term
-      const float z1 = p.max - a0 / p.scale, z0 = p.max - a1 / p.scale;
-      const float slack = 4e-7f * (fabsf(p.max) + fabsf(z0)) + 1e-37f;
-      k_hi = bin == 0 || !(z1 + slack < p.max) ? logit_key(p.max) : logit_key(z1 + slack);
-      k_lo = bin == kBins - 1 || !(z0 - slack > -kLargest) ? logit_key(-kLargest) : logit_key(z0 - slack);
+    if (shift == 32) {        // the first division of [k_lo, k_hi]
       shift = max(0, 32 - __clz(k_hi - k_lo) - (4 + kMantissa));
-    } else {   // the next division of [k_lo, k_hi]
+    } else {
       if (shift == 0) break;
       narrow();
       shift = max(0, shift - (4 + kMantissa));
     }
     cluster_sync();           // the others have read this CTA's histogram
     clear_histogram(sm);
-    for_slice(s, [&](float z, int id) {
+    for_slice(s, key_logit(k_lo), [&](float z, int id) {
       if (!in_bin(z, id)) return;
       const int b = static_cast<int>((k_hi - logit_key(z)) >> shift);
       atomicAdd(&sm.h.cnt[b], 1u);
@@ -374,25 +407,13 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
     __syncthreads();
     return cut;
   }
-  __syncthreads();            // sm.p, in the list's place, is read
-  for_slice(s, [&](float z, int id) {
+  for_slice(s, key_logit(k_lo), [&](float z, int id) {
     if (!in_bin(z, id)) return;
     const uint32_t i = atomicAdd(&sm.n_list, 1u);
     if (i < kList) sm.list[i] = entry_of(logit_key(z), static_cast<uint32_t>(id));
   });
   cluster_sync();
-  // every CTA takes the whole list (the histogram's place: nobody reads that any more)
-  uint32_t off = 0;
-  for (int c = 0; c < C; ++c) {
-    const uint32_t n = min(ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), c)), kList - off);
-    for (uint32_t i = tid; i < n; i += kThreads) {
-      const u64 e = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), c));
-      sm.all.entry[off + i] = e;
-      sm.all.weight[off + i] = p.mass ? mass(key_logit(~static_cast<uint32_t>(e >> 32))) : 1;
-    }
-    off += n;
-  }
-  __syncthreads();
+  const uint32_t off = pull_list(C, p.mass, mass, sm);   // into the histogram's place: nobody reads that any more
   for (uint32_t i = tid; i < off; i += kThreads) {
     const u64 e = sm.all.entry[i], own = sm.all.weight[i];
     u64 before = above;
@@ -406,6 +427,21 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
   return cut;
 }
 
+// Over the n entries of sm.all, 2^bits threads to an entry: sum(e, j) over all j, the same in
+// each of the threads; then `use(i, e, sum)` in the first of them.
+template <class Value, class Use>
+__device__ __forceinline__ void for_pairs(uint32_t n, Smem& sm, Value value, Use use) {
+  const int bits = n <= kThreads / 8 ? 3 : n <= kThreads / 4 ? 2 : n <= kThreads / 2 ? 1 : 0;
+  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1);
+  const u64 e = i < n ? sm.all.entry[i] : 0;
+  u64 sum = 0;
+  if (i < n)
+    for (uint32_t j = part; j < n; j += 1u << bits) sum += value(e, j);
+  for (int o = 1 << bits >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (i < n && part == 0) use(i, e, sum);
+}
+static_assert(kAll <= kThreads, "an entry per thread");
+
 template <bool kMask>
 __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_constant__ FilterArgs a, int C, int len) {
   extern __shared__ __align__(16) uint8_t raw[];
@@ -416,6 +452,7 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int rank = static_cast<int>(cluster_ctarank()), row = blockIdx.x / C, V = a.vocab;
   for (int i = tid; i < kExpSteps; i += kThreads) sm.table[i] = exp_table()[i];
+  if (tid == 0) sm.n_list = 0;
   cluster_arrive_release();   // waited for before the first push
   pdl_wait();
   pdl_launch_dependents();
@@ -424,59 +461,189 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) >> 2) & 3);
   s.base = rank * len - shift;
   const Rule r = rule_of(a, row);
-  // ------------------------------------------------ load, maximum
+  const bool by_k = r.top_k > 0 && r.top_k < V, by_p = r.top_p < 1.f;
+  // ------------------------------------------------ load; maximum and bound
   float m = -INFINITY;
-#pragma unroll 8
-  for (int i = tid; i < len / 4; i += kThreads) {
-    const int x = s.base + 4 * i;
-    float4 v;
-    if (x >= 0 && x + 3 < V) {
-      v = __ldcg(reinterpret_cast<const float4*>(z + x));
-    } else {
-      v.x = x >= 0 && x < V ? __ldcg(z + x) : -INFINITY;
-      v.y = x + 1 >= 0 && x + 1 < V ? __ldcg(z + x + 1) : -INFINITY;
-      v.z = x + 2 >= 0 && x + 2 < V ? __ldcg(z + x + 2) : -INFINITY;
-      v.w = x + 3 >= 0 && x + 3 < V ? __ldcg(z + x + 3) : -INFINITY;
+  if (s.base >= 0 && s.base + len <= V) {
+    const float4* z4 = reinterpret_cast<const float4*>(z + s.base);
+#pragma unroll 4
+    for (int i = tid; i < len / 4; i += kThreads) {
+      float4 v = __ldcg(z4 + i);
+      v = make_float4(sane(v.x), sane(v.y), sane(v.z), sane(v.w));
+      m = fmaxf(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), m);
+      reinterpret_cast<float4*>(s.z)[i] = v;
     }
-    v.x = sane(v.x);
-    v.y = sane(v.y);
-    v.z = sane(v.z);
-    v.w = sane(v.w);
-    m = fmaxf(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), m);
-    reinterpret_cast<float4*>(s.z)[i] = v;
+  } else {
+    for (int i = tid; i < len / 4; i += kThreads) {
+      const int x = s.base + 4 * i;
+      float4 v;
+      if (x >= 0 && x + 3 < V) {
+        v = __ldcg(reinterpret_cast<const float4*>(z + x));
+      } else {
+        v.x = x >= 0 && x < V ? __ldcg(z + x) : -INFINITY;
+        v.y = x + 1 >= 0 && x + 1 < V ? __ldcg(z + x + 1) : -INFINITY;
+        v.z = x + 2 >= 0 && x + 2 < V ? __ldcg(z + x + 2) : -INFINITY;
+        v.w = x + 3 >= 0 && x + 3 < V ? __ldcg(z + x + 3) : -INFINITY;
+      }
+      v = make_float4(sane(v.x), sane(v.y), sane(v.z), sane(v.w));
+      m = fmaxf(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), m);
+      reinterpret_cast<float4*>(s.z)[i] = v;
+    }
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) sm.wmax[w] = m;
+  for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if ((lane & 7) == 0) sm.group[tid >> 3] = m;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) m = fmaxf(m, sm.wmax[i]);
+  // the j-th largest group maximum, j = what this CTA owes to the count above the bound
+  const int owed = (by_k ? r.top_k + C - 1 : kTopPAbove + C - 1) / C;
+  bool listed = (by_k || by_p) && (by_k ? owed <= kMostAbove : true);
+  const int j = min(owed, kMostAbove);
   cluster_wait_acquire();
-  if (tid < C) st_cluster_u32(mapa_shared(smem_addr(&sm.peer_max[rank]), tid), __float_as_uint(m));
+  if (w < 2) {
+    const float own = sm.group[tid];
+    int above = 0;
+    m = -INFINITY;
+#pragma unroll 8
+    for (int i = 0; i < kGroups; ++i) {
+      const float g = sm.group[i];
+      above += g > own || (g == own && i < tid);
+      m = fmaxf(m, g);
+    }
+    if (above == j - 1)
+      for (int c = 0; c < C; ++c)
+        st_cluster_u64(mapa_shared(smem_addr(&sm.peer_max[rank]), c),
+                       __float_as_uint(m) | (static_cast<u64>(__float_as_uint(own)) << 32));
+  }
   cluster_sync();
-  for (int c = 0; c < C; ++c) m = fmaxf(m, sm.peer_max[c]);
+  m = -INFINITY;
+  float bound = kLargest;
+  for (int c = 0; c < C; ++c) {
+    m = fmaxf(m, sm.peer_max[c].x);
+    bound = fminf(bound, sm.peer_max[c].y);
+  }
+  bound = fmaxf(bound, -kLargest);
   // ------------------------------------------------ the cut
   const bool empty = m == -INFINITY;
   const WeightScale ws = weight_scale(m, r.temperature);
   auto mass = [&](float x) { return weight(x, ws, sm.table); };
-  u64 cut = entry_of(logit_key(-kLargest), ~0u);
-  if (!empty) {
-    if (r.top_k > 0 && r.top_k < V)
-      cut = min(cut, search(Part{false, static_cast<u64>(r.top_k), 1.f, m, INFINITY, ~0ull}, s, C, rank, mass, sm));
-    if (r.top_p < 1.f) {
+  const u64 no_cut = entry_of(logit_key(-kLargest), ~0u);
+  u64 cut = no_cut;
+  if (r.min_p > 0.f && !empty) {
+    // the least float z with (z - max) / T >= log(min_p)
+    const double c = static_cast<double>(m) +
+                     static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
+    float cf = static_cast<float>(c);
+    if (static_cast<double>(cf) < c) cf = nextafterf(cf, INFINITY);
+    cut = entry_of(logit_key(fmaxf(fminf(cf, m), -kLargest)), ~0u);
+  }
+  const u64 cut_min_p = cut;
+  listed = listed && !empty;
+  if (listed) {
+    // the candidates, and with top-p alone the sums of the weights
+    u64 sum = 0, list_sum = 0;
+    for_slice(s, by_k ? bound : -kLargest, [&](float x, int id) {
+      const u64 wt = by_k ? 0 : mass(x);
+      sum += wt;
+      if (x >= bound) {
+        list_sum += wt;
+        const uint32_t i = atomicAdd(&sm.n_list, 1u);
+        if (i < kList) sm.list[i] = entry_of(logit_key(x), static_cast<uint32_t>(id));
+      }
+    });
+    if (!by_k) {
+      sum = block_sum(sum, sm.scan);
+      list_sum = block_sum(list_sum, sm.scan);
+      if (tid == 0) {
+        sm.sum = sum;
+        sm.list_sum = list_sum;
+      }
+    }
+    cluster_sync();
+    uint32_t n = 0;
+    u64 total = 0, in_list = 0;
+    for (int c = 0; c < C; ++c) {
+      const uint32_t nc = ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), c));
+      listed = listed && nc <= kList;
+      n += nc;
+      if (!by_k) {
+        total += ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), c));
+        in_list += ld_cluster_u64(mapa_shared(smem_addr(&sm.list_sum), c));
+      }
+    }
+    const u64 f = fraction64(r.top_p);
+    // the fraction of a sum, rounded up; at least 1
+    auto part_of = [&](u64 sum) { return max(__umul64hi(f, sum) + (f * sum != 0 ? 1 : 0), 1ull); };
+    listed = listed && n <= kAll && (by_k || in_list >= part_of(total));
+    if (listed && !kMask && rank != 0) {   // the rest is the first CTA's
+      cluster_sync();
+      return;
+    }
+    if (listed) {
+      pull_list(C, true, mass, sm);
+      if (kMask)
+        cluster_sync();                    // the others have read this CTA's list
+      else
+        cluster_arrive_release();          // they may leave; nobody reads this CTA's
+      // each entry's place in the order, then the weights' sum before it
+      u64 cut_k = ~0ull;
+      if (by_k) {
+        if (tid == 0) sm.cut = ~0ull;
+        __syncthreads();
+        for_pairs(n, sm, [&](u64 e, uint32_t i) { return static_cast<u64>(sm.all.entry[i] < e); },
+                  [&](uint32_t, u64 e, u64 before) {
+                    if (before + 1 == static_cast<u64>(r.top_k)) sm.cut = e;
+                  });
+        __syncthreads();
+        cut_k = sm.cut;
+        cut = min(cut, cut_k);
+      }
+      if (by_p) {
+        if (by_k) {
+          u64 v = 0;
+          if (tid < n && sm.all.entry[tid] <= cut_k) v = sm.all.weight[tid];
+          total = block_sum(v, sm.scan);
+        }
+        const u64 need = part_of(total);
+        for_pairs(n, sm, [&](u64 e, uint32_t i) { return sm.all.entry[i] < e ? sm.all.weight[i] : 0; },
+                  [&](uint32_t i, u64 e, u64 before) {
+                    if (before < need && need <= before + sm.all.weight[i]) sm.cut = e;
+                  });
+        __syncthreads();
+        cut = min(cut, sm.cut);
+      }
+      if (!kMask) {
+        u64 v = 0;
+        if (tid < n) {
+          if (sm.all.entry[tid] > cut) sm.all.weight[tid] = 0;
+          v = sm.all.weight[tid];
+        }
+        total = block_sum(v, sm.scan);
+        const u64 target = __umul64hi(fraction64(a.u[row]), total);
+        for_pairs(n, sm,
+                  [&](u64 e, uint32_t i) {
+                    return static_cast<uint32_t>(sm.all.entry[i]) < static_cast<uint32_t>(e) ? sm.all.weight[i] : 0;
+                  },
+                  [&](uint32_t i, u64 e, u64 before) {
+                    if (before <= target && target < before + sm.all.weight[i])
+                      a.out_tok[row] = static_cast<int>(static_cast<uint32_t>(e));
+                  });
+        cluster_wait_acquire();
+        return;
+      }
+    } else {
+      cluster_sync();                      // the others have read this CTA's counts
+    }
+  }
+  if (!empty && !listed) {
+    u64 found = no_cut;
+    if (by_k) found = min(found, search(Part{false, static_cast<u64>(r.top_k), 1.f, m, INFINITY, ~0ull}, s, C, rank, mass, sm));
+    if (by_p) {
       // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
       const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
-      const bool whole = cut == entry_of(logit_key(-kLargest), ~0u);
-      cut = min(cut, search(Part{true, fraction64(r.top_p), ws.hi, m, deepest, whole ? ~0ull : cut}, s, C, rank, mass, sm));
+      found = min(found, search(Part{true, fraction64(r.top_p), ws.hi, m, deepest, found == no_cut ? ~0ull : found}, s, C,
+                                rank, mass, sm));
     }
-    if (r.min_p > 0.f) {
-      // the least float z with (z - max) / T >= log(min_p)
-      const double c = static_cast<double>(m) +
-                       static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
-      float cf = static_cast<float>(c);
-      if (static_cast<double>(cf) < c) cf = nextafterf(cf, INFINITY);
-      cut = min(cut, entry_of(logit_key(fmaxf(fminf(cf, m), -kLargest)), ~0u));
-    }
+    cut = min(cut_min_p, found);
   }
   const float cut_z = key_logit(~static_cast<uint32_t>(cut >> 32));
   const uint32_t cut_id = static_cast<uint32_t>(cut);
@@ -484,12 +651,19 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   if constexpr (kMask) {
     float* out = a.out + row * a.out_ld;
     const bool aligned = ((reinterpret_cast<uintptr_t>(out) >> 2) & 3) == static_cast<uintptr_t>(shift);
+    const bool inside = aligned && s.base >= 0 && s.base + len <= V;
     for (int i = tid; i < len / 4; i += kThreads) {
       const int x = s.base + 4 * i;
-      const float4 v = reinterpret_cast<const float4*>(s.z)[i];
-      const float4 o = make_float4(kept(v.x, x) ? v.x : -INFINITY, kept(v.y, x + 1) ? v.y : -INFINITY,
-                                   kept(v.z, x + 2) ? v.z : -INFINITY, kept(v.w, x + 3) ? v.w : -INFINITY);
-      if (aligned && x >= 0 && x + 3 < V) {
+      float4 o = reinterpret_cast<const float4*>(s.z)[i];
+      if (fmaxf(fmaxf(o.x, o.y), fmaxf(o.z, o.w)) < cut_z) {
+        o = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      } else {
+        o.x = kept(o.x, x) ? o.x : -INFINITY;
+        o.y = kept(o.y, x + 1) ? o.y : -INFINITY;
+        o.z = kept(o.z, x + 2) ? o.z : -INFINITY;
+        o.w = kept(o.w, x + 3) ? o.w : -INFINITY;
+      }
+      if (inside || (aligned && x >= 0 && x + 3 < V)) {
         *reinterpret_cast<float4*>(out + x) = o;
       } else {
         if (x >= 0 && x < V) out[x] = o.x;
@@ -508,13 +682,13 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     const int i = t * 128 + lane * 4;
     float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     if (i < len) v = *reinterpret_cast<const float4*>(s.z + i);
+    const bool some = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= cut_z;
+    if (!__any_sync(0xffffffffu, some)) return false;
     const int x = s.base + i;
-    const bool k0 = kept(v.x, x), k1 = kept(v.y, x + 1), k2 = kept(v.z, x + 2), k3 = kept(v.w, x + 3);
-    if (!__any_sync(0xffffffffu, k0 || k1 || k2 || k3)) return false;
-    wt[0] = k0 ? mass(v.x) : 0;
-    wt[1] = k1 ? mass(v.y) : 0;
-    wt[2] = k2 ? mass(v.z) : 0;
-    wt[3] = k3 ? mass(v.w) : 0;
+    wt[0] = kept(v.x, x) ? mass(v.x) : 0;
+    wt[1] = kept(v.y, x + 1) ? mass(v.y) : 0;
+    wt[2] = kept(v.z, x + 2) ? mass(v.z) : 0;
+    wt[3] = kept(v.w, x + 3) ? mass(v.w) : 0;
     return true;
   };
   u64 mine = 0;
