@@ -55,12 +55,14 @@ struct WeightScale {
   float max, hi, lo;
 };
 __device__ __forceinline__ WeightScale weight_scale(float row_max, float temperature) {
-  // T below 1e-30 leaves the maxima alone with weight; T = inf weighs all alike
-  const double c = fmin(1.4426950408889634 / static_cast<double>(temperature), 1e30);
+  // T below 1e-30 leaves the maxima alone with weight; T = inf weighs all alike.  A quotient
+  // and its remainder's in 32 bits: 64-bit arithmetic by every thread of a CTA is 2 us.
+  constexpr float kHi = 1.44269504f, kLo = 1.92596299e-8f;   // log2(e)
+  const float T = fmaxf(temperature, 1e-30f);
   WeightScale s;
   s.max = row_max;
-  s.hi = static_cast<float>(c);
-  s.lo = static_cast<float>(c - static_cast<double>(s.hi));
+  s.hi = __fdiv_rn(kHi, T);
+  s.lo = s.hi > 0.f ? __fdiv_rn(fmaf(-s.hi, T, kHi) + kLo, T) : 0.f;
   return s;
 }
 

@@ -11,18 +11,19 @@
 // memory, so that the row is read once however many passes its rule takes:
 //   1. load; the maximum, and a bound: if each CTA has j groups of threads with a logit
 //      above its bound, C j logits of the row lie above the least of the bounds;
-//   2. candidates: the logits above the bound (two or three times as many as top-k keeps, or
-//      about 250), listed by each CTA - with top-p alone also the sum of the slice's weights;
-//   3. where the candidates hold what the rule keeps, the rest is theirs alone: each is
-//      counted against the others for its place in the order, the sum of weights before it
-//      and, among the kept ones, the sum before it in id order.
-//   Else (a nucleus or top-k of hundreds, flat rows, many equal logits) a search per part: a
-//      histogram of the elements' depth below the maximum, 16 bins an octave, with counts
-//      and for top-p the weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add
-//      up each other's bins through distributed shared memory to find the bin with the cut
-//      and list its elements.  A bin with more than the list takes is divided by key
-//      as often as it needs; a single key, by id.
-//   4. the draw: the kept weights' sums slice by slice, then warp by warp; or the mask.
+//   2. top-k up to some hundred: the candidates, the logits above the bound (two or three
+//      times as many as top-k keeps), are listed; the list holds what the rule keeps, and
+//      each entry is counted against the others for its place in the order, the sum of
+//      weights before it and, among the kept ones, the sum before it in id order;
+//   3. else a search per part (top-k, then top-p among what top-k left): a histogram of the
+//      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
+//      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
+//      bins through distributed shared memory to find the bin with the cut, and list
+//      its elements - or all up to there, where they are few enough.  A bin with more
+//      than the list takes (flat rows, many equal logits) is divided by key as often as it
+//      needs; a single key, by id;
+//   4. the draw: from the list where it holds all that is kept, else the kept weights' sums
+//      slice by slice, then warp by warp; or the mask.
 // Every CTA of a cluster takes the same decisions from the same numbers, so no result is
 // passed back but an id among more equal logits than the list takes.
 #include <cuda_runtime.h>
@@ -40,7 +41,8 @@
 namespace memspec {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;     // 64 elements each of the longest slice: what a thread does
+                                  // once per row is a third of its instructions at 512
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxVocab = 131072;
 constexpr float kLargest = 3.402823466e38f;
@@ -54,11 +56,9 @@ constexpr int kMaxCluster = 8;
 constexpr int kMantissa = 4;                 // bins per octave of depth: 2^4
 constexpr int kBins = 16 << kMantissa;       // depths 2^-10 .. 2^6, clamped
 constexpr int kSupers = kBins / 32;          // groups of 32 bins
-constexpr uint32_t kList = 192;              // list entries of a CTA
-constexpr uint32_t kAll = 384;               // of the cluster
-constexpr int kGroups = 64;                  // groups of 8 threads whose maxima give the bound
+constexpr uint32_t kList = 256;              // list entries of a CTA and of the cluster
+constexpr int kGroups = 64;                  // groups of 4 threads whose maxima give the bound
 constexpr int kMostAbove = 56;               // of them above it at most
-constexpr int kTopPAbove = 160;              // logits above the bound for top-p alone
 
 struct alignas(16) Smem {
   u64 table[kExpSteps];
@@ -73,7 +73,7 @@ struct alignas(16) Smem {
       } p;
     };
     struct {
-      u64 entry[kAll], weight[kAll];
+      u64 entry[kList], weight[kList];
     } all;                                   // the cluster's list
   };
   u64 list[kList];                           // this CTA's: (~key << 32) | id
@@ -82,17 +82,15 @@ struct alignas(16) Smem {
   u64 sup_mass[kSupers];
   u64 tail;
   uint32_t n_list;
-  u64 sum, list_sum;                         // weights of the slice, of the list
   u64 p_tail[kMaxCluster];                   // of all CTAs
-  float2 peer_max[kMaxCluster];              // pushed: maximum, bound
+  uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
+  float2 log_min_p;                          // T log(min_p) in two floats
   u64 peer_sum[kMaxCluster];                 // pushed
   u64 scan[kWarps];
-  float group[kGroups];
-  float wmax[kWarps];
+  uint32_t group[kGroups];                   // keys
   uint32_t tie_id;                           // pushed
   u64 cut, total;
 };
-static_assert(sizeof(u64) * 2 * kList <= sizeof(u64) * 2 * kAll, "a search's list fits the cluster's");
 static_assert(3 * (sizeof(Smem) + 16388 * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
 
 // A row's rule, with what "off" means resolved.
@@ -121,11 +119,12 @@ __device__ __forceinline__ u64 warp_sum(u64 v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ u64 warp_scan(u64 v) {   // inclusive
+template <class T>
+__device__ __forceinline__ T warp_scan(T v) {   // inclusive
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const u64 n = __shfl_up_sync(0xffffffffu, v, o);
+    const T n = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += n;
   }
   return v;
@@ -176,6 +175,7 @@ struct Found {
   int bin;
   u64 above;                // sum (count or mass) before the bin
   uint32_t count;           // elements in it
+  uint32_t count_above;     // and before it
   u64 need;                 // what the prefix has to reach
   bool all;                 // the whole set does not exceed it (a count): nothing is cut
 };
@@ -193,9 +193,15 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   if (p.mass && first && tid < C) sm.p_tail[tid] = ld_cluster_u64(mapa_shared(smem_addr(&sm.tail), tid));
   __syncthreads();
   u64 v = 0, tail = 0;
+  uint32_t n = 0;
   if (lane < kSupers)
-    for (int c = 0; c < C; ++c) v += p.mass ? sm.p.mass[c][lane] : sm.p.cnt[c][lane];
+    for (int c = 0; c < C; ++c) {
+      n += sm.p.cnt[c][lane];
+      if (p.mass) v += sm.p.mass[c][lane];
+    }
+  if (!p.mass) v = n;
   u64 incl = warp_scan(v);
+  const uint32_t n_incl = warp_scan(n);
   const u64 total = __shfl_sync(0xffffffffu, incl, 31);
   if (p.mass && first) {
     for (int c = 0; c < C; ++c) tail += sm.p_tail[c];
@@ -208,6 +214,7 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   const unsigned reach = __ballot_sync(0xffffffffu, lane < kSupers && incl >= need);
   const int g = reach ? __ffs(reach) - 1 : kSupers - 1;
   const u64 before = __shfl_sync(0xffffffffu, incl - v, g);
+  const uint32_t n_before = __shfl_sync(0xffffffffu, n_incl - n, g);
   __syncthreads();                                        // p is read
   if (w < C) {
     sm.p.cnt[w][lane] = ld_cluster_u32(mapa_shared(smem_addr(&sm.h.cnt[g * 32 + lane]), w));
@@ -216,7 +223,7 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
                            (static_cast<u64>(ld_cluster_u32(mapa_shared(smem_addr(&sm.h.hi[g * 32 + lane]), w))) << 32);
   }
   __syncthreads();
-  uint32_t n = 0;
+  n = 0;
   v = 0;
   for (int c = 0; c < C; ++c) {
     n += sm.p.cnt[c][lane];
@@ -229,6 +236,7 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   f.bin = g * 32 + b;
   f.above = __shfl_sync(0xffffffffu, incl - v, b);
   f.count = __shfl_sync(0xffffffffu, n, b);
+  f.count_above = n_before + __shfl_sync(0xffffffffu, warp_scan(n) - n, b);
   return f;
 }
 
@@ -276,23 +284,46 @@ __device__ void close_histogram(const Part& p, Smem& sm) {
 // The CTAs' lists into sm.all; returns the number of entries.  All threads.
 template <class Mass>
 __device__ uint32_t pull_list(int C, bool weighted, Mass mass, Smem& sm) {
-  uint32_t off = 0;
-  for (int c = 0; c < C; ++c) {
-    const uint32_t n = min(ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), c)), min(kList, kAll - off));
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-      const u64 e = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), c));
+  // a warp per CTA: lane c has CTA c's count
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  uint32_t n = lane < C ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0;
+  const uint32_t incl = warp_scan(n), all = min(__shfl_sync(0xffffffffu, incl, 31), kList);
+  const uint32_t off = __shfl_sync(0xffffffffu, incl - n, w);
+  n = __shfl_sync(0xffffffffu, n, w);
+  if (w < C)
+    for (uint32_t i = lane; i < n && off + i < kList; i += 32) {
+      const u64 e = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), w));
       sm.all.entry[off + i] = e;
       sm.all.weight[off + i] = weighted ? mass(key_logit(~static_cast<uint32_t>(e >> 32))) : 1;
     }
-    off += n;
-  }
   __syncthreads();
-  return off;
+  return all;
 }
+static_assert(kWarps >= kMaxCluster, "a warp per CTA of the cluster");
+
+// Over the n entries of sm.all, 2^bits threads to an entry: the sum of value(e, j) over all
+// j, then use(i, e, sum) in the first of them.
+template <class Value, class Use>
+__device__ __forceinline__ void for_pairs(uint32_t n, Smem& sm, Value value, Use use) {
+  const int bits = n <= kThreads / 8 ? 3 : n <= kThreads / 4 ? 2 : n <= kThreads / 2 ? 1 : 0;
+  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1);
+  const u64 e = i < n ? sm.all.entry[i] : 0;
+  u64 sum = 0;
+  if (i < n)
+    for (uint32_t j = part; j < n; j += 1u << bits) sum += value(e, j);
+  for (int o = 1 << bits >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (i < n && part == 0) use(i, e, sum);
+}
+static_assert(kList <= kThreads, "an entry per thread");
+
+struct Ended {
+  u64 cut;
+  uint32_t listed;          // > 0: sm.all holds so many entries, all up to the cut among them
+};
 
 // The entry at which the prefix that p asks for ends.
 template <class Mass>
-__device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass, Smem& sm) {
+__device__ Ended search(const Part& p, const Slice& s, int C, int rank, Mass mass, Smem& sm) {
   const int tid = threadIdx.x;
   auto depth = [&](float z) { return (p.max - z) * p.scale; };
   auto takes_part = [&](float z, int id) {
@@ -326,7 +357,7 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
   Found f = find_bin(p, true, p.need, C, sm);
   if (f.all) {
     cluster_sync();           // the others have read this CTA's histogram
-    return p.within;
+    return {p.within, 0};
   }
   const int bin = f.bin;
   // the keys that the bin's elements can have: those of its depths with a margin (depth is
@@ -354,6 +385,8 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
     if (k_hi - k_lo >= 1u << shift) k_lo = k_hi - ((1u << shift) - 1);
   };
   u64 above = f.above;
+  // for the draw it pays to have all of the kept elements
+  const bool whole_list = p.mass && f.count_above + f.count <= kList;
   while (f.count > kList) {
     if (shift == 32) {        // the first division of [k_lo, k_hi]
       shift = max(0, 32 - __clz(k_hi - k_lo) - (4 + kMantissa));
@@ -405,42 +438,51 @@ __device__ u64 search(const Part& p, const Slice& s, int C, int rank, Mass mass,
     cluster_sync();
     const u64 cut = entry_of(k_hi, sm.tie_id);
     __syncthreads();
-    return cut;
+    return {cut, 0};
   }
   for_slice(s, key_logit(k_lo), [&](float z, int id) {
-    if (!in_bin(z, id)) return;
+    if (whole_list) {
+      const float d = depth(z);
+      if ((whole ? z == -INFINITY : !takes_part(z, id)) || d > p.deepest || bin_of(d) > bin) return;
+    } else if (!in_bin(z, id)) {
+      return;
+    }
     const uint32_t i = atomicAdd(&sm.n_list, 1u);
     if (i < kList) sm.list[i] = entry_of(logit_key(z), static_cast<uint32_t>(id));
   });
   cluster_sync();
-  const uint32_t off = pull_list(C, p.mass, mass, sm);   // into the histogram's place: nobody reads that any more
-  for (uint32_t i = tid; i < off; i += kThreads) {
-    const u64 e = sm.all.entry[i], own = sm.all.weight[i];
-    u64 before = above;
-    for (uint32_t j = 0; j < off; ++j)
-      if (sm.all.entry[j] < e) before += sm.all.weight[j];
-    if (before < f.need && f.need <= before + own) sm.cut = e;
-  }
+  const uint32_t n = pull_list(C, p.mass, mass, sm);   // into the histogram's place: nobody reads that any more
+  if (whole_list) above = 0;
+  for_pairs(n, sm, [&](u64 e, uint32_t i) { return sm.all.entry[i] < e ? sm.all.weight[i] : 0; },
+            [&](uint32_t i, u64 e, u64 before) {
+              before += above;
+              if (before < f.need && f.need <= before + sm.all.weight[i]) sm.cut = e;
+            });
   __syncthreads();
   const u64 cut = sm.cut;
   cluster_sync();             // the others have read this CTA's list
-  return cut;
+  return {cut, whole_list ? n : 0};
 }
 
-// Over the n entries of sm.all, 2^bits threads to an entry: sum(e, j) over all j, the same in
-// each of the threads; then `use(i, e, sum)` in the first of them.
-template <class Value, class Use>
-__device__ __forceinline__ void for_pairs(uint32_t n, Smem& sm, Value value, Use use) {
-  const int bits = n <= kThreads / 8 ? 3 : n <= kThreads / 4 ? 2 : n <= kThreads / 2 ? 1 : 0;
-  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1);
-  const u64 e = i < n ? sm.all.entry[i] : 0;
-  u64 sum = 0;
-  if (i < n)
-    for (uint32_t j = part; j < n; j += 1u << bits) sum += value(e, j);
-  for (int o = 1 << bits >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (i < n && part == 0) use(i, e, sum);
+// The draw from the n entries of sm.all up to the cut.
+__device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 cut, Smem& sm) {
+  const uint32_t tid = threadIdx.x;
+  u64 v = 0;
+  if (tid < n) {
+    if (sm.all.entry[tid] > cut) sm.all.weight[tid] = 0;
+    v = sm.all.weight[tid];
+  }
+  const u64 total = block_sum(v, sm.scan);
+  const u64 target = __umul64hi(fraction64(a.u[row]), total);
+  for_pairs(n, sm,
+            [&](u64 e, uint32_t i) {
+              return static_cast<uint32_t>(sm.all.entry[i]) < static_cast<uint32_t>(e) ? sm.all.weight[i] : 0;
+            },
+            [&](uint32_t i, u64 e, u64 before) {
+              if (before <= target && target < before + sm.all.weight[i])
+                a.out_tok[row] = static_cast<int>(static_cast<uint32_t>(e));
+            });
 }
-static_assert(kAll <= kThreads, "an entry per thread");
 
 template <bool kMask>
 __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_constant__ FilterArgs a, int C, int len) {
@@ -462,6 +504,11 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   s.base = rank * len - shift;
   const Rule r = rule_of(a, row);
   const bool by_k = r.top_k > 0 && r.top_k < V, by_p = r.top_p < 1.f;
+  if (r.min_p > 0.f && tid == kThreads - 1) {   // 64-bit arithmetic: one thread's, beside the loads
+    const double l = static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
+    const float hi = static_cast<float>(l);
+    sm.log_min_p = make_float2(hi, static_cast<float>(l - static_cast<double>(hi)));
+  }
   // ------------------------------------------------ load; maximum and bound
   float m = -INFINITY;
   if (s.base >= 0 && s.base + len <= V) {
@@ -491,37 +538,35 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     }
   }
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if ((lane & 7) == 0) sm.group[tid >> 3] = m;
+  for (int o = 1; o < kThreads / kGroups; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (tid % (kThreads / kGroups) == 0) sm.group[tid / (kThreads / kGroups)] = logit_key(m);
   __syncthreads();
-  // the j-th largest group maximum, j = what this CTA owes to the count above the bound
-  const int owed = (by_k ? r.top_k + C - 1 : kTopPAbove + C - 1) / C;
-  bool listed = (by_k || by_p) && (by_k ? owed <= kMostAbove : true);
-  const int j = min(owed, kMostAbove);
+  // the bound: the j-th largest group maximum, j = what this CTA owes to the top k (if that
+  // is more than the groups can give, the bound is not used)
+  const int owed = by_k ? (r.top_k + C - 1) / C : 1, j = min(owed, kMostAbove);
   cluster_wait_acquire();
-  if (w < 2) {
-    const float own = sm.group[tid];
+  if (w < kGroups / 32) {
+    // the groups' keys less their last bits, made different by the group's number: at
+    // least j groups reach the bound without those bits
+    const uint32_t own = (sm.group[tid] & ~(kGroups - 1u)) | tid;
     int above = 0;
-    m = -INFINITY;
-#pragma unroll 8
-    for (int i = 0; i < kGroups; ++i) {
-      const float g = sm.group[i];
-      above += g > own || (g == own && i < tid);
-      m = fmaxf(m, g);
-    }
+#pragma unroll 16
+    for (int i = 0; i < kGroups; ++i) above += ((sm.group[i] & ~(kGroups - 1u)) | i) > own;
+    const uint32_t top = __reduce_max_sync(0xffffffffu, max(sm.group[lane], sm.group[lane + 32]));
     if (above == j - 1)
       for (int c = 0; c < C; ++c)
         st_cluster_u64(mapa_shared(smem_addr(&sm.peer_max[rank]), c),
-                       __float_as_uint(m) | (static_cast<u64>(__float_as_uint(own)) << 32));
+                       top | (static_cast<u64>(own & ~(kGroups - 1u)) << 32));
   }
   cluster_sync();
-  m = -INFINITY;
-  float bound = kLargest;
-  for (int c = 0; c < C; ++c) {
-    m = fmaxf(m, sm.peer_max[c].x);
-    bound = fminf(bound, sm.peer_max[c].y);
+  uint32_t top = 0, least = ~0u;
+  if (lane < C) {
+    const uint2 v = sm.peer_max[lane];
+    top = v.x;
+    least = v.y;
   }
-  bound = fmaxf(bound, -kLargest);
+  m = key_logit(__reduce_max_sync(0xffffffffu, top));
+  const float bound = key_logit(max(__reduce_min_sync(0xffffffffu, least), logit_key(-kLargest)));
   // ------------------------------------------------ the cut
   const bool empty = m == -INFINITY;
   const WeightScale ws = weight_scale(m, r.temperature);
@@ -529,81 +574,49 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   const u64 no_cut = entry_of(logit_key(-kLargest), ~0u);
   u64 cut = no_cut;
   if (r.min_p > 0.f && !empty) {
-    // the least float z with (z - max) / T >= log(min_p)
-    const double c = static_cast<double>(m) +
-                     static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
-    float cf = static_cast<float>(c);
-    if (static_cast<double>(cf) < c) cf = nextafterf(cf, INFINITY);
-    cut = entry_of(logit_key(fmaxf(fminf(cf, m), -kLargest)), ~0u);
+    // the least float z with z >= max + T log(min_p), the product in two floats
+    const float2 l = sm.log_min_p;
+    const float c = m + l.x, part = c - m;
+    const float rest = ((m - (c - part)) + (l.x - part)) + l.y;    // what c lacks
+    uint32_t key = c > -kLargest ? logit_key(c) : logit_key(-kLargest);
+    if (c > -kLargest && rest > 0.f) ++key;
+    cut = entry_of(min(key, logit_key(m)), ~0u);
   }
-  const u64 cut_min_p = cut;
-  listed = listed && !empty;
-  if (listed) {
-    // the candidates, and with top-p alone the sums of the weights
-    u64 sum = 0, list_sum = 0;
-    for_slice(s, by_k ? bound : -kLargest, [&](float x, int id) {
-      const u64 wt = by_k ? 0 : mass(x);
-      sum += wt;
-      if (x >= bound) {
-        list_sum += wt;
-        const uint32_t i = atomicAdd(&sm.n_list, 1u);
-        if (i < kList) sm.list[i] = entry_of(logit_key(x), static_cast<uint32_t>(id));
-      }
+  const u64 fraction = fraction64(r.top_p);
+  uint32_t n = 0;             // > 0: sm.all holds so many entries, all the kept ones among them
+  bool search_k = by_k && !empty;
+  if (search_k && owed <= kMostAbove) {
+    for_slice(s, bound, [&](float x, int id) {
+      if (x < bound) return;
+      const uint32_t i = atomicAdd(&sm.n_list, 1u);
+      if (i < kList) sm.list[i] = entry_of(logit_key(x), static_cast<uint32_t>(id));
     });
-    if (!by_k) {
-      sum = block_sum(sum, sm.scan);
-      list_sum = block_sum(list_sum, sm.scan);
-      if (tid == 0) {
-        sm.sum = sum;
-        sm.list_sum = list_sum;
-      }
-    }
     cluster_sync();
-    uint32_t n = 0;
-    u64 total = 0, in_list = 0;
-    for (int c = 0; c < C; ++c) {
-      const uint32_t nc = ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), c));
-      listed = listed && nc <= kList;
-      n += nc;
-      if (!by_k) {
-        total += ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), c));
-        in_list += ld_cluster_u64(mapa_shared(smem_addr(&sm.list_sum), c));
+    n = __reduce_add_sync(0xffffffffu, lane < C ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0u);
+    if (n <= kList) {
+      search_k = false;
+      if (!kMask && rank != 0) {           // the rest is the first CTA's
+        cluster_sync();
+        return;
       }
-    }
-    const u64 f = fraction64(r.top_p);
-    // the fraction of a sum, rounded up; at least 1
-    auto part_of = [&](u64 sum) { return max(__umul64hi(f, sum) + (f * sum != 0 ? 1 : 0), 1ull); };
-    listed = listed && n <= kAll && (by_k || in_list >= part_of(total));
-    if (listed && !kMask && rank != 0) {   // the rest is the first CTA's
-      cluster_sync();
-      return;
-    }
-    if (listed) {
       pull_list(C, true, mass, sm);
       if (kMask)
         cluster_sync();                    // the others have read this CTA's list
       else
         cluster_arrive_release();          // they may leave; nobody reads this CTA's
-      // each entry's place in the order, then the weights' sum before it
-      u64 cut_k = ~0ull;
-      if (by_k) {
-        if (tid == 0) sm.cut = ~0ull;
-        __syncthreads();
-        for_pairs(n, sm, [&](u64 e, uint32_t i) { return static_cast<u64>(sm.all.entry[i] < e); },
-                  [&](uint32_t, u64 e, u64 before) {
-                    if (before + 1 == static_cast<u64>(r.top_k)) sm.cut = e;
-                  });
-        __syncthreads();
-        cut_k = sm.cut;
-        cut = min(cut, cut_k);
-      }
+      if (tid == 0) sm.cut = ~0ull;
+      __syncthreads();
+      for_pairs(n, sm, [&](u64 e, uint32_t i) { return static_cast<u64>(sm.all.entry[i] < e); },
+                [&](uint32_t, u64 e, u64 before) {
+                  if (before + 1 == static_cast<u64>(r.top_k)) sm.cut = e;
+                });
+      __syncthreads();
+      const u64 cut_k = sm.cut;
+      cut = min(cut, cut_k);
       if (by_p) {
-        if (by_k) {
-          u64 v = 0;
-          if (tid < n && sm.all.entry[tid] <= cut_k) v = sm.all.weight[tid];
-          total = block_sum(v, sm.scan);
-        }
-        const u64 need = part_of(total);
+        const u64 v = tid < n && sm.all.entry[tid] <= cut_k ? sm.all.weight[tid] : 0;
+        const u64 total = block_sum(v, sm.scan);
+        const u64 need = max(__umul64hi(fraction, total) + (fraction * total != 0 ? 1 : 0), 1ull);
         for_pairs(n, sm, [&](u64 e, uint32_t i) { return sm.all.entry[i] < e ? sm.all.weight[i] : 0; },
                   [&](uint32_t i, u64 e, u64 before) {
                     if (before < need && need <= before + sm.all.weight[i]) sm.cut = e;
@@ -612,38 +625,30 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
         cut = min(cut, sm.cut);
       }
       if (!kMask) {
-        u64 v = 0;
-        if (tid < n) {
-          if (sm.all.entry[tid] > cut) sm.all.weight[tid] = 0;
-          v = sm.all.weight[tid];
-        }
-        total = block_sum(v, sm.scan);
-        const u64 target = __umul64hi(fraction64(a.u[row]), total);
-        for_pairs(n, sm,
-                  [&](u64 e, uint32_t i) {
-                    return static_cast<uint32_t>(sm.all.entry[i]) < static_cast<uint32_t>(e) ? sm.all.weight[i] : 0;
-                  },
-                  [&](uint32_t i, u64 e, u64 before) {
-                    if (before <= target && target < before + sm.all.weight[i])
-                      a.out_tok[row] = static_cast<int>(static_cast<uint32_t>(e));
-                  });
+        draw_from_list(a, row, n, cut, sm);
         cluster_wait_acquire();
         return;
       }
     } else {
-      cluster_sync();                      // the others have read this CTA's counts
+      n = 0;
+      cluster_sync();                      // the others have read this CTA's count
     }
   }
-  if (!empty && !listed) {
-    u64 found = no_cut;
-    if (by_k) found = min(found, search(Part{false, static_cast<u64>(r.top_k), 1.f, m, INFINITY, ~0ull}, s, C, rank, mass, sm));
-    if (by_p) {
-      // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
-      const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
-      found = min(found, search(Part{true, fraction64(r.top_p), ws.hi, m, deepest, found == no_cut ? ~0ull : found}, s, C,
-                                rank, mass, sm));
+  u64 within = no_cut;
+  if (search_k) {
+    within = search(Part{false, static_cast<u64>(r.top_k), 1.f, m, INFINITY, ~0ull}, s, C, rank, mass, sm).cut;
+    cut = min(cut, within);
+  }
+  if (by_p && !empty && n == 0) {
+    // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
+    const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
+    const Ended e = search(Part{true, fraction, ws.hi, m, deepest, min(within, no_cut) == no_cut ? ~0ull : within}, s, C,
+                           rank, mass, sm);
+    cut = min(cut, e.cut);
+    if (!kMask && e.listed > 0) {
+      if (rank == 0) draw_from_list(a, row, e.listed, cut, sm);
+      return;
     }
-    cut = min(cut_min_p, found);
   }
   const float cut_z = key_logit(~static_cast<uint32_t>(cut >> 32));
   const uint32_t cut_id = static_cast<uint32_t>(cut);
@@ -710,9 +715,11 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   if (tid < C) st_cluster_u64(mapa_shared(smem_addr(&sm.peer_sum[rank]), tid), slice);
   cluster_sync();
   u64 total = 0;
-  for (int c = 0; c < C; ++c) {
-    if (c < rank) before += sm.peer_sum[c];
-    total += sm.peer_sum[c];
+#pragma unroll
+  for (int c = 0; c < kMaxCluster; ++c) {
+    const u64 v = c < C ? sm.peer_sum[c] : 0;
+    if (c < rank) before += v;
+    total += v;
   }
   if (empty) {
     if (rank == 0 && tid == 0) a.out_tok[row] = -1;
