@@ -45,6 +45,7 @@ constexpr int kThreads = 256;     // 64 elements each of the longest slice: what
                                   // once per row is a third of its instructions at 512
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxVocab = 131072;
+constexpr uint32_t kCopyBytes = 16384;
 constexpr float kLargest = 3.402823466e38f;
 
 typedef unsigned long long u64;
@@ -88,6 +89,7 @@ struct alignas(16) Smem {
   u64 peer_sum[kMaxCluster];                 // pushed
   u64 scan[kWarps];
   uint32_t group[kGroups];                   // keys
+  uint64_t loaded;                           // mbarrier of the slice's copies
   uint32_t tie_id;                           // pushed
   u64 cut, total;
 };
@@ -494,7 +496,11 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int rank = static_cast<int>(cluster_ctarank()), row = blockIdx.x / C, V = a.vocab;
   for (int i = tid; i < kExpSteps; i += kThreads) sm.table[i] = exp_table()[i];
-  if (tid == 0) sm.n_list = 0;
+  if (tid == 0) {
+    sm.n_list = 0;
+    mbar_init(&sm.loaded, 1);
+    fence_mbar_init();
+  }
   cluster_arrive_release();   // waited for before the first push
   pdl_wait();
   pdl_launch_dependents();
@@ -510,32 +516,42 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     sm.log_min_p = make_float2(hi, static_cast<float>(l - static_cast<double>(hi)));
   }
   // ------------------------------------------------ load; maximum and bound
+  // whole float4s of the row by bulk copies (all of a slice's bytes are under way at once:
+  // with loads through registers a quarter), its ragged ends by single loads
+  float4* const s4 = reinterpret_cast<float4*>(s.z);
+  const int q_lo = s.base < 0 ? 1 : 0, q_hi = max(q_lo, min(len, V - s.base) / 4);
+  if (tid == 0 && q_hi > q_lo) {
+    const uint32_t bytes = static_cast<uint32_t>(q_hi - q_lo) * 16;
+    mbar_arrive_expect_tx(&sm.loaded, bytes);
+    for (uint32_t at = 0; at < bytes; at += kCopyBytes)
+      bulk_load(s.z + 4 * q_lo + at / 4, z + s.base + 4 * q_lo + at / 4, min(kCopyBytes, bytes - at), &sm.loaded,
+                l2_policy_evict_normal());
+  }
   float m = -INFINITY;
-  if (s.base >= 0 && s.base + len <= V) {
-    const float4* z4 = reinterpret_cast<const float4*>(z + s.base);
+  auto take = [&](int i, float4 v) {
+    const float4 o = make_float4(sane(v.x), sane(v.y), sane(v.z), sane(v.w));
+    m = fmaxf(fmaxf(fmaxf(o.x, o.y), fmaxf(o.z, o.w)), m);
+    if (v.x != o.x || v.y != o.y || v.z != o.z || v.w != o.w) s4[i] = o;
+  };
+  auto load_quad = [&](int i) {
+    const int x = s.base + 4 * i;
+    float4 v;
+    v.x = x >= 0 && x < V ? __ldcg(z + x) : -INFINITY;
+    v.y = x + 1 >= 0 && x + 1 < V ? __ldcg(z + x + 1) : -INFINITY;
+    v.z = x + 2 >= 0 && x + 2 < V ? __ldcg(z + x + 2) : -INFINITY;
+    v.w = x + 3 >= 0 && x + 3 < V ? __ldcg(z + x + 3) : -INFINITY;
+    s4[i] = v;
+    take(i, v);
+  };
+  if (tid < q_lo) load_quad(tid);
+  for (int i = q_hi + tid; i < len / 4; i += kThreads) load_quad(i);
+  if (q_hi > q_lo) {
+    // the copies may be waited for once the barrier is initialised and they are announced
+    __syncthreads();
+    if (!mbar_wait_bounded(&sm.loaded, 0, nullptr, nullptr))
+      for (int i = q_lo + tid; i < q_hi; i += kThreads) load_quad(i);   // a thread takes what it loads
 #pragma unroll 4
-    for (int i = tid; i < len / 4; i += kThreads) {
-      float4 v = __ldcg(z4 + i);
-      v = make_float4(sane(v.x), sane(v.y), sane(v.z), sane(v.w));
-      m = fmaxf(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), m);
-      reinterpret_cast<float4*>(s.z)[i] = v;
-    }
-  } else {
-    for (int i = tid; i < len / 4; i += kThreads) {
-      const int x = s.base + 4 * i;
-      float4 v;
-      if (x >= 0 && x + 3 < V) {
-        v = __ldcg(reinterpret_cast<const float4*>(z + x));
-      } else {
-        v.x = x >= 0 && x < V ? __ldcg(z + x) : -INFINITY;
-        v.y = x + 1 >= 0 && x + 1 < V ? __ldcg(z + x + 1) : -INFINITY;
-        v.z = x + 2 >= 0 && x + 2 < V ? __ldcg(z + x + 2) : -INFINITY;
-        v.w = x + 3 >= 0 && x + 3 < V ? __ldcg(z + x + 3) : -INFINITY;
-      }
-      v = make_float4(sane(v.x), sane(v.y), sane(v.z), sane(v.w));
-      m = fmaxf(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), m);
-      reinterpret_cast<float4*>(s.z)[i] = v;
-    }
+    for (int i = q_lo + tid; i < q_hi; i += kThreads) take(i, s4[i]);
   }
 #pragma unroll
   for (int o = 1; o < kThreads / kGroups; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
