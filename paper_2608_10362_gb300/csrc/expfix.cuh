@@ -9,10 +9,9 @@
 // between two ids (25 of 11232 in sampling.cu's kernel).  131072 weights stay below 2^63 + 2^17.
 //
 // exp by a table of 2^(i/256) and a cubic for the rest (the table-driven scheme of
-// P. T. P. Tang, ACM TOMS 15 (1989)): y = (z - max) log2(e) / T as an unevaluated sum of
-// two floats, n = round(256 y), y - n / 256 in [-1/512, 1/512], where 2^f - 1 is small
-// enough that 24 bits of it are 34 of the weight.  About 30 instructions, none of them
-// 64-bit floating point (2 a clock and SM here).
+// P. T. P. Tang, ACM TOMS 15 (1989)): 256 y = 256 (z - max) log2(e) / T = n + f with a whole
+// n and |f| <= 1, where 2^(f/256) - 1 is small enough that 24 bits of it are 33 of the
+// weight.  About 30 instructions, none of them 64-bit floating point (2 a clock and SM here).
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -50,10 +49,18 @@ __device__ __forceinline__ const unsigned long long* exp_table() {
   return t.v;
 }
 
-// What weight() needs of a row: the maximum and log2(e) / T in two floats.
+// What weights need of a row: the maximum, and c = log2(e) / T in two floats.
 struct WeightScale {
-  float max, hi, lo;
+  float max, hi, lo;        // c = hi + lo
+  bool near;                // 256 z c stays below 2^22 for the z that have weight: then also
+  float hi256, lo256;       // 256 c,
+  float f_max;              // 256 max c = n_max + f_max,
+  int n_max;
+  float z_deep;             // and a logit without weight
 };
+constexpr float kRound = 12582912.f;          // 1.5 * 2^23: x + kRound has round(x) in its low bits
+constexpr int kRoundBits = 0x4B400000;
+constexpr int kNoWeight = -45 * kExpSteps;    // n at and below which the weight is 0
 __device__ __forceinline__ WeightScale weight_scale(float row_max, float temperature) {
   // T below 1e-30 leaves the maxima alone with weight; T = inf weighs all alike.  A quotient
   // and its remainder's in 32 bits: 64-bit arithmetic by every thread of a CTA is 2 us.
@@ -63,34 +70,49 @@ __device__ __forceinline__ WeightScale weight_scale(float row_max, float tempera
   s.max = row_max;
   s.hi = __fdiv_rn(kHi, T);
   s.lo = s.hi > 0.f ? __fdiv_rn(fmaf(-s.hi, T, kHi) + kLo, T) : 0.f;
+  s.hi256 = s.hi * kExpSteps;
+  s.lo256 = s.lo * kExpSteps;
+  s.near = s.hi > 0.f && fabsf(row_max) * s.hi256 < 4e6f;
+  const float big = fmaf(row_max, s.hi256, kRound);
+  s.n_max = __float_as_int(big) - kRoundBits;
+  s.f_max = fmaf(row_max, s.lo256, fmaf(row_max, s.hi256, kRound - big));
+  s.z_deep = row_max - 47.f / s.hi;
   return s;
 }
 
-// (max - z) log2(e) / T rounded to a float: falls monotonically as z grows (each of the
-// two roundings is monotonic), inf or NaN where z is -inf.
-__device__ __forceinline__ float weight_depth(float z, const WeightScale& s) { return (s.max - z) * s.hi; }
-
-// z finite or -inf, z <= s.max.
-__device__ __forceinline__ unsigned long long weight(float z, const WeightScale& s,
-                                                     const unsigned long long* table) {
-  // max - z = d + e exactly (two-sum)
+// The whole part n of 256 (z - max) c and the rest f, z finite or -inf and z <= s.max;
+// n <= kNoWeight: no weight.  n grows with z (each step is monotonic).
+__device__ __forceinline__ int weight_place(float z, const WeightScale& s, float& f) {
+  if (s.near) {   // 256 z c less 256 max c, part by part
+    z = fmaxf(z, s.z_deep);
+    const float big = fmaf(z, s.hi256, kRound);
+    f = fmaf(z, s.lo256, fmaf(z, s.hi256, kRound - big)) - s.f_max;
+    return __float_as_int(big) - (kRoundBits + s.n_max);
+  }
+  // the difference first: max - z = d + e exactly (two-sum)
   const float d = s.max - z;
   const float b = d - s.max;
   const float e = (s.max - (d - b)) - (z + b);
-  const float yh = d * s.hi;
-  const float yl = fmaf(d, s.hi, -yh) + fmaf(d, s.lo, e * s.hi);
-  // n = round(-256 yh), its integer in the low bits of the sum with 1.5 * 2^23
-  const float big = fmaf(yh, -256.f, 12582912.f);
-  const int n = __float_as_int(big) - 0x4B400000;
-  const float f = fmaf(big - 12582912.f, -1.f / 256.f, -yh) - yl;   // exact but for the subtraction of yl
-  const float u = f * 0.693147180559945f;
-  const float p = fmaf(u * u, fmaf(u, 1.f / 6.f, 0.5f), u);         // 2^f - 1, |p| < 0.0014
+  const float yh = d * s.hi256;
+  const float yl = fmaf(d, s.hi256, -yh) + fmaf(d, s.lo256, e * s.hi256);
+  const float big = kRound - yh;
+  f = ((kRound - big) - yh) - yl;
+  return yh < 46.f * kExpSteps ? __float_as_int(big) - kRoundBits : 2 * kNoWeight;
+}
+__device__ __forceinline__ unsigned long long weight_at(int n, float f, const unsigned long long* table) {
+  const float u = f * static_cast<float>(0.693147180559945 / kExpSteps);
+  const float p = fmaf(u * u, fmaf(u, 1.f / 6.f, 0.5f), u);         // 2^(f/256) - 1, below 0.0028
   const unsigned long long t = table[n & (kExpSteps - 1)];          // [2^62, 2^63)
-  // t * p: the upper half of t times p in units of 2^-40, in units of 2^24
-  const long long r = static_cast<long long>(__mulhi(static_cast<int>(t >> 32), __float2int_rn(p * 1099511627776.f)));
-  const unsigned long long w = t + static_cast<unsigned long long>(r * (1ll << 24));
+  // t * p: the upper half of t times p in units of 2^-39, in units of 2^25
+  const long long r = static_cast<long long>(__mulhi(static_cast<int>(t >> 32), __float2int_rn(p * 549755813888.f)));
+  const unsigned long long w = t + static_cast<unsigned long long>(r * (1ll << 25));
   // 2 floor(x / 2) + 1 is x in the mean, so that truncation adds no drift to a long sum
-  return yh < 45.f ? (w >> (kExpBits - kWeightBits - (n >> 8))) | 1u : 0;
+  return n > kNoWeight ? (w >> (kExpBits - kWeightBits - (n >> 8))) | 1u : 0;
+}
+__device__ __forceinline__ unsigned long long weight(float z, const WeightScale& s, const unsigned long long* table) {
+  float f;
+  const int n = weight_place(z, s, f);
+  return weight_at(n, f, table);
 }
 
 // The float order of logits as unsigned keys (-0 as +0).

@@ -41,25 +41,27 @@
 namespace memspec {
 namespace {
 
-constexpr int kThreads = 256;     // 64 elements each of the longest slice: what a thread does
-                                  // once per row is a third of its instructions at 512
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxVocab = 131072;
+constexpr int kMaxSlice = 16388;             // floats of a CTA's slice: three CTAs per SM
+constexpr int kMaxCluster = 8;
 constexpr uint32_t kCopyBytes = 16384;
 constexpr float kLargest = 3.402823466e38f;
+constexpr int kBins = 256;                   // of a search's histogram
+constexpr int kBinBits = 8;
+constexpr int kSupers = kBins / 32;          // groups of 32 bins
+constexpr int kMantissa = 4;                 // counts: 16 bins an octave of max - z, from 2^-10 to 2^6
+constexpr int kFirstOctave = (127 - 10) << kMantissa;
+constexpr int kPlacesPerBin = 64;            // weights: a bin per quarter of log2 of the weight
+static_assert(-kNoWeight / kPlacesPerBin <= kBins, "every weight has a bin");
+constexpr uint32_t kList = 256;              // list entries of a CTA and of the cluster
+constexpr int kGroups = 64;                  // groups of threads whose maxima give the bound
+constexpr int kMostAbove = 56;               // of them above it at most
+constexpr int kWideCtas = 304;               // launches of at most so many CTAs: 512 threads each
 
 typedef unsigned long long u64;
 
 // NaN as -inf, +inf as the largest finite number.
 __device__ __forceinline__ float sane(float z) { return fminf(fmaxf(z, -INFINITY), kLargest); }
-
-constexpr int kMaxCluster = 8;
-constexpr int kMantissa = 4;                 // bins per octave of depth: 2^4
-constexpr int kBins = 16 << kMantissa;       // depths 2^-10 .. 2^6, clamped
-constexpr int kSupers = kBins / 32;          // groups of 32 bins
-constexpr uint32_t kList = 256;              // list entries of a CTA and of the cluster
-constexpr int kGroups = 64;                  // groups of 4 threads whose maxima give the bound
-constexpr int kMostAbove = 56;               // of them above it at most
 
 struct alignas(16) Smem {
   u64 table[kExpSteps];
@@ -73,9 +75,11 @@ struct alignas(16) Smem {
         uint32_t cnt[kMaxCluster][32];
       } p;
     };
+    u64 entry[kList];                        // the cluster's list, to sort it
     struct {
-      u64 entry[kList], weight[kList];
-    } all;                                   // the cluster's list
+      u64 weight[kList];                     // draw_from_list: weights in the rule's order,
+      uint32_t by_id[kList];                 // and their places in id order
+    } d;
   };
   u64 list[kList];                           // this CTA's: (~key << 32) | id
   // of this CTA, read by the others
@@ -87,13 +91,13 @@ struct alignas(16) Smem {
   uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
   float2 log_min_p;                          // T log(min_p) in two floats
   u64 peer_sum[kMaxCluster];                 // pushed
-  u64 scan[kWarps];
+  u64 scan[16];
   uint32_t group[kGroups];                   // keys
   uint64_t loaded;                           // mbarrier of the slice's copies
   uint32_t tie_id;                           // pushed
-  u64 cut, total;
+  u64 cut;
 };
-static_assert(3 * (sizeof(Smem) + 16388 * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
+static_assert(3 * (sizeof(Smem) + kMaxSlice * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
 
 // A row's rule, with what "off" means resolved.
 struct Rule {
@@ -116,6 +120,7 @@ __device__ __forceinline__ Rule rule_of(const FilterArgs& a, int row) {
   return r;
 }
 
+// ------------------------------------------------ sums over a warp and a CTA of NT threads
 __device__ __forceinline__ u64 warp_sum(u64 v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -131,6 +136,7 @@ __device__ __forceinline__ T warp_scan(T v) {   // inclusive
   }
   return v;
 }
+template <int NT>
 __device__ u64 block_sum(u64 v, u64* scratch) {
   v = warp_sum(v);
   __syncthreads();
@@ -138,8 +144,47 @@ __device__ u64 block_sum(u64 v, u64* scratch) {
   __syncthreads();
   u64 s = 0;
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) s += scratch[i];
+  for (int i = 0; i < NT / 32; ++i) s += scratch[i];
   return s;
+}
+// Inclusive sum over the threads up to this one; *total over all.
+template <int NT>
+__device__ u64 block_scan(u64 v, u64* scratch, u64* total) {
+  const u64 incl = warp_scan(v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 31) scratch[threadIdx.x >> 5] = incl;
+  __syncthreads();
+  u64 before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < NT / 32; ++i) {
+    const u64 x = scratch[i];
+    if (i < static_cast<int>(threadIdx.x >> 5)) before += x;
+    all += x;
+  }
+  *total = all;
+  return before + incl;
+}
+// Ascending values, one per thread, of which the first n threads' matter (n <= kList; the
+// others hold the type's largest): a bitonic network over the next power of two.
+template <class T>
+__device__ void block_sort(T& v, uint32_t n, T* scratch) {
+  const uint32_t i = threadIdx.x;
+  uint32_t size = 32;
+  while (size < n) size *= 2;
+  for (uint32_t k = 2; k <= size; k *= 2)
+    for (uint32_t j = k / 2; j > 0; j /= 2) {
+      T other = v;
+      if (j >= 32) {
+        __syncthreads();
+        if (i < kList) scratch[i] = v;
+        __syncthreads();
+        if (i < kList) other = scratch[i ^ j];
+      } else {
+        other = __shfl_xor_sync(0xffffffffu, v, j);
+      }
+      const bool up = (i & k) == 0 || k == size, low = (i & j) == 0;
+      v = (up == low) == (other < v) ? other : v;
+    }
 }
 // All threads of the cluster: what they wrote before is read after.
 __device__ __forceinline__ void cluster_sync() {
@@ -147,35 +192,48 @@ __device__ __forceinline__ void cluster_sync() {
   cluster_wait_acquire();
 }
 
-// The cut after the last kept id of a row's order: (~key << 32) | id; entries up to it are kept.
+// An element's place in a row's order: (~key << 32) | id.  The cut is the last kept one.
 __device__ __forceinline__ u64 entry_of(uint32_t key, uint32_t id) {
   return (static_cast<u64>(~key) << 32) | id;
 }
+__device__ __forceinline__ float entry_logit(u64 e) { return key_logit(~static_cast<uint32_t>(e >> 32)); }
 
 // A CTA's slice of a row in shared memory: ids base .. base + len - 1, -inf where there is
-// none.  Element i of the slice is held by nobody in particular: passes deal float4s.
+// none.
 struct Slice {
   float* z;
   int base, len;            // len a multiple of 4
 };
 
-struct Part {               // one search: what it looks at and for
-  bool mass;                // top-p: `need` is a fraction of the sum; else a count
-  u64 need;
-  float scale;              // depth = (max - z) * scale
-  float max, deepest;       // elements deeper than `deepest` are not the cut (only their weight counts)
+// Four elements at a time, those of which one at least reaches z_min.  Passes work on the
+// four together, so that their arithmetic and their atomics overlap.
+template <int NT, class Each>
+__device__ __forceinline__ void for_quads(const Slice& s, float z_min, Each each) {
+  const float4* z4 = reinterpret_cast<const float4*>(s.z);
+  for (int i = threadIdx.x; i < s.len / 4; i += NT) {
+    const float4 v = z4[i];
+    if (fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) < z_min) continue;
+    const float z[4] = {v.x, v.y, v.z, v.w};
+    each(z, s.base + 4 * i);
+  }
+}
+
+// ------------------------------------------------ one search: top-k or top-p
+struct Part {
+  u64 need;                 // the count, or (weights) the fraction of the sum, in 2^-64
+  int n_min;                // weights: places below this one are not the cut, only their sum counts
   u64 within;               // entries up to this one take part
 };
 
-__device__ __forceinline__ int bin_of(float depth) {
-  const int b = static_cast<int>(__float_as_uint(depth) >> (23 - kMantissa)) - ((127 - 10) << kMantissa);
+__device__ __forceinline__ int count_bin(float depth) {
+  const int b = static_cast<int>(__float_as_uint(depth) >> (23 - kMantissa)) - kFirstOctave;
   return max(0, min(b, kBins - 1));
 }
 
 // A histogram's bin that holds the cut, by the same steps in every CTA of the cluster.
 struct Found {
   int bin;
-  u64 above;                // sum (count or mass) before the bin
+  u64 above;                // sum (count or weights) before the bin
   uint32_t count;           // elements in it
   uint32_t count_above;     // and before it
   u64 need;                 // what the prefix has to reach
@@ -183,36 +241,37 @@ struct Found {
 };
 
 // After the histogram of every CTA is complete and the cluster has synchronised.
-__device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) {
+template <int NT, bool kMass>
+__device__ Found find_bin(bool first, u64 need, int C, Smem& sm) {
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   Found f;
   // the groups' sums of all CTAs
   if (tid < C * kSupers) {
     const int peer = tid / kSupers, g = tid % kSupers;
     sm.p.cnt[peer][g] = ld_cluster_u32(mapa_shared(smem_addr(&sm.sup_cnt[g]), peer));
-    if (p.mass) sm.p.mass[peer][g] = ld_cluster_u64(mapa_shared(smem_addr(&sm.sup_mass[g]), peer));
+    if (kMass) sm.p.mass[peer][g] = ld_cluster_u64(mapa_shared(smem_addr(&sm.sup_mass[g]), peer));
   }
-  if (p.mass && first && tid < C) sm.p_tail[tid] = ld_cluster_u64(mapa_shared(smem_addr(&sm.tail), tid));
+  if (kMass && first && tid < C) sm.p_tail[tid] = ld_cluster_u64(mapa_shared(smem_addr(&sm.tail), tid));
   __syncthreads();
   u64 v = 0, tail = 0;
   uint32_t n = 0;
   if (lane < kSupers)
     for (int c = 0; c < C; ++c) {
       n += sm.p.cnt[c][lane];
-      if (p.mass) v += sm.p.mass[c][lane];
+      if (kMass) v += sm.p.mass[c][lane];
     }
-  if (!p.mass) v = n;
+  if (!kMass) v = n;
   u64 incl = warp_scan(v);
   const uint32_t n_incl = warp_scan(n);
   const u64 total = __shfl_sync(0xffffffffu, incl, 31);
-  if (p.mass && first) {
+  if (kMass && first) {
     for (int c = 0; c < C; ++c) tail += sm.p_tail[c];
     const u64 s = total + tail, part = need * s;          // the fraction times the sum, rounded up
     need = __umul64hi(need, s) + (part != 0 ? 1 : 0);
     if (need == 0) need = 1;
   }
   f.need = need;
-  f.all = !p.mass && need >= total;
+  f.all = !kMass && need >= total;
   const unsigned reach = __ballot_sync(0xffffffffu, lane < kSupers && incl >= need);
   const int g = reach ? __ffs(reach) - 1 : kSupers - 1;
   const u64 before = __shfl_sync(0xffffffffu, incl - v, g);
@@ -220,7 +279,7 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   __syncthreads();                                        // p is read
   if (w < C) {
     sm.p.cnt[w][lane] = ld_cluster_u32(mapa_shared(smem_addr(&sm.h.cnt[g * 32 + lane]), w));
-    if (p.mass)
+    if (kMass)
       sm.p.mass[w][lane] = ld_cluster_u32(mapa_shared(smem_addr(&sm.h.lo[g * 32 + lane]), w)) |
                            (static_cast<u64>(ld_cluster_u32(mapa_shared(smem_addr(&sm.h.hi[g * 32 + lane]), w))) << 32);
   }
@@ -229,9 +288,9 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   v = 0;
   for (int c = 0; c < C; ++c) {
     n += sm.p.cnt[c][lane];
-    if (p.mass) v += sm.p.mass[c][lane];
+    if (kMass) v += sm.p.mass[c][lane];
   }
-  if (!p.mass) v = n;
+  if (!kMass) v = n;
   incl = before + warp_scan(v);
   const unsigned hit = __ballot_sync(0xffffffffu, incl >= need);
   const int b = hit ? __ffs(hit) - 1 : 31;
@@ -241,40 +300,41 @@ __device__ Found find_bin(const Part& p, bool first, u64 need, int C, Smem& sm) 
   f.count_above = n_before + __shfl_sync(0xffffffffu, warp_scan(n) - n, b);
   return f;
 }
+static_assert(256 / 32 >= kMaxCluster && 256 >= kMaxCluster * kSupers, "a warp per CTA of the cluster");
 
-// The elements of at least z_min (four at a time: some below it too).
-template <class Each>
-__device__ __forceinline__ void for_slice(const Slice& s, float z_min, Each each) {
-  const float4* z4 = reinterpret_cast<const float4*>(s.z);
-  for (int i = threadIdx.x; i < s.len / 4; i += kThreads) {
-    const float4 v = z4[i];
-    if (fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) < z_min) continue;
-    each(v.x, s.base + 4 * i);
-    each(v.y, s.base + 4 * i + 1);
-    each(v.z, s.base + 4 * i + 2);
-    each(v.w, s.base + 4 * i + 3);
+// Elements of a quad into their bins: counts, and weights as 64-bit sums in two words.
+template <bool kMass>
+__device__ __forceinline__ void add_to_bins(Smem& sm, const bool (&in)[4], const int (&bin)[4], const u64 (&w)[4]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (in[q]) atomicAdd(&sm.h.cnt[bin[q]], 1u);
+  if constexpr (kMass) {
+    uint32_t old[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) old[q] = in[q] ? atomicAdd(&sm.h.lo[bin[q]], static_cast<uint32_t>(w[q])) : 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t lo = static_cast<uint32_t>(w[q]);
+      const uint32_t hi = static_cast<uint32_t>(w[q] >> 32) + (old[q] + lo < old[q] ? 1u : 0u);
+      if (in[q] && hi != 0) atomicAdd(&sm.h.hi[bin[q]], hi);
+    }
   }
 }
-
-__device__ __forceinline__ void add_mass(Smem& sm, int bin, u64 w) {
-  const uint32_t lo = static_cast<uint32_t>(w);
-  const uint32_t old = atomicAdd(&sm.h.lo[bin], lo);
-  const uint32_t hi = static_cast<uint32_t>(w >> 32) + (old + lo < old ? 1u : 0u);
-  if (hi != 0) atomicAdd(&sm.h.hi[bin], hi);
-}
+template <int NT>
 __device__ void clear_histogram(Smem& sm) {
   uint32_t* h = reinterpret_cast<uint32_t*>(&sm.h);
-  for (int i = threadIdx.x; i < static_cast<int>(sizeof(sm.h) / 4); i += kThreads) h[i] = 0;
+  for (int i = threadIdx.x; i < static_cast<int>(sizeof(sm.h) / 4); i += NT) h[i] = 0;
   __syncthreads();
 }
 // The groups' sums of this CTA's histogram, then the cluster's barrier.
-__device__ void close_histogram(const Part& p, Smem& sm) {
+template <int NT, bool kMass>
+__device__ void close_histogram(Smem& sm) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   __syncthreads();
-  for (int g = w; g < kSupers; g += kWarps) {
+  for (int g = w; g < kSupers; g += NT / 32) {
     const uint32_t n = __reduce_add_sync(0xffffffffu, sm.h.cnt[g * 32 + lane]);
     u64 m = 0;
-    if (p.mass) m = warp_sum(sm.h.lo[g * 32 + lane] | (static_cast<u64>(sm.h.hi[g * 32 + lane]) << 32));
+    if (kMass) m = warp_sum(sm.h.lo[g * 32 + lane] | (static_cast<u64>(sm.h.hi[g * 32 + lane]) << 32));
     if (lane == 0) {
       sm.sup_cnt[g] = n;
       sm.sup_mass[g] = m;
@@ -283,9 +343,8 @@ __device__ void close_histogram(const Part& p, Smem& sm) {
   cluster_sync();
 }
 
-// The CTAs' lists into sm.all; returns the number of entries.  All threads.
-template <class Mass>
-__device__ uint32_t pull_list(int C, bool weighted, Mass mass, Smem& sm) {
+// The CTAs' lists, an entry per thread (~0 past the last), sorted; returns how many.
+__device__ uint32_t pull_list(int C, u64& e, Smem& sm) {
   // a warp per CTA: lane c has CTA c's count
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   uint32_t n = lane < C ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0;
@@ -293,144 +352,166 @@ __device__ uint32_t pull_list(int C, bool weighted, Mass mass, Smem& sm) {
   const uint32_t off = __shfl_sync(0xffffffffu, incl - n, w);
   n = __shfl_sync(0xffffffffu, n, w);
   if (w < C)
-    for (uint32_t i = lane; i < n && off + i < kList; i += 32) {
-      const u64 e = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), w));
-      sm.all.entry[off + i] = e;
-      sm.all.weight[off + i] = weighted ? mass(key_logit(~static_cast<uint32_t>(e >> 32))) : 1;
-    }
+    for (uint32_t i = lane; i < n && off + i < kList; i += 32)
+      sm.entry[off + i] = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), w));
   __syncthreads();
+  e = threadIdx.x < all ? sm.entry[threadIdx.x] : ~0ull;
+  block_sort(e, all, sm.entry);
   return all;
 }
-static_assert(kWarps >= kMaxCluster, "a warp per CTA of the cluster");
-
-// Over the n entries of sm.all, 2^bits threads to an entry: the sum of value(e, j) over all
-// j, then use(i, e, sum) in the first of them.
-template <class Value, class Use>
-__device__ __forceinline__ void for_pairs(uint32_t n, Smem& sm, Value value, Use use) {
-  const int bits = n <= kThreads / 8 ? 3 : n <= kThreads / 4 ? 2 : n <= kThreads / 2 ? 1 : 0;
-  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1);
-  const u64 e = i < n ? sm.all.entry[i] : 0;
-  u64 sum = 0;
-  if (i < n)
-    for (uint32_t j = part; j < n; j += 1u << bits) sum += value(e, j);
-  for (int o = 1 << bits >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (i < n && part == 0) use(i, e, sum);
-}
-static_assert(kList <= kThreads, "an entry per thread");
 
 struct Ended {
   u64 cut;
-  uint32_t listed;          // > 0: sm.all holds so many entries, all up to the cut among them
+  uint32_t listed;          // > 0: the threads hold so many sorted entries, all up to the cut among them
+  u64 entry;
 };
 
-// The entry at which the prefix that p asks for ends.
-template <class Mass>
-__device__ Ended search(const Part& p, const Slice& s, int C, int rank, Mass mass, Smem& sm) {
+// The entry at which the prefix that p asks for ends.  kMass: by weights, else by count.
+template <int NT, bool kMass>
+__device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, int C, int rank, Smem& sm) {
   const int tid = threadIdx.x;
-  auto depth = [&](float z) { return (p.max - z) * p.scale; };
-  auto takes_part = [&](float z, int id) {
-    return z > -INFINITY && entry_of(logit_key(z), static_cast<uint32_t>(id)) <= p.within;
+  const float z_in = p.within == ~0ull ? -kLargest : entry_logit(p.within);
+  const uint32_t id_in = static_cast<uint32_t>(p.within);
+  auto takes_part = [&](float z, int id) { return z > z_in || (z == z_in && static_cast<uint32_t>(id) <= id_in); };
+  // an element's bin, or one past the last: it takes no part or is not the cut
+  auto bin_of = [&](float z, int id) {
+    int b;
+    if (kMass) {
+      float f;
+      const int n = weight_place(z, ws, f);
+      b = n < p.n_min ? kBins : -n / kPlacesPerBin;
+    } else {
+      b = count_bin(ws.max - z);
+    }
+    return takes_part(z, id) ? b : kBins;
   };
-  const bool whole = p.within == ~0ull;
-  const float z_in = whole ? -kLargest : key_logit(~static_cast<uint32_t>(p.within >> 32));
-  clear_histogram(sm);
+  clear_histogram<NT>(sm);
   if (tid == 0) {
     sm.n_list = 0;
     sm.cut = p.within;
   }
   u64 tail = 0;
-  for_slice(s, z_in, [&](float z, int id) {
-    if (whole ? z == -INFINITY : !takes_part(z, id)) return;
-    const float d = depth(z);
-    const u64 w = p.mass ? mass(z) : 0;
-    if (d > p.deepest) {
-      tail += w;
-      return;
+  for_quads<NT>(s, z_in, [&](const float (&z)[4], int id) {
+    bool in[4];
+    int bin[4];
+    u64 w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      in[q] = takes_part(z[q], id + q);
+      if (kMass) {
+        float f;
+        const int n = weight_place(z[q], ws, f);
+        w[q] = weight_at(n, f, sm.table);
+        bin[q] = -n / kPlacesPerBin;
+        if (n < p.n_min) {
+          tail += in[q] ? w[q] : 0;
+          in[q] = false;
+        }
+      } else {
+        w[q] = 0;
+        bin[q] = count_bin(ws.max - z[q]);
+      }
     }
-    const int b = bin_of(d);
-    atomicAdd(&sm.h.cnt[b], 1u);
-    if (p.mass) add_mass(sm, b, w);
+    add_to_bins<kMass>(sm, in, bin, w);
   });
-  if (p.mass) {
-    tail = block_sum(tail, sm.scan);
+  if (kMass) {
+    tail = block_sum<NT>(tail, sm.scan);
     if (tid == 0) sm.tail = tail;
   }
-  close_histogram(p, sm);
-  Found f = find_bin(p, true, p.need, C, sm);
+  close_histogram<NT, kMass>(sm);
+  Found f = find_bin<NT, kMass>(true, p.need, C, sm);
   if (f.all) {
     cluster_sync();           // the others have read this CTA's histogram
-    return {p.within, 0};
+    return {p.within, 0, 0};
   }
   const int bin = f.bin;
-  // the keys that the bin's elements can have: those of its depths with a margin (depth is
-  // (max - z) * scale, off by some units in the last place of the larger term)
+  // the keys that the bin's elements can have: from the depths at its ends, with a margin
+  // for the roundings of a place or a depth and of these lines
   uint32_t k_lo, k_hi;
   {
-    constexpr int kFirst = (127 - 10) << kMantissa;
-    const float a0 = __uint_as_float(static_cast<uint32_t>(bin + kFirst) << (23 - kMantissa));
-    const float a1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + kFirst) << (23 - kMantissa));
-    const float z1 = p.max - a0 / p.scale, z0 = p.max - a1 / p.scale;
-    const float slack = 4e-7f * (fabsf(p.max) + fabsf(z0)) + 1e-37f;
-    k_hi = bin == 0 || !(z1 + slack < p.max) ? logit_key(p.max) : logit_key(z1 + slack);
-    k_lo = bin == kBins - 1 || !(z0 - slack > -kLargest) ? logit_key(-kLargest) : logit_key(z0 - slack);
+    float d0, d1;             // max - z
+    if (kMass) {
+      d0 = static_cast<float>(bin * kPlacesPerBin - 1) / ws.hi256;
+      d1 = static_cast<float>((bin + 1) * kPlacesPerBin + 1) / ws.hi256;
+    } else {
+      d0 = __uint_as_float(static_cast<uint32_t>(bin + kFirstOctave) << (23 - kMantissa));
+      d1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + kFirstOctave) << (23 - kMantissa));
+    }
+    const float z1 = ws.max - d0, z0 = ws.max - d1;
+    const float slack = 4e-7f * (fabsf(ws.max) + fabsf(z0)) + 1e-37f;
+    k_hi = bin == 0 || !(z1 + slack < ws.max) ? logit_key(ws.max) : logit_key(z1 + slack);
+    k_lo = (!kMass && bin == kBins - 1) || !(z0 - slack > -kLargest) ? logit_key(-kLargest) : logit_key(z0 - slack);
   }
   int shift = 32;             // keys per bin of the last division: 2^shift
-  auto in_bin = [&](float z, int id) {
-    if (whole ? z == -INFINITY : !takes_part(z, id)) return false;
-    const float d = depth(z);
-    if (d > p.deepest || bin_of(d) != bin) return false;
-    const uint32_t k = logit_key(z);
-    return k >= k_lo && k <= k_hi;
-  };
+  float z_lo = key_logit(k_lo), z_hi = key_logit(k_hi);
   auto narrow = [&] {         // to the keys of bin f.bin of the last division
     k_hi -= static_cast<uint32_t>(f.bin) << shift;
     if (k_hi - k_lo >= 1u << shift) k_lo = k_hi - ((1u << shift) - 1);
+    z_lo = key_logit(k_lo);
+    z_hi = key_logit(k_hi);
+  };
+  // for the draw it pays to have all of the kept elements
+  const bool whole_list = kMass && f.count_above + f.count <= kList;
+  // the elements of the bin (whole_list: up to it) of a quad; false: none
+  auto choose = [&](const float (&z)[4], int id, bool (&in)[4]) {
+    const float top = whole_list ? kLargest : z_hi;
+    bool any = false;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) any |= in[q] = z[q] >= z_lo && z[q] <= top;
+    if (!any) return false;
+    any = false;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int b = bin_of(z[q], id + q);
+      any |= in[q] = in[q] && (whole_list ? b <= bin : b == bin);
+    }
+    return any;
   };
   u64 above = f.above;
-  // for the draw it pays to have all of the kept elements
-  const bool whole_list = p.mass && f.count_above + f.count <= kList;
   while (f.count > kList) {
     if (shift == 32) {        // the first division of [k_lo, k_hi]
-      shift = max(0, 32 - __clz(k_hi - k_lo) - (4 + kMantissa));
+      shift = max(0, 32 - __clz(k_hi - k_lo) - kBinBits);
     } else {
       if (shift == 0) break;
       narrow();
-      shift = max(0, shift - (4 + kMantissa));
+      shift = max(0, shift - kBinBits);
     }
     cluster_sync();           // the others have read this CTA's histogram
-    clear_histogram(sm);
-    for_slice(s, key_logit(k_lo), [&](float z, int id) {
-      if (!in_bin(z, id)) return;
-      const int b = static_cast<int>((k_hi - logit_key(z)) >> shift);
-      atomicAdd(&sm.h.cnt[b], 1u);
-      if (p.mass) add_mass(sm, b, mass(z));
+    clear_histogram<NT>(sm);
+    for_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
+      bool in[4];
+      if (!choose(z, id, in)) return;
+      int b[4];
+      u64 w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        b[q] = static_cast<int>((k_hi - logit_key(z[q])) >> shift) & (kBins - 1);
+        w[q] = kMass ? weight(z[q], ws, sm.table) : 0;
+      }
+      add_to_bins<kMass>(sm, in, b, w);
     });
-    close_histogram(p, sm);
-    f = find_bin(p, false, f.need - above, C, sm);
+    close_histogram<NT, kMass>(sm);
+    f = find_bin<NT, kMass>(false, f.need - above, C, sm);
     f.need += above;
     above += f.above;
   }
   if (shift < 32) narrow();
   if (f.count > kList) {      // one key: which of its ids
-    const u64 one = p.mass ? mass(key_logit(k_hi)) : 1;
+    const u64 one = kMass ? weight(z_hi, ws, sm.table) : 1;
     u64 left = (f.need - above + one - 1) / one;       // so many of them, in all CTAs
     // the bin's counts of the CTAs are still in sm.p
     int owner = 0;
     while (owner < C - 1 && left > sm.p.cnt[owner][f.bin & 31]) left -= sm.p.cnt[owner++][f.bin & 31];
     if (owner == rank) {
       // element order is id order: contiguous parts of the slice per thread
-      const int per = (s.len + kThreads - 1) / kThreads, lo = min(tid * per, s.len), hi = min(lo + per, s.len);
-      u64 n = 0;
-      for (int i = lo; i < hi; ++i) n += in_bin(s.z[i], s.base + i);
-      const u64 incl = warp_scan(n);
-      if ((tid & 31) == 31) sm.scan[tid >> 5] = incl;
-      __syncthreads();
-      u64 before = incl - n;
-      for (int i = 0; i < (tid >> 5); ++i) before += sm.scan[i];
-      if (before < left && left <= before + n) {
-        u64 seen = before;
+      const int per = (s.len + NT - 1) / NT, lo = min(tid * per, s.len), hi = min(lo + per, s.len);
+      auto tied = [&](int i) { return s.z[i] == z_hi && takes_part(s.z[i], s.base + i); };
+      u64 n = 0, all;
+      for (int i = lo; i < hi; ++i) n += tied(i);
+      u64 seen = block_scan<NT>(n, sm.scan, &all) - n;
+      if (seen < left && left <= seen + n) {
         for (int i = lo; i < hi; ++i)
-          if (in_bin(s.z[i], s.base + i) && ++seen == left) {
+          if (tied(i) && ++seen == left) {
             for (int c = 0; c < C; ++c)
               st_cluster_u32(mapa_shared(smem_addr(&sm.tie_id), c), static_cast<uint32_t>(s.base + i));
             break;
@@ -440,62 +521,62 @@ __device__ Ended search(const Part& p, const Slice& s, int C, int rank, Mass mas
     cluster_sync();
     const u64 cut = entry_of(k_hi, sm.tie_id);
     __syncthreads();
-    return {cut, 0};
+    return {cut, 0, 0};
   }
-  for_slice(s, key_logit(k_lo), [&](float z, int id) {
-    if (whole_list) {
-      const float d = depth(z);
-      if ((whole ? z == -INFINITY : !takes_part(z, id)) || d > p.deepest || bin_of(d) > bin) return;
-    } else if (!in_bin(z, id)) {
-      return;
-    }
-    const uint32_t i = atomicAdd(&sm.n_list, 1u);
-    if (i < kList) sm.list[i] = entry_of(logit_key(z), static_cast<uint32_t>(id));
+  for_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
+    bool in[4];
+    if (!choose(z, id, in)) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (in[q]) {
+        const uint32_t i = atomicAdd(&sm.n_list, 1u);
+        if (i < kList) sm.list[i] = entry_of(logit_key(z[q]), static_cast<uint32_t>(id + q));
+      }
   });
   cluster_sync();
-  const uint32_t n = pull_list(C, p.mass, mass, sm);   // into the histogram's place: nobody reads that any more
-  if (whole_list) above = 0;
-  for_pairs(n, sm, [&](u64 e, uint32_t i) { return sm.all.entry[i] < e ? sm.all.weight[i] : 0; },
-            [&](uint32_t i, u64 e, u64 before) {
-              before += above;
-              if (before < f.need && f.need <= before + sm.all.weight[i]) sm.cut = e;
-            });
+  u64 e, all;
+  const uint32_t n = pull_list(C, e, sm);   // into the histogram's place: nobody reads that any more
+  const u64 own = static_cast<uint32_t>(tid) >= n ? 0 : kMass ? weight(entry_logit(e), ws, sm.table) : 1;
+  const u64 incl = (whole_list ? 0 : above) + block_scan<NT>(own, sm.scan, &all);
+  if (incl - own < f.need && f.need <= incl) sm.cut = e;
   __syncthreads();
   const u64 cut = sm.cut;
   cluster_sync();             // the others have read this CTA's list
-  return {cut, whole_list ? n : 0};
+  return {cut, whole_list ? n : 0, e};
 }
 
-// The draw from the n entries of sm.all up to the cut.
-__device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 cut, Smem& sm) {
-  const uint32_t tid = threadIdx.x;
-  u64 v = 0;
-  if (tid < n) {
-    if (sm.all.entry[tid] > cut) sm.all.weight[tid] = 0;
-    v = sm.all.weight[tid];
-  }
-  const u64 total = block_sum(v, sm.scan);
+// The draw from the entries up to the cut among the n that the threads hold in order.
+template <int NT>
+__device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 e, u64 cut, const WeightScale& ws,
+                               Smem& sm) {
+  const uint32_t tid = threadIdx.x, t = __syncthreads_count(tid < n && e <= cut);   // kept: the first t
+  if (tid < kList) sm.d.weight[tid] = tid < t ? weight(entry_logit(e), ws, sm.table) : 0;
+  // the kept ids ascending, with their places
+  uint32_t by_id = tid < t ? static_cast<uint32_t>(e) << 8 | tid : ~0u;
+  block_sort(by_id, t, sm.d.by_id);
+  __syncthreads();
+  u64 total;
+  const u64 own = tid < t ? sm.d.weight[by_id & 255u] : 0;
+  const u64 incl = block_scan<NT>(own, sm.scan, &total);
   const u64 target = __umul64hi(fraction64(a.u[row]), total);
-  for_pairs(n, sm,
-            [&](u64 e, uint32_t i) {
-              return static_cast<uint32_t>(sm.all.entry[i]) < static_cast<uint32_t>(e) ? sm.all.weight[i] : 0;
-            },
-            [&](uint32_t i, u64 e, u64 before) {
-              if (before <= target && target < before + sm.all.weight[i])
-                a.out_tok[row] = static_cast<int>(static_cast<uint32_t>(e));
-            });
+  if (incl - own <= target && target < incl) a.out_tok[row] = static_cast<int>(by_id >> 8);
 }
+static_assert(kMaxVocab <= 1 << 24 && kList == 256, "an id and a place in 32 bits");
 
-template <bool kMask>
-__global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_constant__ FilterArgs a, int C, int len) {
+// NT = 512: half the latency of 256, where a launch leaves the chip mostly idle; 256: a third
+// fewer instructions a row (what a thread does once per row), where it fills it.
+template <int NT, bool kMask>
+__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __grid_constant__ FilterArgs a, int C,
+                                                                      int len) {
   extern __shared__ __align__(16) uint8_t raw[];
   Smem& sm = *reinterpret_cast<Smem*>(raw);
   Slice s;
   s.z = reinterpret_cast<float*>(raw + sizeof(Smem));
   s.len = len;
+  constexpr int kWarps = NT / 32;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const int rank = static_cast<int>(cluster_ctarank()), row = blockIdx.x / C, V = a.vocab;
-  for (int i = tid; i < kExpSteps; i += kThreads) sm.table[i] = exp_table()[i];
+  for (int i = tid; i < kExpSteps; i += NT) sm.table[i] = exp_table()[i];
   if (tid == 0) {
     sm.n_list = 0;
     mbar_init(&sm.loaded, 1);
@@ -508,13 +589,6 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   // ids are shifted so that the slice's float4s are aligned in memory
   const int shift = static_cast<int>((reinterpret_cast<uintptr_t>(z) >> 2) & 3);
   s.base = rank * len - shift;
-  const Rule r = rule_of(a, row);
-  const bool by_k = r.top_k > 0 && r.top_k < V, by_p = r.top_p < 1.f;
-  if (r.min_p > 0.f && tid == kThreads - 1) {   // 64-bit arithmetic: one thread's, beside the loads
-    const double l = static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
-    const float hi = static_cast<float>(l);
-    sm.log_min_p = make_float2(hi, static_cast<float>(l - static_cast<double>(hi)));
-  }
   // ------------------------------------------------ load; maximum and bound
   // whole float4s of the row by bulk copies (all of a slice's bytes are under way at once:
   // with loads through registers a quarter), its ragged ends by single loads
@@ -526,6 +600,13 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     for (uint32_t at = 0; at < bytes; at += kCopyBytes)
       bulk_load(s.z + 4 * q_lo + at / 4, z + s.base + 4 * q_lo + at / 4, min(kCopyBytes, bytes - at), &sm.loaded,
                 l2_policy_evict_normal());
+  }
+  const Rule r = rule_of(a, row);
+  const bool by_k = r.top_k > 0 && r.top_k < V, by_p = r.top_p < 1.f;
+  if (r.min_p > 0.f && tid == NT - 1) {   // 64-bit arithmetic: one thread's, beside the loads
+    const double l = static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
+    const float hi = static_cast<float>(l);
+    sm.log_min_p = make_float2(hi, static_cast<float>(l - static_cast<double>(hi)));
   }
   float m = -INFINITY;
   auto take = [&](int i, float4 v) {
@@ -544,18 +625,19 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     take(i, v);
   };
   if (tid < q_lo) load_quad(tid);
-  for (int i = q_hi + tid; i < len / 4; i += kThreads) load_quad(i);
+  for (int i = q_hi + tid; i < len / 4; i += NT) load_quad(i);
   if (q_hi > q_lo) {
     // the copies may be waited for once the barrier is initialised and they are announced
     __syncthreads();
     if (!mbar_wait_bounded(&sm.loaded, 0, nullptr, nullptr))
-      for (int i = q_lo + tid; i < q_hi; i += kThreads) load_quad(i);   // a thread takes what it loads
+      for (int i = q_lo + tid; i < q_hi; i += NT) load_quad(i);   // a thread takes what it loads
 #pragma unroll 4
-    for (int i = q_lo + tid; i < q_hi; i += kThreads) take(i, s4[i]);
+    for (int i = q_lo + tid; i < q_hi; i += NT) take(i, s4[i]);
   }
+  constexpr int kPerGroup = NT / kGroups;
 #pragma unroll
-  for (int o = 1; o < kThreads / kGroups; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (tid % (kThreads / kGroups) == 0) sm.group[tid / (kThreads / kGroups)] = logit_key(m);
+  for (int o = 1; o < kPerGroup; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (tid % kPerGroup == 0) sm.group[tid / kPerGroup] = logit_key(m);
   __syncthreads();
   // the bound: the j-th largest group maximum, j = what this CTA owes to the top k (if that
   // is more than the groups can give, the bound is not used)
@@ -582,11 +664,11 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     least = v.y;
   }
   m = key_logit(__reduce_max_sync(0xffffffffu, top));
-  const float bound = key_logit(max(__reduce_min_sync(0xffffffffu, least), logit_key(-kLargest)));
+  const float bound =
+      r.top_k == 1 ? m : key_logit(max(__reduce_min_sync(0xffffffffu, least), logit_key(-kLargest)));
   // ------------------------------------------------ the cut
   const bool empty = m == -INFINITY;
   const WeightScale ws = weight_scale(m, r.temperature);
-  auto mass = [&](float x) { return weight(x, ws, sm.table); };
   const u64 no_cut = entry_of(logit_key(-kLargest), ~0u);
   u64 cut = no_cut;
   if (r.min_p > 0.f && !empty) {
@@ -599,13 +681,16 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     cut = entry_of(min(key, logit_key(m)), ~0u);
   }
   const u64 fraction = fraction64(r.top_p);
-  uint32_t n = 0;             // > 0: sm.all holds so many entries, all the kept ones among them
+  uint32_t n = 0;             // > 0: so many candidates were listed and hold what is kept
   bool search_k = by_k && !empty;
   if (search_k && owed <= kMostAbove) {
-    for_slice(s, bound, [&](float x, int id) {
-      if (x < bound) return;
-      const uint32_t i = atomicAdd(&sm.n_list, 1u);
-      if (i < kList) sm.list[i] = entry_of(logit_key(x), static_cast<uint32_t>(id));
+    for_quads<NT>(s, bound, [&](const float (&x)[4], int id) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (x[q] >= bound) {
+          const uint32_t i = atomicAdd(&sm.n_list, 1u);
+          if (i < kList) sm.list[i] = entry_of(logit_key(x[q]), static_cast<uint32_t>(id + q));
+        }
     });
     cluster_sync();
     n = __reduce_add_sync(0xffffffffu, lane < C ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0u);
@@ -615,33 +700,26 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
         cluster_sync();
         return;
       }
-      pull_list(C, true, mass, sm);
+      u64 e;
+      pull_list(C, e, sm);
       if (kMask)
         cluster_sync();                    // the others have read this CTA's list
       else
         cluster_arrive_release();          // they may leave; nobody reads this CTA's
-      if (tid == 0) sm.cut = ~0ull;
-      __syncthreads();
-      for_pairs(n, sm, [&](u64 e, uint32_t i) { return static_cast<u64>(sm.all.entry[i] < e); },
-                [&](uint32_t, u64 e, u64 before) {
-                  if (before + 1 == static_cast<u64>(r.top_k)) sm.cut = e;
-                });
-      __syncthreads();
-      const u64 cut_k = sm.cut;
-      cut = min(cut, cut_k);
+      const uint32_t k = min(n, static_cast<uint32_t>(r.top_k));
       if (by_p) {
-        const u64 v = tid < n && sm.all.entry[tid] <= cut_k ? sm.all.weight[tid] : 0;
-        const u64 total = block_sum(v, sm.scan);
+        u64 total;
+        const u64 own = static_cast<uint32_t>(tid) < k ? weight(entry_logit(e), ws, sm.table) : 0;
+        const u64 incl = block_scan<NT>(own, sm.scan, &total);
         const u64 need = max(__umul64hi(fraction, total) + (fraction * total != 0 ? 1 : 0), 1ull);
-        for_pairs(n, sm, [&](u64 e, uint32_t i) { return sm.all.entry[i] < e ? sm.all.weight[i] : 0; },
-                  [&](uint32_t i, u64 e, u64 before) {
-                    if (before < need && need <= before + sm.all.weight[i]) sm.cut = e;
-                  });
-        __syncthreads();
-        cut = min(cut, sm.cut);
+        if (incl - own < need && need <= incl) sm.cut = e;
+      } else if (static_cast<uint32_t>(tid) == k - 1) {
+        sm.cut = e;
       }
+      __syncthreads();
+      cut = min(cut, sm.cut);
       if (!kMask) {
-        draw_from_list(a, row, n, cut, sm);
+        draw_from_list<NT>(a, row, n, e, cut, ws, sm);
         cluster_wait_acquire();
         return;
       }
@@ -652,28 +730,28 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
   }
   u64 within = no_cut;
   if (search_k) {
-    within = search(Part{false, static_cast<u64>(r.top_k), 1.f, m, INFINITY, ~0ull}, s, C, rank, mass, sm).cut;
+    within = search<NT, false>(Part{static_cast<u64>(r.top_k), 0, ~0ull}, s, ws, C, rank, sm).cut;
     cut = min(cut, within);
   }
   if (by_p && !empty && n == 0) {
     // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
     const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
-    const Ended e = search(Part{true, fraction, ws.hi, m, deepest, min(within, no_cut) == no_cut ? ~0ull : within}, s, C,
-                           rank, mass, sm);
+    const int n_min = max(-static_cast<int>(deepest * kExpSteps), kNoWeight + 1);
+    const Ended e = search<NT, true>(Part{fraction, n_min, within >= no_cut ? ~0ull : within}, s, ws, C, rank, sm);
     cut = min(cut, e.cut);
     if (!kMask && e.listed > 0) {
-      if (rank == 0) draw_from_list(a, row, e.listed, cut, sm);
+      if (rank == 0) draw_from_list<NT>(a, row, e.listed, e.entry, cut, ws, sm);
       return;
     }
   }
-  const float cut_z = key_logit(~static_cast<uint32_t>(cut >> 32));
+  const float cut_z = entry_logit(cut);
   const uint32_t cut_id = static_cast<uint32_t>(cut);
   auto kept = [&](float x, int id) { return x > cut_z || (x == cut_z && static_cast<uint32_t>(id) <= cut_id); };
   if constexpr (kMask) {
     float* out = a.out + row * a.out_ld;
     const bool aligned = ((reinterpret_cast<uintptr_t>(out) >> 2) & 3) == static_cast<uintptr_t>(shift);
     const bool inside = aligned && s.base >= 0 && s.base + len <= V;
-    for (int i = tid; i < len / 4; i += kThreads) {
+    for (int i = tid; i < len / 4; i += NT) {
       const int x = s.base + 4 * i;
       float4 o = reinterpret_cast<const float4*>(s.z)[i];
       if (fmaxf(fmaxf(o.x, o.y), fmaxf(o.z, o.w)) < cut_z) {
@@ -706,17 +784,18 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
     const bool some = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= cut_z;
     if (!__any_sync(0xffffffffu, some)) return false;
     const int x = s.base + i;
-    wt[0] = kept(v.x, x) ? mass(v.x) : 0;
-    wt[1] = kept(v.y, x + 1) ? mass(v.y) : 0;
-    wt[2] = kept(v.z, x + 2) ? mass(v.z) : 0;
-    wt[3] = kept(v.w, x + 3) ? mass(v.w) : 0;
+    wt[0] = kept(v.x, x) ? weight(v.x, ws, sm.table) : 0;
+    wt[1] = kept(v.y, x + 1) ? weight(v.y, ws, sm.table) : 0;
+    wt[2] = kept(v.z, x + 2) ? weight(v.z, ws, sm.table) : 0;
+    wt[3] = kept(v.w, x + 3) ? weight(v.w, ws, sm.table) : 0;
     return true;
   };
   u64 mine = 0;
   if (!empty)
+#pragma unroll 2
     for (int t = t_lo; t < t_hi; ++t) {
       u64 wt[4];
-      if (tile_weights(t, wt)) mine += wt[0] + wt[1] + wt[2] + wt[3];
+      if (tile_weights(t, wt)) mine += (wt[0] + wt[1]) + (wt[2] + wt[3]);
     }
   mine = warp_sum(mine);
   __syncthreads();
@@ -767,26 +846,28 @@ __global__ void __launch_bounds__(kThreads, 3) filter_kernel(const __grid_consta
 cudaError_t launch_filter(const FilterArgs& a, cudaStream_t s, bool pdl) {
   if (a.vocab > kMaxVocab) return cudaErrorInvalidValue;
   // as many CTAs per row as its slices need, more while the launch is small
-  constexpr int kMaxSlice = 16388;           // floats: three CTAs per SM
   int C = 1;
   while (C < kMaxCluster &&
          ((a.vocab + 3 + C - 1) / C > kMaxSlice - 3 || (a.rows * C * 2 <= 304 && a.vocab >= 2 * C * 2048)))
     C *= 2;
   const int len = ((a.vocab + 3 + C - 1) / C + 3) / 4 * 4;
-  static std::atomic<bool> set[2][64];
+  // 512 threads while every SM has one CTA at most
+  const bool wide = a.rows * C <= kWideCtas, mask = a.out != nullptr;
+  void (*const kernel)(FilterArgs, int, int) = wide ? (mask ? filter_kernel<512, true> : filter_kernel<512, false>)
+                                                    : (mask ? filter_kernel<256, true> : filter_kernel<256, false>);
+  static std::atomic<bool> set[4][64];
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.rows) * C);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(wide ? 512 : 256);
   cfg.dynamicSmemBytes = sizeof(Smem) + static_cast<size_t>(len) * 4;
   cfg.stream = s;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  const bool mask = a.out != nullptr;
-  if (e == cudaSuccess && (dev >= 64 || !set[mask][dev].load(std::memory_order_relaxed))) {
-    const int most = static_cast<int>(sizeof(Smem) + kMaxSlice * 4);
-    e = mask ? cudaFuncSetAttribute(filter_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)
-             : cudaFuncSetAttribute(filter_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e == cudaSuccess && dev < 64) set[mask][dev].store(true, std::memory_order_relaxed);
+  std::atomic<bool>* done = e == cudaSuccess && dev < 64 ? &set[wide * 2 + mask][dev] : nullptr;
+  if (e == cudaSuccess && (done == nullptr || !done->load(std::memory_order_relaxed))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(sizeof(Smem) + kMaxSlice * 4));
+    if (e == cudaSuccess && done != nullptr) done->store(true, std::memory_order_relaxed);
   }
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[2];
@@ -798,8 +879,7 @@ cudaError_t launch_filter(const FilterArgs& a, cudaStream_t s, bool pdl) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl ? 2 : 1;
-  return mask ? cudaLaunchKernelEx(&cfg, filter_kernel<true>, a, C, len)
-              : cudaLaunchKernelEx(&cfg, filter_kernel<false>, a, C, len);
+  return cudaLaunchKernelEx(&cfg, kernel, a, C, len);
 }
 
 namespace {
