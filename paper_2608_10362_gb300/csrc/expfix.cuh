@@ -82,13 +82,14 @@ __device__ __forceinline__ WeightScale weight_scale(float row_max, float tempera
 
 // The whole part n of 256 (z - max) c and the rest f, z finite or -inf and z <= s.max;
 // n <= kNoWeight: no weight.  n grows with z (each step is monotonic).
-__device__ __forceinline__ int weight_place(float z, const WeightScale& s, float& f) {
-  if (s.near) {   // 256 z c less 256 max c, part by part
-    z = fmaxf(z, s.z_deep);
-    const float big = fmaf(z, s.hi256, kRound);
-    f = fmaf(z, s.lo256, fmaf(z, s.hi256, kRound - big)) - s.f_max;
-    return __float_as_int(big) - (kRoundBits + s.n_max);
-  }
+__device__ __forceinline__ int place_near(float z, const WeightScale& s, float& f) {
+  // 256 z c less 256 max c, part by part
+  z = fmaxf(z, s.z_deep);
+  const float big = fmaf(z, s.hi256, kRound);
+  f = fmaf(z, s.lo256, fmaf(z, s.hi256, kRound - big)) - s.f_max;
+  return __float_as_int(big) - (kRoundBits + s.n_max);
+}
+__device__ __forceinline__ int place_far(float z, const WeightScale& s, float& f) {
   // the difference first: max - z = d + e exactly (two-sum)
   const float d = s.max - z;
   const float b = d - s.max;
@@ -98,6 +99,19 @@ __device__ __forceinline__ int weight_place(float z, const WeightScale& s, float
   const float big = kRound - yh;
   f = ((kRound - big) - yh) - yl;
   return yh < 46.f * kExpSteps ? __float_as_int(big) - kRoundBits : 2 * kNoWeight;
+}
+__device__ __forceinline__ int weight_place(float z, const WeightScale& s, float& f) {
+  return s.near ? place_near(z, s, f) : place_far(z, s, f);
+}
+// Four at once: one branch, and their arithmetic interleaves.
+__device__ __forceinline__ void weight_places(const float (&z)[4], const WeightScale& s, int (&n)[4], float (&f)[4]) {
+  if (s.near) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) n[q] = place_near(z[q], s, f[q]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) n[q] = place_far(z[q], s, f[q]);
+  }
 }
 __device__ __forceinline__ unsigned long long weight_at(int n, float f, const unsigned long long* table) {
   const float u = f * static_cast<float>(0.693147180559945 / kExpSteps);

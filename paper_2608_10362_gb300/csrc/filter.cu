@@ -46,14 +46,15 @@ constexpr int kMaxSlice = 16388;             // floats of a CTA's slice: three C
 constexpr int kMaxCluster = 8;
 constexpr uint32_t kCopyBytes = 16384;
 constexpr float kLargest = 3.402823466e38f;
-constexpr int kBins = 256;                   // of a search's histogram
-constexpr int kBinBits = 8;
+constexpr int kBins = 416;                   // of a search's histogram
+constexpr int kBinBits = 8;                  // of one that divides a bin
 constexpr int kSupers = kBins / 32;          // groups of 32 bins
-constexpr int kMantissa = 4;                 // counts: 16 bins an octave of max - z, from 2^-10 to 2^6
+constexpr int kMantissa = 4;                 // counts: 16 bins an octave of max - z, from 2^-10 on
 constexpr int kFirstOctave = (127 - 10) << kMantissa;
-constexpr int kPlacesPerBin = 64;            // weights: a bin per quarter of log2 of the weight
+constexpr int kPlacesPerBin = 28;            // weights: a bin per ninth of log2 of the weight
 static_assert(-kNoWeight / kPlacesPerBin <= kBins, "every weight has a bin");
 constexpr uint32_t kList = 256;              // list entries of a CTA and of the cluster
+constexpr int kQueue = 4 * kList;            // places in the slice, in the list's memory
 constexpr int kGroups = 64;                  // groups of threads whose maxima give the bound
 constexpr int kMostAbove = 56;               // of them above it at most
 constexpr int kWideCtas = 304;               // launches of at most so many CTAs: 512 threads each
@@ -67,26 +68,27 @@ struct alignas(16) Smem {
   u64 table[kExpSteps];
   union {
     struct {
-      struct {
-        uint32_t cnt[kBins], lo[kBins], hi[kBins];   // count, sum of weights in two words
-      } h;
-      struct {                               // find_bin: the sums of all CTAs
-        u64 mass[kMaxCluster][32];
-        uint32_t cnt[kMaxCluster][32];
-      } p;
-    };
-    u64 entry[kList];                        // the cluster's list, to sort it
+      uint32_t cnt[kBins], lo[kBins], hi[kBins];     // count, sum of weights in two words
+    } h;
+    u64 entry[2][kList];                     // the cluster's list, and sorted
     struct {
       u64 weight[kList];                     // draw_from_list: weights in the rule's order,
-      uint32_t by_id[kList];                 // and their places in id order
+      uint32_t by_id[2][kList];              // ids with places in it, and sorted
     } d;
   };
-  u64 list[kList];                           // this CTA's: (~key << 32) | id
+  union {
+    struct {                                 // find_bin: the sums of all CTAs
+      u64 mass[kMaxCluster][32];
+      uint32_t cnt[kMaxCluster][32];
+    } p;
+    uint16_t queue[kQueue];                  // then places in the slice, of a bin to divide
+    u64 list[kList];                         // then this CTA's entries: (~key << 32) | id
+  };
   // of this CTA, read by the others
   uint32_t sup_cnt[kSupers];
   u64 sup_mass[kSupers];
   u64 tail;
-  uint32_t n_list;
+  uint32_t n_list, n_queue;
   u64 p_tail[kMaxCluster];                   // of all CTAs
   uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
   float2 log_min_p;                          // T log(min_p) in two floats
@@ -164,27 +166,24 @@ __device__ u64 block_scan(u64 v, u64* scratch, u64* total) {
   *total = all;
   return before + incl;
 }
-// Ascending values, one per thread, of which the first n threads' matter (n <= kList; the
-// others hold the type's largest): a bitonic network over the next power of two.
-template <class T>
-__device__ void block_sort(T& v, uint32_t n, T* scratch) {
-  const uint32_t i = threadIdx.x;
-  uint32_t size = 32;
-  while (size < n) size *= 2;
-  for (uint32_t k = 2; k <= size; k *= 2)
-    for (uint32_t j = k / 2; j > 0; j /= 2) {
-      T other = v;
-      if (j >= 32) {
-        __syncthreads();
-        if (i < kList) scratch[i] = v;
-        __syncthreads();
-        if (i < kList) other = scratch[i ^ j];
-      } else {
-        other = __shfl_xor_sync(0xffffffffu, v, j);
-      }
-      const bool up = (i & k) == 0 || k == size, low = (i & j) == 0;
-      v = (up == low) == (other < v) ? other : v;
-    }
+// The n <= kList different values of `in`, ascending, to `out`: each counted against the
+// others by as many threads as there are to an entry (up to 255 comparisons; a bitonic
+// network took twice as long at 100 entries and as long at 256).  All threads.
+template <int NT, class T>
+__device__ void rank_sort(const T* in, T* out, uint32_t n) {
+  int bits = 0;
+  while (bits < 4 && n << (bits + 1) <= NT) ++bits;
+  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1);
+  uint32_t rank = 0;
+  T v{};
+  if (i < n) {
+    v = in[i];
+#pragma unroll 4
+    for (uint32_t j = part; j < n; j += 1u << bits) rank += in[j] < v;
+  }
+  for (int o = 1 << bits >> 1; o > 0; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
+  if (i < n && part == 0) out[rank] = v;
+  __syncthreads();
 }
 // All threads of the cluster: what they wrote before is read after.
 __device__ __forceinline__ void cluster_sync() {
@@ -216,6 +215,41 @@ __device__ __forceinline__ void for_quads(const Slice& s, float z_min, Each each
     const float z[4] = {v.x, v.y, v.z, v.w};
     each(z, s.base + 4 * i);
   }
+}
+
+// The same with all of a warp's threads (nothing past the end, for which z is -inf).
+template <int NT, class Each>
+__device__ __forceinline__ void for_warp_quads(const Slice& s, float z_min, Each each) {
+  const float4* z4 = reinterpret_cast<const float4*>(s.z);
+  const int quads = s.len / 4, lane = threadIdx.x & 31;
+  for (int i0 = static_cast<int>(threadIdx.x) - lane; i0 < quads; i0 += NT) {
+    const int i = i0 + lane;
+    const float4 v = i < quads ? z4[i] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (!__any_sync(0xffffffffu, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= z_min)) continue;
+    const float z[4] = {v.x, v.y, v.z, v.w};
+    each(z, s.base + 4 * i);
+  }
+}
+// Places in a list for the chosen elements of a warp's quads, by one atomic.
+struct Places {
+  uint32_t at[4];
+};
+__device__ __forceinline__ bool reserve(const bool (&in)[4], uint32_t* counter, Places& p) {
+  const unsigned below = (1u << (threadIdx.x & 31)) - 1;
+  uint32_t all = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const unsigned m = __ballot_sync(0xffffffffu, in[q]);
+    p.at[q] = all + __popc(m & below);
+    all += __popc(m);
+  }
+  if (all == 0) return false;
+  uint32_t base = 0;
+  if ((threadIdx.x & 31) == 0) base = atomicAdd(counter, all);
+  base = __shfl_sync(0xffffffffu, base, 0);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) p.at[q] += base;
+  return true;
 }
 
 // ------------------------------------------------ one search: top-k or top-p
@@ -344,6 +378,7 @@ __device__ void close_histogram(Smem& sm) {
 }
 
 // The CTAs' lists, an entry per thread (~0 past the last), sorted; returns how many.
+template <int NT>
 __device__ uint32_t pull_list(int C, u64& e, Smem& sm) {
   // a warp per CTA: lane c has CTA c's count
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -353,10 +388,10 @@ __device__ uint32_t pull_list(int C, u64& e, Smem& sm) {
   n = __shfl_sync(0xffffffffu, n, w);
   if (w < C)
     for (uint32_t i = lane; i < n && off + i < kList; i += 32)
-      sm.entry[off + i] = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), w));
+      sm.entry[0][off + i] = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), w));
   __syncthreads();
-  e = threadIdx.x < all ? sm.entry[threadIdx.x] : ~0ull;
-  block_sort(e, all, sm.entry);
+  rank_sort<NT>(sm.entry[0], sm.entry[1], all);
+  e = threadIdx.x < all ? sm.entry[1][threadIdx.x] : ~0ull;
   return all;
 }
 
@@ -364,22 +399,27 @@ struct Ended {
   u64 cut;
   uint32_t listed;          // > 0: the threads hold so many sorted entries, all up to the cut among them
   u64 entry;
+  bool gone;                // kAlone: this CTA has nothing more to do
 };
 
-// The entry at which the prefix that p asks for ends.  kMass: by weights, else by count.
-template <int NT, bool kMass>
+// The entry at which the prefix that p asks for ends.  kMass: by weights, else by count;
+// kWhole: every id takes part; kAlone: where all that is kept is listed, the first CTA goes
+// on alone (the others' `gone`).
+template <int NT, bool kMass, bool kWhole, bool kAlone>
 __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, int C, int rank, Smem& sm) {
   const int tid = threadIdx.x;
-  const float z_in = p.within == ~0ull ? -kLargest : entry_logit(p.within);
+  const float z_in = kWhole ? -kLargest : entry_logit(p.within);
   const uint32_t id_in = static_cast<uint32_t>(p.within);
-  auto takes_part = [&](float z, int id) { return z > z_in || (z == z_in && static_cast<uint32_t>(id) <= id_in); };
+  auto takes_part = [&](float z, int id) {
+    return kWhole ? z > -INFINITY : z > z_in || (z == z_in && static_cast<uint32_t>(id) <= id_in);
+  };
   // an element's bin, or one past the last: it takes no part or is not the cut
   auto bin_of = [&](float z, int id) {
     int b;
     if (kMass) {
       float f;
       const int n = weight_place(z, ws, f);
-      b = n < p.n_min ? kBins : -n / kPlacesPerBin;
+      b = n < p.n_min ? kBins : static_cast<int>(static_cast<unsigned>(-n) / kPlacesPerBin);
     } else {
       b = count_bin(ws.max - z);
     }
@@ -388,6 +428,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
   clear_histogram<NT>(sm);
   if (tid == 0) {
     sm.n_list = 0;
+    sm.n_queue = 0;
     sm.cut = p.within;
   }
   u64 tail = 0;
@@ -395,19 +436,22 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     bool in[4];
     int bin[4];
     u64 w[4];
+    if (kMass) {
+      int n[4];
+      float f[4];
+      weight_places(z, ws, n, f);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      in[q] = takes_part(z[q], id + q);
-      if (kMass) {
-        float f;
-        const int n = weight_place(z[q], ws, f);
-        w[q] = weight_at(n, f, sm.table);
-        bin[q] = -n / kPlacesPerBin;
-        if (n < p.n_min) {
-          tail += in[q] ? w[q] : 0;
-          in[q] = false;
-        }
-      } else {
+      for (int q = 0; q < 4; ++q) {
+        w[q] = weight_at(n[q], f[q], sm.table);
+        if (!kWhole && !takes_part(z[q], id + q)) w[q] = 0;
+        in[q] = n[q] >= p.n_min && (kWhole || w[q] != 0);
+        tail += in[q] ? 0 : w[q];
+        bin[q] = static_cast<int>(static_cast<unsigned>(-n[q]) / kPlacesPerBin);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        in[q] = takes_part(z[q], id + q);
         w[q] = 0;
         bin[q] = count_bin(ws.max - z[q]);
       }
@@ -422,7 +466,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
   Found f = find_bin<NT, kMass>(true, p.need, C, sm);
   if (f.all) {
     cluster_sync();           // the others have read this CTA's histogram
-    return {p.within, 0, 0};
+    return {p.within, 0, 0, false};
   }
   const int bin = f.bin;
   // the keys that the bin's elements can have: from the depths at its ends, with a margin
@@ -468,6 +512,42 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     return any;
   };
   u64 above = f.above;
+  // To divide a bin, its elements' places in the slice (of those in its range of keys) are
+  // queued, up to kQueued per thread, and a thread keeps its share in registers.  (A pass
+  // over the slice spends its whole body on every 128 elements with one of them.)
+  constexpr int kQueued = kQueue / NT;
+  float mine_z[kQueued];
+  int mine_id[kQueued];
+  bool queued = false;
+  if (f.count > kList) {
+    __syncthreads();          // sm.p, in the queue's place, is read
+    for_warp_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
+      bool in[4];
+      Places at;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) in[q] = z[q] >= z_lo && z[q] <= z_hi;
+      if (!reserve(in, &sm.n_queue, at)) return;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (in[q] && at.at[q] < kQueue) sm.queue[at.at[q]] = static_cast<uint16_t>(id + q - s.base);
+    });
+    __syncthreads();
+    const uint32_t n = sm.n_queue;
+    queued = n <= kQueue;     // each CTA for itself
+    if (queued)
+#pragma unroll
+      for (int q = 0; q < kQueued; ++q) {
+        const uint32_t i = q * NT + tid;
+        mine_z[q] = -INFINITY;
+        mine_id[q] = 0;
+        if (i < n) {
+          const int at = sm.queue[i];
+          const float z = s.z[at];
+          mine_id[q] = s.base + at;
+          if (bin_of(z, mine_id[q]) == bin) mine_z[q] = z;
+        }
+      }
+  }
   while (f.count > kList) {
     if (shift == 32) {        // the first division of [k_lo, k_hi]
       shift = max(0, 32 - __clz(k_hi - k_lo) - kBinBits);
@@ -478,18 +558,34 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     }
     cluster_sync();           // the others have read this CTA's histogram
     clear_histogram<NT>(sm);
-    for_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
-      bool in[4];
-      if (!choose(z, id, in)) return;
+    auto divide = [&](const float (&z)[4], const bool (&in)[4]) {
       int b[4];
       u64 w[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        b[q] = static_cast<int>((k_hi - logit_key(z[q])) >> shift) & (kBins - 1);
+        b[q] = static_cast<int>((k_hi - logit_key(z[q])) >> shift) & ((1 << kBinBits) - 1);
         w[q] = kMass ? weight(z[q], ws, sm.table) : 0;
       }
       add_to_bins<kMass>(sm, in, b, w);
-    });
+    };
+    if (queued) {
+#pragma unroll
+      for (int q4 = 0; q4 < kQueued; q4 += 4) {
+        float z[4];
+        bool in[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          z[q] = q4 + q < kQueued ? mine_z[q4 + q < kQueued ? q4 + q : 0] : -INFINITY;
+          in[q] = z[q] >= z_lo && z[q] <= z_hi;
+        }
+        if (in[0] || in[1] || in[2] || in[3]) divide(z, in);
+      }
+    } else {
+      for_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
+        bool in[4];
+        if (choose(z, id, in)) divide(z, in);
+      });
+    }
     close_histogram<NT, kMass>(sm);
     f = find_bin<NT, kMass>(false, f.need - above, C, sm);
     f.need += above;
@@ -521,28 +617,41 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     cluster_sync();
     const u64 cut = entry_of(k_hi, sm.tie_id);
     __syncthreads();
-    return {cut, 0, 0};
+    return {cut, 0, 0, false};
   }
-  for_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
-    bool in[4];
-    if (!choose(z, id, in)) return;
+  __syncthreads();            // sm.p, in the list's place, is read (the queue is in registers)
+  if (queued) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (in[q]) {
+    for (int q = 0; q < kQueued; ++q)
+      if (mine_z[q] >= z_lo && mine_z[q] <= z_hi) {
         const uint32_t i = atomicAdd(&sm.n_list, 1u);
-        if (i < kList) sm.list[i] = entry_of(logit_key(z[q]), static_cast<uint32_t>(id + q));
+        if (i < kList) sm.list[i] = entry_of(logit_key(mine_z[q]), static_cast<uint32_t>(mine_id[q]));
       }
-  });
+  } else {
+    for_warp_quads<NT>(s, z_lo, [&](const float (&z)[4], int id) {
+      bool in[4];
+      Places at;
+      choose(z, id, in);
+      if (!reserve(in, &sm.n_list, at)) return;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (in[q] && at.at[q] < kList) sm.list[at.at[q]] = entry_of(logit_key(z[q]), static_cast<uint32_t>(id + q));
+    });
+  }
   cluster_sync();
+  if (kAlone && whole_list && rank != 0) {
+    cluster_sync();           // the first CTA has read this one's list
+    return {0, 0, 0, true};
+  }
   u64 e, all;
-  const uint32_t n = pull_list(C, e, sm);   // into the histogram's place: nobody reads that any more
+  const uint32_t n = pull_list<NT>(C, e, sm);   // into the histogram's place: nobody reads that any more
   const u64 own = static_cast<uint32_t>(tid) >= n ? 0 : kMass ? weight(entry_logit(e), ws, sm.table) : 1;
   const u64 incl = (whole_list ? 0 : above) + block_scan<NT>(own, sm.scan, &all);
   if (incl - own < f.need && f.need <= incl) sm.cut = e;
   __syncthreads();
   const u64 cut = sm.cut;
   cluster_sync();             // the others have read this CTA's list
-  return {cut, whole_list ? n : 0, e};
+  return {cut, whole_list ? n : 0, e, false};
 }
 
 // The draw from the entries up to the cut among the n that the threads hold in order.
@@ -550,11 +659,13 @@ template <int NT>
 __device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 e, u64 cut, const WeightScale& ws,
                                Smem& sm) {
   const uint32_t tid = threadIdx.x, t = __syncthreads_count(tid < n && e <= cut);   // kept: the first t
-  if (tid < kList) sm.d.weight[tid] = tid < t ? weight(entry_logit(e), ws, sm.table) : 0;
-  // the kept ids ascending, with their places
-  uint32_t by_id = tid < t ? static_cast<uint32_t>(e) << 8 | tid : ~0u;
-  block_sort(by_id, t, sm.d.by_id);
+  if (tid < t) {
+    sm.d.weight[tid] = weight(entry_logit(e), ws, sm.table);
+    sm.d.by_id[0][tid] = static_cast<uint32_t>(e) << 8 | tid;
+  }
   __syncthreads();
+  rank_sort<NT>(sm.d.by_id[0], sm.d.by_id[1], t);   // the kept ids ascending
+  const uint32_t by_id = tid < t ? sm.d.by_id[1][tid] : 0;
   u64 total;
   const u64 own = tid < t ? sm.d.weight[by_id & 255u] : 0;
   const u64 incl = block_scan<NT>(own, sm.scan, &total);
@@ -684,7 +795,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   uint32_t n = 0;             // > 0: so many candidates were listed and hold what is kept
   bool search_k = by_k && !empty;
   if (search_k && owed <= kMostAbove) {
-    for_quads<NT>(s, bound, [&](const float (&x)[4], int id) {
+    for_warp_quads<NT>(s, bound, [&](const float (&x)[4], int id) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         if (x[q] >= bound) {
@@ -701,7 +812,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
         return;
       }
       u64 e;
-      pull_list(C, e, sm);
+      pull_list<NT>(C, e, sm);
       if (kMask)
         cluster_sync();                    // the others have read this CTA's list
       else
@@ -730,17 +841,20 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   }
   u64 within = no_cut;
   if (search_k) {
-    within = search<NT, false>(Part{static_cast<u64>(r.top_k), 0, ~0ull}, s, ws, C, rank, sm).cut;
+    within = search<NT, false, true, false>(Part{static_cast<u64>(r.top_k), 0, ~0ull}, s, ws, C, rank, sm).cut;
     cut = min(cut, within);
   }
   if (by_p && !empty && n == 0) {
     // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
     const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
     const int n_min = max(-static_cast<int>(deepest * kExpSteps), kNoWeight + 1);
-    const Ended e = search<NT, true>(Part{fraction, n_min, within >= no_cut ? ~0ull : within}, s, ws, C, rank, sm);
+    const Part part{fraction, n_min, within >= no_cut ? ~0ull : within};
+    const Ended e = within >= no_cut ? search<NT, true, true, !kMask>(part, s, ws, C, rank, sm)
+                                     : search<NT, true, false, !kMask>(part, s, ws, C, rank, sm);
+    if (e.gone) return;
     cut = min(cut, e.cut);
     if (!kMask && e.listed > 0) {
-      if (rank == 0) draw_from_list<NT>(a, row, e.listed, e.entry, cut, ws, sm);
+      draw_from_list<NT>(a, row, e.listed, e.entry, cut, ws, sm);
       return;
     }
   }
@@ -784,10 +898,15 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     const bool some = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= cut_z;
     if (!__any_sync(0xffffffffu, some)) return false;
     const int x = s.base + i;
-    wt[0] = kept(v.x, x) ? weight(v.x, ws, sm.table) : 0;
-    wt[1] = kept(v.y, x + 1) ? weight(v.y, ws, sm.table) : 0;
-    wt[2] = kept(v.z, x + 2) ? weight(v.z, ws, sm.table) : 0;
-    wt[3] = kept(v.w, x + 3) ? weight(v.w, ws, sm.table) : 0;
+    const float z[4] = {v.x, v.y, v.z, v.w};
+    int n[4];
+    float f[4];
+    weight_places(z, ws, n, f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      wt[q] = weight_at(n[q], f[q], sm.table);
+      if (cut != no_cut && !kept(z[q], x + q)) wt[q] = 0;
+    }
     return true;
   };
   u64 mine = 0;
