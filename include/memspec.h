@@ -248,7 +248,7 @@ memspec_status memspec_set_active_draft(memspec_ctx* ctx, int32_t draft_id);
  * from steady-state throughput, Section 4.1):
  * copies the prompt, runs the target and the active draft over all prompt
  * tokens but the last (chunks of up to 128 rows), and resets the request's
- * iteration counter.  Host-synchronising.  Errors: INVALID_ARG, CUDA. */
+ * iteration counter and its sampling rule.  Host-synchronising.  Errors: INVALID_ARG, CUDA. */
 memspec_status memspec_prefill(memspec_ctx* ctx, int32_t req, const int32_t* tokens_host,
                                int32_t n, uint64_t seed);
 
@@ -256,6 +256,19 @@ memspec_status memspec_prefill(memspec_ctx* ctx, int32_t req, const int32_t* tok
  * of them must have been prefilled.  (Batching is this library's; the paper
  * evaluates batch 1.)  Errors: INVALID_ARG. */
 memspec_status memspec_set_batch(memspec_ctx* ctx, int32_t batch);
+
+/* The sampling rule of request req in the steps at temperature > 0 from here on
+ * (until set again, or the request's prefill): the draws of its draft steps and
+ * both distributions of its acceptance test are cut by top_k (0: off), top_p in
+ * (0, 1] (1: off) and min_p in [0, 1] (0: off), as memspec_filter in
+ * memspec_ops.h defines them; so are its tree steps' draws.  The emitted tokens
+ * then follow the cut target distribution.  The steps that use it leave the cut
+ * logits in the draft's, the target's and the tree's logit buffers.  Set it
+ * between steps, not between a draft step and its acceptance.  Greedy steps (T
+ * == 0) are not affected.  Draft steps with a rule need the per-op kernels: with
+ * launch_mode PASS or draft_kernel FUSED they return UNSUPPORTED.  (The paper
+ * evaluates greedy decoding.)  Errors: INVALID_ARG, CUDA.  Enqueue only. */
+memspec_status memspec_set_sampling(memspec_ctx* ctx, int32_t req, int32_t top_k, float top_p, float min_p);
 
 /* ---- the draft-then-verify step ----------------------------------------- */
 

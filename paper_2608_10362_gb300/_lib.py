@@ -116,6 +116,7 @@ EXPORTS = {
     "memspec_prefill": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.c_int32,
                                   C.c_uint64]),
     "memspec_set_batch": (C.c_int, [C.c_void_p, C.c_int32]),
+    "memspec_set_sampling": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_float]),
     "memspec_draft_step": (C.c_int, [C.c_void_p, C.c_int32, C.c_float]),
     "memspec_verify_step": (C.c_int, [C.c_void_p, C.c_int32]),
     "memspec_tree_step": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p]),

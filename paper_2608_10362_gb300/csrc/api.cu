@@ -400,8 +400,10 @@ struct GraphKey {
   int kind, draft, K;
   uint32_t tbits;
   int batch;
+  bool ruled = false;   // with sampling rules
   bool operator<(const GraphKey& o) const {
-    return std::tie(kind, draft, K, tbits, batch) < std::tie(o.kind, o.draft, o.K, o.tbits, o.batch);
+    return std::tie(kind, draft, K, tbits, batch, ruled) <
+           std::tie(o.kind, o.draft, o.K, o.tbits, o.batch, o.ruled);
   }
 };
 
@@ -448,6 +450,10 @@ struct memspec_ctx {
   int* tree_samples = nullptr;              // the walk's outcome and the rows' logits
   TreeResult* tree_result = nullptr;
   float* tree_z = nullptr;
+  int* rule_k = nullptr;                    // sampling rules of the requests
+  float* rule_p = nullptr;
+  float* rule_min_p = nullptr;
+  uint64_t ruled = 0;                       // bit r: request r has one
   float* rope_cos[2] = {nullptr, nullptr};  // hd 64, hd 128
   float* rope_sin[2] = {nullptr, nullptr};
   size_t ws_bytes = 0;
@@ -569,6 +575,9 @@ size_t layout_workspace(const memspec_init_params* p, memspec_ctx* c, uint8_t* b
   const size_t o_ad = w.take(static_cast<size_t>(B) * (2 * K + 2) * 4);
   const size_t o_ac = w.take(static_cast<size_t>(B) * 4);
   const size_t o_sc = w.take(static_cast<size_t>(B) * 4);
+  const size_t o_rk = w.take(static_cast<size_t>(B) * 4);
+  const size_t o_rp = w.take(static_cast<size_t>(B) * 4);
+  const size_t o_rm = w.take(static_cast<size_t>(B) * 4);
   const size_t o_td = w.take(sizeof(TreeDesc));
   const size_t o_ts = w.take(static_cast<size_t>(kTreeRows) * 4);
   const size_t o_tr = w.take(sizeof(TreeResult));
@@ -630,6 +639,9 @@ size_t layout_workspace(const memspec_init_params* p, memspec_ctx* c, uint8_t* b
     c->acc_dbg = reinterpret_cast<float*>(base + o_ad);
     c->acc_cnt = reinterpret_cast<int*>(base + o_ac);
     c->smp_cnt = reinterpret_cast<int*>(base + o_sc);
+    c->rule_k = reinterpret_cast<int*>(base + o_rk);
+    c->rule_p = reinterpret_cast<float*>(base + o_rp);
+    c->rule_min_p = reinterpret_cast<float*>(base + o_rm);
     c->tree_desc = reinterpret_cast<TreeDesc*>(base + o_td);
     c->tree_samples = reinterpret_cast<int*>(base + o_ts);
     c->tree_result = reinterpret_cast<TreeResult*>(base + o_tr);
@@ -1170,6 +1182,7 @@ memspec_status run_ops_separately(memspec_ctx* c, const std::vector<PassOp>& ops
                      : launch_attention(op.u.at, op.grid, c->main, c->pdl);
       break;
       case OP_SAMPLE: e = launch_sample(op.u.s, c->main, c->pdl); break;
+      case OP_FILTER: e = launch_filter(op.u.f, c->main, c->pdl); break;
       case OP_ACCEPT: e = launch_accept(op.u.acc, c->main, false); break;
       case OP_TREE_WALK: e = launch_tree_walk(op.u.tw, c->main); break;
       case OP_TREE_COMPACT: e = launch_tree_compact(op.u.tc, op.n_units, c->main); break;
@@ -1367,6 +1380,48 @@ memspec_status enqueue_forward(memspec_ctx* c, ModelRT& m, const FwdSpec& f) {
     if (s != MEMSPEC_OK) return s;
   }
   return run_ops_separately(c, ops);
+}
+
+// Whether a step of the first `batch` requests at temperature T cuts logits (a greedy one
+// needs no cut: no rule drops the largest logit).
+bool step_ruled(const memspec_ctx* c, int batch, float T) {
+  static_assert(kMaxGroups <= 64, "a bit per request");
+  return T > 0.f && (c->ruled & (batch < 64 ? (1ull << batch) - 1 : ~0ull)) != 0;
+}
+// Rows of logits cut in place by the rules of their requests, rows_per of them each.
+void emit_filter(const memspec_ctx* c, float* logits, long long ld, int rows, int rows_per, float T,
+                 std::vector<PassOp>& ops) {
+  FilterArgs a{};
+  a.logits = logits;
+  a.ld = ld;
+  a.rows = rows;
+  a.vocab = c->vocab;
+  a.rows_per_rule = rows_per;
+  a.temperature = T;
+  a.top_ks = c->rule_k;
+  a.top_ps = c->rule_p;
+  a.min_ps = c->rule_min_p;
+  a.out = logits;
+  a.out_ld = ld;
+  PassOp op{};
+  op.type = OP_FILTER;
+  op.n_units = rows;
+  op.u.f = a;
+  ops.push_back(op);
+}
+// Set one request's rule on the device (on the main stream, after what is enqueued).
+memspec_status put_rule(memspec_ctx* c, int req, int top_k, float top_p, float min_p) {
+  // a captured copy would read these arguments at every replay
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(c->main, &capture);
+  if (e == cudaSuccess && capture != cudaStreamCaptureStatusNone) e = cudaErrorIllegalState;
+  if (e == cudaSuccess) e = cudaMemcpyAsync(c->rule_k + req, &top_k, 4, cudaMemcpyHostToDevice, c->main);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(c->rule_p + req, &top_p, 4, cudaMemcpyHostToDevice, c->main);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(c->rule_min_p + req, &min_p, 4, cudaMemcpyHostToDevice, c->main);
+  if (e != cudaSuccess) return cuda_fail(c, e, "sampling rule copy");
+  const uint64_t bit = 1ull << req;
+  c->ruled = top_k > 0 || top_p < 1.f || min_p > 0.f ? c->ruled | bit : c->ruled & ~bit;
+  return MEMSPEC_OK;
 }
 
 void drop_graphs_of_draft(memspec_ctx* c, int draft) {
@@ -1730,6 +1785,9 @@ memspec_status memspec_init(const memspec_init_params* p, void* workspace_dev, m
     e = launch_rope_table(c->rope_cos[0], c->rope_sin[0], p->max_seq, 32, p->target.rope_base, c->main);
   if (e == cudaSuccess)
     e = launch_rope_table(c->rope_cos[1], c->rope_sin[1], p->max_seq, 64, p->target.rope_base, c->main);
+  const std::vector<float> ones(p->max_batch, 1.f);   // top-p off
+  if (e == cudaSuccess)
+    e = cudaMemcpyAsync(c->rule_p, ones.data(), ones.size() * 4, cudaMemcpyHostToDevice, c->main);
   if (e == cudaSuccess) e = cudaStreamSynchronize(c->main);
   if (e != cudaSuccess) {
     g_op_error = std::string("init: ") + cudaGetErrorString(e);
@@ -1910,6 +1968,8 @@ memspec_status memspec_prefill(memspec_ctx* c, int32_t req, const int32_t* token
   if (e == cudaSuccess) e = cudaMemcpy(c->state + req * kStateInts, st, sizeof(st), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(c->seeds + req, &sd, 8, cudaMemcpyHostToDevice);
   if (e != cudaSuccess) return cuda_fail(c, e, "prefill copies");
+  if (c->ruled >> req & 1)
+    if (memspec_status s = put_rule(c, req, 0, 1.f, 0.f); s != MEMSPEC_OK) return s;
   if (memspec_status s = prefill_range(c, c->target, req, 0, n - 1); s != MEMSPEC_OK) return s;
   // every registered draft restarts from zero for this request; the active one
   // is brought up to date now, the others when they become active
@@ -1934,6 +1994,15 @@ memspec_status memspec_prefill(memspec_ctx* c, int32_t req, const int32_t* token
   return MEMSPEC_OK;
 }
 
+memspec_status memspec_set_sampling(memspec_ctx* c, int32_t req, int32_t top_k, float top_p, float min_p) {
+  if (c == nullptr) return MEMSPEC_ERR_INVALID_ARG;
+  if (req < 0 || req >= c->p.max_batch) return fail(c, MEMSPEC_ERR_INVALID_ARG, "request out of range");
+  if (top_k < 0) return fail(c, MEMSPEC_ERR_INVALID_ARG, "top_k must be >= 0");
+  if (!(top_p > 0.f && top_p <= 1.f)) return fail(c, MEMSPEC_ERR_INVALID_ARG, "top_p must be in (0, 1]");
+  if (!(min_p >= 0.f && min_p <= 1.f)) return fail(c, MEMSPEC_ERR_INVALID_ARG, "min_p must be in [0, 1]");
+  return put_rule(c, req, top_k, top_p, min_p);
+}
+
 memspec_status memspec_set_batch(memspec_ctx* c, int32_t batch) {
   if (c == nullptr) return MEMSPEC_ERR_INVALID_ARG;
   if (batch < 1 || batch > c->p.max_batch) return fail(c, MEMSPEC_ERR_INVALID_ARG, "batch out of range");
@@ -1952,6 +2021,9 @@ memspec_status memspec_draft_step(memspec_ctx* c, int32_t K, float T) {
   if (s != MEMSPEC_OK) return s;
   const int B = c->batch;
   const int id = c->active;
+  const bool ruled = step_ruled(c, B, T);
+  if (ruled && (c->pass_kernel || c->p.draft_kernel == MEMSPEC_DRAFT_KERNEL_FUSED))
+    return fail(c, MEMSPEC_ERR_UNSUPPORTED, "sampling rules need the per-op draft kernels");
   // The fused kernel runs on request only: one launch of grid-wide phases took less
   // time than per-op launches while those were 8 to 10 us each, but not since
   // gemm_small.cu (160M draft, K = 4, context 2048: 1.52 ms against 1.32; four requests
@@ -1965,7 +2037,7 @@ memspec_status memspec_draft_step(memspec_ctx* c, int32_t K, float T) {
     return run_fused_draft(c, GraphKey{3, id, K, fbits(T), B}, fa);
   }
   c->last_draft_fused = false;
-  GraphKey key{0, id, K, fbits(T), B};
+  GraphKey key{0, id, K, fbits(T), B, ruled};
   return run_pass(c, key, true, [&](std::vector<PassOp>& ops) -> memspec_status {
     for (int j = 1; j <= K; ++j) {
       FwdSpec f{};
@@ -1979,6 +2051,7 @@ memspec_status memspec_draft_step(memspec_ctx* c, int32_t K, float T) {
       f.out_group_stride = static_cast<long long>(K) * c->vocab;
       memspec_status st = emit_forward(c, d.rt, f, ops);
       if (st != MEMSPEC_OK) return st;
+      if (ruled) emit_filter(c, f.logits, f.out_group_stride, B, 1, T, ops);
       SampleArgs sa{};
       sa.logits = f.logits;
       sa.row_stride = f.out_group_stride;
@@ -2026,8 +2099,11 @@ memspec_status memspec_accept_commit(memspec_ctx* c, int32_t K, float T, int32_t
   const int B = c->batch;
   const int id = c->active;
   if (id < 0) return fail(c, MEMSPEC_ERR_NOT_RESIDENT, "no active draft");
-  GraphKey key{2, id, K, fbits(T), B};
+  const bool ruled = step_ruled(c, B, T);
+  GraphKey key{2, id, K, fbits(T), B, ruled};
   memspec_status s = run_pass(c, key, false, [&](std::vector<PassOp>& ops) -> memspec_status {
+    // the draft's rows were cut when its tokens were drawn
+    if (ruled) emit_filter(c, c->zt, c->vocab, B * (K + 1), K + 1, T, ops);
     AcceptArgs a{};
     a.zt = c->zt;
     a.zd = c->zd;
@@ -2095,7 +2171,8 @@ memspec_status memspec_tree_step(memspec_ctx* c, int32_t n_nodes, const int32_t*
   if (e != cudaSuccess) return cuda_fail(c, e, "tree copy");
   const int R = t.n_rows;
   const ModelRT& tm = c->target;
-  GraphKey key{4, -1, R, fbits(T), 1};
+  const bool ruled = step_ruled(c, 1, T);
+  GraphKey key{4, -1, R, fbits(T), 1, ruled};
   memspec_status s = run_pass(c, key, false, [&](std::vector<PassOp>& ops) -> memspec_status {
     FwdSpec f{};
     f.mode = PLAN_TREE;
@@ -2106,6 +2183,7 @@ memspec_status memspec_tree_step(memspec_ctx* c, int32_t n_nodes, const int32_t*
     memspec_status st = emit_forward(c, c->target, f, ops);
     if (st != MEMSPEC_OK) return st;
     if (!ops.empty() && ops.front().type == OP_EMBED) ops.front().u.e.tree = c->tree_desc;
+    if (ruled) emit_filter(c, c->tree_z, c->vocab, R, R, T, ops);
     SampleArgs sa{};
     sa.logits = c->tree_z;
     sa.row_stride = c->vocab;

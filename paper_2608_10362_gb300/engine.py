@@ -245,6 +245,13 @@ class Engine:
     def set_batch(self, batch: int):
         self._call(self.lib.memspec_set_batch, batch)
 
+    def set_sampling(self, req: int, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
+        """The sampling rule of request `req` in steps at T > 0, until set again or the
+        request's next prefill (no argument: none)."""
+        if top_k != int(top_k) or not 0 <= top_k < 1 << 31:
+            raise ValueError(f"top_k must be a whole number from 0 to 2^31 - 1, not {top_k!r}")
+        self._call(self.lib.memspec_set_sampling, req, int(top_k), C.c_float(top_p), C.c_float(min_p))
+
     def draft_step(self, K: int, temperature: float):
         self._call(self.lib.memspec_draft_step, K, C.c_float(temperature))
 
