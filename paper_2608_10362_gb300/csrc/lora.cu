@@ -12,8 +12,8 @@
 //      the sums are added warp by warp, then pushed into the CTA of the cluster that owns
 //      the element and added rank by rank: one order, one t.
 //   2. expand: y = base + scale B t.  t enters as three bf16 planes, which hold all its 24
-//      bits.  The columns of four n = 8 tiles are dealt so that a thread's results are 8
-//      consecutive floats of a row.  B, the base and the ids are read while the shrink
+//      bits.  The columns of four n = 8 tiles are dealt so that a thread's results are
+//      two float4s of a row.  B, the base and the ids are read while the shrink
 //      launch still runs (everything before it has completed when this one starts).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -308,9 +308,10 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
   const long long items = static_cast<long long>(chunks) * cols;
   long long at = items * blockIdx.x / gridDim.x;
   const long long end = items * (blockIdx.x + 1) / gridDim.x;
-  // column of MMA column g of tile j: 8 (g / 2) + 2 j + g % 2, so that a thread's results
-  // (columns 2 t, 2 t + 1 of each tile) are columns 8 t .. 8 t + 7
-  const int bcol = 8 * (g >> 1) + (g & 1);
+  // column of MMA column g of tile j: 16 (j / 2) + 4 (g / 2) + 2 (j % 2) + g % 2, so that a
+  // thread's results of two tiles (their columns 2 t, 2 t + 1) are columns 4 t .. 4 t + 3 of 16:
+  // four threads write 64 bytes of a row at once
+  const int bcol = 4 * (g >> 1) + (g & 1);
   bool waited = false;
   while (at < end) {
     const int c = static_cast<int>(at / cols);
@@ -347,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
         const int r = sm.chunk.row[m * 16 + h * 8 + g];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          const int x = c0 + 8 * t + 4 * q;
+          const int x = c0 + 16 * q + 4 * t;
           base[h][q] = r >= 0 && x < a.n && a.base != nullptr
                            ? __ldcg(reinterpret_cast<const float4*>(a.base + r * a.ld_base + x))
                            : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
           uint4 bv[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int col = bcol + 2 * j;
+            const int col = bcol + 16 * (j >> 1) + 2 * (j & 1);
             const uint4* p = &sm.b[w][stage][col * kPieces];
             if (KT == 1) {
               const uint2 u = reinterpret_cast<const uint2*>(p)[t];
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
             const int r = sm.chunk.row[m * 16 + h * 8 + g];
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-              const int x = c0 + 8 * t + 4 * q;
+              const int x = c0 + 16 * q + 4 * t;
               if (r < 0 || x >= a.n) continue;
               float4 o = base[h][q];
               if (rank > 0) {   // else the base's own bits
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-              sm.turn[w][h * 8 + g][2 * t + q] =
+              sm.turn[w][h * 8 + g][4 * q + t] =
                   make_float4(acc[2 * q][2 * h], acc[2 * q][2 * h + 1], acc[2 * q + 1][2 * h], acc[2 * q + 1][2 * h + 1]);
           __syncwarp();
           const int x = c0 + lane;
