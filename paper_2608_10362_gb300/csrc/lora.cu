@@ -52,10 +52,6 @@ struct LoraArgs {
   int vec;                  // 1: base and y take 16-byte accesses at every fourth column
 };
 
-__device__ __forceinline__ int rank_of(const LoraArgs& a, int id) {
-  return a.ranks == nullptr ? a.rank : max(0, min(a.ranks[id], a.rank));
-}
-
 // D += A B, 16 x 8 x 16.
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
@@ -71,11 +67,14 @@ struct Chunks {
   int distinct[kWarps];
   int leaders[kWarps];
   int row[CH];              // the selected chunk's rows, ascending; -1 past the last
-  int id, first;
+  int id, first, rank;      // rank 0: no adapter, or an empty one
+  float scale;
 };
 // What a thread knows of row threadIdx.x.
 struct RowPlace {
   int id;                   // -1: no adapter
+  int rank;                 // of its adapter (0: none), and its scale: loaded while rows are counted
+  float scale;
   int pos;                  // rows of the same adapter before it
   int chunk;                // the chunk that it leads, or -1
 };
@@ -91,6 +90,8 @@ __device__ int find_chunks(const LoraArgs& a, Chunks<CH>& s, RowPlace& p) {
     p.id = __ldcg(a.ids + tid);
     if (p.id < 0 || p.id >= a.n_adapters) p.id = -1;
   }
+  p.rank = p.id < 0 ? 0 : a.ranks == nullptr ? a.rank : __ldcg(a.ranks + p.id);
+  p.scale = p.id < 0 || a.scales == nullptr ? 1.f : __ldcg(a.scales + p.id);
   p.pos = 0;
   if (w * 32 < a.rows) {
     const unsigned same = __match_any_sync(0xffffffffu, p.id);
@@ -130,6 +131,8 @@ __device__ void select_chunk(const LoraArgs& a, const RowPlace& p, int c, Chunks
   if (p.chunk == c) {
     s.id = p.id;
     s.first = p.pos;
+    s.rank = max(0, min(p.rank, a.rank));
+    s.scale = p.scale;
   }
   __syncthreads();
   if (tid < a.rows && p.id == s.id && p.pos >= s.first && p.pos < s.first + CH) s.row[p.pos - s.first] = tid;
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_consta
   RowPlace place;
   const bool found = static_cast<int>(blockIdx.y) < find_chunks(a, sm.chunk, place);
   if (found) select_chunk(a, place, blockIdx.y, sm.chunk);
-  const int rank = found && sm.chunk.id >= 0 ? rank_of(a, sm.chunk.id) : 0;
+  const int rank = found ? sm.chunk.rank : 0;
   if (j0 >= rank) {
     cluster_wait_acquire();
     return;
@@ -320,8 +323,8 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
     at += hi - lo;
     select_chunk(a, place, c, sm.chunk);
     const int id = sm.chunk.id;
-    const int rank = id < 0 ? 0 : rank_of(a, id);
-    const float scale = id < 0 || a.scales == nullptr ? 1.f : __ldcg(a.scales + id);
+    const int rank = sm.chunk.rank;
+    const float scale = sm.chunk.scale;
     // a thread's 8 ranks of 32 (KT = 1: 4 of 16) are split over two steps
     const int steps = KT == 1 ? (rank + 15) / 16 : (rank + 31) / 32 * 2;
     int tiles = 0;
@@ -361,7 +364,21 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
       if (i < mine && rank > 0) load_b(lo + w + i * kWarps, i);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    if (a.vec && mine > 0) load_base(0, (lo + w) * kCols);
+    float first[4];           // rows that no 16-byte access fits: the base of a tile's first four
+    auto load_first = [&](int m, int c0) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int r = sm.chunk.row[m * 16 + q];
+        first[q] = r >= 0 && a.base != nullptr && c0 + lane < a.n ? __ldcg(a.base + r * a.ld_base + c0 + lane) : 0.f;
+      }
+    };
+    auto load_next = [&](int m, int c0) {
+      if (a.vec)
+        load_base(m, c0);
+      else
+        load_first(m, c0);
+    };
+    if (mine > 0) load_next(0, (lo + w) * kCols);
     if (!waited) {
       pdl_wait();
       pdl_launch_dependents();
@@ -452,11 +469,6 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
               *reinterpret_cast<float4*>(a.y + r * a.ldy + x) = o;
             }
           }
-          // the base of what this warp does next
-          if (m + 1 < tiles)
-            load_base(m + 1, c0);
-          else if (i + 1 < mine)
-            load_base(0, c0 + kWarps * kCols);
         } else {
           // through shared memory: a lane per column, 128 bytes of a row at once
           __syncwarp();
@@ -475,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 r[q] = sm.chunk.row[m * 16 + i4 + q];
-                o[q] = r[q] >= 0 && a.base != nullptr ? __ldcg(a.base + r[q] * a.ld_base + x) : 0.f;
+                o[q] = i4 == 0 ? first[q] : r[q] >= 0 && a.base != nullptr ? __ldcg(a.base + r[q] * a.ld_base + x) : 0.f;
               }
               if (r[0] < 0) break;
 #pragma unroll
@@ -487,6 +499,11 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
             }
           }
         }
+        // the base of what this warp does next
+        if (m + 1 < tiles)
+          load_next(m + 1, c0);
+        else if (i + 1 < mine)
+          load_next(0, c0 + kWarps * kCols);
       }
       __syncwarp();   // the stage is read before it is filled again
     }
