@@ -740,8 +740,10 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   if (q_hi > q_lo) {
     // the copies may be waited for once the barrier is initialised and they are announced
     __syncthreads();
-    if (!mbar_wait_bounded(&sm.loaded, 0, nullptr, nullptr))
+    if (!mbar_wait_bounded(&sm.loaded, 0, nullptr, nullptr)) {
+      mbar_wait_drain(&sm.loaded, 0);
       for (int i = q_lo + tid; i < q_hi; i += NT) load_quad(i);   // a thread takes what it loads
+    }
 #pragma unroll 4
     for (int i = q_lo + tid; i < q_hi; i += NT) take(i, s4[i]);
   }
