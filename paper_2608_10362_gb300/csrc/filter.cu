@@ -19,7 +19,8 @@
 //      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
 //      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
 //      bins through distributed shared memory to find the bin with the cut, and list
-//      its elements - or all up to there, where they are few enough.  A bin with more
+//      its elements - or all up to there, where they are few enough; top-p alone lists
+//      candidates on the way, and is done where they hold p of the sum.  A bin with more
 //      than the list takes (flat rows, many equal logits) is divided by key as often as it
 //      needs; a single key, by id;
 //   4. the draw: from the list where it holds all that is kept, else the kept weights' sums
@@ -57,6 +58,7 @@ constexpr uint32_t kList = 256;              // list entries of a CTA and of the
 constexpr int kQueue = 4 * kList;            // places in the slice, in the list's memory
 constexpr int kGroups = 64;                  // groups of threads whose maxima give the bound
 constexpr int kMostAbove = 56;               // of them above it at most
+constexpr int kTopPAbove = 96;               // logits above the bound for top-p alone
 constexpr int kWideCtas = 304;               // launches of at most so many CTAs: 512 threads each
 
 typedef unsigned long long u64;
@@ -87,9 +89,8 @@ struct alignas(16) Smem {
   // of this CTA, read by the others
   uint32_t sup_cnt[kSupers];
   u64 sup_mass[kSupers];
-  u64 tail;
-  uint32_t n_list, n_queue;
-  u64 p_tail[kMaxCluster];                   // of all CTAs
+  u64 sum, listed_sum;                       // of the slice's weights, of the candidates'
+  uint32_t n_list, n_candidates, n_queue;
   uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
   float2 log_min_p;                          // T log(min_p) in two floats
   u64 peer_sum[kMaxCluster];                 // pushed
@@ -167,19 +168,35 @@ __device__ u64 block_scan(u64 v, u64* scratch, u64* total) {
   return before + incl;
 }
 // The n <= kList different values of `in`, ascending, to `out`: each counted against the
-// others by as many threads as there are to an entry (up to 255 comparisons; a bitonic
-// network took twice as long at 100 entries and as long at 256).  All threads.
-template <int NT, class T>
-__device__ void rank_sort(const T* in, T* out, uint32_t n) {
+// others by as many threads as there are to an entry (a bitonic network took twice as long
+// at 100 entries).  `in` is padded with larger values to rank_padded(n).  All threads.
+template <int NT>
+__device__ __forceinline__ int rank_bits(uint32_t n) {   // 2^bits threads to an entry, 16 at most
   int bits = 0;
   while (bits < 4 && n << (bits + 1) <= NT) ++bits;
-  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1);
+  return bits;
+}
+template <int NT>
+__device__ __forceinline__ uint32_t rank_padded(uint32_t n) {
+  const uint32_t step = 8u << rank_bits<NT>(n);
+  return (n + step - 1) & ~(step - 1);
+}
+static_assert(kList % (8 << 4) == 0, "the padding fits the list");
+template <int NT, class T>
+__device__ void rank_sort(const T* in, T* out, uint32_t n) {
+  const int bits = rank_bits<NT>(n);
+  const uint32_t i = threadIdx.x >> bits, part = threadIdx.x & ((1u << bits) - 1), end = rank_padded<NT>(n);
   uint32_t rank = 0;
   T v{};
   if (i < n) {
     v = in[i];
-#pragma unroll 4
-    for (uint32_t j = part; j < n; j += 1u << bits) rank += in[j] < v;
+    for (uint32_t j = part; j < end; j += 8u << bits) {
+      T x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = in[j + (u << bits)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += x[u] < v;
+    }
   }
   for (int o = 1 << bits >> 1; o > 0; o >>= 1) rank += __shfl_xor_sync(0xffffffffu, rank, o);
   if (i < n && part == 0) out[rank] = v;
@@ -256,6 +273,7 @@ __device__ __forceinline__ bool reserve(const bool (&in)[4], uint32_t* counter, 
 struct Part {
   u64 need;                 // the count, or (weights) the fraction of the sum, in 2^-64
   int n_min;                // weights: places below this one are not the cut, only their sum counts
+  float bound;              // weights of all ids: candidates are listed on the way
   u64 within;               // entries up to this one take part
 };
 
@@ -276,7 +294,7 @@ struct Found {
 
 // After the histogram of every CTA is complete and the cluster has synchronised.
 template <int NT, bool kMass>
-__device__ Found find_bin(bool first, u64 need, int C, Smem& sm) {
+__device__ Found find_bin(u64 need, int C, Smem& sm) {
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   Found f;
   // the groups' sums of all CTAs
@@ -285,9 +303,8 @@ __device__ Found find_bin(bool first, u64 need, int C, Smem& sm) {
     sm.p.cnt[peer][g] = ld_cluster_u32(mapa_shared(smem_addr(&sm.sup_cnt[g]), peer));
     if (kMass) sm.p.mass[peer][g] = ld_cluster_u64(mapa_shared(smem_addr(&sm.sup_mass[g]), peer));
   }
-  if (kMass && first && tid < C) sm.p_tail[tid] = ld_cluster_u64(mapa_shared(smem_addr(&sm.tail), tid));
   __syncthreads();
-  u64 v = 0, tail = 0;
+  u64 v = 0;
   uint32_t n = 0;
   if (lane < kSupers)
     for (int c = 0; c < C; ++c) {
@@ -298,12 +315,6 @@ __device__ Found find_bin(bool first, u64 need, int C, Smem& sm) {
   u64 incl = warp_scan(v);
   const uint32_t n_incl = warp_scan(n);
   const u64 total = __shfl_sync(0xffffffffu, incl, 31);
-  if (kMass && first) {
-    for (int c = 0; c < C; ++c) tail += sm.p_tail[c];
-    const u64 s = total + tail, part = need * s;          // the fraction times the sum, rounded up
-    need = __umul64hi(need, s) + (part != 0 ? 1 : 0);
-    if (need == 0) need = 1;
-  }
   f.need = need;
   f.all = !kMass && need >= total;
   const unsigned reach = __ballot_sync(0xffffffffu, lane < kSupers && incl >= need);
@@ -377,18 +388,25 @@ __device__ void close_histogram(Smem& sm) {
   cluster_sync();
 }
 
-// The CTAs' lists, an entry per thread (~0 past the last), sorted; returns how many.
+// The fraction (in 2^-64) of a sum, rounded up, but 1 at least: what a prefix has to reach.
+__device__ __forceinline__ u64 part_of(u64 fraction, u64 sum) {
+  return max(__umul64hi(fraction, sum) + (fraction * sum != 0 ? 1 : 0), 1ull);
+}
+
+// The CTAs' lists (`count` of each), an entry per thread (~0 past the last), sorted; returns
+// how many.
 template <int NT>
-__device__ uint32_t pull_list(int C, u64& e, Smem& sm) {
+__device__ uint32_t pull_list(int C, const uint32_t* count, u64& e, Smem& sm) {
   // a warp per CTA: lane c has CTA c's count
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  uint32_t n = lane < C ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0;
+  uint32_t n = lane < C ? ld_cluster_u32(mapa_shared(smem_addr(count), lane)) : 0;
   const uint32_t incl = warp_scan(n), all = min(__shfl_sync(0xffffffffu, incl, 31), kList);
   const uint32_t off = __shfl_sync(0xffffffffu, incl - n, w);
   n = __shfl_sync(0xffffffffu, n, w);
   if (w < C)
     for (uint32_t i = lane; i < n && off + i < kList; i += 32)
       sm.entry[0][off + i] = ld_cluster_u64(mapa_shared(smem_addr(&sm.list[i]), w));
+  if (threadIdx.x >= all && threadIdx.x < rank_padded<NT>(all)) sm.entry[0][threadIdx.x] = ~0ull;
   __syncthreads();
   rank_sort<NT>(sm.entry[0], sm.entry[1], all);
   e = threadIdx.x < all ? sm.entry[1][threadIdx.x] : ~0ull;
@@ -427,11 +445,11 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
   };
   clear_histogram<NT>(sm);
   if (tid == 0) {
-    sm.n_list = 0;
-    sm.n_queue = 0;
+    sm.n_list = sm.n_candidates = sm.n_queue = 0;
     sm.cut = p.within;
   }
-  u64 tail = 0;
+  constexpr bool kCandidates = kMass && kWhole;
+  u64 sum = 0, listed_sum = 0;
   for_quads<NT>(s, z_in, [&](const float (&z)[4], int id) {
     bool in[4];
     int bin[4];
@@ -445,7 +463,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
         w[q] = weight_at(n[q], f[q], sm.table);
         if (!kWhole && !takes_part(z[q], id + q)) w[q] = 0;
         in[q] = n[q] >= p.n_min && (kWhole || w[q] != 0);
-        tail += in[q] ? 0 : w[q];
+        sum += w[q];
         bin[q] = static_cast<int>(static_cast<unsigned>(-n[q]) / kPlacesPerBin);
       }
     } else {
@@ -457,13 +475,52 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
       }
     }
     add_to_bins<kMass>(sm, in, bin, w);
+    if (kCandidates && fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) >= p.bound) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (z[q] >= p.bound) {
+          listed_sum += w[q];
+          const uint32_t i = atomicAdd(&sm.n_candidates, 1u);
+          if (i < kList) sm.list[i] = entry_of(logit_key(z[q]), static_cast<uint32_t>(id + q));
+        }
+    }
   });
   if (kMass) {
-    tail = block_sum<NT>(tail, sm.scan);
-    if (tid == 0) sm.tail = tail;
+    sum = block_sum<NT>(sum, sm.scan);
+    if (kCandidates) listed_sum = block_sum<NT>(listed_sum, sm.scan);
+    if (tid == 0) {
+      sm.sum = sum;
+      sm.listed_sum = listed_sum;
+    }
   }
   close_histogram<NT, kMass>(sm);
-  Found f = find_bin<NT, kMass>(true, p.need, C, sm);
+  u64 need = p.need;
+  if (kMass) {
+    // lane c: CTA c's sums
+    const int lane = tid & 31;
+    const bool peer = lane < C;
+    need = part_of(p.need, warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), lane)) : 0));
+    if (kCandidates) {
+      const uint32_t n =
+          __reduce_add_sync(0xffffffffu, peer ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_candidates), lane)) : 0u);
+      const u64 listed = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.listed_sum), lane)) : 0);
+      if (n <= kList && listed >= need) {   // what is kept is among the candidates
+        if (kAlone && rank != 0) {
+          cluster_sync();
+          return {0, 0, 0, true};
+        }
+        u64 e, all;
+        pull_list<NT>(C, &sm.n_candidates, e, sm);
+        cluster_sync();       // the others have read this CTA's list and sums
+        const u64 own = static_cast<uint32_t>(tid) < n ? weight(entry_logit(e), ws, sm.table) : 0;
+        const u64 incl = block_scan<NT>(own, sm.scan, &all);
+        if (incl - own < need && need <= incl) sm.cut = e;
+        __syncthreads();
+        return {sm.cut, n, e, false};
+      }
+    }
+  }
+  Found f = find_bin<NT, kMass>(need, C, sm);
   if (f.all) {
     cluster_sync();           // the others have read this CTA's histogram
     return {p.within, 0, 0, false};
@@ -587,7 +644,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
       });
     }
     close_histogram<NT, kMass>(sm);
-    f = find_bin<NT, kMass>(false, f.need - above, C, sm);
+    f = find_bin<NT, kMass>(f.need - above, C, sm);
     f.need += above;
     above += f.above;
   }
@@ -644,7 +701,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     return {0, 0, 0, true};
   }
   u64 e, all;
-  const uint32_t n = pull_list<NT>(C, e, sm);   // into the histogram's place: nobody reads that any more
+  const uint32_t n = pull_list<NT>(C, &sm.n_list, e, sm);   // into the histogram's place: nobody reads that any more
   const u64 own = static_cast<uint32_t>(tid) >= n ? 0 : kMass ? weight(entry_logit(e), ws, sm.table) : 1;
   const u64 incl = (whole_list ? 0 : above) + block_scan<NT>(own, sm.scan, &all);
   if (incl - own < f.need && f.need <= incl) sm.cut = e;
@@ -662,6 +719,8 @@ __device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 e, 
   if (tid < t) {
     sm.d.weight[tid] = weight(entry_logit(e), ws, sm.table);
     sm.d.by_id[0][tid] = static_cast<uint32_t>(e) << 8 | tid;
+  } else if (tid < rank_padded<NT>(t)) {
+    sm.d.by_id[0][tid] = ~0u;
   }
   __syncthreads();
   rank_sort<NT>(sm.d.by_id[0], sm.d.by_id[1], t);   // the kept ids ascending
@@ -754,7 +813,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   __syncthreads();
   // the bound: the j-th largest group maximum, j = what this CTA owes to the top k (if that
   // is more than the groups can give, the bound is not used)
-  const int owed = by_k ? (r.top_k + C - 1) / C : 1, j = min(owed, kMostAbove);
+  const int owed = ((by_k ? r.top_k : kTopPAbove) + C - 1) / C, j = min(owed, kMostAbove);
   cluster_wait_acquire();
   if (w < kGroups / 32) {
     // the groups' keys less their last bits, made different by the group's number: at
@@ -814,7 +873,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
         return;
       }
       u64 e;
-      pull_list<NT>(C, e, sm);
+      pull_list<NT>(C, &sm.n_list, e, sm);
       if (kMask)
         cluster_sync();                    // the others have read this CTA's list
       else
@@ -824,7 +883,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
         u64 total;
         const u64 own = static_cast<uint32_t>(tid) < k ? weight(entry_logit(e), ws, sm.table) : 0;
         const u64 incl = block_scan<NT>(own, sm.scan, &total);
-        const u64 need = max(__umul64hi(fraction, total) + (fraction * total != 0 ? 1 : 0), 1ull);
+        const u64 need = part_of(fraction, total);
         if (incl - own < need && need <= incl) sm.cut = e;
       } else if (static_cast<uint32_t>(tid) == k - 1) {
         sm.cut = e;
@@ -843,14 +902,14 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   }
   u64 within = no_cut;
   if (search_k) {
-    within = search<NT, false, true, false>(Part{static_cast<u64>(r.top_k), 0, ~0ull}, s, ws, C, rank, sm).cut;
+    within = search<NT, false, true, false>(Part{static_cast<u64>(r.top_k), 0, 0.f, ~0ull}, s, ws, C, rank, sm).cut;
     cut = min(cut, within);
   }
   if (by_p && !empty && n == 0) {
     // ids deeper than log2(2 V / (1 - p)) hold less than half of 1 - p of the mass together
     const float deepest = log2f(2.f * V / (1.f - fmaxf(r.top_p, 0.f))) + 0.01f;
     const int n_min = max(-static_cast<int>(deepest * kExpSteps), kNoWeight + 1);
-    const Part part{fraction, n_min, within >= no_cut ? ~0ull : within};
+    const Part part{fraction, n_min, bound, within >= no_cut ? ~0ull : within};
     const Ended e = within >= no_cut ? search<NT, true, true, !kMask>(part, s, ws, C, rank, sm)
                                      : search<NT, true, false, !kMask>(part, s, ws, C, rank, sm);
     if (e.gone) return;
