@@ -1073,7 +1073,7 @@ bool filter_args(FilterArgs& a, const float* logits, int64_t ld, int32_t rows, i
     why = "logits must be 4-byte aligned";
   else if (rows < 1 || rows > 65535 || vocab < 1 || vocab > kMaxVocab)
     why = "rows must be in 1..65535 and vocab in 1..131072";
-  else if (ld < vocab || ld > INT64_C(1) << 40)
+  else if (rows > 1 && (ld < vocab || ld > INT64_C(1) << 40))
     why = "the row stride must be at least vocab";
   else if (f->temperature_dev == nullptr && !(f->temperature >= 0.f))
     why = "temperature must be >= 0";
@@ -1145,7 +1145,7 @@ memspec_status memspec_op_filter_logits(const float* logits, int64_t ld, int32_t
     memspec::set_op_error("out must be a 4-byte aligned pointer");
     return MEMSPEC_ERR_INVALID_ARG;
   }
-  if (out_ld < vocab || out_ld > INT64_C(1) << 40 || (out == logits && out_ld != ld)) {
+  if (rows > 1 && (out_ld < vocab || out_ld > INT64_C(1) << 40 || (out == logits && out_ld != ld))) {
     memspec::set_op_error("out's row stride must be at least vocab, and in place the logits' own");
     return MEMSPEC_ERR_INVALID_ARG;
   }

@@ -602,9 +602,9 @@ memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x, int6
     return MEMSPEC_ERR_INVALID_ARG;
   } else if (adapters->n_adapters < 1 || n_out > (1 << 24) || k > (1 << 24)) {
     why = "n_adapters must be at least 1, n_out and k at most 2^24";
-  } else if (ldx < k || ldx % 8 != 0 || ldy < n_out || (base != nullptr && ld_base < n_out)) {
+  } else if (rows > 1 && (ldx < k || ldx % 8 != 0 || ldy < n_out || (base != nullptr && ld_base < n_out))) {
     why = "row strides must cover a row, x's a multiple of 8";
-  } else if (base == y && ld_base != ldy) {
+  } else if (rows > 1 && base == y && ld_base != ldy) {
     why = "in place, base and y have one row stride";
   } else if (misaligned(x, 16) || misaligned(adapters->a_dev, 16) || misaligned(adapters->b_dev, 16) ||
              misaligned(scratch, 16) || misaligned(y, 4) || misaligned(base, 4) || misaligned(ids, 4) ||
@@ -635,8 +635,8 @@ memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x, int6
   a.n_adapters = adapters->n_adapters;
   a.rank = adapters->rank;
   a.t = static_cast<float*>(scratch);
-  a.vec = n_out % 4 == 0 && ldy % 4 == 0 && !misaligned(y, 16) &&
-          (base == nullptr || (ld_base % 4 == 0 && !misaligned(base, 16)));
+  a.vec = n_out % 4 == 0 && (rows == 1 || ldy % 4 == 0) && !misaligned(y, 16) &&
+          (base == nullptr || ((rows == 1 || ld_base % 4 == 0) && !misaligned(base, 16)));
   const cudaError_t e = launch_lora(a, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) {
     set_op_error(std::string("lora launch: ") + cudaGetErrorString(e));

@@ -495,11 +495,17 @@ def _rows_arg(name: str, t: torch.Tensor, dtype, like: torch.Tensor | None = Non
 
 
 def _same_or_apart(name_a: str, a: torch.Tensor, name_b: str, b: torch.Tensor) -> None:
-    """Refuse two 2-D tensors that share memory without being the same rows."""
-    span = lambda t: (t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size())
+    """Refuse two 2-D tensors of one shape that share memory without being the same rows
+    (side by side in the rows of a larger tensor they do not)."""
+    n, size = a.shape[1], a.element_size()
+    span = lambda t: (t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + n) * size)
     (a0, a1), (b0, b1) = span(a), span(b)
-    if a0 < b1 and b0 < a1 and (a0, a.stride()) != (b0, b.stride()):
-        raise ValueError(f"{name_a} overlaps {name_b} without being the same rows")
+    if a0 >= b1 or b0 >= a1 or (a0, a.stride()) == (b0, b.stride()):
+        return
+    ld = a.stride(0)
+    if ld == b.stride(0) and n <= (b0 - a0) // size % ld <= ld - n:
+        return
+    raise ValueError(f"{name_a} overlaps {name_b} without being the same rows")
 
 
 def _used_on(stream: torch.cuda.Stream | None, *made: torch.Tensor) -> None:

@@ -192,6 +192,36 @@ def test_filtered_draws_repeat_and_run_under_a_graph():
             assert torch.equal(t, wt) and torch.equal(m, wm)
 
 
+def test_many_rows_and_rows_far_apart():
+    """More rows than the chip holds at once; row strides past 2^31 elements; a mask beside the
+    logits in the rows of one tensor."""
+    import torch
+    from paper_2608_10362_gb300 import op_filter_logits, op_sample_filtered
+    z, u = _logits("peaked", 50, 97), _uniforms(50)
+    many = torch.from_numpy(z).cuda().repeat(800, 1)
+    got = op_sample_filtered(many, torch.from_numpy(u).cuda().repeat(800), temperature=0.8, top_k=20, top_p=0.9)
+    want = [F.draw(z[r], u[r], 0.8, 20, 0.9) for r in range(50)]
+    assert torch.equal(got.cpu().view(800, 50), torch.tensor(want, dtype=torch.int32).expand(800, 50))
+    far = 1 << 30
+    raw = torch.zeros(2 * far + 97, device="cuda")
+    rows = torch.as_strided(raw, (3, 97), (far, 1))
+    rows.copy_(torch.from_numpy(z[:3]))
+    assert op_sample_filtered(rows, torch.from_numpy(u[:3]).cuda(), temperature=0.8, top_k=20, top_p=0.9).tolist() == want[:3]
+    op_filter_logits(rows, top_k=5, out=rows)
+    assert np.array_equal(rows.cpu().numpy(), np.stack([F.mask(r, 1.0, 5) for r in z[:3]]))
+    del raw, rows
+    both = torch.zeros(50, 200, device="cuda")
+    both[:, :97] = torch.from_numpy(z)
+    op_filter_logits(both[:, :97], top_k=5, out=both[:, 100:197])
+    assert np.array_equal(both[:, 100:197].cpu().numpy(), np.stack([F.mask(r, 1.0, 5) for r in z]))
+    assert np.array_equal(both[:, :97].cpu().numpy(), z) and bool((both[:, 97:100] == 0).all())
+    # uniforms outside [0, 1): the first kept id, the last
+    ids = np.sort(F.kept(z[0], 1.0, 7))
+    odd = torch.tensor([-1.0, 1.0, math.inf, float("nan")], device="cuda")
+    four = torch.from_numpy(z[:1]).cuda().repeat(4, 1)
+    assert op_sample_filtered(four, odd, top_k=7).tolist() == [ids[0], ids[-1], ids[-1], ids[0]]
+
+
 def test_filter_arguments_are_refused():
     import torch
     from paper_2608_10362_gb300 import MemSpecError, op_filter_logits, op_sample_filtered
@@ -353,6 +383,44 @@ def test_lora_repeats_on_one_scratch_of_any_content_and_under_graphs():
         torch.cuda.synchronize()
         for o, f in zip(outs, first[::-1] if swap else first):
             assert torch.equal(o, f)
+
+
+def test_lora_single_rows_at_any_stride_and_rows_far_apart():
+    import torch
+    from paper_2608_10362_gb300 import op_lora
+    x, a, b, ids, scales, ranks, base = _lora_case(3, 100, 64, 16, 2, "each", whole=True)
+    want, _ = F.lora(x, a, b, ids, scales, ranks, base)
+    rest = (_cuda(a).bfloat16(), _cuda(b).bfloat16(), _cuda(ids)[1:2].clone(), _cuda(scales), _cuda(ranks))
+    one = torch.zeros(3, 67, device="cuda", dtype=torch.bfloat16)
+    one[0, :64] = _cuda(x)[1]
+    odd = torch.zeros(3, 103, device="cuda")
+    odd[0, :100] = _cuda(base)[1]
+    got = op_lora(one[:1, :64], *rest, base=odd[:1, :100])
+    assert np.array_equal(got.cpu().numpy(), want[1:2].astype(np.float32))
+    got = op_lora(one[:1, :64].expand(1, 64), *rest, base=odd[0, :100].unsqueeze(0).expand(1, 100))
+    assert np.array_equal(got.cpu().numpy(), want[1:2].astype(np.float32))
+    far = 1 << 30
+    raw, rawx = torch.zeros(2 * far + 100, device="cuda"), torch.zeros(2 * far + 64, device="cuda", dtype=torch.bfloat16)
+    y, xs = torch.as_strided(raw, (3, 100), (far, 1)), torch.as_strided(rawx, (3, 64), (far, 1))
+    y.copy_(_cuda(base))
+    xs.copy_(_cuda(x))
+    op_lora(xs, _cuda(a).bfloat16(), _cuda(b).bfloat16(), _cuda(ids), _cuda(scales), _cuda(ranks), base=y, y=y)
+    assert np.array_equal(y.cpu().numpy(), want.astype(np.float32))
+
+
+def test_lora_infinities_stay_in_their_rows():
+    import torch
+    from paper_2608_10362_gb300 import op_lora
+    x, a, b, ids, scales, ranks, base = _lora_case(20, 200, 128, 16, 4, "each", seed=6)
+    ranks[:] = 16
+    want, size = F.lora(x, a, b, ids, scales, ranks, base)
+    x[5, 17], x[9, 3] = np.inf, np.nan
+    a[2, 3, 5], b[3, 100, 2] = np.nan, np.inf
+    got = op_lora(_cuda(x).bfloat16(), _cuda(a).bfloat16(), _cuda(b).bfloat16(), _cuda(ids), _cuda(scales), _cuda(ranks),
+                  _cuda(base)).cpu().numpy()
+    fine = np.array([r for r in range(20) if ids[r] in (0, 1) and r not in (5, 9)])
+    assert np.all(np.abs(got[fine] - want[fine]) <= (128 + 16 + 4) * 2.0 ** -23 * size[fine])
+    assert np.all(np.isfinite(np.delete(got[ids == 3], 100, axis=1)))
 
 
 def test_lora_arguments_are_refused():
