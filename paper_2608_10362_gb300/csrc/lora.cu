@@ -8,6 +8,7 @@
 // and B and by reading and writing y, one or a few rows at a time fill no tcgen05 tile, and
 // fragments come straight from memory (the contraction index is permuted so that a thread's
 // fragments of two steps are 16 consecutive bytes).
+// Two launches, or for short calls one that does the work of both (fused_kernel):
 //   1. shrink: t = A x.  A cluster of 8 CTAs splits k, the 8 warps of a CTA split its part;
 //      the sums are added warp by warp, then pushed into the CTA of the cluster that owns
 //      the element and added rank by rank: one order, one t.
@@ -139,59 +140,33 @@ __device__ void select_chunk(const LoraArgs& a, const RowPlace& p, int c, Chunks
   __syncthreads();
 }
 
-// t[row][j] for a chunk of up to 16 MT rows and 8 NT of the adapter's ranks.  Grid (cluster
-// of kSplits over k, chunks, groups of 8 NT ranks).
-template <int MT, int NT>
-struct ShrinkSmem {
-  static constexpr int kFrags = MT * NT * 32;   // a lane's four sums of a 16 x 8 tile
-  Chunks<MT * 16> chunk;
-  float4 warp[kWarps][kFrags];                  // a warp's sums
-  float4 split[kSplits][kFrags / kSplits];      // this CTA's sums, from each CTA of the cluster
-};
+// ------------------------------------------------ t = A x
 __device__ __forceinline__ void add4(float4& s, const float4& v) {
   s.x += v.x;
   s.y += v.y;
   s.z += v.z;
   s.w += v.w;
 }
-
+// This warp's sums over its part of CTA `split`'s columns: ranks j0 .. j0 + 8 NT - 1 (below
+// `rank`) of adapter id and up to 16 MT rows (row[]: -1 for none), `tiles` 16-row tiles of them.
 template <int MT, int NT>
-__global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_constant__ LoraArgs a) {
-  extern __shared__ __align__(16) uint8_t raw[];
-  typedef ShrinkSmem<MT, NT> S;
-  S& sm = *reinterpret_cast<S*>(raw);
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x, j0 = blockIdx.z * NT * 8;
-  cluster_arrive_release();   // waited for before the first push into a peer
-  pdl_wait();
-  pdl_launch_dependents();
-  // the CTAs of a cluster have one chunk and one rank group: they leave together
-  RowPlace place;
-  const bool found = static_cast<int>(blockIdx.y) < find_chunks(a, sm.chunk, place);
-  if (found) select_chunk(a, place, blockIdx.y, sm.chunk);
-  const int rank = found ? sm.chunk.rank : 0;
-  if (j0 >= rank) {
-    cluster_wait_acquire();
-    return;
-  }
+__device__ __forceinline__ void shrink_sums(const LoraArgs& a, const int* row, int id, int rank, int j0, int split,
+                                            int tiles, float (&acc)[MT][NT][4]) {
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const bf16* xr[MT][2];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int r = sm.chunk.row[m * 16 + h * 8 + g];
+      const int r = row[m * 16 + h * 8 + g];
       xr[m][h] = r < 0 ? nullptr : a.x + r * a.ldx + 8 * t;
     }
   const bf16* ar[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int j = j0 + n * 8 + g;
-    ar[n] = j < rank ? a.a + (static_cast<long long>(sm.chunk.id) * a.rank + j) * a.k + 8 * t : nullptr;
+    ar[n] = j < rank ? a.a + (static_cast<long long>(id) * a.rank + j) * a.k + 8 * t : nullptr;
   }
-  int tiles = 0;              // 16-row tiles with rows
-#pragma unroll
-  for (int m = 0; m < MT; ++m) tiles += sm.chunk.row[m * 16] >= 0;
-  float acc[MT][NT][4] = {};
   const int blocks = (a.k + 31) / 32;         // of 32 columns
   const int end = static_cast<int>(static_cast<long long>(split + 1) * blocks / kSplits);
   const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -228,23 +203,67 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_consta
       }
     }
   }
+}
+// The warps' sums added up and pushed to the CTA of the cluster that owns the element: from
+// there split[c] (`own` lanes' sums) of every CTA c are complete after the next cluster
+// barrier.  All threads; the cluster's first barrier has been arrived at.
+template <int MT, int NT>
+__device__ __forceinline__ void share_sums(const float (&acc)[MT][NT][4], int tiles, int split, int own,
+                                           float4 (*warp)[MT * NT * 32], float4 (*to)[MT * NT * 32 / kSplits]) {
+  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     if (m >= tiles) break;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      sm.warp[w][(m * NT + n) * 32 + lane] = make_float4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
+      warp[w][(m * NT + n) * 32 + lane] = make_float4(acc[m][n][0], acc[m][n][1], acc[m][n][2], acc[m][n][3]);
   }
   __syncthreads();
   cluster_wait_acquire();
-  const int own = tiles * NT * 32 / kSplits;
   for (int f = tid; f < own * kSplits; f += kThreads) {
-    float4 s = sm.warp[0][f];
+    float4 s = warp[0][f];
 #pragma unroll
-    for (int i = 1; i < kWarps; ++i) add4(s, sm.warp[i][f]);
-    const int to = f / own;
-    st_cluster_f4(mapa_shared(smem_addr(&sm.split[split][f - to * own]), to), s);
+    for (int i = 1; i < kWarps; ++i) add4(s, warp[i][f]);
+    const int owner = f / own;
+    st_cluster_f4(mapa_shared(smem_addr(&to[split][f - owner * own]), owner), s);
   }
+}
+
+// t[row][j] for a chunk of up to 16 MT rows and 8 NT of the adapter's ranks.  Grid (cluster
+// of kSplits over k, chunks, groups of 8 NT ranks).
+template <int MT, int NT>
+struct ShrinkSmem {
+  static constexpr int kFrags = MT * NT * 32;   // a lane's four sums of a 16 x 8 tile
+  Chunks<MT * 16> chunk;
+  float4 warp[kWarps][kFrags];                  // a warp's sums
+  float4 split[kSplits][kFrags / kSplits];      // this CTA's sums, from each CTA of the cluster
+};
+
+template <int MT, int NT>
+__global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_constant__ LoraArgs a) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  typedef ShrinkSmem<MT, NT> S;
+  S& sm = *reinterpret_cast<S*>(raw);
+  const int tid = threadIdx.x, split = blockIdx.x, j0 = blockIdx.z * NT * 8;
+  cluster_arrive_release();   // waited for before the first push into a peer
+  pdl_wait();
+  pdl_launch_dependents();
+  // the CTAs of a cluster have one chunk and one rank group: they leave together
+  RowPlace place;
+  const bool found = static_cast<int>(blockIdx.y) < find_chunks(a, sm.chunk, place);
+  if (found) select_chunk(a, place, blockIdx.y, sm.chunk);
+  const int rank = found ? sm.chunk.rank : 0;
+  if (j0 >= rank) {
+    cluster_wait_acquire();
+    return;
+  }
+  int tiles = 0;              // 16-row tiles with rows
+#pragma unroll
+  for (int m = 0; m < MT; ++m) tiles += sm.chunk.row[m * 16] >= 0;
+  float acc[MT][NT][4] = {};
+  shrink_sums<MT, NT>(a, sm.chunk.row, sm.chunk.id, rank, j0, split, tiles, acc);
+  const int own = tiles * NT * 32 / kSplits;
+  share_sums<MT, NT>(acc, tiles, split, own, sm.warp, sm.split);
   cluster_arrive_release();
   cluster_wait_acquire();
   for (int i = tid; i < own; i += kThreads) {
@@ -260,25 +279,8 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_consta
   }
 }
 
-// y = base + scale B t.  Work is (chunk of up to 32 rows, 32 columns) items in that order,
-// cut evenly over as many CTAs as are resident at once; a warp takes every eighth item of
-// its CTA's part of a chunk, B's columns arriving by cp.async kStages items ahead (loads
-// into registers as they were needed left half the time waiting: gate/up of 144 rows 30
-// us).  KT: steps of 16 ranks.
-constexpr int kExpandTiles = 2;
-constexpr int kCols = 32;
-template <int KT>
-struct ExpandSmem {
-  static constexpr int kPieces = KT * 2;           // of 8 ranks, per column
-  static constexpr int kStages = KT <= 2 ? 4 : KT == 4 ? 3 : 2;
-  uint4 b[kWarps][kStages][kCols * kPieces];
-  uint4 t[kExpandTiles][KT][3][32];   // fragments of t's planes, one per lane
-  Chunks<kExpandTiles * 16> chunk;
-  float4 turn[kWarps][16][8 + 1];     // a warp's tile where rows are not 16-byte aligned (else
-                                      // not there)
-  static constexpr size_t bytes(bool vec) { return vec ? sizeof(ExpandSmem) - sizeof(turn) : sizeof(ExpandSmem); }
-  static constexpr int per_sm(bool vec) { return KT <= 4 && 2 * (bytes(vec) + 1024) <= 228 * 1024 ? 2 : 1; }
-};
+// ------------------------------------------------ y = base + scale B t
+constexpr int kCols = 32;     // of an item: what a warp takes at a time
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -290,65 +292,73 @@ __device__ __forceinline__ float bf16_part(float x) { return __bfloat162float(__
 __device__ __forceinline__ uint32_t within(uint32_t pair, int r, int rank) {
   return r + 1 < rank ? pair : (r < rank ? pair & 0xffffu : 0u);
 }
-
 __device__ __forceinline__ void copy16_async(void* dst, const void* src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(in ? 16 : 0)
                : "memory");
 }
 
+// KT: steps of 16 ranks.  B's columns arrive by cp.async kStages items ahead (loads into
+// registers as they were needed left a warp waiting half the time: gate/up of 144 rows 30 us).
 template <int KT>
-__global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const __grid_constant__ LoraArgs a) {
-  typedef ExpandSmem<KT> S;
-  constexpr int kPieces = S::kPieces, kStages = S::kStages;
-  extern __shared__ __align__(16) uint8_t raw[];
-  S& sm = *reinterpret_cast<S*>(raw);
-  const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  // the ids, B, base and scales may be read now: the launch before this one (shrink) lets
-  // it start only after its own wait, so all that came earlier has completed
-  RowPlace place;
-  const int chunks = find_chunks(a, sm.chunk, place);
-  const int cols = (a.n + kCols - 1) / kCols;
-  const long long items = static_cast<long long>(chunks) * cols;
-  long long at = items * blockIdx.x / gridDim.x;
-  const long long end = items * (blockIdx.x + 1) / gridDim.x;
-  // column of MMA column g of tile j: 16 (j / 2) + 4 (g / 2) + 2 (j % 2) + g % 2, so that a
-  // thread's results of two tiles (their columns 2 t, 2 t + 1) are columns 4 t .. 4 t + 3 of 16:
-  // four threads write 64 bytes of a row at once
-  const int bcol = 4 * (g >> 1) + (g & 1);
-  bool waited = false;
-  while (at < end) {
-    const int c = static_cast<int>(at / cols);
-    const int lo = static_cast<int>(at - static_cast<long long>(c) * cols);
-    const int hi = static_cast<int>(min(static_cast<long long>(cols), lo + (end - at)));
-    at += hi - lo;
-    select_chunk(a, place, c, sm.chunk);
-    const int id = sm.chunk.id;
-    const int rank = sm.chunk.rank;
-    const float scale = sm.chunk.scale;
-    // a thread's 8 ranks of 32 (KT = 1: 4 of 16) are split over two steps
-    const int steps = KT == 1 ? (rank + 15) / 16 : (rank + 31) / 32 * 2;
-    int tiles = 0;
+struct Ring {
+  static constexpr int kPieces = KT * 2;           // of 8 ranks, per column
+  static constexpr int kStages = KT <= 2 ? 4 : KT == 4 ? 3 : 2;
+  uint4 b[kStages][kCols * kPieces];
+};
+typedef float4 Turn[16][8 + 1];     // a warp's tile where rows are not 16-byte aligned
+// The fragments of t's three planes of up to MT 16-row tiles, a uint4 per lane.
+template <int KT, int MT>
+struct Planes {
+  uint4 v[MT][KT][3][32];
+};
+
+// One warp's items lo + w, lo + w + 8, ... below hi of a chunk.
+template <int KT, int MT>
+struct ExpandWarp {
+  static constexpr int kPieces = Ring<KT>::kPieces, kStages = Ring<KT>::kStages;
+  const LoraArgs& a;
+  Ring<KT>& ring;
+  Turn& turn;
+  const int* row;
+  int rank, tiles, lo, mine;
+  float scale;
+  const bf16* bp;
+  float4 base[2][2];
+  float first[4];             // rows that no 16-byte access fits: the base of a tile's first four
+
+  template <int CH>
+  __device__ ExpandWarp(const LoraArgs& args, Ring<KT>& r, Turn& t, const Chunks<CH>& c, int from, int to)
+      : a(args), ring(r), turn(t), row(c.row), rank(c.rank), tiles(0), scale(c.scale) {
+    static_assert(CH == MT * 16, "the chunk's rows");
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
-    for (int m = 0; m < kExpandTiles; ++m) tiles += sm.chunk.row[m * 16] >= 0;
-    // lane's piece of kPieces columns of an item: piece lane % kPieces, swapped by fours
-    // in odd columns so that two columns' pieces lie in different banks
-    const int piece = lane % kPieces;
-    const bf16* bp = a.b + (static_cast<long long>(max(id, 0)) * a.n + lane / kPieces) * a.rank + piece * 8;
-    auto load_b = [&](int item, int stage) {
-      const int c0 = item * kCols;
+    for (int m = 0; m < MT; ++m) tiles += row[m * 16] >= 0;
+    lo = from + w;
+    mine = to > lo ? (to - lo + kWarps - 1) / kWarps : 0;
+    bp = a.b + (static_cast<long long>(max(c.id, 0)) * a.n + lane / kPieces) * a.rank + lane % kPieces * 8;
+  }
+  // a thread's 8 ranks of 32 (KT = 1: 4 of 16) are split over two steps
+  __device__ int steps() const { return KT == 1 ? (rank + 15) / 16 : (rank + 31) / 32 * 2; }
+  __device__ int column(int item) const { return (lo + item * kWarps) * kCols; }
+
+  // lane's piece of kPieces columns of an item: piece lane % kPieces, swapped by fours in odd
+  // columns so that two columns' pieces lie in different banks
+  __device__ void load_b(int item) {
+    const int c0 = column(item), lane = threadIdx.x & 31, piece = lane % kPieces;
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int col = lane / kPieces + i * (32 / kPieces);
-        const bool in = c0 + col < a.n && piece * 8 < rank;
-        copy16_async(&sm.b[w][stage][col * kPieces + (KT >= 4 ? piece ^ ((col & 1) << 2) : piece)],
-                     in ? bp + static_cast<long long>(c0 + i * (32 / kPieces)) * a.rank : a.b, in);
-      }
-    };
-    float4 base[2][2];
-    auto load_base = [&](int m, int c0) {
+    for (int i = 0; i < kPieces; ++i) {
+      const int col = lane / kPieces + i * (32 / kPieces);
+      const bool in = c0 + col < a.n && piece * 8 < rank;
+      copy16_async(&ring.b[item % kStages][col * kPieces + (KT >= 4 ? piece ^ ((col & 1) << 2) : piece)],
+                   in ? bp + static_cast<long long>(c0 + i * (32 / kPieces)) * a.rank : a.b, in);
+    }
+  }
+  __device__ void load_base(int m, int c0) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    if (a.vec) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int r = sm.chunk.row[m * 16 + h * 8 + g];
+        const int r = row[m * 16 + h * 8 + g];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           const int x = c0 + 16 * q + 4 * t;
@@ -357,62 +367,32 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
                            : make_float4(0.f, 0.f, 0.f, 0.f);
         }
       }
-    };
-    const int mine = hi - lo > w ? (hi - lo - w + kWarps - 1) / kWarps : 0;   // items of this warp
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) {
-      if (i < mine && rank > 0) load_b(lo + w + i * kWarps, i);
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    float first[4];           // rows that no 16-byte access fits: the base of a tile's first four
-    auto load_first = [&](int m, int c0) {
+    } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int r = sm.chunk.row[m * 16 + q];
+        const int r = row[m * 16 + q];
         first[q] = r >= 0 && a.base != nullptr && c0 + lane < a.n ? __ldcg(a.base + r * a.ld_base + c0 + lane) : 0.f;
       }
-    };
-    auto load_next = [&](int m, int c0) {
-      if (a.vec)
-        load_base(m, c0);
-      else
-        load_first(m, c0);
-    };
-    if (mine > 0) load_next(0, (lo + w) * kCols);
-    if (!waited) {
-      pdl_wait();
-      pdl_launch_dependents();
-      waited = true;
     }
-    for (int i = tid; i < tiles * steps * 32; i += kThreads) {
-      const int l = i & 31, s = (i >> 5) % steps, m = (i >> 5) / steps;
-      // the ranks of a lane's fragments of step s: as they lie in its pieces of B
-      const int r = KT == 1 ? 4 * (l & 3) : (s >> 1) * 32 + 8 * (l & 3) + (s & 1) * 4;
-      float v[2][4] = {};
+  }
+  // The first loads: they do not depend on t.
+  __device__ void start() {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int row = sm.chunk.row[m * 16 + h * 8 + (l >> 2)];
-        if (row < 0 || r >= rank) continue;
-        const float4 q = __ldcg(reinterpret_cast<const float4*>(a.t + row * a.rank + r));
-        v[h][0] = q.x;
-        v[h][1] = r + 1 < rank ? q.y : 0.f;
-        v[h][2] = r + 2 < rank ? q.z : 0.f;
-        v[h][3] = r + 3 < rank ? q.w : 0.f;
-      }
-#pragma unroll
-      for (int p = 0; p < 3; ++p) {
-        sm.t[m][s][p][l] = make_uint4(pack_bf16(v[0][0], v[0][1]), pack_bf16(v[1][0], v[1][1]),
-                                      pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][2], v[1][3]));
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) v[h][q] -= bf16_part(v[h][q]);
-      }
+    for (int i = 0; i < kStages - 1; ++i) {
+      if (i < mine && rank > 0) load_b(i);
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __syncthreads();
+    if (mine > 0) load_base(0, column(0));
+  }
+  __device__ void run(const Planes<KT, MT>& planes) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    // column of MMA column g of tile j: 16 (j / 2) + 4 (g / 2) + 2 (j % 2) + g % 2, so that a
+    // thread's results of two tiles (their columns 2 t, 2 t + 1) are columns 4 t .. 4 t + 3 of
+    // 16: four threads write 64 bytes of a row at once
+    const int bcol = 4 * (g >> 1) + (g & 1), n_steps = steps();
     for (int i = 0; i < mine; ++i) {
-      const int c0 = (lo + w + i * kWarps) * kCols, stage = i % kStages;
-      if (i + kStages - 1 < mine && rank > 0) load_b(lo + w + (i + kStages - 1) * kWarps, (i + kStages - 1) % kStages);
+      const int c0 = column(i);
+      if (i + kStages - 1 < mine && rank > 0) load_b(i + kStages - 1);
       asm volatile("cp.async.commit_group;" ::: "memory");
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       __syncwarp();
@@ -420,12 +400,12 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
         float acc[4][4] = {};
 #pragma unroll
         for (int s2 = 0; s2 < (KT + 1) / 2; ++s2) {
-          if (2 * s2 >= steps) break;
+          if (2 * s2 >= n_steps) break;
           uint4 bv[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int col = bcol + 16 * (j >> 1) + 2 * (j & 1);
-            const uint4* p = &sm.b[w][stage][col * kPieces];
+            const uint4* p = &ring.b[i % kStages][col * kPieces];
             if (KT == 1) {
               const uint2 u = reinterpret_cast<const uint2*>(p)[t];
               bv[j] = make_uint4(u.x, u.y, 0u, 0u);
@@ -444,70 +424,220 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
           for (int o = 0; o < (KT == 1 ? 1 : 2); ++o) {
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-              const uint4 f = sm.t[m][2 * s2 + o][p][lane];
+              const uint4 f = planes.v[m][2 * s2 + o][p][lane];
               const uint32_t fa[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
               for (int j = 0; j < 4; ++j) mma(acc[j], fa, o ? bv[j].z : bv[j].x, o ? bv[j].w : bv[j].y);
             }
           }
         }
-        if (a.vec) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = sm.chunk.row[m * 16 + h * 8 + g];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const int x = c0 + 16 * q + 4 * t;
-              if (r < 0 || x >= a.n) continue;
-              float4 o = base[h][q];
-              if (rank > 0) {   // else the base's own bits
-                o.x = fmaf(scale, acc[2 * q][2 * h], o.x);
-                o.y = fmaf(scale, acc[2 * q][2 * h + 1], o.y);
-                o.z = fmaf(scale, acc[2 * q + 1][2 * h], o.z);
-                o.w = fmaf(scale, acc[2 * q + 1][2 * h + 1], o.w);
-              }
-              *reinterpret_cast<float4*>(a.y + r * a.ldy + x) = o;
-            }
-          }
-        } else {
-          // through shared memory: a lane per column, 128 bytes of a row at once
-          __syncwarp();
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-              sm.turn[w][h * 8 + g][4 * q + t] =
-                  make_float4(acc[2 * q][2 * h], acc[2 * q][2 * h + 1], acc[2 * q + 1][2 * h], acc[2 * q + 1][2 * h + 1]);
-          __syncwarp();
-          const int x = c0 + lane;
-          if (x < a.n) {
-            for (int i4 = 0; i4 < 16; i4 += 4) {
-              float o[4];
-              int r[4];
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                r[q] = sm.chunk.row[m * 16 + i4 + q];
-                o[q] = i4 == 0 ? first[q] : r[q] >= 0 && a.base != nullptr ? __ldcg(a.base + r[q] * a.ld_base + x) : 0.f;
-              }
-              if (r[0] < 0) break;
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                if (r[q] < 0) continue;
-                if (rank > 0) o[q] = fmaf(scale, reinterpret_cast<const float*>(&sm.turn[w][i4 + q][0])[lane], o[q]);
-                a.y[r[q] * a.ldy + x] = o[q];
-              }
-            }
-          }
-        }
+        if (a.vec)
+          store(m, c0, acc);
+        else
+          store_turned(m, c0, acc);
         // the base of what this warp does next
         if (m + 1 < tiles)
-          load_next(m + 1, c0);
+          load_base(m + 1, c0);
         else if (i + 1 < mine)
-          load_next(0, c0 + kWarps * kCols);
+          load_base(0, column(i + 1));
       }
       __syncwarp();   // the stage is read before it is filled again
     }
   }
+  __device__ void store(int m, int c0, const float (&acc)[4][4]) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = row[m * 16 + h * 8 + g];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int x = c0 + 16 * q + 4 * t;
+        if (r < 0 || x >= a.n) continue;
+        float4 o = base[h][q];
+        if (rank > 0) {   // else the base's own bits
+          o.x = fmaf(scale, acc[2 * q][2 * h], o.x);
+          o.y = fmaf(scale, acc[2 * q][2 * h + 1], o.y);
+          o.z = fmaf(scale, acc[2 * q + 1][2 * h], o.z);
+          o.w = fmaf(scale, acc[2 * q + 1][2 * h + 1], o.w);
+        }
+        *reinterpret_cast<float4*>(a.y + r * a.ldy + x) = o;
+      }
+    }
+  }
+  // Through shared memory: a lane per column, 128 bytes of a row at once.
+  __device__ void store_turned(int m, int c0, const float (&acc)[4][4]) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        turn[h * 8 + g][4 * q + t] =
+            make_float4(acc[2 * q][2 * h], acc[2 * q][2 * h + 1], acc[2 * q + 1][2 * h], acc[2 * q + 1][2 * h + 1]);
+    __syncwarp();
+    const int x = c0 + lane;
+    if (x >= a.n) return;
+    for (int i4 = 0; i4 < 16; i4 += 4) {
+      float o[4];
+      int r[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        r[q] = row[m * 16 + i4 + q];
+        o[q] = i4 == 0 ? first[q] : r[q] >= 0 && a.base != nullptr ? __ldcg(a.base + r[q] * a.ld_base + x) : 0.f;
+      }
+      if (r[0] < 0) break;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (r[q] < 0) continue;
+        if (rank > 0) o[q] = fmaf(scale, reinterpret_cast<const float*>(&turn[i4 + q][0])[lane], o[q]);
+        a.y[r[q] * a.ldy + x] = o[q];
+      }
+    }
+  }
+};
+
+// The second of two launches.  Work is (chunk of up to 32 rows, item) pairs in that order, cut
+// evenly over as many CTAs as are resident at once (cut by their bytes instead: no faster, and
+// a microsecond more to find a CTA's part).
+constexpr int kExpandTiles = 2;
+template <int KT>
+struct ExpandSmem {
+  Ring<KT> ring[kWarps];
+  Planes<KT, kExpandTiles> planes;
+  Chunks<kExpandTiles * 16> chunk;
+  Turn turn[kWarps];          // not there where rows are 16-byte aligned
+  static constexpr size_t bytes(bool vec) { return vec ? sizeof(ExpandSmem) - sizeof(turn) : sizeof(ExpandSmem); }
+  static constexpr int per_sm(bool vec) { return KT <= 4 && 2 * (bytes(vec) + 1024) <= 228 * 1024 ? 2 : 1; }
+};
+
+template <int KT>
+__global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const __grid_constant__ LoraArgs a) {
+  typedef ExpandSmem<KT> S;
+  extern __shared__ __align__(16) uint8_t raw[];
+  S& sm = *reinterpret_cast<S*>(raw);
+  const int tid = threadIdx.x, w = tid >> 5;
+  // the ids, B, base and scales may be read now: the launch before this one (shrink) lets
+  // it start only after its own wait, so all that came earlier has completed
+  RowPlace place;
+  const int chunks = find_chunks(a, sm.chunk, place);
+  const int cols = (a.n + kCols - 1) / kCols;
+  const long long items = static_cast<long long>(chunks) * cols;
+  long long at = items * blockIdx.x / gridDim.x;
+  const long long end = items * (blockIdx.x + 1) / gridDim.x;
+  bool waited = false;
+  while (at < end) {
+    const int c = static_cast<int>(at / cols);
+    const int lo = static_cast<int>(at - static_cast<long long>(c) * cols);
+    const int hi = static_cast<int>(min(static_cast<long long>(cols), lo + (end - at)));
+    at += hi - lo;
+    select_chunk(a, place, c, sm.chunk);
+    ExpandWarp<KT, kExpandTiles> e(a, sm.ring[w], sm.turn[w], sm.chunk, lo, hi);
+    e.start();
+    if (!waited) {
+      pdl_wait();
+      pdl_launch_dependents();
+      waited = true;
+    }
+    const int steps = e.steps();
+    for (int i = tid; i < e.tiles * steps * 32; i += kThreads) {
+      const int l = i & 31, s = (i >> 5) % steps, m = (i >> 5) / steps;
+      // the ranks of a lane's fragments of step s: as they lie in its pieces of B
+      const int r = KT == 1 ? 4 * (l & 3) : (s >> 1) * 32 + 8 * (l & 3) + (s & 1) * 4;
+      float v[2][4] = {};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = sm.chunk.row[m * 16 + h * 8 + (l >> 2)];
+        if (row < 0 || r >= e.rank) continue;
+        const float4 q = __ldcg(reinterpret_cast<const float4*>(a.t + row * a.rank + r));
+        v[h][0] = q.x;
+        v[h][1] = r + 1 < e.rank ? q.y : 0.f;
+        v[h][2] = r + 2 < e.rank ? q.z : 0.f;
+        v[h][3] = r + 3 < e.rank ? q.w : 0.f;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        sm.planes.v[m][s][p][l] = make_uint4(pack_bf16(v[0][0], v[0][1]), pack_bf16(v[1][0], v[1][1]),
+                                             pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][2], v[1][3]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[h][q] -= bf16_part(v[h][q]);
+      }
+    }
+    __syncthreads();
+    e.run(sm.planes);
+  }
+}
+
+// ------------------------------------------------ both at once, for few rows
+// A cluster of kSplits CTAs takes a chunk of up to 16 rows: they share the sums of t as the
+// shrink launch does, each then sends its elements' planes to all, and takes an eighth of the
+// columns - or, where n is long, of the grid's z-th part of them, for which t is computed again
+// (A is in L2).  Its first columns of B and of the base are under way meanwhile.
+template <int KT>
+struct FusedSmem {
+  static constexpr int NT = KT * 2, kFrags = NT * 32;
+  Ring<KT> ring[kWarps];
+  Planes<KT, 1> planes;
+  float4 warp[kWarps][kFrags];
+  float4 split[kSplits][kFrags / kSplits];
+  Chunks<16> chunk;
+  Turn turn[kWarps];
+};
+
+template <int KT>
+__global__ void __launch_bounds__(kThreads, KT == 1 ? 2 : 1) fused_kernel(const __grid_constant__ LoraArgs a) {
+  typedef FusedSmem<KT> S;
+  constexpr int NT = S::NT;
+  extern __shared__ __align__(16) uint8_t raw[];
+  S& sm = *reinterpret_cast<S*>(raw);
+  const int tid = threadIdx.x, w = tid >> 5, split = blockIdx.x;
+  cluster_arrive_release();   // waited for before the first push into a peer
+  pdl_wait();
+  pdl_launch_dependents();
+  // the CTAs of a cluster have one chunk: they leave together
+  RowPlace place;
+  if (static_cast<int>(blockIdx.y) >= find_chunks(a, sm.chunk, place)) {
+    cluster_wait_acquire();
+    return;
+  }
+  select_chunk(a, place, blockIdx.y, sm.chunk);
+  const int cols = (a.n + kCols - 1) / kCols, part = blockIdx.z * kSplits + split, parts = gridDim.z * kSplits;
+  ExpandWarp<KT, 1> e(a, sm.ring[w], sm.turn[w], sm.chunk, static_cast<int>(static_cast<long long>(cols) * part / parts),
+                      static_cast<int>(static_cast<long long>(cols) * (part + 1) / parts));
+  e.start();
+  if (e.rank > 0) {
+    constexpr int own = S::kFrags / kSplits;
+    float acc[1][NT][4] = {};
+    shrink_sums<1, NT>(a, sm.chunk.row, sm.chunk.id, e.rank, 0, split, 1, acc);
+    share_sums<1, NT>(acc, 1, split, own, sm.warp, sm.split);
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    // an owned element to one CTA per thread: two rows' pairs of ranks, three planes
+    for (int i = tid; i < own * kSplits; i += kThreads) {
+      const int mine = i % own, to = i / own;
+      float4 s = sm.split[0][mine];
+#pragma unroll
+      for (int c = 1; c < kSplits; ++c) add4(s, sm.split[c][mine]);
+      const int f = split * own + mine, l = f & 31, j = (f >> 5) * 8 + 2 * (l & 3);
+      // the lane and the word that hold ranks j, j + 1 (run()'s order), rows g and g + 8
+      const int step = KT == 1 ? 0 : (j >> 5) * 2 + (j >> 2 & 1), t = KT == 1 ? j >> 2 : j >> 3 & 3;
+      const int word = j & 2;
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        const uint32_t at = mapa_shared(smem_addr(&sm.planes.v[0][step][p][(l & ~3) | t]) + word * 4, to);
+        st_cluster_u32(at, pack_bf16(s.x, s.y));
+        st_cluster_u32(at + 4, pack_bf16(s.z, s.w));
+        s.x -= bf16_part(s.x);
+        s.y -= bf16_part(s.y);
+        s.z -= bf16_part(s.z);
+        s.w -= bf16_part(s.w);
+      }
+    }
+    cluster_arrive_release();
+  }
+  cluster_wait_acquire();
+  e.run(sm.planes);
 }
 
 // Opt a kernel in to more than 48 KB of shared memory, once per device.
@@ -546,6 +676,19 @@ cudaError_t launch_expand(const LoraArgs& a, cudaLaunchConfig_t cfg) {
   return cudaLaunchKernelEx(&cfg, expand_kernel<KT>, a);
 }
 
+template <int KT>
+cudaError_t launch_fused(const LoraArgs& a, cudaLaunchConfig_t cfg) {
+  static_assert(sizeof(FusedSmem<KT>) <= 227 * 1024, "shared memory");
+  static std::atomic<bool> set[64];
+  const int chunks = std::min(a.rows, a.n_adapters + 1 + a.rows / 16);
+  // parts of at most 4096 columns (512 a CTA), while the launch is a few CTAs per SM
+  const int parts = std::min((a.n + 4095) / 4096, std::max(1, 76 / chunks));
+  cfg.gridDim = dim3(kSplits, chunks, parts);
+  cfg.dynamicSmemBytes = sizeof(FusedSmem<KT>);
+  if (const cudaError_t e = allow_smem(fused_kernel<KT>, cfg.dynamicSmemBytes, set); e != cudaSuccess) return e;
+  return cudaLaunchKernelEx(&cfg, fused_kernel<KT>, a);
+}
+
 cudaError_t launch_lora(const LoraArgs& a, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads);
@@ -559,6 +702,14 @@ cudaError_t launch_lora(const LoraArgs& a, cudaStream_t s) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
+  // One launch where the GPU's part is so short that a call's time is the host's: 2 to 2.5 us
+  // less there (16.9 -> 14.6 us at 1 x 4096 x 4096, 17.2 -> 14.9 at 16 rows with an adapter each;
+  // on the GPU 4.4 -> 4.9 and 6.4 -> 6.0).  Over longer rows of many adapters, or with more
+  // of A per CTA, two launches spread better: 16 x 28672 with 16 adapters 10.6 us (one launch 15.2),
+  // 21 x 32003 11.8 (25.4), 32 rows of 8 adapters of rank 64 at n = 28672 12.7 (33.9).
+  const int chunks = std::min(a.rows, a.n_adapters + 1 + a.rows / 16);
+  if (a.rank <= 32 && static_cast<long long>(chunks) * a.n <= 1 << 16 && static_cast<long long>(a.k) * a.rank <= 1 << 18)
+    return a.rank <= 16 ? launch_fused<1>(a, cfg) : launch_fused<2>(a, cfg);
   const cudaError_t e = a.rows <= 32 ? launch_shrink<1, 2>(a, cfg) : launch_shrink<2, 4>(a, cfg);
   if (e != cudaSuccess) return e;
   cfg.numAttrs = 1;
