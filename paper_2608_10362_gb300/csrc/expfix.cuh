@@ -114,11 +114,13 @@ __device__ __forceinline__ void weight_places(const float (&z)[4], const WeightS
   }
 }
 __device__ __forceinline__ unsigned long long weight_at(int n, float f, const unsigned long long* table) {
-  const float u = f * static_cast<float>(0.693147180559945 / kExpSteps);
-  const float p = fmaf(u * u, fmaf(u, 1.f / 6.f, 0.5f), u);         // 2^(f/256) - 1, below 0.0028
+  constexpr double kLn = 0.693147180559945 / kExpSteps, kScale = 549755813888.0;   // 2^39
+  // 2^39 (2^(f/256) - 1), the parenthesis below 0.0028
+  const float p = fmaf(fmaf(f, static_cast<float>(kScale * kLn * kLn * kLn / 6), static_cast<float>(kScale * kLn * kLn / 2)),
+                       f, static_cast<float>(kScale * kLn)) * f;
   const unsigned long long t = table[n & (kExpSteps - 1)];          // [2^62, 2^63)
-  // t * p: the upper half of t times p in units of 2^-39, in units of 2^25
-  const long long r = static_cast<long long>(__mulhi(static_cast<int>(t >> 32), __float2int_rn(p * 549755813888.f)));
+  // t times that: its upper half times p, in units of 2^25
+  const long long r = static_cast<long long>(__mulhi(static_cast<int>(t >> 32), __float2int_rn(p)));
   const unsigned long long w = t + static_cast<unsigned long long>(r * (1ll << 25));
   // 2 floor(x / 2) + 1 is x in the mean, so that truncation adds no drift to a long sum
   return n > kNoWeight ? (w >> (kExpBits - kWeightBits - (n >> 8))) | 1u : 0;
