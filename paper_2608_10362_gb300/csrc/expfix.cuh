@@ -103,14 +103,15 @@ __device__ __forceinline__ int place_far(float z, const WeightScale& s, float& f
 __device__ __forceinline__ int weight_place(float z, const WeightScale& s, float& f) {
   return s.near ? place_near(z, s, f) : place_far(z, s, f);
 }
-// Four at once: one branch, and their arithmetic interleaves.
-__device__ __forceinline__ void weight_places(const float (&z)[4], const WeightScale& s, int (&n)[4], float (&f)[4]) {
+// Several at once: one branch, and their arithmetic interleaves.
+template <int N>
+__device__ __forceinline__ void weight_places(const float (&z)[N], const WeightScale& s, int (&n)[N], float (&f)[N]) {
   if (s.near) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) n[q] = place_near(z[q], s, f[q]);
+    for (int q = 0; q < N; ++q) n[q] = place_near(z[q], s, f[q]);
   } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) n[q] = place_far(z[q], s, f[q]);
+    for (int q = 0; q < N; ++q) n[q] = place_far(z[q], s, f[q]);
   }
 }
 __device__ __forceinline__ unsigned long long weight_at(int n, float f, const unsigned long long* table) {

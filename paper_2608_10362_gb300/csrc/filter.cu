@@ -971,12 +971,26 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     return true;
   };
   u64 mine = 0;
-  if (!empty)
-#pragma unroll 2
+  if (cut == no_cut && !empty) {   // nothing is cut: two tiles' arithmetic at a time (56 us for 65
+                                   // over 144 rows of 128256)
+    const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    for (int t = t_lo; t < t_hi; t += 2) {
+      const int i = t * 128 + lane * 4;
+      const float4 v0 = i < len ? *reinterpret_cast<const float4*>(s.z + i) : none;
+      const float4 v1 = t + 1 < t_hi && i + 128 < len ? *reinterpret_cast<const float4*>(s.z + i + 128) : none;
+      const float z[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+      int n[8];
+      float f[8];
+      weight_places(z, ws, n, f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) mine += weight_at(n[q], f[q], sm.table);
+    }
+  } else if (!empty) {
     for (int t = t_lo; t < t_hi; ++t) {
       u64 wt[4];
       if (tile_weights(t, wt)) mine += (wt[0] + wt[1]) + (wt[2] + wt[3]);
     }
+  }
   mine = warp_sum(mine);
   __syncthreads();
   if (lane == 0) sm.scan[w] = mine;
