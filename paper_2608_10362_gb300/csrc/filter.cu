@@ -94,7 +94,7 @@ struct alignas(16) Smem {
   uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
   float2 log_min_p;                          // T log(min_p) in two floats
   u64 peer_sum[kMaxCluster];                 // pushed
-  u64 scan[16];
+  u64 scan[32];
   uint32_t group[kGroups];                   // keys
   uint64_t loaded;                           // mbarrier of the slice's copies
   uint32_t tie_id;                           // pushed
@@ -139,16 +139,24 @@ __device__ __forceinline__ T warp_scan(T v) {   // inclusive
   }
   return v;
 }
+// Two sums over the block, to thread 0.
 template <int NT>
-__device__ u64 block_sum(u64 v, u64* scratch) {
-  v = warp_sum(v);
+__device__ void block_sums(u64& x, u64& y, u64* scratch) {
+  x = warp_sum(x);
+  y = warp_sum(y);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  if ((threadIdx.x & 31) == 0) {
+    scratch[threadIdx.x >> 5] = x;
+    scratch[NT / 32 + (threadIdx.x >> 5)] = y;
+  }
   __syncthreads();
-  u64 s = 0;
+  if (threadIdx.x > 0) return;
+  x = y = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 32; ++i) s += scratch[i];
-  return s;
+  for (int i = 0; i < NT / 32; ++i) {
+    x += scratch[i];
+    y += scratch[NT / 32 + i];
+  }
 }
 // Inclusive sum over the threads up to this one; *total over all.
 template <int NT>
@@ -486,8 +494,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     }
   });
   if (kMass) {
-    sum = block_sum<NT>(sum, sm.scan);
-    if (kCandidates) listed_sum = block_sum<NT>(listed_sum, sm.scan);
+    block_sums<NT>(sum, listed_sum, sm.scan);
     if (tid == 0) {
       sm.sum = sum;
       sm.listed_sum = listed_sum;
