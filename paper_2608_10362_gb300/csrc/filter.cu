@@ -451,11 +451,11 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     }
     return takes_part(z, id) ? b : kBins;
   };
-  clear_histogram<NT>(sm);
-  if (tid == 0) {
+  if (tid == 0) {             // before the barrier in clear_histogram: the pass counts candidates
     sm.n_list = sm.n_candidates = sm.n_queue = 0;
     sm.cut = p.within;
   }
+  clear_histogram<NT>(sm);
   constexpr bool kCandidates = kMass && kWhole;
   u64 sum = 0, listed_sum = 0;
   for_quads<NT>(s, z_in, [&](const float (&z)[4], int id) {
