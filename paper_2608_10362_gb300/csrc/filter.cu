@@ -59,7 +59,6 @@ constexpr int kQueue = 4 * kList;            // places in the slice, in the list
 constexpr int kGroups = 64;                  // groups of threads whose maxima give the bound
 constexpr int kMostAbove = 56;               // of them above it at most
 constexpr int kTopPAbove = 96;               // logits above the bound for top-p alone
-constexpr int kWideCtas = 304;               // launches of at most so many CTAs: 512 threads each
 
 typedef unsigned long long u64;
 
@@ -456,7 +455,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     sm.cut = p.within;
   }
   clear_histogram<NT>(sm);
-  constexpr bool kCandidates = kMass && kWhole;
+  constexpr bool kCandidates = kMass && kWhole && !kAlone;   // else they were tried before
   u64 sum = 0, listed_sum = 0;
   for_quads<NT>(s, z_in, [&](const float (&z)[4], int id) {
     bool in[4];
@@ -718,6 +717,13 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
   return {cut, whole_list ? n : 0, e, false};
 }
 
+// 2^x, off by at most 2^-22 of itself; subnormal results as 0.
+__device__ __forceinline__ float rough_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // The draw from the entries up to the cut among the n that the threads hold in order.
 template <int NT>
 __device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 e, u64 cut, const WeightScale& ws,
@@ -861,6 +867,77 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   }
   const u64 fraction = fraction64(r.top_p);
   uint32_t n = 0;             // > 0: so many candidates were listed and hold what is kept
+  if constexpr (!kMask) {
+    // Top-p alone: the candidates' weights are summed exactly, all others' to 2^-17 of their
+    // sum: that tells what the prefix has to reach but for the last bits, and with them where
+    // it ends unless that is within those bits of a border.  (x - max, c and their product are
+    // off by 2^-24 of themselves each, so an exponent above -46 by 2^-16.9 and the power by
+    // 2^-17.4 of itself, besides the instruction's 2^-22; a thread's sum by 19 roundings.)
+    if (by_p && !by_k && !empty && ws.hi > 0.f) {
+      float sum = 0.f;
+      u64 listed = 0;
+      for_quads<NT>(s, -INFINITY, [&](const float (&x)[4], int id) {
+        float e[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) e[q] = rough_exp2((x[q] - m) * ws.hi);
+        if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= bound) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (x[q] >= bound) {
+              e[q] = 0.f;
+              listed += weight(x[q], ws, sm.table);
+              const uint32_t i = atomicAdd(&sm.n_list, 1u);
+              if (i < kList) sm.list[i] = entry_of(logit_key(x[q]), static_cast<uint32_t>(id + q));
+            }
+        }
+        sum += (e[0] + e[1]) + (e[2] + e[3]);
+      });
+      u64 rest = __float2ull_rn(sum * 70368744177664.f);   // 2^46
+      block_sums<NT>(listed, rest, sm.scan);
+      if (tid == 0) {
+        sm.listed_sum = listed;
+        sm.sum = rest;
+        sm.cut = 0;                        // no entry
+      }
+      cluster_sync();
+      const bool peer = lane < C;
+      n = __reduce_add_sync(0xffffffffu, peer ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0u);
+      listed = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.listed_sum), lane)) : 0);
+      rest = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), lane)) : 0);
+      // weights are whole numbers, and 0 where the power is below 2^-45: 4 per id for both
+      const u64 error = rest == 0 ? 0 : (rest >> 16) + 4 * static_cast<u64>(V);
+      u64 need = part_of(fraction, listed + rest - error);
+      const u64 need_most = part_of(fraction, listed + rest + error);
+      if (n <= kList && listed >= need_most) {
+        if (rank != 0) {                   // the rest is the first CTA's
+          cluster_sync();
+          return;
+        }
+        u64 e, all;
+        pull_list<NT>(C, &sm.n_list, e, sm);
+        cluster_arrive_release();          // they may leave; nobody reads this CTA's
+        const u64 own = static_cast<uint32_t>(tid) < n ? weight(entry_logit(e), ws, sm.table) : 0;
+        const u64 incl = block_scan<NT>(own, sm.scan, &all);
+        if (incl - own < need && need_most <= incl) sm.cut = e;
+        __syncthreads();
+        if (sm.cut == 0) {                 // a border between the two: the row's exact sum
+          u64 v = 0;
+#pragma unroll 4
+          for (int i = tid; i < V; i += NT) v += weight(sane(__ldcg(z + i)), ws, sm.table);
+          block_scan<NT>(v, sm.scan, &all);
+          need = part_of(fraction, all);
+          if (incl - own < need && need <= incl) sm.cut = e;
+          __syncthreads();
+        }
+        cut = min(cut, sm.cut);
+        draw_from_list<NT>(a, row, n, e, cut, ws, sm);
+        cluster_wait_acquire();
+        return;
+      }
+      n = 0;
+      cluster_sync();                      // the others have read this CTA's counts and sums
+    }
+  }
   bool search_k = by_k && !empty;
   if (search_k && owed <= kMostAbove) {
     for_warp_quads<NT>(s, bound, [&](const float (&x)[4], int id) {
@@ -1053,7 +1130,7 @@ cudaError_t launch_filter(const FilterArgs& a, cudaStream_t s, bool pdl) {
     C *= 2;
   const int len = ((a.vocab + 3 + C - 1) / C + 3) / 4 * 4;
   // 512 threads while every SM has one CTA at most
-  const bool wide = a.rows * C <= kWideCtas, mask = a.out != nullptr;
+  const bool wide = a.rows * C <= (C == 8 ? 272 : C == 4 ? 288 : 304), mask = a.out != nullptr;
   void (*const kernel)(FilterArgs, int, int) = wide ? (mask ? filter_kernel<512, true> : filter_kernel<512, false>)
                                                     : (mask ? filter_kernel<256, true> : filter_kernel<256, false>);
   static std::atomic<bool> set[4][64];
