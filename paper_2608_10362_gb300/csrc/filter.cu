@@ -93,11 +93,12 @@ struct alignas(16) Smem {
   uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
   float2 log_min_p;                          // T log(min_p) in two floats
   u64 peer_sum[kMaxCluster];                 // pushed
-  u64 scan[32];
+  u64 scan[48];
   uint32_t group[kGroups];                   // keys
   uint64_t loaded;                           // mbarrier of the slice's copies
   uint32_t tie_id;                           // pushed
   u64 cut;
+  u64 deep_sum;                              // of the slice's weights below a bound, roughly; read by the others
 };
 static_assert(3 * (sizeof(Smem) + kMaxSlice * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
 
@@ -138,23 +139,22 @@ __device__ __forceinline__ T warp_scan(T v) {   // inclusive
   }
   return v;
 }
-// Two sums over the block, to thread 0.
-template <int NT>
-__device__ void block_sums(u64& x, u64& y, u64* scratch) {
-  x = warp_sum(x);
-  y = warp_sum(y);
+// N sums over the block, to thread 0.
+template <int NT, int N>
+__device__ void block_sums(u64 (&v)[N], u64* scratch) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) {
-    scratch[threadIdx.x >> 5] = x;
-    scratch[NT / 32 + (threadIdx.x >> 5)] = y;
-  }
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int k = 0; k < N; ++k) scratch[k * (NT / 32) + (threadIdx.x >> 5)] = v[k];
   __syncthreads();
   if (threadIdx.x > 0) return;
-  x = y = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 32; ++i) {
-    x += scratch[i];
-    y += scratch[NT / 32 + i];
+  for (int k = 0; k < N; ++k) {
+    v[k] = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) v[k] += scratch[k * (NT / 32) + i];
   }
 }
 // Inclusive sum over the threads up to this one; *total over all.
@@ -292,16 +292,18 @@ __device__ __forceinline__ int count_bin(float depth) {
 // A histogram's bin that holds the cut, by the same steps in every CTA of the cluster.
 struct Found {
   int bin;
-  u64 above;                // sum (count or weights) before the bin
+  u64 above, own;           // sum (count or weights) before the bin, and its own
   uint32_t count;           // elements in it
   uint32_t count_above;     // and before it
+  u64 total;                // of all bins
   u64 need;                 // what the prefix has to reach
   bool all;                 // the whole set does not exceed it (a count): nothing is cut
 };
 
-// After the histogram of every CTA is complete and the cluster has synchronised.
-template <int NT, bool kMass>
-__device__ Found find_bin(u64 need, int C, Smem& sm) {
+// After the histogram of every CTA is complete and the cluster has synchronised; need_of: what
+// the prefix has to reach, from the sum of all bins.
+template <int NT, bool kMass, class NeedOf>
+__device__ Found find_bin(NeedOf need_of, int C, Smem& sm) {
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   Found f;
   // the groups' sums of all CTAs
@@ -322,6 +324,8 @@ __device__ Found find_bin(u64 need, int C, Smem& sm) {
   u64 incl = warp_scan(v);
   const uint32_t n_incl = warp_scan(n);
   const u64 total = __shfl_sync(0xffffffffu, incl, 31);
+  const u64 need = need_of(total);
+  f.total = total;
   f.need = need;
   f.all = !kMass && need >= total;
   const unsigned reach = __ballot_sync(0xffffffffu, lane < kSupers && incl >= need);
@@ -348,24 +352,25 @@ __device__ Found find_bin(u64 need, int C, Smem& sm) {
   const int b = hit ? __ffs(hit) - 1 : 31;
   f.bin = g * 32 + b;
   f.above = __shfl_sync(0xffffffffu, incl - v, b);
+  f.own = __shfl_sync(0xffffffffu, v, b);
   f.count = __shfl_sync(0xffffffffu, n, b);
   f.count_above = n_before + __shfl_sync(0xffffffffu, warp_scan(n) - n, b);
   return f;
 }
 static_assert(256 / 32 >= kMaxCluster && 256 >= kMaxCluster * kSupers, "a warp per CTA of the cluster");
 
-// Elements of a quad into their bins: counts, and weights as 64-bit sums in two words.
-template <bool kMass>
-__device__ __forceinline__ void add_to_bins(Smem& sm, const bool (&in)[4], const int (&bin)[4], const u64 (&w)[4]) {
+// N elements into their bins: counts, and weights as 64-bit sums in two words.
+template <bool kMass, int N>
+__device__ __forceinline__ void add_to_bins(Smem& sm, const bool (&in)[N], const int (&bin)[N], const u64 (&w)[N]) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < N; ++q)
     if (in[q]) atomicAdd(&sm.h.cnt[bin[q]], 1u);
   if constexpr (kMass) {
-    uint32_t old[4];
+    uint32_t old[N];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) old[q] = in[q] ? atomicAdd(&sm.h.lo[bin[q]], static_cast<uint32_t>(w[q])) : 0;
+    for (int q = 0; q < N; ++q) old[q] = in[q] ? atomicAdd(&sm.h.lo[bin[q]], static_cast<uint32_t>(w[q])) : 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < N; ++q) {
       const uint32_t lo = static_cast<uint32_t>(w[q]);
       const uint32_t hi = static_cast<uint32_t>(w[q] >> 32) + (old[q] + lo < old[q] ? 1u : 0u);
       if (in[q] && hi != 0) atomicAdd(&sm.h.hi[bin[q]], hi);
@@ -418,6 +423,11 @@ __device__ uint32_t pull_list(int C, const uint32_t* count, u64& e, Smem& sm) {
   rank_sort<NT>(sm.entry[0], sm.entry[1], all);
   e = threadIdx.x < all ? sm.entry[1][threadIdx.x] : ~0ull;
   return all;
+}
+
+// A margin for the roundings of a place or a depth, and of a logit z from it.
+__device__ __forceinline__ float slack_at(float z, const WeightScale& ws) {
+  return 4e-7f * (fabsf(ws.max) + fabsf(z)) + 1e-37f;
 }
 
 struct Ended {
@@ -493,10 +503,11 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     }
   });
   if (kMass) {
-    block_sums<NT>(sum, listed_sum, sm.scan);
+    u64 sums[2] = {sum, listed_sum};
+    block_sums<NT>(sums, sm.scan);
     if (tid == 0) {
-      sm.sum = sum;
-      sm.listed_sum = listed_sum;
+      sm.sum = sums[0];
+      sm.listed_sum = sums[1];
     }
   }
   close_histogram<NT, kMass>(sm);
@@ -526,14 +537,13 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
       }
     }
   }
-  Found f = find_bin<NT, kMass>(need, C, sm);
+  Found f = find_bin<NT, kMass>([&](u64) { return need; }, C, sm);
   if (f.all) {
     cluster_sync();           // the others have read this CTA's histogram
     return {p.within, 0, 0, false};
   }
   const int bin = f.bin;
-  // the keys that the bin's elements can have: from the depths at its ends, with a margin
-  // for the roundings of a place or a depth and of these lines
+  // the keys that the bin's elements can have: from the depths at its ends
   uint32_t k_lo, k_hi;
   {
     float d0, d1;             // max - z
@@ -545,7 +555,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
       d1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + kFirstOctave) << (23 - kMantissa));
     }
     const float z1 = ws.max - d0, z0 = ws.max - d1;
-    const float slack = 4e-7f * (fabsf(ws.max) + fabsf(z0)) + 1e-37f;
+    const float slack = slack_at(z0, ws);
     k_hi = bin == 0 || !(z1 + slack < ws.max) ? logit_key(ws.max) : logit_key(z1 + slack);
     k_lo = (!kMass && bin == kBins - 1) || !(z0 - slack > -kLargest) ? logit_key(-kLargest) : logit_key(z0 - slack);
   }
@@ -650,7 +660,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
       });
     }
     close_histogram<NT, kMass>(sm);
-    f = find_bin<NT, kMass>(f.need - above, C, sm);
+    f = find_bin<NT, kMass>([&](u64) { return f.need - above; }, C, sm);
     f.need += above;
     above += f.above;
   }
@@ -724,6 +734,121 @@ __device__ __forceinline__ float rough_exp2(float x) {
   return y;
 }
 
+// What a prefix by weights has to reach, `fraction` of a sum known to within `error`.
+struct Need {
+  u64 fraction, least, most;
+  __device__ __forceinline__ Need(u64 f, u64 sum, u64 error)
+      : fraction(f), least(part_of(f, sum - error)), most(part_of(f, sum + error)) {}
+};
+// The entry where the prefix ends, among sorted ones e of weight `own` behind a sum of
+// `before`, which the threads of the first CTA hold (alone) or of every one; then every list
+// has been read.  Within the error of a border all CTAs sum their slices exactly.
+template <int NT>
+__device__ __forceinline__ u64 end_of(const Need& need, u64 before, u64 own, u64 e, bool alone, const Slice& s,
+                                      const WeightScale& ws, int C, int rank, Smem& sm) {
+  const int tid = threadIdx.x;
+  const bool here = !alone || rank == 0;
+  u64 incl = 0, all;
+  if (here) {
+    incl = before + block_scan<NT>(own, sm.scan, &all);
+    if (incl - own < need.least && need.most <= incl) sm.cut = e;
+    __syncthreads();
+    if (alone && tid > 0 && tid < C) st_cluster_u64(mapa_shared(smem_addr(&sm.cut), tid), sm.cut);
+  }
+  cluster_sync();
+  u64 cut = sm.cut;
+  if (cut == 0) {
+    u64 sums[1] = {0};
+    for_quads<NT>(s, -kLargest, [&](const float (&z)[4], int) {
+      int n[4];
+      float f[4];
+      weight_places(z, ws, n, f);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sums[0] += weight_at(n[q], f[q], sm.table);
+    });
+    block_sums<NT>(sums, sm.scan);
+    if (tid == 0) sm.sum = sums[0];
+    cluster_sync();
+    const int lane = tid & 31;
+    const u64 exact =
+        part_of(need.fraction, warp_sum(lane < C ? ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), lane)) : 0));
+    if (here && incl - own < exact && exact <= incl) sm.cut = e;
+    cluster_sync();           // the others have read this CTA's sum
+    cut = sm.cut;
+  }
+  return cut;
+}
+// The same of a row whose ids below z_min weigh `deep` together, within `error`, and are not
+// the cut: the others, which have to be few, are queued and go into the histogram.  No cut
+// (0) where it takes more: more ids, or a bin's division.
+template <int NT>
+__device__ Ended search_above(u64 fraction, u64 deep, u64 error, float z_min, const Slice& s, const WeightScale& ws,
+                              int C, int rank, Smem& sm) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  if (tid == 0) {
+    sm.n_list = sm.n_queue = 0;
+    sm.cut = 0;
+  }
+  clear_histogram<NT>(sm);
+  for_warp_quads<NT>(s, z_min, [&](const float (&z)[4], int id) {
+    bool in[4];
+    Places at;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) in[q] = z[q] >= z_min;
+    if (!reserve(in, &sm.n_queue, at)) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (in[q] && at.at[q] < kQueue) sm.queue[at.at[q]] = static_cast<uint16_t>(id + q - s.base);
+  });
+  __syncthreads();
+  constexpr int kQueued = kQueue / NT;
+  u64 mine[kQueued], w[kQueued];
+  bool in[kQueued];
+  int bin[kQueued];
+#pragma unroll
+  for (int q = 0; q < kQueued; ++q) {
+    const uint32_t i = q * NT + tid;
+    in[q] = i < min(sm.n_queue, static_cast<uint32_t>(kQueue));
+    w[q] = 0;
+    bin[q] = kBins;
+    if (!in[q]) continue;
+    const int at = sm.queue[i];
+    float f;
+    const int n = weight_place(s.z[at], ws, f);
+    w[q] = weight_at(n, f, sm.table);
+    in[q] = w[q] != 0;
+    if (in[q]) bin[q] = static_cast<int>(static_cast<unsigned>(-n) / kPlacesPerBin);
+    mine[q] = entry_of(logit_key(s.z[at]), static_cast<uint32_t>(s.base + at));
+  }
+  add_to_bins<true>(sm, in, bin, w);
+  close_histogram<NT, true>(sm);
+  const bool fits = __all_sync(
+      0xffffffffu, lane >= C || ld_cluster_u32(mapa_shared(smem_addr(&sm.n_queue), min(lane, C - 1))) <= kQueue);
+  const Found f = find_bin<NT, true>([&](u64 total) { return part_of(fraction, total + deep - error); }, C, sm);
+  const Need need(fraction, f.total + deep, error);
+  if (!fits || need.most > f.above + f.own || f.count > kList) {
+    cluster_sync();           // the others have read this CTA's histogram
+    return {0, 0, 0, false};
+  }
+  const bool whole_list = f.count_above + f.count <= kList;
+  __syncthreads();            // sm.p, in the list's place, is read (the queue is in registers)
+#pragma unroll
+  for (int q = 0; q < kQueued; ++q)
+    if (whole_list ? bin[q] <= f.bin : bin[q] == f.bin) {
+      const uint32_t i = atomicAdd(&sm.n_list, 1u);
+      if (i < kList) sm.list[i] = mine[q];
+    }
+  cluster_sync();
+  u64 e = ~0ull, own = 0;
+  uint32_t n = 0;
+  if (!whole_list || rank == 0) {
+    n = pull_list<NT>(C, &sm.n_list, e, sm);   // into the histogram's place: nobody reads that any more
+    own = static_cast<uint32_t>(tid) < n ? weight(entry_logit(e), ws, sm.table) : 0;
+  }
+  const u64 cut = end_of<NT>(need, whole_list ? 0 : f.above, own, e, whole_list, s, ws, C, rank, sm);
+  return {cut, whole_list ? n : 0, e, whole_list && rank != 0};
+}
+
 // The draw from the entries up to the cut among the n that the threads hold in order.
 template <int NT>
 __device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 e, u64 cut, const WeightScale& ws,
@@ -785,7 +910,8 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
                 l2_policy_evict_normal());
   }
   const Rule r = rule_of(a, row);
-  const bool by_k = r.top_k > 0 && r.top_k < V, by_p = r.top_p < 1.f;
+  const bool by_k = r.top_k > 0 && r.top_k < V;
+  bool by_p = r.top_p < 1.f;
   if (r.min_p > 0.f && tid == NT - 1) {   // 64-bit arithmetic: one thread's, beside the loads
     const double l = static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
     const float hi = static_cast<float>(l);
@@ -872,10 +998,15 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     // sum: that tells what the prefix has to reach but for the last bits, and with them where
     // it ends unless that is within those bits of a border.  (x - max, c and their product are
     // off by 2^-24 of themselves each, so an exponent above -46 by 2^-16.9 and the power by
-    // 2^-17.4 of itself, besides the instruction's 2^-22; a thread's sum by 19 roundings.)
-    if (by_p && !by_k && !empty && ws.hi > 0.f) {
-      float sum = 0.f;
+    // 2^-17.4 of itself, besides the instruction's 2^-22; a thread's sums by 19
+    // roundings: 2^-17.1 in all.)
+    // Rows whose candidates lie within 4 octaves are flat: more ids than these hold the sum.
+    if (by_p && !by_k && !empty && (m - bound) * ws.hi > 4.f) {
+      float sum = 0.f, deep4[4] = {};
       u64 listed = 0;
+      // 3 to 6 octaves below the bound: the queues hold what lies above of a row whose weights
+      // fall by rank^-1.4
+      const float z_deep = fmaxf(bound - static_cast<float>(34 - __clz(C)) / ws.hi, -kLargest);
       for_quads<NT>(s, -INFINITY, [&](const float (&x)[4], int id) {
         float e[4];
 #pragma unroll
@@ -891,51 +1022,57 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
             }
         }
         sum += (e[0] + e[1]) + (e[2] + e[3]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (x[q] < z_deep) deep4[q] += e[q];
       });
-      u64 rest = __float2ull_rn(sum * 70368744177664.f);   // 2^46
-      block_sums<NT>(listed, rest, sm.scan);
+      constexpr float kOne = 70368744177664.f;   // 2^46
+      u64 sums[3] = {listed, __float2ull_rn(sum * kOne), 
+                     __float2ull_rn(((deep4[0] + deep4[1]) + (deep4[2] + deep4[3])) * kOne)};
+      block_sums<NT>(sums, sm.scan);
       if (tid == 0) {
-        sm.listed_sum = listed;
-        sm.sum = rest;
+        sm.listed_sum = sums[0];
+        sm.sum = sums[1];
+        sm.deep_sum = sums[2];
         sm.cut = 0;                        // no entry
       }
       cluster_sync();
       const bool peer = lane < C;
       n = __reduce_add_sync(0xffffffffu, peer ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_list), lane)) : 0u);
       listed = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.listed_sum), lane)) : 0);
-      rest = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), lane)) : 0);
+      const u64 rest = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.sum), lane)) : 0);
+      const u64 deep = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.deep_sum), lane)) : 0);
       // weights are whole numbers, and 0 where the power is below 2^-45: 4 per id for both
-      const u64 error = rest == 0 ? 0 : (rest >> 16) + 4 * static_cast<u64>(V);
-      u64 need = part_of(fraction, listed + rest - error);
-      const u64 need_most = part_of(fraction, listed + rest + error);
-      if (n <= kList && listed >= need_most) {
-        if (rank != 0) {                   // the rest is the first CTA's
-          cluster_sync();
-          return;
+      const u64 whole = 4 * static_cast<u64>(V);
+      const u64 error = rest == 0 ? 0 : (rest >> 17) + whole;
+      const Need need(fraction, listed + rest, error);
+      if (n <= kList && listed >= need.most) {
+        u64 e = ~0ull, own = 0;
+        if (rank == 0) {                   // the rest is the first CTA's
+          pull_list<NT>(C, &sm.n_list, e, sm);
+          own = static_cast<uint32_t>(tid) < n ? weight(entry_logit(e), ws, sm.table) : 0;
         }
-        u64 e, all;
-        pull_list<NT>(C, &sm.n_list, e, sm);
-        cluster_arrive_release();          // they may leave; nobody reads this CTA's
-        const u64 own = static_cast<uint32_t>(tid) < n ? weight(entry_logit(e), ws, sm.table) : 0;
-        const u64 incl = block_scan<NT>(own, sm.scan, &all);
-        if (incl - own < need && need_most <= incl) sm.cut = e;
-        __syncthreads();
-        if (sm.cut == 0) {                 // a border between the two: the row's exact sum
-          u64 v = 0;
-#pragma unroll 4
-          for (int i = tid; i < V; i += NT) v += weight(sane(__ldcg(z + i)), ws, sm.table);
-          block_scan<NT>(v, sm.scan, &all);
-          need = part_of(fraction, all);
-          if (incl - own < need && need <= incl) sm.cut = e;
-          __syncthreads();
-        }
-        cut = min(cut, sm.cut);
-        draw_from_list<NT>(a, row, n, e, cut, ws, sm);
-        cluster_wait_acquire();
+        cut = min(cut, end_of<NT>(need, 0, own, e, true, s, ws, C, rank, sm));
+        if (rank == 0) draw_from_list<NT>(a, row, n, e, cut, ws, sm);
         return;
       }
       n = 0;
       cluster_sync();                      // the others have read this CTA's counts and sums
+      // more than the list takes, but not by far: most of the sum is the candidates', and the
+      // ids that are not deep hold all that is kept
+      const u64 deep_error = deep == 0 ? 0 : (deep >> 17) + whole;
+      if (rest <= listed && listed + rest - error >= need.most + deep + deep_error) {
+        const Ended e = search_above<NT>(fraction, deep, deep_error, z_deep, s, ws, C, rank, sm);
+        if (e.gone) return;
+        if (e.cut != 0) {
+          cut = min(cut, e.cut);
+          if (e.listed > 0) {
+            draw_from_list<NT>(a, row, e.listed, e.entry, cut, ws, sm);
+            return;
+          }
+          by_p = false;                    // done
+        }
+      }
     }
   }
   bool search_k = by_k && !empty;

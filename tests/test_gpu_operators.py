@@ -120,18 +120,19 @@ def test_borders_among_equal_weights_are_exact(vocab):
     assert n.tolist() == np.maximum(1, np.ceil(f.astype(np.float64) * vocab)).astype(int).tolist()
 
 
-@pytest.mark.parametrize("vocab", [4000, 50000, 128256])
-def test_top_p_next_to_a_border(vocab):
+@pytest.mark.parametrize("T,first,step,last", [(0.6, 0, 3, 200), (1.0, 20, 60, 1500)])
+@pytest.mark.parametrize("vocab", [4000, 15000, 50000, 128256])
+def test_top_p_next_to_a_border(vocab, T, first, step, last):
     """p is the float nearest to the share of the first j ids: above it or below by some 1e-8,
     where the weights of the ids behind the candidates decide to their last bits."""
     import torch
     from paper_2608_10362_gb300 import op_filter_logits, op_sample_filtered
-    rows, T = 24, float(np.float32(0.6))
+    rows, T = 24, float(np.float32(T))
     z, u, p = _logits("peaked", rows, vocab, 3), _uniforms(rows), np.empty(rows, np.float32)
     for r in range(rows):
         w = np.sort(np.exp((z[r].astype(np.float64) - z[r].max()) / T))[::-1]
         share = np.cumsum(w) / np.sum(w)
-        j = next(j for j in range(3 * r % 40, 200) if 2.0 ** -30 < abs(np.float32(share[j]) - share[j]) < 2.0 ** -24)
+        j = next(j for j in range(first + step * r % last, last) if 2.0 ** -30 < abs(np.float32(share[j]) - share[j]) < 2.0 ** -24)
         p[r] = share[j]
     zt, pt = torch.from_numpy(z).cuda(), torch.from_numpy(p).cuda()
     got = op_sample_filtered(zt, torch.from_numpy(u).cuda(), temperature=T, top_p=pt).cpu().numpy()
