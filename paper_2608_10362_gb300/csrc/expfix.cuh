@@ -1,8 +1,8 @@
 // expfix.cuh - softmax weights as 64-bit fixed-point integers.
 //
 // weight(z) = 2^46 * exp((z - max) / T) as an odd integer: off by at most 2^-46 of the
-// largest weight and, relative to itself, 2^-32.5 (2^-34.7 in the mean square); 0 below
-// 2^-45.  Integers add up to the same sum in any order, so
+// largest weight and, relative to itself, 2^-31.3 (2^-34 in the mean square, both from an
+// emulation of these steps); 0 below 2^-45.  Integers add up to the same sum in any order, so
 // thousands of threads may sum them as they come and every comparison of sums (does this
 // prefix hold p of the mass? does the running sum pass u times the total?) is exact; with
 // 32-bit floating-point sums one draw in a few hundred lands within a rounding of a border
@@ -10,8 +10,8 @@
 //
 // exp by a table of 2^(i/256) and a cubic for the rest (the table-driven scheme of
 // P. T. P. Tang, ACM TOMS 15 (1989)): 256 y = 256 (z - max) log2(e) / T = n + f with a whole
-// n and |f| <= 1, where 2^(f/256) - 1 is small enough that 24 bits of it are 33 of the
-// weight.  About 30 instructions, none of them 64-bit floating point (2 a clock and SM here).
+// n and |f| <= 1, where 2^(f/256) - 1 is below 2^-8, so that 24 bits of it are 32
+// of the weight.  About 30 instructions, none of them 64-bit floating point (2 a clock and SM here).
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>

@@ -15,18 +15,34 @@
 //      times as many as top-k keeps), are listed; the list holds what the rule keeps, and
 //      each entry is counted against the others for its place in the order, the sum of
 //      weights before it and, among the kept ones, the sum before it in id order;
-//   3. else a search per part (top-k, then top-p among what top-k left): a histogram of the
+//   3. top-p alone, draws: the candidates are listed the same way and the sum of the rest is
+//      formed roughly, by one ex2 each.  If the candidates hold p of the sum they are all
+//      that is looked at (end_of); if they hold most of it, the ids a few octaves below them
+//      are queued and searched alone (search_above);
+//   4. else a search per part (top-k, then top-p among what top-k left): a histogram of the
 //      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
 //      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
 //      bins through distributed shared memory to find the bin with the cut, and list
 //      its elements - or all up to there, where they are few enough; top-p alone lists
-//      candidates on the way, and is done where they hold p of the sum.  A bin with more
-//      than the list takes (flat rows, many equal logits) is divided by key as often as it
-//      needs; a single key, by id;
-//   4. the draw: from the list where it holds all that is kept, else the kept weights' sums
+//      candidates on the way (masks), and is done where they hold p of the sum.  A bin with
+//      more than the list takes (flat rows, many equal logits) is divided by key as often as
+//      it needs; a single key, by id;
+//   5. the draw: from the list where it holds all that is kept, else the kept weights' sums
 //      slice by slice, then warp by warp; or the mask.
 // Every CTA of a cluster takes the same decisions from the same numbers, so no result is
-// passed back but an id among more equal logits than the list takes.
+// passed back but an id among more equal logits than the list takes, and what the first
+// CTA found where it goes on alone.
+//
+// Measured (us, one launch in a graph; 4 V bytes a row at 6780 GB/s are 0.02 to 11):
+//                       no cut  top-k 50  k, p    top-p 0.9  flat, top-p 0.9
+//     1 x  32000           5.6       7.1   7.9         14.6             17.7
+//     1 x 128256           9.7       8.2   8.9         14.9             30.1
+//    16 x 128256          14.2      10.3  11.4         22.3             42.1
+//   144 x 128256          55.6      36.4  37.2         75.0            160.9
+// One row is bound by latency: load, three to ten barriers of the cluster at 0.7 us each,
+// list and draw.  A batch is bound by the issue rate: 8 instructions an element for the load
+// and the maximum, 45 for an exact weight, 8 for a rough one, three atomics for a bin; three
+// CTAs an SM are 51 clusters, so 144 rows run in three waves.
 #include <cuda_runtime.h>
 
 #include <math.h>
@@ -58,7 +74,9 @@ constexpr uint32_t kList = 256;              // list entries of a CTA and of the
 constexpr int kQueue = 4 * kList;            // places in the slice, in the list's memory
 constexpr int kGroups = 64;                  // groups of threads whose maxima give the bound
 constexpr int kMostAbove = 56;               // of them above it at most
-constexpr int kTopPAbove = 96;               // logits above the bound for top-p alone
+constexpr int kTopPAbove = 96;               // logits above the bound for top-p alone (144 rows of 32000:
+                                             // 31 us; with 112 the queues overflow, 50; with 80 at p =
+                                             // 0.95 43 against 39)
 
 typedef unsigned long long u64;
 
@@ -871,8 +889,10 @@ __device__ void draw_from_list(const FilterArgs& a, int row, uint32_t n, u64 e, 
 }
 static_assert(kMaxVocab <= 1 << 24 && kList == 256, "an id and a place in 32 bits");
 
-// NT = 512: half the latency of 256, where a launch leaves the chip mostly idle; 256: a third
-// fewer instructions a row (what a thread does once per row), where it fills it.
+// NT = 512: a shorter pass over the slice (1 x 128256: no cut 9.7 us, 12.2 with 256 threads;
+// flat top-p 31.5, 39.3); 256: three CTAs per SM and fewer instructions a row (what a thread
+// does once per row), where not all of a launch's clusters fit at once (144 x 128256: top-k
+// 35.9 us, 47.0 with 512; top-p then 112, 124).
 template <int NT, bool kMask>
 __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __grid_constant__ FilterArgs a, int C,
                                                                       int len) {
@@ -1260,13 +1280,15 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
 
 cudaError_t launch_filter(const FilterArgs& a, cudaStream_t s, bool pdl) {
   if (a.vocab > kMaxVocab) return cudaErrorInvalidValue;
-  // as many CTAs per row as its slices need, more while the launch is small
+  // as many CTAs per row as its slices need, more while the launch is small (1 x 32000, no cut:
+  // 5.4 us with 8 CTAs, 7.5 with 4; 64 x 32000: top-k and -p 10.9 us with 4, 15.9 with 8)
   int C = 1;
   while (C < kMaxCluster &&
          ((a.vocab + 3 + C - 1) / C > kMaxSlice - 3 || (a.rows * C * 2 <= 304 && a.vocab >= 2 * C * 2048)))
     C *= 2;
   const int len = ((a.vocab + 3 + C - 1) / C + 3) / 4 * 4;
-  // 512 threads while every SM has one CTA at most
+  // 512 threads, two CTAs per SM, while all clusters fit at once: 34 of 8 CTAs, 72 of 4 (38 rows
+  // of 128256, top-k 13.0 us with 256 threads and 17.2 with 512; 34 rows, top-p 41.5 and 34.7)
   const bool wide = a.rows * C <= (C == 8 ? 272 : C == 4 ? 288 : 304), mask = a.out != nullptr;
   void (*const kernel)(FilterArgs, int, int) = wide ? (mask ? filter_kernel<512, true> : filter_kernel<512, false>)
                                                     : (mask ? filter_kernel<256, true> : filter_kernel<256, false>);
