@@ -141,8 +141,9 @@ typedef struct memspec_filter {
  * rule on this is memspec_op_sample's draw (but for roundings at a border
  * between two ids, which here are those of the weights alone).
  * logits_dev: row r (fp32) starts at logits_dev + r * ld, ld >= vocab; u_dev:
- * fp32 [rows] in [0, 1) (below: as 0, 1 and above: the last kept id).  rows in 1..65535, vocab in 1..131072.  Enqueued on
- * `stream`; nothing is allocated.  Errors: INVALID_ARG, CUDA. */
+ * fp32 [rows] in [0, 1) (below: as 0, 1 and above: the last kept id).  rows in
+ * 1..65535, vocab in 1..131072.  Enqueued on `stream`; nothing is allocated.
+ * Errors: INVALID_ARG, CUDA. */
 memspec_status memspec_op_sample_filtered(const float* logits_dev, int64_t ld, int32_t rows, int32_t vocab,
                                           const memspec_filter* filter, const float* u_dev,
                                           int32_t* out_dev, void* stream);
@@ -176,14 +177,17 @@ memspec_status memspec_op_lora_scratch_bytes(int32_t rows, int32_t n_out, int32_
  * row r (ids_dev: int32 [rows]; an id outside 0..n_adapters-1: no adapter,
  * y[r] = base[r]).  base_dev is typically what memspec_op_linear or
  * memspec_op_linear_int4 gave for the same x, or NULL for 0; it may be y_dev
- * (then ld_base == ldy), otherwise the two must not overlap.
- * x bf16, base and y fp32; rows at strides ldx, ld_base, ldy (elements, at least
- * a row; ldx a multiple of 8; of a single row they are not read).  rows in 1..256, k a positive multiple of 8, n_out
- * and k at most 2^24; x, A, B and scratch 16-byte aligned.  Products are of
- * bf16 values, sums fp32; A x enters the second product with all its 24 bits.
+ * (then ld_base == ldy), otherwise the two must not overlap; y and scratch
+ * overlap nothing else.  x bf16, base and y fp32; rows at strides ldx, ld_base,
+ * ldy (elements, at least a row and at most 2^40; ldx a multiple of 8; of a
+ * single row they are not read).  rows in 1..256, k a positive multiple of 8,
+ * n_adapters, n_out and k at most 2^24; x, A, B and scratch 16-byte aligned.
+ * Products are of bf16 values, sums fp32; A x enters the second product with
+ * all its 24 bits.
  * Deterministic.  A row of x or an adapter with an infinity or a NaN among the
  * values that are used makes its own rows of y unspecified, no others.
- * scratch_dev: memspec_op_lora_scratch_bytes bytes of any content; calls that may overlap need scratches of their own.
+ * scratch_dev: memspec_op_lora_scratch_bytes bytes of any content; calls that
+ * may overlap need scratches of their own.
  * Errors: INVALID_ARG, CUDA. */
 memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x_dev, int64_t ldx,
                                const int32_t* ids_dev, const float* base_dev, int64_t ld_base,

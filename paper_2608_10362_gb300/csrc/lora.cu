@@ -763,10 +763,11 @@ memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x, int6
     why = "null pointer";
   } else if (memspec_op_lora_scratch_bytes(rows, n_out, k, adapters->rank, &need) != MEMSPEC_OK) {
     return MEMSPEC_ERR_INVALID_ARG;
-  } else if (adapters->n_adapters < 1 || n_out > (1 << 24) || k > (1 << 24)) {
-    why = "n_adapters must be at least 1, n_out and k at most 2^24";
-  } else if (rows > 1 && (ldx < k || ldx % 8 != 0 || ldy < n_out || (base != nullptr && ld_base < n_out))) {
-    why = "row strides must cover a row, x's a multiple of 8";
+  } else if (adapters->n_adapters < 1 || std::max({adapters->n_adapters, n_out, k}) > (1 << 24)) {
+    why = "n_adapters must be at least 1, n_adapters, n_out and k at most 2^24";
+  } else if (rows > 1 && (ldx < k || ldx % 8 != 0 || ldy < n_out || (base != nullptr && ld_base < n_out) ||
+                          std::max({ldx, ldy, base != nullptr ? ld_base : 0}) > INT64_C(1) << 40)) {
+    why = "row strides must cover a row and be at most 2^40, x's a multiple of 8";
   } else if (rows > 1 && base == y && ld_base != ldy) {
     why = "in place, base and y have one row stride";
   } else if (misaligned(x, 16) || misaligned(adapters->a_dev, 16) || misaligned(adapters->b_dev, 16) ||

@@ -114,7 +114,8 @@ def test_filter_refuses_output_rows_that_do_not_fit(lib):
     dict(rows=257), dict(n=0), dict(n=(1 << 24) + 1), dict(k=12), dict(k=0), dict(rank=0), dict(rank=12),
     dict(rank=136), dict(adapters=0), dict(ldx=56), dict(ldx=68), dict(ldy=31), dict(ld_base=31),
     dict(base=P + 0x1000, ld_base=40), dict(x=P + 8), dict(a=P + 2), dict(b=P + 4), dict(scratch=P + 8),
-    dict(y=P + 2), dict(base=P + 1), dict(ids=P + 1), dict(scales=P + 2), dict(ranks=P + 2), dict(nb=16)])
+    dict(y=P + 2), dict(base=P + 1), dict(ids=P + 1), dict(scales=P + 2), dict(ranks=P + 2), dict(nb=16),
+    dict(adapters=(1 << 24) + 1), dict(adapters=(1 << 31) - 1), dict(ldx=1 << 41), dict(ldy=1 << 41), dict(ld_base=1 << 41)])
 def test_lora_refuses(lib, bad):
     from paper_2608_10362_gb300 import _lib
     v = {**dict(a=P, b=P, x=P, ids=P, y=P + 0x1000, base=P + 0x2000, scratch=P, rows=4, n=32, k=64, rank=8, adapters=2,
