@@ -18,6 +18,9 @@ What it restates, and where it comes from:
   feed-forward, LM head.
 * ``int4`` - the group-wise INT4 weight-only linear layer of the paper's GPTQ
   INT4 targets (Section 4.1): w = (q - z) s per group of inputs, y = x W^T.
+* ``filtering`` - top-k, top-p and min-p by their definitions, the draw from what
+  they keep, and low-rank adapters; pinned against cases worked by hand and the
+  merged weight (tests/test_oracle_filtering.py).
 * ``scheduler`` - MemSpec's draft cache update and runtime loop (Sections
   3.3-3.4, Algorithms 2-3) and the MAB-Async baseline (Sections 2.3, 4.1).
 * ``tree`` - verification of a draft tree in one target pass and the walk that
