@@ -13,16 +13,17 @@
 //      the sums are added warp by warp, then pushed into the CTA of the cluster that owns
 //      the element and added rank by rank: one order, one t.
 //   2. expand: y = base + scale B t.  t enters as three bf16 planes, which hold all its 24
-//      bits.  The columns of four n = 8 tiles are dealt so that a thread's results are
-//      two float4s of a row.  B, the base and the ids are read while the shrink
+//      bits.  The columns of n = 8 tiles are dealt so that a thread's results are float4s of a
+//      row.  B, the base and the ids are read while the shrink
 //      launch still runs (everything before it has completed when this one starts).
 //
 // Measured (us in a graph, inputs from memory; floor: every operand moved once at 6780 GB/s):
 // 1 row, 4096 x 4096, rank 16: 4.9 (floor 0.04; a call is 14, the host's); 16 rows of 16
 // adapters: 6.0 (0.54); 144 rows of 16 adapters, n 28672, k 4096, ranks up to 64: 26.7 (9.95;
 // 20.6 with the operands in L2): 5 to 7 us until t is there, then the expand loop at 6 to
-// 7 TB/s; 256 rows of one adapter, n 4096, k 14336, rank 128: 21.4 (3.0), 14 of them the
-// shrink's, whose 16 groups of 32 ranks and rows read 58 MB through L2; 21 rows, n 32003: 11.7
+// 7 TB/s; 256 rows of one adapter, n 4096, k 14336, rank 128: 18.4 (3.0), two to
+// find the chunk, five for 58 MB through L2 in groups of 32 ranks and rows, two for the sums'
+// exchange, four to five in the expansion, the rest launches; 21 rows, n 32003: 11.7
 // (1.95), a base and a y without alignment moved 4 bytes at a time.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -238,7 +239,8 @@ __device__ __forceinline__ void share_sums(const float (&acc)[MT][NT][4], int ti
 }
 
 // t[row][j] for a chunk of up to 16 MT rows and 8 NT of the adapter's ranks.  Grid (cluster
-// of kSplits over k, chunks, groups of 8 NT ranks).
+// of kSplits over k, groups of 8 NT ranks, chunks): CTAs past the last chunk, which the host does
+// not know, come last.
 template <int MT, int NT>
 struct ShrinkSmem {
   static constexpr int kFrags = MT * NT * 32;   // a lane's four sums of a 16 x 8 tile
@@ -252,14 +254,14 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_consta
   extern __shared__ __align__(16) uint8_t raw[];
   typedef ShrinkSmem<MT, NT> S;
   S& sm = *reinterpret_cast<S*>(raw);
-  const int tid = threadIdx.x, split = blockIdx.x, j0 = blockIdx.z * NT * 8;
+  const int tid = threadIdx.x, split = blockIdx.x, j0 = blockIdx.y * NT * 8;
   cluster_arrive_release();   // waited for before the first push into a peer
   pdl_wait();
   pdl_launch_dependents();
   // the CTAs of a cluster have one chunk and one rank group: they leave together
   RowPlace place;
-  const bool found = static_cast<int>(blockIdx.y) < find_chunks(a, sm.chunk, place);
-  if (found) select_chunk(a, place, blockIdx.y, sm.chunk);
+  const bool found = static_cast<int>(blockIdx.z) < find_chunks(a, sm.chunk, place);
+  if (found) select_chunk(a, place, blockIdx.z, sm.chunk);
   const int rank = found ? sm.chunk.rank : 0;
   if (j0 >= rank) {
     cluster_wait_acquire();
@@ -288,7 +290,6 @@ __global__ void __launch_bounds__(kThreads, 2) shrink_kernel(const __grid_consta
 }
 
 // ------------------------------------------------ y = base + scale B t
-constexpr int kCols = 32;     // of an item: what a warp takes at a time
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -309,6 +310,9 @@ __device__ __forceinline__ void copy16_async(void* dst, const void* src, bool in
 // registers as they were needed left a warp waiting half the time: gate/up of 144 rows 30 us).
 template <int KT>
 struct Ring {
+  // of an item, what a warp takes at a time; 16 leave room for CTAs of the launch before (256
+  // rows, n 4096, k 14336, rank 128: 18.4 us, 21.4 with 32 columns and one CTA per SM)
+  static constexpr int kCols = KT <= 4 ? 32 : 16;
   static constexpr int kPieces = KT * 2;           // of 8 ranks, per column
   static constexpr int kStages = KT <= 2 ? 4 : KT == 4 ? 3 : 2;
   uint4 b[kStages][kCols * kPieces];
@@ -323,6 +327,7 @@ struct Planes {
 // One warp's items lo + w, lo + w + 8, ... below hi of a chunk.
 template <int KT, int MT>
 struct ExpandWarp {
+  static constexpr int kCols = Ring<KT>::kCols, kTiles = kCols / 8, kQuads = kCols / 16;
   static constexpr int kPieces = Ring<KT>::kPieces, kStages = Ring<KT>::kStages;
   const LoraArgs& a;
   Ring<KT>& ring;
@@ -331,7 +336,7 @@ struct ExpandWarp {
   int rank, tiles, lo, mine;
   float scale;
   const bf16* bp;
-  float4 base[2][2];
+  float4 base[2][kQuads];
   float first[4];             // rows that no 16-byte access fits: the base of a tile's first four
 
   template <int CH>
@@ -354,7 +359,7 @@ struct ExpandWarp {
   __device__ void load_b(int item) {
     const int c0 = column(item), lane = threadIdx.x & 31, piece = lane % kPieces;
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
+    for (int i = 0; i < kCols * kPieces / 32; ++i) {
       const int col = lane / kPieces + i * (32 / kPieces);
       const bool in = c0 + col < a.n && piece * 8 < rank;
       copy16_async(&ring.b[item % kStages][col * kPieces + (KT >= 4 ? piece ^ ((col & 1) << 2) : piece)],
@@ -368,7 +373,7 @@ struct ExpandWarp {
       for (int h = 0; h < 2; ++h) {
         const int r = row[m * 16 + h * 8 + g];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < kQuads; ++q) {
           const int x = c0 + 16 * q + 4 * t;
           base[h][q] = r >= 0 && x < a.n && a.base != nullptr
                            ? __ldcg(reinterpret_cast<const float4*>(a.base + r * a.ld_base + x))
@@ -379,7 +384,7 @@ struct ExpandWarp {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int r = row[m * 16 + q];
-        first[q] = r >= 0 && a.base != nullptr && c0 + lane < a.n ? __ldcg(a.base + r * a.ld_base + c0 + lane) : 0.f;
+        first[q] = r >= 0 && a.base != nullptr && lane < kCols && c0 + lane < a.n ? __ldcg(a.base + r * a.ld_base + c0 + lane) : 0.f;
       }
     }
   }
@@ -405,13 +410,13 @@ struct ExpandWarp {
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       __syncwarp();
       for (int m = 0; m < tiles; ++m) {
-        float acc[4][4] = {};
+        float acc[kTiles][4] = {};
 #pragma unroll
         for (int s2 = 0; s2 < (KT + 1) / 2; ++s2) {
           if (2 * s2 >= n_steps) break;
-          uint4 bv[4];
+          uint4 bv[kTiles];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < kTiles; ++j) {
             const int col = bcol + 16 * (j >> 1) + 2 * (j & 1);
             const uint4* p = &ring.b[i % kStages][col * kPieces];
             if (KT == 1) {
@@ -435,7 +440,7 @@ struct ExpandWarp {
               const uint4 f = planes.v[m][2 * s2 + o][p][lane];
               const uint32_t fa[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-              for (int j = 0; j < 4; ++j) mma(acc[j], fa, o ? bv[j].z : bv[j].x, o ? bv[j].w : bv[j].y);
+              for (int j = 0; j < kTiles; ++j) mma(acc[j], fa, o ? bv[j].z : bv[j].x, o ? bv[j].w : bv[j].y);
             }
           }
         }
@@ -452,13 +457,13 @@ struct ExpandWarp {
       __syncwarp();   // the stage is read before it is filled again
     }
   }
-  __device__ void store(int m, int c0, const float (&acc)[4][4]) {
+  __device__ void store(int m, int c0, const float (&acc)[kTiles][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int r = row[m * 16 + h * 8 + g];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      for (int q = 0; q < kQuads; ++q) {
         const int x = c0 + 16 * q + 4 * t;
         if (r < 0 || x >= a.n) continue;
         float4 o = base[h][q];
@@ -473,18 +478,18 @@ struct ExpandWarp {
     }
   }
   // Through shared memory: a lane per column, 128 bytes of a row at once.
-  __device__ void store_turned(int m, int c0, const float (&acc)[4][4]) {
+  __device__ void store_turned(int m, int c0, const float (&acc)[kTiles][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     __syncwarp();
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int q = 0; q < 2; ++q)
+      for (int q = 0; q < kQuads; ++q)
         turn[h * 8 + g][4 * q + t] =
             make_float4(acc[2 * q][2 * h], acc[2 * q][2 * h + 1], acc[2 * q + 1][2 * h], acc[2 * q + 1][2 * h + 1]);
     __syncwarp();
     const int x = c0 + lane;
-    if (x >= a.n) return;
+    if (lane >= kCols || x >= a.n) return;
     for (int i4 = 0; i4 < 16; i4 += 4) {
       float o[4];
       int r[4];
@@ -515,11 +520,11 @@ struct ExpandSmem {
   Chunks<kExpandTiles * 16> chunk;
   Turn turn[kWarps];          // not there where rows are 16-byte aligned
   static constexpr size_t bytes(bool vec) { return vec ? sizeof(ExpandSmem) - sizeof(turn) : sizeof(ExpandSmem); }
-  static constexpr int per_sm(bool vec) { return KT <= 4 && 2 * (bytes(vec) + 1024) <= 228 * 1024 ? 2 : 1; }
+  static constexpr int per_sm(bool vec) { return 2 * (bytes(vec) + 1024) <= 228 * 1024 ? 2 : 1; }
 };
 
 template <int KT>
-__global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const __grid_constant__ LoraArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_constant__ LoraArgs a) {
   typedef ExpandSmem<KT> S;
   extern __shared__ __align__(16) uint8_t raw[];
   S& sm = *reinterpret_cast<S*>(raw);
@@ -528,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, KT <= 4 ? 2 : 1) expand_kernel(const
   // it start only after its own wait, so all that came earlier has completed
   RowPlace place;
   const int chunks = find_chunks(a, sm.chunk, place);
-  const int cols = (a.n + kCols - 1) / kCols;
+  const int cols = (a.n + Ring<KT>::kCols - 1) / Ring<KT>::kCols;
   const long long items = static_cast<long long>(chunks) * cols;
   long long at = items * blockIdx.x / gridDim.x;
   const long long end = items * (blockIdx.x + 1) / gridDim.x;
@@ -610,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, KT == 1 ? 2 : 1) fused_kernel(const 
     return;
   }
   select_chunk(a, place, blockIdx.y, sm.chunk);
-  const int cols = (a.n + kCols - 1) / kCols, part = blockIdx.z * kSplits + split, parts = gridDim.z * kSplits;
+  const int cols = (a.n + Ring<KT>::kCols - 1) / Ring<KT>::kCols, part = blockIdx.z * kSplits + split, parts = gridDim.z * kSplits;
   ExpandWarp<KT, 1> e(a, sm.ring[w], sm.turn[w], sm.chunk, static_cast<int>(static_cast<long long>(cols) * part / parts),
                       static_cast<int>(static_cast<long long>(cols) * (part + 1) / parts));
   e.start();
@@ -664,7 +669,7 @@ template <int MT, int NT>
 cudaError_t launch_shrink(const LoraArgs& a, cudaLaunchConfig_t cfg) {
   static_assert(sizeof(ShrinkSmem<MT, NT>) <= 113 * 1024, "shared memory for two CTAs per SM");
   static std::atomic<bool> set[64];
-  cfg.gridDim = dim3(kSplits, std::min(a.rows, a.n_adapters + 1 + a.rows / (MT * 16)), (a.rank + NT * 8 - 1) / (NT * 8));
+  cfg.gridDim = dim3(kSplits, (a.rank + NT * 8 - 1) / (NT * 8), std::min(a.rows, a.n_adapters + 1 + a.rows / (MT * 16)));
   cfg.dynamicSmemBytes = sizeof(ShrinkSmem<MT, NT>);
   if (const cudaError_t e = allow_smem(shrink_kernel<MT, NT>, cfg.dynamicSmemBytes, set); e != cudaSuccess) return e;
   return cudaLaunchKernelEx(&cfg, shrink_kernel<MT, NT>, a);
@@ -673,10 +678,10 @@ cudaError_t launch_shrink(const LoraArgs& a, cudaLaunchConfig_t cfg) {
 template <int KT>
 cudaError_t launch_expand(const LoraArgs& a, cudaLaunchConfig_t cfg) {
   typedef ExpandSmem<KT> S;
-  static_assert(sizeof(S) <= 227 * 1024 && S::per_sm(true) == (KT <= 4 ? 2 : 1), "shared memory");
+  static_assert(sizeof(S) <= 227 * 1024 && S::per_sm(true) == 2, "shared memory");
   static std::atomic<bool> set[64];
   // one item per warp, or as many CTAs as are resident at once
-  const long long items = static_cast<long long>((a.n + kCols - 1) / kCols) *
+  const long long items = static_cast<long long>((a.n + Ring<KT>::kCols - 1) / Ring<KT>::kCols) *
                           std::min(a.rows, a.n_adapters + 1 + a.rows / (kExpandTiles * 16));
   cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>((items + kWarps - 1) / kWarps, 152 * S::per_sm(a.vec))));
   cfg.dynamicSmemBytes = S::bytes(a.vec);
@@ -684,14 +689,15 @@ cudaError_t launch_expand(const LoraArgs& a, cudaLaunchConfig_t cfg) {
   return cudaLaunchKernelEx(&cfg, expand_kernel<KT>, a);
 }
 
+// At most so many chunks of 16 rows, and parts of at most 4096 columns (512 a CTA).
+int fused_chunks(const LoraArgs& a) { return std::min(a.rows, a.n_adapters + 1 + a.rows / 16); }
+int fused_parts(const LoraArgs& a) { return (a.n + 4095) / 4096; }
+
 template <int KT>
 cudaError_t launch_fused(const LoraArgs& a, cudaLaunchConfig_t cfg) {
   static_assert(sizeof(FusedSmem<KT>) <= 227 * 1024, "shared memory");
   static std::atomic<bool> set[64];
-  const int chunks = std::min(a.rows, a.n_adapters + 1 + a.rows / 16);
-  // parts of at most 4096 columns (512 a CTA), while the launch is a few CTAs per SM
-  const int parts = std::min((a.n + 4095) / 4096, std::max(1, 76 / chunks));
-  cfg.gridDim = dim3(kSplits, chunks, parts);
+  cfg.gridDim = dim3(kSplits, fused_chunks(a), fused_parts(a));
   cfg.dynamicSmemBytes = sizeof(FusedSmem<KT>);
   if (const cudaError_t e = allow_smem(fused_kernel<KT>, cfg.dynamicSmemBytes, set); e != cudaSuccess) return e;
   return cudaLaunchKernelEx(&cfg, fused_kernel<KT>, a);
@@ -710,13 +716,13 @@ cudaError_t launch_lora(const LoraArgs& a, cudaStream_t s) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  // One launch where the GPU's part is so short that a call's time is the host's: 2 to 2.5 us
-  // less there (16.9 -> 14.6 us at 1 x 4096 x 4096, 17.2 -> 14.9 at 16 rows with an adapter each;
-  // on the GPU 4.4 -> 4.9 and 6.4 -> 6.0).  Over longer rows of many adapters, or with more
-  // of A per CTA, two launches spread better: 16 x 28672 with 16 adapters 10.6 us (one launch 15.2),
-  // 21 x 32003 11.8 (25.4), 32 rows of 8 adapters of rank 64 at n = 28672 12.7 (33.9).
-  const int chunks = std::min(a.rows, a.n_adapters + 1 + a.rows / 16);
-  if (a.rank <= 32 && static_cast<long long>(chunks) * a.n <= 1 << 16 && static_cast<long long>(a.k) * a.rank <= 1 << 18)
+  // One launch while its clusters fit at once, two CTAs per SM up to rank 16 and one up to 32: a
+  // call is 2 to 2.5 us shorter on the host (16.9 -> 14.6 us at 1 x 4096 x 4096), and mostly on the
+  // GPU (64 rows, n 1024: 4.4 us, two launches 6.1; 144 rows of 16 adapters, n 4096, rank 16: 7.4,
+  // 8.1; 64 rows, k 14336, rank 32: 7.2, 9.1; but 1 x 4096 x 4096 4.9, 4.4).  In two waves it is
+  // the longer one: 256 rows, n 11008, rank 16 15.8 us (11.5), 16 rows of 16 adapters, n 1024,
+  // rank 32 8.3 (5.8).
+  if (a.rank <= 32 && fused_chunks(a) * fused_parts(a) <= (a.rank <= 16 ? 34 : 14))
     return a.rank <= 16 ? launch_fused<1>(a, cfg) : launch_fused<2>(a, cfg);
   // 16 rows and ranks a CTA where there are few rows, for more CTAs: 16 rows, k 14336, rank 128
   // 7.1 us (with 32 by 32 7.9), 32 rows of one adapter of rank 64 6.4 (6.8); beyond, 32 by 32

@@ -317,7 +317,9 @@ LORA = [(1, 64, 64, 8, 1, "one"), (1, 1, 8, 8, 1, "one"), (3, 33, 72, 16, 2, "ea
         (16, 1000, 4096, 16, 16, "each"), (17, 513, 520, 24, 4, "one"), (21, 3001, 2048, 40, 8, "random"),
         (64, 256, 1032, 64, 5, "random"), (144, 1536, 768, 64, 16, "each"), (255, 130, 264, 128, 3, "random"),
         (256, 768, 2304, 128, 2, "one"), (256, 95, 64, 8, 256, "each"), (12, 640, 640, 48, 4, "none"),
-        (2, 8192, 14336, 128, 2, "each"), (33, 100, 40, 56, 40, "random")]
+        (2, 8192, 14336, 128, 2, "each"), (33, 100, 40, 56, 40, "random"), (30, 9001, 136, 16, 3, "random"),
+        (200, 700, 512, 32, 1, "one"), (256, 4096, 256, 8, 16, "each"), (256, 4100, 64, 16, 1, "one"),
+        (150, 40, 2048, 32, 2, "random"), (7, 16400, 3000, 24, 2, "each")]
 
 
 @pytest.mark.parametrize("with_ranks", [True, False])
