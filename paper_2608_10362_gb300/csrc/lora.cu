@@ -23,7 +23,7 @@
 // 20.6 with the operands in L2): 5 to 7 us until t is there, then the expand loop at 6 to
 // 7 TB/s; 256 rows of one adapter, n 4096, k 14336, rank 128: 18.4 (3.0), two to
 // find the chunk, five for 58 MB through L2 in groups of 32 ranks and rows, two for the sums'
-// exchange, four to five in the expansion, the rest launches; 21 rows, n 32003: 11.7
+// exchange, four to five in the expansion, the rest launches; 21 rows, n 32003: 10.8
 // (1.95), a base and a y without alignment moved 4 bytes at a time.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -328,6 +328,7 @@ struct Planes {
 template <int KT, int MT>
 struct ExpandWarp {
   static constexpr int kCols = Ring<KT>::kCols, kTiles = kCols / 8, kQuads = kCols / 16;
+  static constexpr int kRows = kCols / 2;   // of a tile, that a lane has where rows fit no 16-byte access
   static constexpr int kPieces = Ring<KT>::kPieces, kStages = Ring<KT>::kStages;
   const LoraArgs& a;
   Ring<KT>& ring;
@@ -336,8 +337,9 @@ struct ExpandWarp {
   int rank, tiles, lo, mine;
   float scale;
   const bf16* bp;
-  float4 base[2][kQuads];
-  float first[4];             // rows that no 16-byte access fits: the base of a tile's first four
+  // of what is stored next: rows g, g + 8 of kQuads float4s, or a column of kRows rows (loaded as they
+  // were stored, four rows at a time, 81 us for 40 at 144 x 32003)
+  float base[kRows];
 
   template <int CH>
   __device__ ExpandWarp(const LoraArgs& args, Ring<KT>& r, Turn& t, const Chunks<CH>& c, int from, int to)
@@ -375,16 +377,22 @@ struct ExpandWarp {
 #pragma unroll
         for (int q = 0; q < kQuads; ++q) {
           const int x = c0 + 16 * q + 4 * t;
-          base[h][q] = r >= 0 && x < a.n && a.base != nullptr
-                           ? __ldcg(reinterpret_cast<const float4*>(a.base + r * a.ld_base + x))
-                           : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 v = r >= 0 && x < a.n && a.base != nullptr
+                               ? __ldcg(reinterpret_cast<const float4*>(a.base + r * a.ld_base + x))
+                               : make_float4(0.f, 0.f, 0.f, 0.f);
+          float* const b = base + (h * kQuads + q) * 4;
+          b[0] = v.x;
+          b[1] = v.y;
+          b[2] = v.z;
+          b[3] = v.w;
         }
       }
     } else {
+      const int x = c0 + lane % kCols;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int r = row[m * 16 + q];
-        first[q] = r >= 0 && a.base != nullptr && lane < kCols && c0 + lane < a.n ? __ldcg(a.base + r * a.ld_base + c0 + lane) : 0.f;
+      for (int i = 0; i < kRows; ++i) {
+        const int r = row[m * 16 + lane / kCols * kRows + i];
+        base[i] = r >= 0 && a.base != nullptr && x < a.n ? __ldcg(a.base + r * a.ld_base + x) : 0.f;
       }
     }
   }
@@ -466,7 +474,8 @@ struct ExpandWarp {
       for (int q = 0; q < kQuads; ++q) {
         const int x = c0 + 16 * q + 4 * t;
         if (r < 0 || x >= a.n) continue;
-        float4 o = base[h][q];
+        const float* const b = base + (h * kQuads + q) * 4;
+        float4 o = make_float4(b[0], b[1], b[2], b[3]);
         if (rank > 0) {   // else the base's own bits
           o.x = fmaf(scale, acc[2 * q][2 * h], o.x);
           o.y = fmaf(scale, acc[2 * q][2 * h + 1], o.y);
@@ -477,7 +486,7 @@ struct ExpandWarp {
       }
     }
   }
-  // Through shared memory: a lane per column, 128 bytes of a row at once.
+  // Through shared memory: a lane per column, 128 bytes of a row at once or 64 of two.
   __device__ void store_turned(int m, int c0, const float (&acc)[kTiles][4]) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     __syncwarp();
@@ -488,30 +497,24 @@ struct ExpandWarp {
         turn[h * 8 + g][4 * q + t] =
             make_float4(acc[2 * q][2 * h], acc[2 * q][2 * h + 1], acc[2 * q + 1][2 * h], acc[2 * q + 1][2 * h + 1]);
     __syncwarp();
-    const int x = c0 + lane;
-    if (lane >= kCols || x >= a.n) return;
-    for (int i4 = 0; i4 < 16; i4 += 4) {
-      float o[4];
-      int r[4];
+    const int x = c0 + lane % kCols, i0 = lane / kCols * kRows;
+    if (x >= a.n) return;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        r[q] = row[m * 16 + i4 + q];
-        o[q] = i4 == 0 ? first[q] : r[q] >= 0 && a.base != nullptr ? __ldcg(a.base + r[q] * a.ld_base + x) : 0.f;
-      }
-      if (r[0] < 0) break;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (r[q] < 0) continue;
-        if (rank > 0) o[q] = fmaf(scale, reinterpret_cast<const float*>(&turn[i4 + q][0])[lane], o[q]);
-        a.y[r[q] * a.ldy + x] = o[q];
-      }
+    for (int i = 0; i < kRows; ++i) {
+      const int r = row[m * 16 + i0 + i];
+      if (r < 0) break;
+      float o = base[i];
+      if (rank > 0) o = fmaf(scale, reinterpret_cast<const float*>(&turn[i0 + i][0])[lane % kCols], o);
+      a.y[r * a.ldy + x] = o;
     }
   }
 };
 
-// The second of two launches.  Work is (chunk of up to 32 rows, item) pairs in that order, cut
-// evenly over as many CTAs as are resident at once (cut by their bytes instead: no faster, and
-// a microsecond more to find a CTA's part).
+// The second of two launches, as many CTAs as are resident at once.  Each has a part of one
+// chunk's (up to 32 rows') items; where there are more chunks than CTAs, an even part of all
+// (chunk, item) pairs in that order.  (Such parts for all calls: the CTAs with the end of one
+// chunk and the start of the next finish last, 11.5 us for 10.8 at 21 x 32003.  Cut by their
+// bytes: no faster, and a microsecond more to find a CTA's part.)
 constexpr int kExpandTiles = 2;
 template <int KT>
 struct ExpandSmem {
@@ -535,8 +538,17 @@ __global__ void __launch_bounds__(kThreads, 2) expand_kernel(const __grid_consta
   const int chunks = find_chunks(a, sm.chunk, place);
   const int cols = (a.n + Ring<KT>::kCols - 1) / Ring<KT>::kCols;
   const long long items = static_cast<long long>(chunks) * cols;
-  long long at = items * blockIdx.x / gridDim.x;
-  const long long end = items * (blockIdx.x + 1) / gridDim.x;
+  const int ctas = gridDim.x, cta = blockIdx.x;
+  long long at, end;
+  if (chunks <= ctas) {       // CTAs [c ctas / chunks, (c + 1) ctas / chunks), rounded up, for chunk c
+    const int c = cta * chunks / ctas, first = (c * ctas + chunks - 1) / chunks;
+    const int of = ((c + 1) * ctas + chunks - 1) / chunks - first, part = cta - first;
+    at = static_cast<long long>(c) * cols + static_cast<long long>(cols) * part / of;
+    end = static_cast<long long>(c) * cols + static_cast<long long>(cols) * (part + 1) / of;
+  } else {
+    at = items * cta / ctas;
+    end = items * (cta + 1) / ctas;
+  }
   bool waited = false;
   while (at < end) {
     const int c = static_cast<int>(at / cols);
