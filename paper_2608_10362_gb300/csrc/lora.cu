@@ -100,8 +100,6 @@ __device__ int find_chunks(const LoraArgs& a, Chunks<CH>& s, RowPlace& p) {
     p.id = __ldcg(a.ids + tid);
     if (p.id < 0 || p.id >= a.n_adapters) p.id = -1;
   }
-  p.rank = p.id < 0 ? 0 : a.ranks == nullptr ? a.rank : __ldcg(a.ranks + p.id);
-  p.scale = p.id < 0 || a.scales == nullptr ? 1.f : __ldcg(a.scales + p.id);
   p.pos = 0;
   if (w * 32 < a.rows) {
     const unsigned same = __match_any_sync(0xffffffffu, p.id);
@@ -119,6 +117,10 @@ __device__ int find_chunks(const LoraArgs& a, Chunks<CH>& s, RowPlace& p) {
         p.pos += q.x == p.id ? q.y : 0;
       }
     leads = tid < a.rows && p.pos % CH == 0;
+  }
+  if (leads) {
+    p.rank = p.id < 0 ? 0 : a.ranks == nullptr ? a.rank : __ldcg(a.ranks + p.id);
+    p.scale = p.id < 0 || a.scales == nullptr ? 1.f : __ldcg(a.scales + p.id);
   }
   const unsigned mask = __ballot_sync(0xffffffffu, leads);
   if (lane == 0) s.leaders[w] = __popc(mask);
@@ -179,7 +181,7 @@ __device__ __forceinline__ void shrink_sums(const LoraArgs& a, const int* row, i
   const int blocks = (a.k + 31) / 32;         // of 32 columns
   const int end = static_cast<int>(static_cast<long long>(split + 1) * blocks / kSplits);
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  constexpr int kAhead = MT * 2 + NT <= 4 ? 4 : 2;    // blocks loaded together
+  constexpr int kAhead = MT * 2 + NT <= 4 ? 4 : MT * 2 + NT <= 8 ? 2 : 1;   // blocks loaded together
   for (int b0 = static_cast<int>(static_cast<long long>(split) * blocks / kSplits) + w; b0 < end;
        b0 += kWarps * kAhead) {
     uint4 xv[kAhead][MT][2], av[kAhead][NT];
@@ -736,11 +738,20 @@ cudaError_t launch_lora(const LoraArgs& a, cudaStream_t s) {
   // rank 32 8.3 (5.8).
   if (a.rank <= 32 && fused_chunks(a) * fused_parts(a) <= (a.rank <= 16 ? 34 : 14))
     return a.rank <= 16 ? launch_fused<1>(a, cfg) : launch_fused<2>(a, cfg);
-  // 16 rows and ranks a CTA where there are few rows, for more CTAs: 16 rows, k 14336, rank 128
-  // 7.1 us (with 32 by 32 7.9), 32 rows of one adapter of rank 64 6.4 (6.8); beyond, 32 by 32
-  // reads A and x less often: 144 rows of 16 adapters 10.2 us (16 by 16 14.3), 256 rows of one
-  // of rank 128 21.5 (33.6)
-  const cudaError_t e = a.rows <= 32 ? launch_shrink<1, 2>(a, cfg) : launch_shrink<2, 4>(a, cfg);
+  // The first product's tile: as small as fits the chip in one wave of clusters, 34 of two CTAs
+  // per SM, or nearly.  Up to 32 rows 16 by 16 ranks (16 rows, k 14336, rank 128 6.4 us, by 32 7.4, by
+  // 64 8.8), then by 32 (16 rows of 16 adapters of rank 64 8.4; 10.7, 9.7), then by 64; more rows 32
+  // by 32 (256 rows of one adapter, rank 64 10.3, 16 by 64 11.3; 144 rows, n 28672 26.3, 29.0) and
+  // with many adapters 16 by 64 (256 rows of 32, rank 128 25.7, 32 by 32 31.9; 64 rows of 64, rank 64
+  // 27.0, 31.8).
+  auto clusters = [&](int rows, int ranks) {
+    return std::min(a.rows, a.n_adapters + 1 + a.rows / rows) * ((a.rank + ranks - 1) / ranks);
+  };
+  const cudaError_t e = a.rows <= 32 ? (clusters(16, 16) <= 34   ? launch_shrink<1, 2>(a, cfg)
+                                        : clusters(16, 32) <= 64 ? launch_shrink<1, 4>(a, cfg)
+                                                                 : launch_shrink<1, 8>(a, cfg))
+                        : clusters(32, 32) <= 52 ? launch_shrink<2, 4>(a, cfg)
+                                                 : launch_shrink<1, 8>(a, cfg);
   if (e != cudaSuccess) return e;
   cfg.numAttrs = 1;
   return a.rank <= 16   ? launch_expand<1>(a, cfg)

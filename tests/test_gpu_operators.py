@@ -319,6 +319,7 @@ LORA = [(1, 64, 64, 8, 1, "one"), (1, 1, 8, 8, 1, "one"), (3, 33, 72, 16, 2, "ea
         (256, 768, 2304, 128, 2, "one"), (256, 95, 64, 8, 256, "each"), (12, 640, 640, 48, 4, "none"),
         (2, 8192, 14336, 128, 2, "each"), (33, 100, 40, 56, 40, "random"), (30, 9001, 136, 16, 3, "random"),
         (200, 700, 512, 32, 1, "one"), (256, 4096, 256, 8, 16, "each"), (256, 4100, 64, 16, 1, "one"),
+        (20, 90, 640, 64, 20, "each"), (40, 200, 320, 72, 30, "random"), (32, 64, 2000, 120, 32, "each"),
         (150, 40, 2048, 32, 2, "random"), (7, 16400, 3000, 24, 2, "each")]
 
 
