@@ -19,6 +19,8 @@
 //      formed roughly, by one ex2 each.  If the candidates hold p of the sum they are all
 //      that is looked at (end_of); if they hold most of it, the ids a few octaves below them
 //      are queued and searched alone (search_above);
+//      Draws under larger k: the ids above the bound, or a little below it, are queued the
+//      same way and searched by count, then by weights;
 //   4. else a search per part (top-k, then top-p among what top-k left): a histogram of the
 //      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
 //      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
@@ -74,6 +76,7 @@ constexpr uint32_t kList = 256;              // list entries of a CTA and of the
 constexpr int kQueue = 4 * kList;            // places in the slice, in the list's memory
 constexpr int kGroups = 64;                  // groups of threads whose maxima give the bound
 constexpr int kMostAbove = 56;               // of them above it at most
+constexpr int kMostBelow = 200;              // of logits of a CTA an octave below the bound
 constexpr int kTopPAbove = 96;               // logits above the bound for top-p alone (144 rows of 32000:
                                              // 31 us; with 112 the queues overflow, 50; with 80 at p =
                                              // 0.95 43 against 39)
@@ -752,15 +755,17 @@ __device__ __forceinline__ float rough_exp2(float x) {
   return y;
 }
 
-// What a prefix by weights has to reach, `fraction` of a sum known to within `error`.
+// What a prefix has to reach: a count, or `fraction` of a sum known to within `error`.
 struct Need {
   u64 fraction, least, most;
+  __device__ __forceinline__ explicit Need(u64 count) : fraction(0), least(count), most(count) {}
   __device__ __forceinline__ Need(u64 f, u64 sum, u64 error)
       : fraction(f), least(part_of(f, sum - error)), most(part_of(f, sum + error)) {}
 };
 // The entry where the prefix ends, among sorted ones e of weight `own` behind a sum of
 // `before`, which the threads of the first CTA hold (alone) or of every one; then every list
-// has been read.  Within the error of a border all CTAs sum their slices exactly.
+// has been read.  Within the error of a border (of a row where every id takes part) all CTAs
+// sum their slices exactly.
 template <int NT>
 __device__ __forceinline__ u64 end_of(const Need& need, u64 before, u64 own, u64 e, bool alone, const Slice& s,
                                       const WeightScale& ws, int C, int rank, Smem& sm) {
@@ -775,7 +780,7 @@ __device__ __forceinline__ u64 end_of(const Need& need, u64 before, u64 own, u64
   }
   cluster_sync();
   u64 cut = sm.cut;
-  if (cut == 0) {
+  if (cut == 0 && need.least < need.most) {
     u64 sums[1] = {0};
     for_quads<NT>(s, -kLargest, [&](const float (&z)[4], int) {
       int n[4];
@@ -796,13 +801,16 @@ __device__ __forceinline__ u64 end_of(const Need& need, u64 before, u64 own, u64
   }
   return cut;
 }
-// The same of a row whose ids below z_min weigh `deep` together, within `error`, and are not
-// the cut: the others, which have to be few, are queued and go into the histogram.  No cut
-// (0) where it takes more: more ids, or a bin's division.
-template <int NT>
-__device__ Ended search_above(u64 fraction, u64 deep, u64 error, float z_min, const Slice& s, const WeightScale& ws,
-                              int C, int rank, Smem& sm) {
+// A search (kMass: by weights, need a fraction of their sum; else by count) among the ids from
+// z_min on, which have to be few, up to the entry `within`: they are queued and go into the
+// histogram.  Those below z_min weigh `deep` together, within `error`, and are not the cut.  No
+// cut (0) where it takes more: more ids, or a bin's division.  may_leave: where all that is
+// kept is listed, the first CTA goes on alone.
+template <int NT, bool kMass>
+__device__ Ended search_above(u64 wanted, u64 deep, u64 error, float z_min, u64 within, bool may_leave, const Slice& s,
+                              const WeightScale& ws, int C, int rank, Smem& sm) {
   const int tid = threadIdx.x, lane = tid & 31;
+  __syncthreads();            // sm.cut is read
   if (tid == 0) {
     sm.n_list = sm.n_queue = 0;
     sm.cut = 0;
@@ -819,6 +827,8 @@ __device__ Ended search_above(u64 fraction, u64 deep, u64 error, float z_min, co
       if (in[q] && at.at[q] < kQueue) sm.queue[at.at[q]] = static_cast<uint16_t>(id + q - s.base);
   });
   __syncthreads();
+  // bins of equal width (by weights' places or depth's octaves, 256 ids and more stand in one)
+  const float per = ws.max > z_min ? kBins / (ws.max - z_min) : 0.f;
   constexpr int kQueued = kQueue / NT;
   u64 mine[kQueued], w[kQueued];
   bool in[kQueued];
@@ -831,19 +841,19 @@ __device__ Ended search_above(u64 fraction, u64 deep, u64 error, float z_min, co
     bin[q] = kBins;
     if (!in[q]) continue;
     const int at = sm.queue[i];
-    float f;
-    const int n = weight_place(s.z[at], ws, f);
-    w[q] = weight_at(n, f, sm.table);
-    in[q] = w[q] != 0;
-    if (in[q]) bin[q] = static_cast<int>(static_cast<unsigned>(-n) / kPlacesPerBin);
-    mine[q] = entry_of(logit_key(s.z[at]), static_cast<uint32_t>(s.base + at));
+    const float z = s.z[at];
+    mine[q] = entry_of(logit_key(z), static_cast<uint32_t>(s.base + at));
+    if (kMass) w[q] = weight(z, ws, sm.table);
+    in[q] = mine[q] <= within && (!kMass || w[q] != 0);
+    if (in[q]) bin[q] = min(static_cast<int>((ws.max - z) * per), kBins - 1);
   }
-  add_to_bins<true>(sm, in, bin, w);
-  close_histogram<NT, true>(sm);
+  add_to_bins<kMass>(sm, in, bin, w);
+  close_histogram<NT, kMass>(sm);
   const bool fits = __all_sync(
       0xffffffffu, lane >= C || ld_cluster_u32(mapa_shared(smem_addr(&sm.n_queue), min(lane, C - 1))) <= kQueue);
-  const Found f = find_bin<NT, true>([&](u64 total) { return part_of(fraction, total + deep - error); }, C, sm);
-  const Need need(fraction, f.total + deep, error);
+  const Found f = find_bin<NT, kMass>(
+      [&](u64 total) { return kMass ? part_of(wanted, total + deep - error) : wanted; }, C, sm);
+  const Need need = kMass ? Need(wanted, f.total + deep, error) : Need(wanted);
   if (!fits || need.most > f.above + f.own || f.count > kList) {
     cluster_sync();           // the others have read this CTA's histogram
     return {0, 0, 0, false};
@@ -857,14 +867,15 @@ __device__ Ended search_above(u64 fraction, u64 deep, u64 error, float z_min, co
       if (i < kList) sm.list[i] = mine[q];
     }
   cluster_sync();
+  const bool alone = whole_list && may_leave;
   u64 e = ~0ull, own = 0;
   uint32_t n = 0;
-  if (!whole_list || rank == 0) {
+  if (!alone || rank == 0) {
     n = pull_list<NT>(C, &sm.n_list, e, sm);   // into the histogram's place: nobody reads that any more
-    own = static_cast<uint32_t>(tid) < n ? weight(entry_logit(e), ws, sm.table) : 0;
+    own = static_cast<uint32_t>(tid) >= n ? 0 : kMass ? weight(entry_logit(e), ws, sm.table) : 1;
   }
-  const u64 cut = end_of<NT>(need, whole_list ? 0 : f.above, own, e, whole_list, s, ws, C, rank, sm);
-  return {cut, whole_list ? n : 0, e, whole_list && rank != 0};
+  const u64 cut = end_of<NT>(need, whole_list ? 0 : f.above, own, e, alone, s, ws, C, rank, sm);
+  return {cut, whole_list ? n : 0, e, alone && rank != 0};
 }
 
 // The draw from the entries up to the cut among the n that the threads hold in order.
@@ -1082,7 +1093,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
       // ids that are not deep hold all that is kept
       const u64 deep_error = deep == 0 ? 0 : (deep >> 17) + whole;
       if (rest <= listed && listed + rest - error >= need.most + deep + deep_error) {
-        const Ended e = search_above<NT>(fraction, deep, deep_error, z_deep, s, ws, C, rank, sm);
+        const Ended e = search_above<NT, true>(fraction, deep, deep_error, z_deep, ~0ull, true, s, ws, C, rank, sm);
         if (e.gone) return;
         if (e.cut != 0) {
           cut = min(cut, e.cut);
@@ -1142,6 +1153,30 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     }
   }
   u64 within = no_cut;
+  if constexpr (!kMask) {
+    // Large k: the ids above the bound, or an octave below it where that is not sure to leave
+    // so many (for 200 per CTA it mostly does: 144 x 128256, k 1000, p 0.9 131 -> 84 us; for more
+    // it would be tried in vain, 144 x 32000 37 us for 32); then top-p among what is left of them.
+    if (search_k && owed <= kMostBelow && ws.hi > 0.f) {
+      const float z_low = owed <= kMostAbove ? bound : fmaxf(bound - 1.f / ws.hi, -kLargest);
+      Ended e = search_above<NT, false>(static_cast<u64>(r.top_k), 0, 0, z_low, ~0ull, !by_p, s, ws, C, rank, sm);
+      if (e.gone) return;
+      if (e.cut != 0) {
+        search_k = false;
+        within = e.cut;
+        if (by_p) {
+          e = search_above<NT, true>(fraction, 0, 0, entry_logit(within), within, true, s, ws, C, rank, sm);
+          if (e.gone) return;
+          by_p = e.cut == 0;
+        }
+        cut = min(cut, e.cut != 0 ? e.cut : within);
+        if (e.cut != 0 && e.listed > 0) {
+          draw_from_list<NT>(a, row, e.listed, e.entry, cut, ws, sm);
+          return;
+        }
+      }
+    }
+  }
   if (search_k) {
     within = search<NT, false, true, false>(Part{static_cast<u64>(r.top_k), 0, 0.f, ~0ull}, s, ws, C, rank, sm).cut;
     cut = min(cut, within);

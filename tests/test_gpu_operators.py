@@ -148,20 +148,26 @@ def test_top_p_next_to_a_border(vocab, T, first, step, last):
 @pytest.mark.parametrize("rows,vocab", [(64, 900), (64, 15000), (160, 15000), (48, 32003), (160, 32000), (32, 70000),
                                         (96, 65537), (8, 131072), (64, 128256)])
 def test_draws_are_those_from_the_mask(rows, vocab, kind):
-    """A draw under top-p is the draw without a rule from the logits that the mask keeps: the
+    """A draw under a rule is the draw without one from the logits that the mask keeps: the
     maximum and so every kept weight is the same, and both have to be equal to the last bit.
-    Temperatures that leave one id up to all of them."""
+    Temperatures that leave one id up to all of them, top-k below, at and above what the
+    candidates hold."""
     import torch
     from paper_2608_10362_gb300 import op_filter_logits, op_sample_filtered
     z = torch.from_numpy(_logits(kind, min(rows, 16), vocab, 7)).cuda().repeat(rows // min(rows, 16), 1)
     u = torch.from_numpy(_uniforms(rows, 7)).cuda()
+    rules = []
     for T in (1e-20, 0.02, 0.3, 0.6, 1.0, 1.5, 20.0, 1e20, math.inf):
         for p in (1e-6, 0.1, 0.5, 0.9, 0.95, 0.99, 0.9999):
             for min_p in (0.0, 0.02):
-                rule = dict(temperature=T, top_p=p, min_p=min_p)
-                got = op_sample_filtered(z, u, **rule)
-                want = op_sample_filtered(op_filter_logits(z, **rule), u, temperature=T)
-                assert torch.equal(got, want), (rule, torch.nonzero(got != want)[:5])
+                rules.append(dict(temperature=T, top_p=p, min_p=min_p))
+        for k in (60, 257, 449, 1000, 1600, 5000):
+            for p in (1.0, 0.98, 0.6):
+                rules.append(dict(temperature=T, top_k=k, top_p=p))
+    for rule in rules:
+        got = op_sample_filtered(z, u, **rule)
+        want = op_sample_filtered(op_filter_logits(z, **rule), u, temperature=rule["temperature"])
+        assert torch.equal(got, want), (rule, torch.nonzero(got != want)[:5])
 
 
 def test_rule_arrays_out_of_range_mean_what_the_header_says():
