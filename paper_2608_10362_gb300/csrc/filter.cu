@@ -18,9 +18,8 @@
 //   3. top-p alone, draws: the candidates are listed the same way and the sum of the rest is
 //      formed roughly, by one ex2 each.  If the candidates hold p of the sum they are all
 //      that is looked at (end_of); if they hold most of it, the ids a few octaves below them
-//      are queued and searched alone (search_above);
-//      Draws under larger k: the ids above the bound, or a little below it, are queued the
-//      same way and searched by count, then by weights;
+//      are queued and searched alone (search_above).  Draws under larger k queue the ids
+//      above the bound, or a little below it, and search those by count, then by weights;
 //   4. else a search per part (top-k, then top-p among what top-k left): a histogram of the
 //      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
 //      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
@@ -36,11 +35,11 @@
 // CTA found where it goes on alone.
 //
 // Measured (us, one launch in a graph; 4 V bytes a row at 6780 GB/s are 0.02 to 11):
-//                       no cut  top-k 50  k, p    top-p 0.9  flat, top-p 0.9
-//     1 x  32000           5.6       7.1   7.9         14.6             17.7
-//     1 x 128256           9.7       8.2   8.9         14.9             30.1
-//    16 x 128256          14.2      10.3  11.4         22.3             42.1
-//   144 x 128256          55.6      36.4  37.2         75.0            160.9
+//                       no cut  top-k 50  k, p  k 1000, p 0.9  top-p 0.9  flat, top-p 0.9
+//     1 x  32000           5.6       7.1   7.9          15.7       14.6             17.7
+//     1 x 128256           9.7       8.2   8.9                     14.9             30.1
+//    16 x 128256          14.2      10.3  11.4          25.6       22.3             42.1
+//   144 x 128256          55.6      36.4  37.2          84.4       75.0            160.9
 // One row is bound by latency: load, three to ten barriers of the cluster at 0.7 us each,
 // list and draw.  A batch is bound by the issue rate: 8 instructions an element for the load
 // and the maximum, 45 for an exact weight, 8 for a rough one, three atomics for a bin; three
@@ -1107,7 +1106,11 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     }
   }
   bool search_k = by_k && !empty;
-  if (search_k && owed <= kMostAbove) {
+  // j groups' maxima of 64 stand for 64 log(64 / (64 - j)) logits of the CTA: where those of the
+  // cluster would pass 9/10 of the list, draws go to the queues at once (144 x 128256, k 240: 64 us
+  // for 75)
+  const int most = kMask ? kMostAbove : C == 8 ? 23 : C == 4 ? 37 : C == 2 ? 53 : kMostAbove;
+  if (search_k && owed <= most) {
     for_warp_quads<NT>(s, bound, [&](const float (&x)[4], int id) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
