@@ -485,7 +485,7 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
     sm.cut = p.within;
   }
   clear_histogram<NT>(sm);
-  constexpr bool kCandidates = kMass && kWhole && !kAlone;   // else they were tried before
+  constexpr bool kCandidates = kMass && kWhole && !kAlone;   // draws (kAlone) have tried them before
   u64 sum = 0, listed_sum = 0;
   for_quads<NT>(s, z_in, [&](const float (&z)[4], int id) {
     bool in[4];
@@ -542,10 +542,6 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
           __reduce_add_sync(0xffffffffu, peer ? ld_cluster_u32(mapa_shared(smem_addr(&sm.n_candidates), lane)) : 0u);
       const u64 listed = warp_sum(peer ? ld_cluster_u64(mapa_shared(smem_addr(&sm.listed_sum), lane)) : 0);
       if (n <= kList && listed >= need) {   // what is kept is among the candidates
-        if (kAlone && rank != 0) {
-          cluster_sync();
-          return {0, 0, 0, true};
-        }
         u64 e, all;
         pull_list<NT>(C, &sm.n_candidates, e, sm);
         cluster_sync();       // the others have read this CTA's list and sums
