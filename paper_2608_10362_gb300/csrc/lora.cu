@@ -21,7 +21,7 @@
 // 1 row, 4096 x 4096, rank 16: 4.9 (floor 0.04; a call is 14, the host's); 16 rows of 16
 // adapters: 6.0 (0.54); 144 rows of 16 adapters, n 28672, k 4096, ranks up to 64: 26.7 (9.95;
 // 20.6 with the operands in L2): 8 us until t is there, then 18 for 77 MB, the first CTAs done
-// after 9 (adapters' ranks differ); 256 rows of one adapter, n 4096, k 14336, rank 128: 18.4 (3.0), two to
+// after 9; 256 rows of one adapter, n 4096, k 14336, rank 128: 18.4 (3.0), two to
 // find the chunk, five for 58 MB through L2 in groups of 32 ranks and rows, two for the sums'
 // exchange, four to five in the expansion, the rest launches; 21 rows, n 32003: 10.8
 // (1.95), a base and a y without alignment moved 4 bytes at a time.
