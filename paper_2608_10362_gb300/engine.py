@@ -375,6 +375,26 @@ def _call_on(dev: int, stream, fn, *args) -> int:
         return fn(*args, s)
 
 
+def _new(stream, make, size, dtype, device) -> torch.Tensor:
+    """make(size): memory that a call on `stream` (None: the current one) uses.  A block of
+    the caching allocator that was freed on one stream may still be in use by that stream's
+    queued kernels, so the memory comes from the stream that the call runs on."""
+    if stream is None:
+        return make(size, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(size, dtype=dtype, device=device)
+
+
+def _new_result(stream, *size, dtype, device) -> torch.Tensor:
+    """_new for what is returned: the caller will mostly use it on the current stream, and
+    its memory must not be handed out again while that does."""
+    if stream is None:
+        return torch.empty(size, dtype=dtype, device=device)
+    t = _new(stream, torch.empty, size, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 @functools.lru_cache(maxsize=512)
 def _linear_scratch_bytes(rows: int, n_out: int, k: int) -> int:
     lib = _lib.load()
@@ -391,11 +411,11 @@ def op_linear(x: torch.Tensor, w: torch.Tensor, scratch: torch.Tensor | None = N
     n_out = w.shape[0]
     nb = _linear_scratch_bytes(rows, n_out, k)
     if scratch is None:
-        scratch = torch.zeros(nb + 256, dtype=torch.uint8, device=x.device)
+        scratch = _new(stream, torch.zeros, nb + 256, dtype=torch.uint8, device=x.device)
     start = scratch.data_ptr()
     base = (start + 255) & ~255
     nb = max(0, scratch.nbytes - (base - start))
-    y = torch.empty((rows, n_out), dtype=torch.float32, device=x.device)
+    y = _new_result(stream, rows, n_out, dtype=torch.float32, device=x.device)
     st = lib.memspec_op_linear(x.data_ptr(), w.data_ptr(), y.data_ptr(), rows, n_out, k, base, nb, None,
                                _raw_stream(x, stream))
     if st:
@@ -414,7 +434,7 @@ def op_linear_noalloc(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor | None =
     rows, k = x.shape
     n_out = w.shape[0]
     if y is None:
-        y = torch.empty((rows, n_out), dtype=torch.float32, device=x.device)
+        y = _new_result(stream, rows, n_out, dtype=torch.float32, device=x.device)
     st = lib.memspec_op_linear_noalloc(x.data_ptr(), w.data_ptr(), y.data_ptr(), rows, n_out, k,
                                        None if status is None else status.data_ptr(), _raw_stream(x, stream))
     if st:
@@ -433,7 +453,7 @@ def int4_pack(qweight: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
     nbytes = lib.memspec_int4_packed_bytes(n_out, k)
     if nbytes < 0:
         raise MemSpecError(_lib.ERR_INVALID_ARG, f"bad INT4 shape n={n_out} k={k}")
-    packed = torch.empty(nbytes, dtype=torch.uint8, device=qweight.device)
+    packed = _new_result(stream, nbytes, dtype=torch.uint8, device=qweight.device)
     _check(lib, lib.memspec_int4_pack(qweight.data_ptr(), scales.data_ptr(), zeros.data_ptr(), n_out, k,
                                       packed.data_ptr(), _raw_stream(qweight, stream)))
     return packed
@@ -448,7 +468,7 @@ def op_linear_int4(x: torch.Tensor, packed: torch.Tensor, n_out: int, y: torch.T
     lib = _lib.load()
     rows, k = x.shape
     if y is None:
-        y = torch.empty((rows, n_out), dtype=torch.float32, device=x.device)
+        y = _new_result(stream, rows, n_out, dtype=torch.float32, device=x.device)
     st = lib.memspec_op_linear_int4(x.data_ptr(), packed.data_ptr(), y.data_ptr(), rows, n_out, k,
                                     None if status is None else status.data_ptr(), _raw_stream(x, stream))
     if st:
@@ -508,14 +528,6 @@ def _same_or_apart(name_a: str, a: torch.Tensor, name_b: str, b: torch.Tensor) -
     raise ValueError(f"{name_a} overlaps {name_b} without being the same rows")
 
 
-def _used_on(stream: torch.cuda.Stream | None, *made: torch.Tensor) -> None:
-    """Tensors made here on the current stream are in use on `stream` until its work is
-    done: their memory must not be handed out again before."""
-    if stream is not None:
-        for t in made:
-            t.record_stream(stream)
-
-
 def _filter(logits: torch.Tensor, temperature, top_k, top_p, min_p) -> _lib.Filter:
     f = _lib.Filter()
     for name, v, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
@@ -561,8 +573,7 @@ def op_sample_filtered(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, t
         _cuda_arg("u", u, _F32, (rows,), logits)
     f = _filter(logits, temperature, top_k, top_p, min_p)
     if out is None:
-        out = torch.empty((rows,), dtype=_I32, device=logits.device)
-        _used_on(stream, out)
+        out = _new_result(stream, rows, dtype=_I32, device=logits.device)
     else:
         _cuda_arg("out", out, _I32, (rows,), logits)
     st = _call_on(dev, stream, lib.memspec_op_sample_filtered, logits.data_ptr(), ld, rows, vocab, C.byref(f),
@@ -580,8 +591,7 @@ def op_filter_logits(logits: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, 
     rows, vocab, ld, dev = _logits_arg(logits)
     f = _filter(logits, temperature, top_k, top_p, min_p)
     if out is None:
-        out = torch.empty((rows, vocab), dtype=_F32, device=logits.device)
-        _used_on(stream, out)
+        out = _new_result(stream, rows, vocab, dtype=_F32, device=logits.device)
         out_ld = vocab
     elif out is logits:
         out_ld = ld
@@ -663,8 +673,7 @@ def op_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor
         ldx = _rows_arg("x", x, _BF16)
         ld_base = 0 if base is None else _rows_arg("base", base, _F32)
     if y is None:
-        y = torch.empty((rows, n_out), dtype=_F32, device=x.device)
-        _used_on(stream, y)
+        y = _new_result(stream, rows, n_out, dtype=_F32, device=x.device)
         ldy = n_out
     elif y is base:
         ldy = ld_base
@@ -675,8 +684,8 @@ def op_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor
         if base is not None:
             _same_or_apart("y", y, "base", base)
     if scratch is None:
-        scratch = torch.empty(_lora_scratch_bytes(rows, n_out, k, rank), dtype=torch.uint8, device=x.device)
-        _used_on(stream, scratch)
+        scratch = _new(stream, torch.empty, _lora_scratch_bytes(rows, n_out, k, rank), dtype=torch.uint8,
+                       device=x.device)
     elif scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be contiguous on {x.device}")
     f = _lib.Lora(a.data_ptr(), b.data_ptr(), None if scales is None else scales.data_ptr(),
