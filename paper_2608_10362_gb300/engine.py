@@ -395,6 +395,15 @@ def _new_result(stream, *size, dtype, device) -> torch.Tensor:
     return t
 
 
+def _used_on(stream, *tensors: torch.Tensor | None) -> None:
+    """Tensors of the caller that a call on `stream` reads or writes: their memory must not be
+    handed out again before that stream is done with them (of a temporary, none would know)."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 @functools.lru_cache(maxsize=512)
 def _linear_scratch_bytes(rows: int, n_out: int, k: int) -> int:
     lib = _lib.load()
@@ -416,6 +425,7 @@ def op_linear(x: torch.Tensor, w: torch.Tensor, scratch: torch.Tensor | None = N
     base = (start + 255) & ~255
     nb = max(0, scratch.nbytes - (base - start))
     y = _new_result(stream, rows, n_out, dtype=torch.float32, device=x.device)
+    _used_on(stream, x, w, scratch)
     st = lib.memspec_op_linear(x.data_ptr(), w.data_ptr(), y.data_ptr(), rows, n_out, k, base, nb, None,
                                _raw_stream(x, stream))
     if st:
@@ -435,6 +445,7 @@ def op_linear_noalloc(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor | None =
     n_out = w.shape[0]
     if y is None:
         y = _new_result(stream, rows, n_out, dtype=torch.float32, device=x.device)
+    _used_on(stream, x, w, y, status)
     st = lib.memspec_op_linear_noalloc(x.data_ptr(), w.data_ptr(), y.data_ptr(), rows, n_out, k,
                                        None if status is None else status.data_ptr(), _raw_stream(x, stream))
     if st:
@@ -453,6 +464,7 @@ def int4_pack(qweight: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
     nbytes = lib.memspec_int4_packed_bytes(n_out, k)
     if nbytes < 0:
         raise MemSpecError(_lib.ERR_INVALID_ARG, f"bad INT4 shape n={n_out} k={k}")
+    _used_on(stream, qweight, scales, zeros)
     packed = _new_result(stream, nbytes, dtype=torch.uint8, device=qweight.device)
     _check(lib, lib.memspec_int4_pack(qweight.data_ptr(), scales.data_ptr(), zeros.data_ptr(), n_out, k,
                                       packed.data_ptr(), _raw_stream(qweight, stream)))
@@ -469,6 +481,7 @@ def op_linear_int4(x: torch.Tensor, packed: torch.Tensor, n_out: int, y: torch.T
     rows, k = x.shape
     if y is None:
         y = _new_result(stream, rows, n_out, dtype=torch.float32, device=x.device)
+    _used_on(stream, x, packed, y, status)
     st = lib.memspec_op_linear_int4(x.data_ptr(), packed.data_ptr(), y.data_ptr(), rows, n_out, k,
                                     None if status is None else status.data_ptr(), _raw_stream(x, stream))
     if st:
@@ -542,6 +555,10 @@ def _filter(logits: torch.Tensor, temperature, top_k, top_p, min_p) -> _lib.Filt
     return f
 
 
+def _tensors(*parts) -> list[torch.Tensor]:
+    return [v for v in parts if isinstance(v, torch.Tensor)]
+
+
 _F32, _I32, _BF16 = torch.float32, torch.int32, torch.bfloat16
 
 
@@ -576,6 +593,8 @@ def op_sample_filtered(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, t
         out = _new_result(stream, rows, dtype=_I32, device=logits.device)
     else:
         _cuda_arg("out", out, _I32, (rows,), logits)
+    if stream is not None:
+        _used_on(stream, logits, u, out, *_tensors(temperature, top_k, top_p, min_p))
     st = _call_on(dev, stream, lib.memspec_op_sample_filtered, logits.data_ptr(), ld, rows, vocab, C.byref(f),
                   u.data_ptr(), out.data_ptr())
     if st:
@@ -600,6 +619,8 @@ def op_filter_logits(logits: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, 
         if out.shape != logits.shape:
             raise ValueError(f"out must be {list(logits.shape)}, not {list(out.shape)}")
         _same_or_apart("out", out, "logits", logits)
+    if stream is not None:
+        _used_on(stream, logits, out, *_tensors(temperature, top_k, top_p, min_p))
     st = _call_on(dev, stream, lib.memspec_op_filter_logits, logits.data_ptr(), ld, rows, vocab, C.byref(f),
                   out.data_ptr(), out_ld)
     if st:
@@ -688,6 +709,7 @@ def op_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor
                        device=x.device)
     elif scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be contiguous on {x.device}")
+    _used_on(stream, x, a, b, ids, scales, ranks, base, y, scratch)
     f = _lib.Lora(a.data_ptr(), b.data_ptr(), None if scales is None else scales.data_ptr(),
                   None if ranks is None else ranks.data_ptr(), n, rank)
     st = _call_on(dev, stream, lib.memspec_op_lora, C.byref(f), x.data_ptr(), ldx, ids.data_ptr(),

@@ -60,3 +60,32 @@ def test_calls_beside_queued_work_on_the_current_stream(name):
             torch.full((n,), 9, dtype=torch.uint8, device="cuda")
     torch.cuda.synchronize()
     assert torch.equal(copy, want)
+
+
+@pytest.mark.parametrize("name", ["linear", "sample_filtered", "filter_logits", "lora"])
+def test_temporaries_live_until_the_stream_of_the_call_is_done(name):
+    """Inputs that are freed when the call returns, while the stream has not begun with it: their
+    memory is not written by what the current stream does next."""
+    import paper_2608_10362_gb300 as pkg
+    g = torch.Generator(device="cuda").manual_seed(6)
+    mk = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()
+    x, w, a, b = mk(8, 512), mk(4096, 512), mk(2, 64, 512), mk(2, 4096, 64)
+    ids, base = torch.tensor([0, 1, -1, 1, 0, 0, 1, 0], dtype=torch.int32, device="cuda"), mk(8, 4096).float()
+    z, u, p = mk(64, 4096).float(), torch.rand(64, device="cuda", generator=g), torch.full((64,), 0.9, device="cuda")
+    c = torch.Tensor.clone
+    call = {"linear": lambda s: pkg.op_linear(c(x), c(w), stream=s),
+            "sample_filtered": lambda s: pkg.op_sample_filtered(c(z), c(u), top_p=c(p), stream=s),
+            "filter_logits": lambda s: pkg.op_filter_logits(c(z), top_p=c(p), stream=s),
+            "lora": lambda s: pkg.op_lora(c(x), c(a), c(b), c(ids), base=c(base), stream=s)}[name]
+    want = call(None)
+    side = torch.cuda.Stream()
+    call(side)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)             # some 50 ms: the copies are complete long before
+    got = call(side)
+    for n in [1 << k for k in range(9, 23)]:
+        for _ in range(4):
+            torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)

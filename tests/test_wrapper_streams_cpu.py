@@ -101,3 +101,13 @@ def test_memory_comes_from_the_stream_of_the_call(allocations, name):
     LOG.clear()
     call(None, *tensors)
     assert allocations and all(s is CURRENT for _, s in allocations) and not LOG
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_the_callers_tensors_are_recorded_on_the_stream_of_the_call(allocations, name):
+    tensors, call = CALLS[name]
+    tensors = tensors()
+    LOG.clear()
+    call(SIDE, *tensors)
+    used = [p for what, p, s in LOG if s is SIDE]
+    assert all(t.data_ptr() in used for t in tensors)
