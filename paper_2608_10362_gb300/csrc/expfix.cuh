@@ -49,14 +49,16 @@ __device__ __forceinline__ const unsigned long long* exp_table() {
   return t.v;
 }
 
-// What weights need of a row: the maximum, and c = log2(e) / T in two floats.
+// What weights need of a row: the maximum, and c = log2(e) / T.
 struct WeightScale {
-  float max, hi, lo;        // c = hi + lo
+  float max;
+  float scale;              // above T = 2^64: 2^-64, of logits and T alike, else 1
+  float hi256, lo256;       // 256 c / scale in two floats
   bool near;                // 256 z c stays below 2^22 for the z that have weight: then also
-  float hi256, lo256;       // 256 c,
-  float f_max;              // 256 max c = n_max + f_max,
+  float f_max;              // 256 max c = n_max + f_max
   int n_max;
   float z_deep;             // and a logit without weight
+  __device__ __forceinline__ float c() const { return hi256 * scale / kExpSteps; }   // for estimates
 };
 constexpr float kRound = 12582912.f;          // 1.5 * 2^23: x + kRound has round(x) in its low bits
 constexpr int kRoundBits = 0x4B400000;
@@ -64,19 +66,23 @@ constexpr int kNoWeight = -45 * kExpSteps;    // n at and below which the weight
 __device__ __forceinline__ WeightScale weight_scale(float row_max, float temperature) {
   // T below 1e-30 leaves the maxima alone with weight; T = inf weighs all alike.  A quotient
   // and its remainder's in 32 bits: 64-bit arithmetic by every thread of a CTA is 2 us.
+  // Above T = 2^64 differences of logits that count may pass the largest float (infinities
+  // count as it, and masks may be of its negative) and c's lower part falls below the smallest
+  // one: logits and T are taken 2^-64 fold (exactly, but for logits below 2^-62, whose
+  // differences are no part of such a T), always the long way.
   constexpr float kHi = 1.44269504f, kLo = 1.92596299e-8f;   // log2(e)
-  const float T = fmaxf(temperature, 1e-30f);
   WeightScale s;
   s.max = row_max;
-  s.hi = __fdiv_rn(kHi, T);
-  s.lo = s.hi > 0.f ? __fdiv_rn(fmaf(-s.hi, T, kHi) + kLo, T) : 0.f;
-  s.hi256 = s.hi * kExpSteps;
-  s.lo256 = s.lo * kExpSteps;
-  s.near = s.hi > 0.f && fabsf(row_max) * s.hi256 < 4e6f;
+  s.scale = temperature > 18446744073709551616.f ? 5.42101086e-20f : 1.f;
+  const float T = fmaxf(temperature, 1e-30f) * s.scale;
+  const float hi = __fdiv_rn(kHi, T), lo = hi > 0.f ? __fdiv_rn(fmaf(-hi, T, kHi) + kLo, T) : 0.f;
+  s.hi256 = hi * kExpSteps;
+  s.lo256 = lo * kExpSteps;
+  s.near = s.scale == 1.f && fabsf(row_max) * s.hi256 < 4e6f;
   const float big = fmaf(row_max, s.hi256, kRound);
   s.n_max = __float_as_int(big) - kRoundBits;
   s.f_max = fmaf(row_max, s.lo256, fmaf(row_max, s.hi256, kRound - big));
-  s.z_deep = row_max - 47.f / s.hi;
+  s.z_deep = row_max - 47.f / hi;
   return s;
 }
 
@@ -91,9 +97,11 @@ __device__ __forceinline__ int place_near(float z, const WeightScale& s, float& 
 }
 __device__ __forceinline__ int place_far(float z, const WeightScale& s, float& f) {
   // the difference first: max - z = d + e exactly (two-sum)
-  const float d = s.max - z;
-  const float b = d - s.max;
-  const float e = (s.max - (d - b)) - (z + b);
+  const float top = s.max * s.scale;
+  z *= s.scale;
+  const float d = top - z;
+  const float b = d - top;
+  const float e = (top - (d - b)) - (z + b);
   const float yh = d * s.hi256;
   const float yl = fmaf(d, s.hi256, -yh) + fmaf(d, s.lo256, e * s.hi256);
   const float big = kRound - yh;

@@ -564,8 +564,8 @@ __device__ Ended search(const Part& p, const Slice& s, const WeightScale& ws, in
   {
     float d0, d1;             // max - z
     if (kMass) {
-      d0 = static_cast<float>(bin * kPlacesPerBin - 1) / ws.hi256;
-      d1 = static_cast<float>((bin + 1) * kPlacesPerBin + 1) / ws.hi256;
+      d0 = static_cast<float>(bin * kPlacesPerBin - 1) / (ws.hi256 * ws.scale);
+      d1 = static_cast<float>((bin + 1) * kPlacesPerBin + 1) / (ws.hi256 * ws.scale);
     } else {
       d0 = __uint_as_float(static_cast<uint32_t>(bin + kFirstOctave) << (23 - kMantissa));
       d1 = __uint_as_float(static_cast<uint32_t>(bin + 1 + kFirstOctave) << (23 - kMantissa));
@@ -1027,16 +1027,17 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     // 2^-17.4 of itself, besides the instruction's 2^-22; a thread's sums by 19
     // roundings: 2^-17.1 in all.)
     // Rows whose candidates lie within 4 octaves are flat: more ids than these hold the sum.
-    if (by_p && !by_k && !empty && (m - bound) * ws.hi > 4.f) {
+    // (Past T = 2^64 x - m may overflow where its weight does not vanish.)
+    if (by_p && !by_k && !empty && ws.scale == 1.f && (m - bound) * ws.c() > 4.f) {
       float sum = 0.f, deep4[4] = {};
       u64 listed = 0;
       // 3 to 6 octaves below the bound: the queues hold what lies above of a row whose weights
       // fall by rank^-1.4
-      const float z_deep = fmaxf(bound - static_cast<float>(34 - __clz(C)) / ws.hi, -kLargest);
+      const float z_deep = fmaxf(bound - static_cast<float>(34 - __clz(C)) / ws.c(), -kLargest);
       for_quads<NT>(s, -INFINITY, [&](const float (&x)[4], int id) {
         float e[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) e[q] = rough_exp2((x[q] - m) * ws.hi);
+        for (int q = 0; q < 4; ++q) e[q] = rough_exp2((x[q] - m) * ws.c());
         if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= bound) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -1156,8 +1157,8 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
     // Large k: the ids above the bound, or an octave below it where that is not sure to leave
     // so many (for 200 per CTA it mostly does: 144 x 128256, k 1000, p 0.9 131 -> 84 us; for more
     // it would be tried in vain, 144 x 32000 37 us for 32); then top-p among what is left of them.
-    if (search_k && owed <= kMostBelow && ws.hi > 0.f) {
-      const float z_low = owed <= kMostAbove ? bound : fmaxf(bound - 1.f / ws.hi, -kLargest);
+    if (search_k && owed <= kMostBelow && ws.c() > 0.f) {
+      const float z_low = owed <= kMostAbove ? bound : fmaxf(bound - 1.f / ws.c(), -kLargest);
       Ended e = search_above<NT, false>(static_cast<u64>(r.top_k), 0, 0, z_low, ~0ull, !by_p, s, ws, C, rank, sm);
       if (e.gone) return;
       if (e.cut != 0) {

@@ -1,0 +1,49 @@
+"""Sampling rules at the ends of what 32 bits hold, against their 64-bit definition."""
+import numpy as np
+import pytest
+
+from oracle import filtering as F
+
+pytestmark = pytest.mark.gpu
+
+HOT = [1e19, 2e19, 1e28, 1e36, 1e37, 3e37, 1e38, 2e38, F.LARGEST, np.inf]
+
+
+def _wide(kind, rows, vocab, seed=0):
+    """Logits over all that fp32 holds: steps (infinities, the largest and the lowest finite
+    number, NaN and some between, many equal) or spread evenly."""
+    rng = np.random.default_rng([seed, rows, vocab])
+    if kind == "steps":
+        v = np.array([np.inf, F.LARGEST, 2e38, 12.0, 0.0, -1e38, -F.LARGEST, -np.inf, np.nan], np.float32)
+        return v[rng.choice(len(v), (rows, vocab), p=[.02, .02, .1, .2, .2, .2, .2, .03, .03])]
+    return (rng.uniform(-1, 1, (rows, vocab)) * F.LARGEST).astype(np.float32)
+
+
+def _both(z, u, rules):
+    """Draws and masks on the GPU, one rule per row."""
+    import torch
+    from paper_2608_10362_gb300 import op_filter_logits, op_sample_filtered
+    per = [torch.tensor([float(r[i]) if i != 1 else r[i] for r in rules], dtype=torch.int32 if i == 1 else torch.float32,
+                        device="cuda") for i in range(4)]
+    zt = torch.from_numpy(z).cuda()
+    return (op_sample_filtered(zt, torch.from_numpy(u).cuda(), *per).cpu().numpy(),
+            op_filter_logits(zt, *per).cpu().numpy())
+
+
+def _uniforms(rows, seed=0):
+    return ((2 * np.random.default_rng([seed, rows]).integers(0, 1 << 23, rows) + 1) * 2.0 ** -24).astype(np.float32)
+
+
+def _compare(z, u, rules):
+    drawn, masked = _both(z, u, rules)
+    for r, rule in enumerate(rules):
+        assert np.array_equal(masked[r], F.mask(z[r], *rule)), (r, rule)
+        assert drawn[r] == F.draw(z[r], u[r], *rule), (r, rule)
+
+
+@pytest.mark.parametrize("kind", ["steps", "spread"])
+@pytest.mark.parametrize("vocab", [300, 5000, 40000])
+def test_temperatures_up_to_infinity_over_logits_of_any_size(kind, vocab):
+    """max - z passes the largest float, 1 / T falls below the smallest normal one."""
+    rules = [(T, k, p, 0.0) for T in HOT for k, p in ((0, 1.0), (0, 0.9), (0, 0.3), (100, 1.0), (150, 0.8), (1200, 0.7))]
+    _compare(_wide(kind, len(rules), vocab), _uniforms(len(rules)), rules)
