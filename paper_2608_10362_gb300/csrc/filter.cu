@@ -111,7 +111,7 @@ struct alignas(16) Smem {
   u64 sum, listed_sum;                       // of the slice's weights, of the candidates'
   uint32_t n_list, n_candidates, n_queue;
   uint2 peer_max[kMaxCluster];               // pushed: keys of the maximum and the bound
-  float2 log_min_p;                          // T log(min_p) in two floats
+  float2 log_min_p;                          // T log(min_p) in two floats, scaled
   u64 peer_sum[kMaxCluster];                 // pushed
   u64 scan[48];
   uint32_t group[kGroups];                   // keys
@@ -939,7 +939,8 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   const bool by_k = r.top_k > 0 && r.top_k < V;
   bool by_p = r.top_p < 1.f;
   if (r.min_p > 0.f && tid == NT - 1) {   // 64-bit arithmetic: one thread's, beside the loads
-    const double l = static_cast<double>(r.temperature) * log(static_cast<double>(fminf(r.min_p, 1.f)));
+    const double l = static_cast<double>(r.temperature) * (r.min_p < 1.f ? logit_scale(r.temperature) : 1.f) *
+                     log(static_cast<double>(fminf(r.min_p, 1.f)));
     const float hi = static_cast<float>(l);
     sm.log_min_p = make_float2(hi, static_cast<float>(l - static_cast<double>(hi)));
   }
@@ -1009,12 +1010,14 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 2) filter_kernel(const __g
   const u64 no_cut = entry_of(logit_key(-kLargest), ~0u);
   u64 cut = no_cut;
   if (r.min_p > 0.f && !empty) {
-    // the least float z with z >= max + T log(min_p), the product in two floats
+    // the least float z with z >= max + T log(min_p), the product in two floats; all of it
+    // scaled where T may take the product past the largest float
     const float2 l = sm.log_min_p;
-    const float c = m + l.x, part = c - m;
-    const float rest = ((m - (c - part)) + (l.x - part)) + l.y;    // what c lacks
-    uint32_t key = c > -kLargest ? logit_key(c) : logit_key(-kLargest);
-    if (c > -kLargest && rest > 0.f) ++key;
+    const float scale = r.min_p < 1.f ? ws.scale : 1.f, top = m * scale, lowest = -kLargest * scale;
+    const float c = top + l.x, part = c - top;
+    const float rest = ((top - (c - part)) + (l.x - part)) + l.y;  // what c lacks
+    uint32_t key = c > lowest ? logit_key(scale == 1.f ? c : c * 18446744073709551616.f) : logit_key(-kLargest);
+    if (c > lowest && rest > 0.f) ++key;
     cut = entry_of(min(key, logit_key(m)), ~0u);
   }
   const u64 fraction = fraction64(r.top_p);

@@ -47,3 +47,12 @@ def test_temperatures_up_to_infinity_over_logits_of_any_size(kind, vocab):
     """max - z passes the largest float, 1 / T falls below the smallest normal one."""
     rules = [(T, k, p, 0.0) for T in HOT for k, p in ((0, 1.0), (0, 0.9), (0, 0.3), (100, 1.0), (150, 0.8), (1200, 0.7))]
     _compare(_wide(kind, len(rules), vocab), _uniforms(len(rules)), rules)
+
+
+@pytest.mark.parametrize("kind", ["steps", "spread"])
+@pytest.mark.parametrize("vocab", [300, 5000, 40000])
+def test_min_p_at_temperatures_up_to_infinity(kind, vocab):
+    """T log(min_p) passes the largest float where the bound max + T log(min_p) does not."""
+    rules = [(T, k, p, m) for T in HOT for m in (1e-30, 0.01, 0.1, 0.5, 0.9, 1 - 2.0 ** -24, 1.0)
+             for k, p in ((0, 1.0), (120, 0.9))]
+    _compare(_wide(kind, len(rules), vocab, 1), _uniforms(len(rules), 1), rules)
