@@ -115,7 +115,8 @@ memspec_status memspec_op_sample(const float* logits_dev, int32_t rows, int32_t 
  *   top_p  of those, the shortest prefix whose weights sum to at least top_p
  *          times the sum over them (1: all)
  *   min_p  the ids with w_i >= min_p (0: all)
- * temperature 0: the first id of the largest logit alone.
+ * temperature 0: the first id of the largest logit alone; above 0 and below
+ * 1e-30: 1e-30.
  * A NaN logit counts as -inf, +inf as the largest finite float; an id at -inf is
  * never kept.  Sums and their comparisons are exact over weights that are off by
  * at most 2^-31 of themselves (and 2^-46 of the largest; below 2^-45 of it they

@@ -18,6 +18,11 @@ def sane(z: np.ndarray) -> np.ndarray:
     return np.where(np.isnan(z), -np.inf, np.minimum(z, LARGEST))
 
 
+def counts_as(T: float) -> float:
+    """A temperature above 0 and below 1e-30 is 1e-30."""
+    return max(T, 1e-30) if T > 0 else T
+
+
 def order_of(z: np.ndarray) -> np.ndarray:
     """The ids with a finite logit in the rule's order."""
     o = np.argsort(-z, kind="stable")
@@ -26,7 +31,7 @@ def order_of(z: np.ndarray) -> np.ndarray:
 
 def kept(z: np.ndarray, T: float, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0) -> np.ndarray:
     """Kept ids of one row, in the rule's order.  T, top_p, min_p as float32 holds them."""
-    T, top_p, min_p = (float(np.float32(v)) for v in (T, top_p, min_p))
+    T, top_p, min_p = (float(np.float32(v)) for v in (counts_as(T), top_p, min_p))
     z = sane(z)
     o = order_of(z)
     if len(o) == 0 or not T > 0:
@@ -53,7 +58,7 @@ def draw(z: np.ndarray, u: float, T: float, *rule) -> int:
     if len(ids) == 0:
         return -1
     z = sane(z)[ids]
-    w = np.exp((z - z.max()) / float(np.float32(T))) if T > 0 else np.ones(1)
+    w = np.exp((z - z.max()) / float(np.float32(counts_as(T)))) if T > 0 else np.ones(1)
     cum = np.cumsum(w)
     return int(ids[np.argmax(cum > float(u) * cum[-1])])
 

@@ -62,6 +62,8 @@ struct WeightScale {
 };
 constexpr float kRound = 12582912.f;          // 1.5 * 2^23: x + kRound has round(x) in its low bits
 constexpr int kRoundBits = 0x4B400000;
+constexpr float kLowest = 1e-30f;             // temperatures above 0 count as this at least: 1 / T and
+                                              // its lower part are normal numbers
 constexpr int kNoWeight = -45 * kExpSteps;    // n at and below which the weight is 0
 // Above T = 2^64 differences of logits that count may pass the largest float (infinities count
 // as it, and masks may be of its negative) and c's lower part falls below the smallest one:
@@ -71,13 +73,13 @@ __device__ __forceinline__ float logit_scale(float temperature) {
   return temperature > 18446744073709551616.f ? 5.42101086e-20f : 1.f;
 }
 __device__ __forceinline__ WeightScale weight_scale(float row_max, float temperature) {
-  // T below 1e-30 leaves the maxima alone with weight; T = inf weighs all alike.  A quotient
-  // and its remainder's in 32 bits: 64-bit arithmetic by every thread of a CTA is 2 us.
+  // T from kLowest to inf (which weighs all alike).  A quotient and its remainder's in 32 bits:
+  // 64-bit arithmetic by every thread of a CTA is 2 us.
   constexpr float kHi = 1.44269504f, kLo = 1.92596299e-8f;   // log2(e)
   WeightScale s;
   s.max = row_max;
   s.scale = logit_scale(temperature);
-  const float T = fmaxf(temperature, 1e-30f) * s.scale;
+  const float T = temperature * s.scale;
   const float hi = __fdiv_rn(kHi, T), lo = hi > 0.f ? __fdiv_rn(fmaf(-hi, T, kHi) + kLo, T) : 0.f;
   s.hi256 = hi * kExpSteps;
   s.lo256 = lo * kExpSteps;

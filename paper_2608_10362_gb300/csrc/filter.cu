@@ -140,6 +140,7 @@ __device__ __forceinline__ Rule rule_of(const FilterArgs& a, int row) {
     r.top_p = 1.f;
     r.min_p = 0.f;
   }
+  r.temperature = fmaxf(r.temperature, kLowest);
   return r;
 }
 

@@ -56,3 +56,12 @@ def test_min_p_at_temperatures_up_to_infinity(kind, vocab):
     rules = [(T, k, p, m) for T in HOT for m in (1e-30, 0.01, 0.1, 0.5, 0.9, 1 - 2.0 ** -24, 1.0)
              for k, p in ((0, 1.0), (120, 0.9))]
     _compare(_wide(kind, len(rules), vocab, 1), _uniforms(len(rules), 1), rules)
+
+
+def test_temperatures_below_the_lowest_count_as_it():
+    """All parts of a rule take 1e-30 for a smaller temperature above 0: logits some 1e-31 apart."""
+    rng = np.random.default_rng(4)
+    z = (np.round(rng.normal(size=(40, 3000)) * 8) * 1e-31).astype(np.float32)
+    rules = [(T, k, p, m) for T in (1e-45, 1e-38, 1e-33, 9e-31, 1e-30) for m in (0.0, 0.3)
+             for k, p in ((0, 1.0), (0, 0.9), (100, 1.0), (900, 0.8))]
+    _compare(z, _uniforms(len(rules), 2), rules)

@@ -149,3 +149,12 @@ def test_wrappers_refuse_host_tensors(lib):
                                      torch.zeros(2, dtype=torch.int32))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_temperatures_below_the_lowest_count_as_it():
+    z = np.array([0.0, -0.5, -1.0, -2.0]) * 1e-30           # weights 1, 0.61, 0.37, 0.14 at T = 1e-30
+    for T in (1e-45, 1e-38, 1e-31, 1e-30):
+        assert F.kept(z, T, 0, 1.0, 0.3).tolist() == [0, 1, 2]
+        assert F.kept(z, T, 0, 0.7).tolist() == [0, 1]
+        assert F.draw(z, 0.9, T) == 2
+    assert F.kept(z, 0.0, 3).tolist() == [0]
