@@ -47,6 +47,7 @@
 #include <cuda_runtime.h>
 
 #include <math.h>
+#include <stddef.h>
 
 #include <atomic>
 #include <string>
@@ -121,6 +122,17 @@ struct alignas(16) Smem {
   u64 deep_sum;                              // of the slice's weights below a bound, roughly; read by the others
 };
 static_assert(3 * (sizeof(Smem) + kMaxSlice * 4 + 1024) <= 228 * 1024, "three CTAs per SM");
+// Shared memory begins on a 16-byte boundary: what is accessed by 8 bytes (plainly or from other
+// CTAs) lies on multiples of 8, the slice behind it, by 16, on one of 16.
+static_assert(offsetof(Smem, table) % 8 == 0 && offsetof(Smem, h) % 8 == 0 && offsetof(Smem, p) % 8 == 0 &&
+                  offsetof(Smem, sup_mass) % 8 == 0 && offsetof(Smem, sum) % 8 == 0 &&
+                  offsetof(Smem, listed_sum) % 8 == 0 && offsetof(Smem, deep_sum) % 8 == 0 &&
+                  offsetof(Smem, peer_max) % 8 == 0 && offsetof(Smem, log_min_p) % 8 == 0 &&
+                  offsetof(Smem, peer_sum) % 8 == 0 && offsetof(Smem, scan) % 8 == 0 &&
+                  offsetof(Smem, loaded) % 8 == 0 && offsetof(Smem, cut) % 8 == 0 && sizeof(Smem) % 16 == 0 &&
+                  offsetof(Smem, entry) == offsetof(Smem, h) && offsetof(Smem, d) == offsetof(Smem, h) &&
+                  offsetof(Smem, list) == offsetof(Smem, p) && offsetof(Smem, queue) == offsetof(Smem, p),
+              "aligned");
 
 // A row's rule, with what "off" means resolved.
 struct Rule {

@@ -65,3 +65,27 @@ def test_temperatures_below_the_lowest_count_as_it():
     rules = [(T, k, p, m) for T in (1e-45, 1e-38, 1e-33, 9e-31, 1e-30) for m in (0.0, 0.3)
              for k, p in ((0, 1.0), (0, 0.9), (100, 1.0), (900, 0.8))]
     _compare(z, _uniforms(len(rules), 2), rules)
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 3, 4, 5])
+def test_single_ids_at_every_alignment(vocab):
+    """The shortest rows under every kind of rule, in place and not, wherever they begin."""
+    import torch
+    from paper_2608_10362_gb300 import op_filter_logits, op_sample_filtered
+    z = np.array([[0.5, -1.0, 0.5, 2.0, np.nan], [-np.inf, 3.0, np.inf, -F.LARGEST, 0.0]], np.float32)[:, :vocab]
+    rules = [(1.0, 0, 0.9, 0.0), (1.0, 0, 1e-3, 0.0), (0.7, 1, 0.9, 0.0), (0.7, 2, 0.5, 0.1), (2.0, 0, 1.0, 0.4),
+             (0.0, 0, 1.0, 0.0), (1.0, 0, 1.0, 0.0)]
+    u = torch.tensor([0.3], device="cuda")
+    for at in range(4):
+        for row in z:
+            raw = torch.full((at + vocab + 4,), 1e30, device="cuda")
+            zt = raw[at:at + vocab].view(1, vocab)
+            for rule in rules:
+                zt.copy_(torch.from_numpy(row))
+                kw = dict(zip(("temperature", "top_k", "top_p", "min_p"), rule))
+                want = F.mask(row, *rule)
+                assert op_sample_filtered(zt, u, **kw).tolist() == [F.draw(row, float(u[0]), *rule)]
+                assert np.array_equal(op_filter_logits(zt, **kw).cpu().numpy()[0], want)
+                op_filter_logits(zt, **kw, out=zt)
+                assert np.array_equal(zt.cpu().numpy()[0], want)
+                assert bool((raw[:at] == 1e30).all()) and bool((raw[at + vocab:] == 1e30).all())
