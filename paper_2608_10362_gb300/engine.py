@@ -533,10 +533,11 @@ def _same_or_apart(name_a: str, a: torch.Tensor, name_b: str, b: torch.Tensor) -
     n, size = a.shape[1], a.element_size()
     span = lambda t: (t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + n) * size)
     (a0, a1), (b0, b1) = span(a), span(b)
-    if a0 >= b1 or b0 >= a1 or (a0, a.stride()) == (b0, b.stride()):
+    one = a.shape[0] == 1                    # then the row stride says nothing
+    if a0 >= b1 or b0 >= a1 or (a0 == b0 and (one or a.stride(0) == b.stride(0))):
         return
     ld = a.stride(0)
-    if ld == b.stride(0) and n <= (b0 - a0) // size % ld <= ld - n:
+    if not one and ld == b.stride(0) and n <= (b0 - a0) // size % ld <= ld - n:
         return
     raise ValueError(f"{name_a} overlaps {name_b} without being the same rows")
 
