@@ -89,3 +89,39 @@ def test_single_ids_at_every_alignment(vocab):
                 op_filter_logits(zt, **kw, out=zt)
                 assert np.array_equal(zt.cpu().numpy()[0], want)
                 assert bool((raw[:at] == 1e30).all()) and bool((raw[at + vocab:] == 1e30).all())
+
+
+def _sparse_lora(adapters, rank, k, n, rows, ids, seed):
+    """A call on zeros but for some whole numbers in the adapters that the rows have: the result by
+    picking those out."""
+    import torch
+    from paper_2608_10362_gb300 import op_lora
+    rng = np.random.default_rng(seed)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    a, b = torch.zeros(adapters, rank, k, **bf), torch.zeros(adapters, n, rank, **bf)
+    x = torch.zeros(rows, k, **bf)
+    cols = np.unique(np.concatenate([[0, k - 1], rng.integers(0, k, 60)]))
+    outs = np.unique(np.concatenate([[0, n - 1], rng.integers(0, n, 60)]))
+    xv = rng.integers(-3, 4, (rows, len(cols)))
+    x[:, torch.from_numpy(cols).cuda()] = torch.from_numpy(xv).to(**bf)
+    base = torch.from_numpy(rng.integers(-50, 51, (rows, n)).astype(np.float32)).cuda()
+    want = base.clone()
+    for i in sorted({i for i in ids if 0 <= i < adapters}):
+        av, bv = rng.integers(-3, 4, (rank, len(cols))), rng.integers(-3, 4, (len(outs), rank))
+        a[i, :, torch.from_numpy(cols).cuda()] = torch.from_numpy(av).to(**bf)
+        b[i, torch.from_numpy(outs).cuda()] = torch.from_numpy(bv).to(**bf)
+        for r in np.flatnonzero(np.array(ids) == i):
+            want[int(r), torch.from_numpy(outs).cuda()] += torch.from_numpy(bv @ (av @ xv[r])).float().cuda()
+    got = op_lora(x, a, b, torch.tensor(ids, dtype=torch.int32, device="cuda"), base=base)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("adapters,rank,k,n,rows", [
+    (70, 128, 262144, 64, 3),          # A past 2^31 elements
+    (70, 128, 64, 262144, 3),          # B
+    (300, 32, 262144, 40, 40), (300, 16, 64, 524288, 2),
+    (1, 8, 1 << 24, 32, 2), (2, 8, 64, 1 << 24, 2), (1, 32, 64, (1 << 24) - 3, 1),   # the longest rows
+    (1 << 24, 8, 8, 1, 5)])            # the most adapters
+def test_adapters_past_what_32_bits_address(adapters, rank, k, n, rows):
+    ids = [adapters - 1, 0, adapters, adapters - 1, adapters // 2][:rows] + [adapters - 1 - r % 3 for r in range(max(0, rows - 5))]
+    _sparse_lora(adapters, rank, k, n, rows, ids, rank + rows)
