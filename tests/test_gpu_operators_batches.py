@@ -69,3 +69,40 @@ def test_top_p_next_to_a_border_in_a_batch(rows, vocab, T, first, step, last):
     for r in range(rows):
         assert np.array_equal(masked[r], F.mask(z[r], T, 0, p[r])), r
         assert got[r] == F.draw(z[r], u[r], T, 0, p[r]), r
+
+
+@pytest.mark.parametrize("rows,rank,vocab", [(4, 16, 4096), (16, 64, 9000), (100, 32, 4003), (144, 128, 32000)])
+def test_calls_back_to_back_give_what_calls_apart_give(rows, rank, vocab):
+    """Shared projection, adapters in place, mask in place, draw: each reads what the call before it
+    writes and starts before that has ended; the same with the GPU waited for after each."""
+    import torch
+    from paper_2608_10362_gb300 import op_filter_logits, op_linear, op_lora, op_sample_filtered
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    mk = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    k, n = 512, 5
+    xs = [mk(rows, k).bfloat16() for _ in range(n)]
+    w, a, b = (mk(vocab, k) * 0.1).bfloat16(), (mk(n, rank, k) * 0.05).bfloat16(), mk(n, vocab, rank).bfloat16()
+    ids = torch.randint(-1, n, (rows,), device="cuda", generator=g, dtype=torch.int32)
+    u = torch.rand(rows, device="cuda", generator=g)
+    T = 0.5 + torch.rand(rows, device="cuda", generator=g)
+    scratch = torch.empty(rows * rank * 4, dtype=torch.uint8, device="cuda")
+
+    def run(x, wait):
+        z = op_linear(x, w)
+        wait()
+        op_lora(x, a, b, ids, base=z, y=z, scratch=scratch)
+        wait()
+        first = op_sample_filtered(z, u, T, top_p=0.9)
+        wait()
+        op_filter_logits(z, T, top_p=0.9, out=z)
+        wait()
+        return first, op_sample_filtered(z, u, T), z
+
+    want = [run(x, torch.cuda.synchronize) for x in xs]
+    for _ in range(8):
+        got = [run(x, lambda: None) for x in xs]
+        torch.cuda.synchronize()
+        for one, other in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(one, other))
+    for first, second, _ in want:
+        assert torch.equal(first, second)        # a draw under a rule is one from its mask
