@@ -119,7 +119,7 @@ memspec_status memspec_op_sample(const float* logits_dev, int32_t rows, int32_t 
  * 1e-30: 1e-30.
  * A NaN logit counts as -inf, +inf as the largest finite float; an id at -inf is
  * never kept.  Sums and their comparisons are exact over weights that are off by
- * at most 2^-31 of themselves (and 2^-46 of the largest; below 2^-45 of it they
+ * at most 2^-29.9 of themselves (and 2^-46 of the largest; below 2^-45 of it they
  * are 0): the same input gives the same result however the work is split.
  * Each part is one number for all rows, or (pointer not NULL) a device array of
  * one value per row, which the call cannot check: there a temperature that is

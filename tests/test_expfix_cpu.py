@@ -60,14 +60,20 @@ def weights(tmp_path_factory):
 
 
 def _check(weights, top, T, z):
-    """Off by at most 2^-31 of the weight and 2^-46 of the largest one (a unit), 0 below 2^-45;
-    the exponential in 64 bits by 2^-46 of itself at most (its argument above -32)."""
+    """Off by at most 2^-29.9 of the weight and 2^-46 of the largest one (a unit), 0 below 2^-45;
+    the exponential in 64 bits by 2^-46 of itself at most (its argument above -32).
+
+    2^-29.9, with 256 (z - max) c = n + f: of z and of the maximum, 256 z c (|256 z c| < 2^22) has a
+    first product that is off by 2^-26 (its rest is at most 1/2), plus its lower part (at most
+    1/4) by 2^-25; their difference f (at most 1.5) by 2^-24: 5 * 2^-25 together, which is ln 2 / 256
+    times that of the weight, 2^-31.2.  The cubic's value is at most 2^-7.9 and its coefficients,
+    the inner sums and the last product are off by 2^-25, 2^-24.5 and 2^-24 of it: 2^-30.8."""
     top, T, z = (np.asarray(a, np.float32) for a in (top, T, z))
     got = weights(top, T, z).astype(np.float64)
     with np.errstate(over="ignore", under="ignore", invalid="ignore"):
         want = 2.0 ** 46 * np.exp((z.astype(np.float64) - top.astype(np.float64)) / T.astype(np.float64))
     want = np.where(z == -np.inf, 0.0, want)
-    bad = np.abs(got - want) > want * 2.0 ** -31 + 1 + 2.0 * (got == 0)
+    bad = np.abs(got - want) > want * 2.0 ** -29.9 + 1 + 2.0 * (got == 0)
     assert not bad.any(), [tuple(np.broadcast_to(a, bad.shape)[bad][0] for a in (top, T, z, got, want)), bad.sum()]
 
 
@@ -79,6 +85,15 @@ def test_ordinary_logits(weights):
     z = (top - T * rng.uniform(0, 33, n)).astype(np.float32)
     _check(weights, top, T, z)
     _check(weights, top, T, top)
+
+
+def test_logits_far_from_zero(weights):
+    """256 z c as large as the short way takes them, where its roundings are largest."""
+    rng = np.random.default_rng(3)
+    n = 400000
+    T = np.exp(rng.uniform(np.log(0.05), np.log(5), n)).astype(np.float32)
+    top = (T * rng.uniform(5000, 12000, n) * rng.choice([-1, 1], n)).astype(np.float32)
+    _check(weights, top, T, (top - T * rng.uniform(0, 33, n)).astype(np.float32))
 
 
 def test_logits_and_temperatures_of_any_size(weights):
