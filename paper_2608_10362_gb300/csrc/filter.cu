@@ -21,8 +21,9 @@
 //      are queued and searched alone (search_above).  Draws under larger k queue the ids
 //      above the bound, or a little below it, and search those by count, then by weights;
 //   4. else a search per part (top-k, then top-p among what top-k left): a histogram of the
-//      elements' depth below the maximum, 16 bins an octave, with counts and for top-p the
-//      weights' sums, exact in 64 bits by two 32-bit atomics; the CTAs add up each other's
+//      elements.  For top-k counts, by depth below the maximum, 16 bins an octave of it; for
+//      top-p counts and sums of weights (exact in 64 bits by two 32-bit atomics), by weight, nine
+//      bins an octave of it (the queues of 3. have bins of one width).  The CTAs add up each other's
 //      bins through distributed shared memory to find the bin with the cut, and list
 //      its elements - or all up to there, where they are few enough; top-p alone lists
 //      candidates on the way (masks), and is done where they hold p of the sum.  A bin with
@@ -36,14 +37,18 @@
 //
 // Measured (us, one launch in a graph; 4 V bytes a row at 6780 GB/s are 0.02 to 11):
 //                       no cut  top-k 50  k, p  k 1000, p 0.9  top-p 0.9  flat, top-p 0.9
-//     1 x  32000           5.6       7.1   7.9          15.7       14.6             17.7
-//     1 x 128256           9.7       8.2   8.9                     14.9             30.1
-//    16 x 128256          14.2      10.3  11.4          25.6       22.3             42.1
-//   144 x 128256          55.6      36.4  37.2          84.4       75.0            160.9
-// One row is bound by latency: load, three to ten barriers of the cluster at 0.7 us each,
-// list and draw.  A batch is bound by the issue rate: 8 instructions an element for the load
-// and the maximum, 45 for an exact weight, 8 for a rough one, three atomics for a bin; three
-// CTAs an SM are 51 clusters, so 144 rows run in three waves.
+//     1 x  32000           5.5       6.9   7.6          15.4       14.3             17.9
+//     1 x 128256           9.6       7.9   8.7          19.3       14.9             30.2
+//    16 x 128256          14.1      10.2  11.3          25.5       22.5             42.5
+//   144 x 128256          56.2      36.2  37.3          84.4       76.2            161.8
+// (op_sample, which knows no rule, takes 19.1 for the last one without a cut; greedy rows 32.2
+// here, 13.3 there.)  One row is bound by latency: load, three to ten barriers of the cluster at
+// 0.7 us each, list and draw.  A batch is bound by how rows are held: a row keeps a cluster of 8
+// CTAs and its shared memory from load to draw, 51 rows fit, so that 144 run in three waves whose
+// CTAs load, then wait, then search together.  An SM has a CTA for 70 to 79% of the time, and
+// then 37 to 47% of its issue slots are used; warps wait at barriers most, without a cut for the
+// weights' arithmetic (50 instructions an element, 8 of them load and maximum, some 30 the weight;
+// 8 for a rough weight).
 #include <cuda_runtime.h>
 
 #include <math.h>

@@ -18,13 +18,18 @@
 //      launch still runs (everything before it has completed when this one starts).
 //
 // Measured (us in a graph, inputs from memory; floor: every operand moved once at 6780 GB/s):
-// 1 row, 4096 x 4096, rank 16: 4.9 (floor 0.04; a call is 14, the host's); 16 rows of 16
-// adapters: 6.0 (0.54); 144 rows of 16 adapters, n 28672, k 4096, ranks up to 64: 26.7 (9.95;
+// 1 row, 4096 x 4096, rank 16: 4.8 (floor 0.04; a call is 12 to 16, the host's); 16 rows of 16
+// adapters: 5.9 (0.54); 144 rows of 16 adapters, n 28672, k 4096, ranks up to 64: 26.2 (9.95;
 // 20.6 with the operands in L2): 8 us until t is there, then 18 for 77 MB, the first CTAs done
 // after 9; 256 rows of one adapter, n 4096, k 14336, rank 128: 18.4 (3.0), two to
 // find the chunk, five for 58 MB through L2 in groups of 32 ranks and rows, two for the sums'
-// exchange, four to five in the expansion, the rest launches; 21 rows, n 32003: 10.8
+// exchange, four to five in the expansion, the rest launches; 21 rows, n 32003: 10.6
 // (1.95), a base and a y without alignment moved 4 bytes at a time.
+//
+// Products are exact and every sum is fp32, but the tensor cores' additions may truncate, where
+// separate ones round: over long k and many ranks the result is up to some twice as far from 64 bits
+// as sums in 32 bits are (256 rows, k 14336, rank 128: 4.7e-7 of its norm, 2.9e-7; 144 rows, k 4096,
+// rank 64: 0.9e-7, 2.0e-7; one row, rank 16: 0.5e-7, 0.6e-7).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

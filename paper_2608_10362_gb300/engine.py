@@ -354,7 +354,9 @@ def _as_triples(weights):
 # ------------------------------------------------------------------ op-level calls
 # These wrap one or two kernel launches of a few microseconds, so the wrapper's own
 # time counts: the stream is read as a raw handle, and what is a function of sizes
-# alone is remembered by size.
+# alone is remembered by size.  With `stream` the launches go there: inputs have to be
+# complete in its order, and its work done (or waited for) before the result is used elsewhere;
+# memory is kept for both sides by _new, _new_result and _used_on.
 def _raw_stream(x: torch.Tensor, stream) -> int:
     """cudaStream_t of `stream`, else of the current stream of x's device."""
     if stream is not None:
