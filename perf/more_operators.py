@@ -239,7 +239,7 @@ def prepare(case, seed):
         s.prefix = _store(case, seed, 20, 1, case["prefix"])
     s.q = _normal(seed, 1, (n, H, hd), 2.0)
     s.mask = None if mask is None else dev(mask)
-    s.scratch = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    s.scratch = torch.empty((64 << 20) + 16 * n * H * (hd + 8), dtype=torch.uint8, device=DEV)
     return s
 
 
