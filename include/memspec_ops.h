@@ -195,6 +195,119 @@ memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x_dev, 
                                float* y_dev, int64_t ldy, int32_t rows, int32_t n_out, int32_t k,
                                void* scratch_dev, size_t scratch_bytes, void* stream);
 
+/* ---- a layer's cache and attention -----------------------------------------
+ * What lies between a layer's Q/K/V projection and its O projection, for callers
+ * that put layers together from the calls above; the steps' own projections and
+ * attention are others.
+ *
+ * The keys and values of one layer: position `pos` of sequence `seq` in head h
+ * starts at k_dev + seq * seq_stride + h * head_stride + pos * pos_stride
+ * (elements; a stride of a dimension of size 1 is not read), head_dim values
+ * without gaps.  Without scales they are bf16 (a layer of a context's own cache is
+ * one of these); with them signed 8-bit codes, value = code * scale, one fp32
+ * scale per vector at scale + seq * scale_seq_stride + ...  A scale below 2^-64
+ * counts as 2^-64.  k and v 16-byte aligned, their strides multiples of 16 bytes. */
+typedef struct memspec_kv {
+  void* k_dev;
+  void* v_dev;
+  float* k_scale_dev;       /* NULL, then v_scale_dev too: bf16 */
+  float* v_scale_dev;
+  int64_t seq_stride, head_stride, pos_stride;
+  int64_t scale_seq_stride, scale_head_stride, scale_pos_stride;
+  int32_t n_seq, n_heads, max_pos;
+  int32_t head_dim;         /* 64 or 128 */
+} memspec_kv;
+
+/* Which rows of a call belong to which sequence: rows starts[b] .. starts[b+1]-1
+ * to the cache's b-th, whose positions with these rows' own are lens[b]; row j of
+ * the n has slot lens[b] - n + j.  A sequence may have no rows.  Both arrays are
+ * the device's and cannot be checked: starts have to ascend; what lies outside the
+ * call's rows, and slots outside 0..max_pos-1, do not count.  Rows in no sequence
+ * are left as they were in every output. */
+typedef struct memspec_batch {
+  const int32_t* starts_dev;   /* [n_seq + 1] */
+  const int32_t* lens_dev;     /* [n_seq] */
+  int32_t n_seq;               /* 1..1024, at most the cache's */
+  int32_t rows;                /* of the call's tensors: 1..65535 */
+} memspec_batch;
+
+typedef enum memspec_value_type { MEMSPEC_F32 = 0, MEMSPEC_BF16 = 1 } memspec_value_type;
+
+/* cos and sin of pos * base^(-2i/head_dim), angles in 64 bits: fp32
+ * [2][positions][head_dim/2]. */
+memspec_status memspec_op_rope_table(int32_t positions, int32_t head_dim, float base, float* table_dev,
+                                     void* stream);
+
+typedef struct memspec_append {
+  const void* qkv_dev;        /* rows of [n_heads | kv heads | kv heads][head_dim] */
+  int32_t qkv_type;           /* memspec_value_type */
+  int32_t n_heads;            /* 1..1024 */
+  int64_t ld;                 /* elements from row to row, even (of a single row not read) */
+  const float* rope_dev;      /* memspec_op_rope_table's, or NULL: no rotation */
+  int32_t rope_positions;
+  int32_t prefix_len;         /* positions before the cache's first slot */
+  const int32_t* offsets_dev; /* [rows] or NULL: j */
+  const void* q_gain_dev;     /* bf16 [head_dim], or NULL with k_gain_dev: no norms */
+  const void* k_gain_dev;
+  float eps;                  /* >= 0 */
+  void* q_dev;                /* out: bf16 [rows][n_heads][head_dim] */
+} memspec_append;
+
+/* The rows of a Q/K/V projection (memspec_op_linear's result, say) into queries and
+ * into the cache, at the rows' slots.  Each head's q and k become
+ * x / sqrt(mean(x^2) + eps) * gain, then the pairs (i, i + head_dim/2) are turned by
+ * the angles of position prefix_len + lens[b] - n + offset (a draft tree's row: its
+ * depth).  q is rounded to bf16; k and v to bf16, or to codes rint(x / s) with
+ * s = max(max|x|, 127 * 2^-64) / 127 over the vector.  Arithmetic is fp32.  A row
+ * whose slot or position (where there is a table) is out of range leaves the cache
+ * as it was, and its q is 0.  A vector with an infinity or a NaN is not finite when
+ * it is read, others are not affected.  The cache's vectors must not overlap, nor
+ * q any other argument; qkv is aligned to two elements.
+ * Allocates nothing.  Errors: INVALID_ARG, CUDA. */
+memspec_status memspec_op_kv_append(const memspec_batch* batch, const memspec_kv* kv,
+                                    const memspec_append* args, void* stream);
+
+/* The rows' keys and values as the cache holds them: bf16 [rows][kv heads][head_dim]
+ * each, codes times their scale rounded once; 0 at a slot out of range.  Allocates
+ * nothing.  Errors: INVALID_ARG, CUDA. */
+memspec_status memspec_op_kv_read(const memspec_batch* batch, const memspec_kv* kv, void* k_out_dev,
+                                  void* v_out_dev, void* stream);
+
+typedef struct memspec_attention {
+  const void* q_dev;            /* bf16 [rows][n_heads][head_dim], 16-byte aligned */
+  int64_t ldq;                  /* elements from row to row, a multiple of 8 */
+  void* out_dev;                /* bf16 [rows][n_heads][head_dim], 16-byte aligned */
+  int64_t ldo;                  /* as ldq (of a single row neither is read) */
+  int32_t n_heads;              /* a multiple of the cache's, up to 64 times it */
+  float scale;                  /* of q . k, finite */
+  const int32_t* tree_dev;      /* [rows] or NULL */
+  const memspec_kv* prefix;     /* or NULL: its sequence 0 is before every sequence's positions */
+  int32_t prefix_len;           /* 0..prefix->max_pos */
+  int32_t max_rows;             /* of one sequence: what the call is laid out for (1..rows) */
+} memspec_attention;
+
+/* Scratch bytes of memspec_op_attention.  Errors: INVALID_ARG. */
+memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, const memspec_kv* kv,
+                                                  const memspec_attention* args, size_t* bytes);
+
+/* out = sum_i w_i v_i / sum_i w_i, w_i = exp(scale q . k_i), for every row and head
+ * (head h reads head h / (n_heads / kv heads) of the cache), over the prefix and the
+ * sequence's slots up to the row's own; with tree_dev over its slots before the
+ * first row's own and those of the rows j < 32 of the sequence whose bit j is set.
+ * A row that sees nothing gives 0.  All sequences share the prefix, which is read
+ * once for all of them; it has the cache's heads and head_dim, its own strides and
+ * type.  q . k and sums are fp32; the weights enter the product with v in 16 bits
+ * (of bf16 caches bf16, of codes fp16), off by half a step of it each.
+ * Slots that a row does not see do not reach it, whatever they hold; an infinity
+ * or a NaN in q, or in a key or value that it sees, makes that row and head
+ * unspecified.  q may be out if ldq == ldo; else out overlaps no other argument.
+ * A sequence of more than max_rows rows gives the same, at another speed.
+ * Deterministic.  scratch_dev: 16-byte aligned, any content; calls that may overlap
+ * need scratches of their own.  Allocates nothing.  Errors: INVALID_ARG, CUDA. */
+memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv* kv,
+                                    const memspec_attention* args, void* scratch_dev, size_t scratch_bytes,
+                                    void* stream);
+
 /* Message describing the last failed op-level call (or memspec_init) on this
  * host thread; never NULL. */
 const char* memspec_op_last_error(void);

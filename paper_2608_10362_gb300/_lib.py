@@ -96,6 +96,35 @@ class Lora(C.Structure):
                 ("ranks_dev", C.c_void_p), ("n_adapters", C.c_int32), ("rank", C.c_int32)]
 
 
+# a layer's cache and attention (memspec_ops.h)
+F32, BF16 = 0, 1
+
+
+class Kv(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("k_scale_dev", C.c_void_p),
+                ("v_scale_dev", C.c_void_p), ("seq_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("pos_stride", C.c_int64), ("scale_seq_stride", C.c_int64), ("scale_head_stride", C.c_int64),
+                ("scale_pos_stride", C.c_int64), ("n_seq", C.c_int32), ("n_heads", C.c_int32),
+                ("max_pos", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Batch(C.Structure):
+    _fields_ = [("starts_dev", C.c_void_p), ("lens_dev", C.c_void_p), ("n_seq", C.c_int32), ("rows", C.c_int32)]
+
+
+class Append(C.Structure):
+    _fields_ = [("qkv_dev", C.c_void_p), ("qkv_type", C.c_int32), ("n_heads", C.c_int32), ("ld", C.c_int64),
+                ("rope_dev", C.c_void_p), ("rope_positions", C.c_int32), ("prefix_len", C.c_int32),
+                ("offsets_dev", C.c_void_p), ("q_gain_dev", C.c_void_p), ("k_gain_dev", C.c_void_p),
+                ("eps", C.c_float), ("q_dev", C.c_void_p)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("q_dev", C.c_void_p), ("ldq", C.c_int64), ("out_dev", C.c_void_p), ("ldo", C.c_int64),
+                ("n_heads", C.c_int32), ("scale", C.c_float), ("tree_dev", C.c_void_p), ("prefix", C.POINTER(Kv)),
+                ("prefix_len", C.c_int32), ("max_rows", C.c_int32)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "memspec_weights_bytes": (C.c_int, [C.POINTER(ModelCfg), C.POINTER(C.c_size_t)]),
@@ -147,6 +176,13 @@ EXPORTS = {
     "memspec_op_lora": (C.c_int, [C.POINTER(Lora), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
                                   C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                   C.c_size_t, C.c_void_p]),
+    "memspec_op_rope_table": (C.c_int, [C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p]),
+    "memspec_op_kv_append": (C.c_int, [C.POINTER(Batch), C.POINTER(Kv), C.POINTER(Append), C.c_void_p]),
+    "memspec_op_kv_read": (C.c_int, [C.POINTER(Batch), C.POINTER(Kv), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "memspec_op_attention_scratch_bytes": (C.c_int, [C.POINTER(Batch), C.POINTER(Kv), C.POINTER(Attention),
+                                                     C.POINTER(C.c_size_t)]),
+    "memspec_op_attention": (C.c_int, [C.POINTER(Batch), C.POINTER(Kv), C.POINTER(Attention), C.c_void_p,
+                                       C.c_size_t, C.c_void_p]),
     "memspec_op_last_error": (C.c_char_p, []),
     "memspec_pack_matrix": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
                                       C.c_size_t, C.c_void_p]),
