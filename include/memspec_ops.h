@@ -206,7 +206,9 @@ memspec_status memspec_op_lora(const memspec_lora* adapters, const void* x_dev, 
  * without gaps.  Without scales they are bf16 (a layer of a context's own cache is
  * one of these); with them signed 8-bit codes, value = code * scale, one fp32
  * scale per vector at scale + seq * scale_seq_stride + ...  A scale below 2^-64
- * counts as 2^-64.  k and v 16-byte aligned, their strides multiples of 16 bytes. */
+ * counts as 2^-64.  k and v 16-byte aligned, their strides multiples of 16 bytes and
+ * at most 2^38 elements, positions at least head_dim apart.  Sequences or heads may
+ * lie on one another (stride 0) in a cache that is only read. */
 typedef struct memspec_kv {
   void* k_dev;
   void* v_dev;
@@ -214,7 +216,8 @@ typedef struct memspec_kv {
   float* v_scale_dev;
   int64_t seq_stride, head_stride, pos_stride;
   int64_t scale_seq_stride, scale_head_stride, scale_pos_stride;
-  int32_t n_seq, n_heads, max_pos;
+  int32_t n_seq, n_heads;   /* heads: 1..1024 */
+  int32_t max_pos;          /* positions: 1..2^30 */
   int32_t head_dim;         /* 64 or 128 */
 } memspec_kv;
 

@@ -1,0 +1,300 @@
+// attn_join.cu - memspec_op_attention: which kernels a call's parts run, and the launch that joins
+// the records of units whose keys several CTAs had (attn_plan.cuh).
+//
+// A record is HD sums of weights times values, the maximum the weights were taken against and their
+// sum; records of one vector add up after each is scaled to the largest maximum, in the order of
+// the line.  A warp takes a row's head, its lanes the elements.
+#include <algorithm>
+#include <string>
+
+#include "attn_plan.cuh"
+#include "ptx.cuh"
+
+namespace memspec {
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+// Up to so many vectors per head of k and v: attn_rows.cu, in units of so many; more: attn_tiles.cu
+constexpr int kRowsVectors = 16;
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ JoinArgs a) {
+  constexpr int E = HD / 32;
+  __shared__ int found[4];
+  const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32, heads = a.group * a.kv_heads;
+  // (starts and lens were complete before the launch before this one began)
+  if (threadIdx.x == 0) found[0] = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.n_seq; b += kThreads) {
+    const SeqRows s = seq_rows(a.starts, a.lens, b, a.rows);
+    if (row >= s.row0 && row < s.row0 + s.n) found[0] = b, found[1] = s.row0, found[2] = s.n, found[3] = s.len;
+  }
+  __syncthreads();
+  pdl_wait();
+  pdl_launch_dependents();
+  const int h = blockIdx.y * kWarps + warp;
+  if (found[0] < 0 || h >= heads) return;
+  const int kv_head = h / a.group;
+  float top = kStart, den = 0.f, sum[E] = {};
+  bool any = false;
+#pragma unroll 1
+  for (int p = 0; p < a.parts; ++p) {
+    const JoinPart& part = a.part[p];
+    const bool own = part.at < 0;
+    const int b = own ? found[0] : part.at;
+    const uint32_t base = part.bases[b], total = part.bases[part.list];
+    const uint32_t vecs = (own ? found[2] : a.rows) * a.group, vec = (row - (own ? found[1] : 0)) * a.group + h - kv_head * a.group;
+    const uint32_t tiles = tiles_of(own ? min(max(found[3], 0), a.max_pos) : part.keys);
+    const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit, units = (vecs + part.unit - 1) / part.unit;
+    const uint32_t per_tile = part.pairs ? (vecs + 127) / 128 : units, w = part.pairs && vecs - unit * part.unit > 128 ? 2 : 1;
+    const bool pair = w == 2;
+    const uint32_t t0 = base + kv_head * (per_tile * tiles + units * part.start) +
+                        unit * ((part.pairs ? 2 : 1) * tiles + part.start);
+    const Pieces pieces(part.ctas, total, part.pairs ? 2 : 1);
+    // who has the first tile, the second and the last one: the CTAs between the first two have none
+    const int c0 = pieces.owner(t0), c1 = tiles > 1 ? pieces.owner(t0 + part.start + (tiles - 1) * w) : c0;
+    const int gap = tiles > 1 ? max(static_cast<int>(pieces.owner(t0 + part.start + w)) - c0 - 1, 0) : 0;
+    if (c0 == c1 && part.full == nullptr) continue;   // written by that CTA
+    any = true;
+    // The vector's records: `copies` of each CTA, one of attn_rows.cu, of attn_tiles.cu's smaller units two.
+    // attn_rows.cu's are one after another, attn_tiles.cu's side by side (chunks of 4 floats `chunk` apart)
+    const int copies = part.pairs && !pair ? 2 : 1, n = (c1 - c0 + 1 - gap) * copies;
+    const bool whole = c0 == c1;
+    const long long all = static_cast<long long>(a.rows) * heads, i = whole ? static_cast<long long>(row) * heads + h : in_unit;
+    const long long side = whole ? 2 * all : part.unit, chunk = part.pairs ? 4 * side : 4;
+    const float* first = (whole ? part.full : part.slots + 2 * c0 * static_cast<long long>(part.unit * kRecord<HD>)) +
+                         i * (part.pairs ? 4 : kRecord<HD>);
+    const long long to_md = part.pairs ? HD * side - 2 * i : HD;
+    // a stretch's records further on for each CTA, those of the one that begins the unit one further
+    auto record = [&](int r) {
+      const int c = copies == 2 ? r >> 1 : r, w = copies == 2 ? r & 1 : 0;
+      return first + (c > 0 ? 2 * (c + gap) : whole ? 0 : 1) * static_cast<long long>(part.unit * kRecord<HD>) +
+             w * (whole ? all : 128) * 4;
+    };
+    auto md_of = [&](int r) { return record(r) + to_md - (copies == 2 && (r & 1) ? 2 * (whole ? all : 128) : 0); };
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 32) {   // a lane has a record's maximum and sum of weights
+      const int here = min(n - i0, 32);
+      float2 md = make_float2(kStart, 0.f);
+      if (lane < here) md = *reinterpret_cast<const float2*>(md_of(i0 + lane));
+      float now = fmaxf(top, md.x);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) now = fmaxf(now, __shfl_xor_sync(~0u, now, o));
+      const float was = ex2(top - now), by = ex2(md.x - now);
+      float d = by * md.y;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(~0u, d, o);
+      den = fmaf(den, was, d);
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] *= was;
+#pragma unroll 4
+      for (int r = 0; r < here; ++r) {
+        const float f = __shfl_sync(~0u, by, r);
+        const float* rec = record(i0 + r) + (lane * E / 4) * chunk + lane * E % 4;
+        if constexpr (E == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(rec);
+          sum[0] = fmaf(x.x, f, sum[0]), sum[1] = fmaf(x.y, f, sum[1]);
+          sum[2] = fmaf(x.z, f, sum[2]), sum[3] = fmaf(x.w, f, sum[3]);
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(rec);
+          sum[0] = fmaf(x.x, f, sum[0]), sum[1] = fmaf(x.y, f, sum[1]);
+        }
+      }
+      top = now;
+    }
+  }
+  if (!any) return;
+  const float by = den == 0.f ? 0.f : 1.f / den;
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + h * HD + lane * E);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) out[e / 2] = pack_bf16(sum[e] * by, sum[e + 1] * by);
+}
+
+// ---------------------------------------------------------------- host
+// A launch of one of the two kernels over the batch's own keys, the prefix's, or both.
+struct Launch {
+  bool tiles, own, prefix, codes;
+  int nt;                       // attn_rows.cu: units of 8 nt vectors
+  size_t bases, slots;          // in the scratch
+  int ctas() const { return tiles ? kTilesCtas : rows_ctas(codes, nt); }
+  int unit() const { return tiles ? kTilesUnit : 8 * nt; }
+};
+struct Layout {
+  Launch launch[2];
+  int n;
+  size_t full[2], total;        // records of the cache's, of the prefix's units
+};
+
+Layout lay_out(const memspec_batch* b, const memspec_kv* kv, const memspec_attention* p) {
+  Layout l{};
+  const int group = p->n_heads / kv->n_heads;
+  const bool two = p->prefix != nullptr && p->prefix_len > 0;
+  auto launch = [&](const memspec_kv* part, long long vecs) {
+    Launch x{};
+    x.codes = part->k_scale_dev != nullptr;
+    x.tiles = vecs > kRowsVectors;
+    x.nt = vecs > 8 ? 2 : 1;
+    return x;
+  };
+  l.launch[0] = launch(kv, static_cast<long long>(p->max_rows) * group);
+  l.launch[0].own = true;
+  l.n = 1;
+  if (two) {
+    Launch x = launch(p->prefix, static_cast<long long>(b->rows) * group);
+    if (x.tiles && l.launch[0].tiles && x.codes == l.launch[0].codes) {
+      l.launch[0].prefix = true;
+    } else {
+      x.prefix = true;
+      l.launch[l.n++] = x;
+    }
+  }
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += (bytes + 255) & ~size_t{255};
+    return was;
+  };
+  const size_t record = (kv->head_dim + 4) * sizeof(float);
+  const size_t all = static_cast<size_t>(b->rows) * p->n_heads * record;
+  for (int i = 0; i < l.n; ++i) {
+    Launch& x = l.launch[i];
+    x.bases = take((static_cast<size_t>(b->n_seq) + 2) * sizeof(uint32_t));
+    x.slots = take(size_t{2} * x.ctas() * x.unit() * record);
+    // (attn_tiles.cu leaves two records of a vector, and never writes the result itself)
+    if (x.own && (two || x.tiles)) l.full[0] = take(all * (x.tiles ? 2 : 1));
+    if (x.prefix) l.full[1] = take(all * (x.tiles ? 2 : 1));
+  }
+  l.total = at;
+  return l;
+}
+
+bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+const char* attention_problem(const memspec_batch* b, const memspec_kv* kv, const memspec_attention* p) {
+  if (const char* why = kv_problem(kv, false)) return why;
+  if (const char* why = batch_problem(b, kv)) return why;
+  if (p == nullptr) return "null pointer";
+  if (p->n_heads < 1 || p->n_heads % kv->n_heads != 0 || p->n_heads / kv->n_heads > 64)
+    return "n_heads must be a multiple of the cache's heads, up to 64 times as many";
+  if (p->max_rows < 1 || p->max_rows > b->rows) return "max_rows must be in 1..rows";
+  if (!(p->scale >= -3e38f && p->scale <= 3e38f)) return "scale must be finite";
+  if (p->prefix != nullptr) {
+    if (const char* why = kv_problem(p->prefix, false)) return why;
+    if (p->prefix->n_heads != kv->n_heads || p->prefix->head_dim != kv->head_dim)
+      return "the prefix must have the cache's heads and head_dim";
+    if (p->prefix_len < 0 || p->prefix_len > p->prefix->max_pos) return "prefix_len must be in 0..the prefix's max_pos";
+  }
+  // tiles are counted in 32 bits; every vector tile has at most this many
+  const double vts = static_cast<double>(b->rows) * (p->n_heads / kv->n_heads) / 8 + b->n_seq;
+  const double keys = std::max(kv->max_pos, p->prefix != nullptr ? p->prefix_len : 0);
+  if (vts * kv->n_heads * (keys / kTile + 1 + kTilesStart) >= 4e9) return "too many rows for so many positions: split the call";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace memspec
+
+extern "C" {
+
+memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, const memspec_kv* kv,
+                                                  const memspec_attention* p, size_t* bytes) {
+  using namespace memspec;
+  const char* why = bytes == nullptr ? "null pointer" : attention_problem(batch, kv, p);
+  if (why != nullptr) {
+    set_op_error(why);
+    return MEMSPEC_ERR_INVALID_ARG;
+  }
+  *bytes = lay_out(batch, kv, p).total;
+  return MEMSPEC_OK;
+}
+
+memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv* kv, const memspec_attention* p,
+                                    void* scratch, size_t scratch_bytes, void* stream) {
+  using namespace memspec;
+  const char* why = attention_problem(batch, kv, p);
+  Layout l{};
+  if (why == nullptr) {
+    const int64_t row = static_cast<int64_t>(p->n_heads) * kv->head_dim;
+    l = lay_out(batch, kv, p);
+    if (p->q_dev == nullptr || p->out_dev == nullptr || scratch == nullptr) {
+      why = "null pointer";
+    } else if (misaligned(p->q_dev, 16) || misaligned(p->out_dev, 16) || misaligned(scratch, 16) ||
+               misaligned(p->tree_dev, 4)) {
+      why = "q, out and scratch must be 16-byte aligned, tree 4-byte";
+    } else if (batch->rows > 1 && (p->ldq < row || p->ldo < row || p->ldq % 8 != 0 || p->ldo % 8 != 0 ||
+                                   std::max(p->ldq, p->ldo) > INT64_C(1) << 40)) {
+      why = "row strides must be multiples of 8 that cover a row, at most 2^40";
+    } else if (p->q_dev == p->out_dev) {
+      why = "out must not be q";
+    } else if (scratch_bytes < l.total) {
+      why = "scratch too small";
+    }
+  }
+  if (why != nullptr) {
+    set_op_error(why);
+    return MEMSPEC_ERR_INVALID_ARG;
+  }
+  char* const mem = static_cast<char*>(scratch);
+  const bool two = p->prefix != nullptr && p->prefix_len > 0;
+  ListArgs a{};
+  a.kv[0] = kv_view(kv);
+  if (two) a.kv[1] = kv_view(p->prefix);
+  a.starts = batch->starts_dev;
+  a.lens = batch->lens_dev;
+  a.rows = batch->rows;
+  a.q = static_cast<const bf16*>(p->q_dev);
+  a.ldq = batch->rows > 1 ? p->ldq : 0;
+  a.scale = p->scale * 1.4426950408889634f;
+  a.group = p->n_heads / kv->n_heads;
+  a.kv_heads = kv->n_heads;
+  a.group_magic = a.group == 1 ? 0u : static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group);
+  a.ldo = batch->rows > 1 ? p->ldo : 0;
+  JoinArgs j{};
+  j.starts = batch->starts_dev;
+  j.lens = batch->lens_dev;
+  j.n_seq = batch->n_seq;
+  j.rows = batch->rows;
+  j.max_pos = kv->max_pos;
+  j.group = a.group;
+  j.kv_heads = kv->n_heads;
+  j.out = static_cast<bf16*>(p->out_dev);
+  j.ldo = a.ldo;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaSuccess;
+  for (int i = 0; i < l.n && e == cudaSuccess; ++i) {
+    const Launch& x = l.launch[i];
+    a.n_own = x.own ? batch->n_seq : 0;
+    a.prefix_len = x.prefix ? p->prefix_len : 0;
+    a.tree = x.own ? p->tree_dev : nullptr;
+    const bool direct = !two && !x.tiles;
+    a.out = direct ? j.out : nullptr;
+    for (int k = 0; k < 2; ++k) a.full[k] = direct ? nullptr : reinterpret_cast<float*>(mem + l.full[k]);
+    a.slots = reinterpret_cast<float*>(mem + x.slots);
+    a.bases = reinterpret_cast<uint32_t*>(mem + x.bases);
+    for (int k = 0; k < 2; ++k)
+      if (k == 0 ? x.own : x.prefix)
+        j.part[j.parts++] = {a.bases, a.slots, a.full[k], x.ctas(), a.n_own + (x.prefix ? 1 : 0), k == 0 ? -1 : a.n_own,
+                             p->prefix_len, x.unit(), x.tiles ? kTilesStart : kRowsStart, x.tiles ? 1 : 0};
+    e = x.tiles ? launch_attn_tiles(kv->head_dim, x.codes, a, cfg)
+                : launch_attn_rows(kv->head_dim, x.codes, x.nt, a, cfg);
+  }
+  if (e == cudaSuccess) {
+    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3(batch->rows, (p->n_heads + kWarps - 1) / kWarps);
+    e = kv->head_dim == 64 ? cudaLaunchKernelEx(&cfg, join_kernel<64>, j) : cudaLaunchKernelEx(&cfg, join_kernel<128>, j);
+  }
+  if (e != cudaSuccess) {
+    set_op_error(std::string("attention launch: ") + cudaGetErrorString(e));
+    return MEMSPEC_ERR_CUDA;
+  }
+  return MEMSPEC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,744 @@
+// attn_tiles.cu - attention over a caller's cache for many query vectors per key: the verify
+// rows of a batch, prompts, and a prefix that all rows share (memspec_op_attention).
+//
+// A unit (attn_plan.cuh) is up to 256 query vectors of one head of k and v.  The vectors are the
+// rows of tcgen05 MMAs of M = 128, S = Q K^T and O += P V over tiles of 128 keys, S and O in
+// tensor memory, P written over S.  Two softmax warpgroups, a thread per row:
+//   units of more than 128 vectors: each has 128 of them and both halves of every tile, so that
+//   a tile that was read once serves 256 vectors;
+//   smaller ones: both have the same vectors, and a half of every tile each.
+// A step is 64 keys of a warpgroup: its scores pass through registers once, and S has two buffers, so
+// that the next step's MMAs run during this one's softmax.
+// Every CTA takes an equal piece of the call's work whatever the lengths are, and leaves records
+// of sums (two per vector for the smaller units) that attn_join.cu puts together.
+//
+// K and V pass through two slots each in shared memory, K-major and N-major alike [key][hd] with the
+// 128-byte swizzle.  bf16 comes by TMA; codes are turned into fp16 on the way, which
+// holds them exactly, by the warps that fetch them.  K's scales multiply the scores, V's are added as
+// logarithms: the weights are w' = p * scale_v, against a maximum of their own kind, and the sum of p
+// that of w' / scale_v; so no range of scales overflows fp16.  Q is taken to fp16 by a power of two.
+//
+// Roles (512 threads): warps 0-3, 4-7 softmax, 8-11 copies, 12 and 13 the MMAs of
+// each, 14 Q, 15 which units these are.  Every wait is bounded; after one that ran out the CTA's remaining records are NaN.
+#include <algorithm>
+#include <atomic>
+
+#include "attn_plan.cuh"
+#include "ptx.cuh"
+
+namespace memspec {
+
+namespace {
+
+constexpr int kThreads = 512, kCopy = 64, kQ = 32;   // kCopy: for K, and as many for V
+constexpr int kSlots = 4;               // tiles in shared memory: K of two, V of two
+constexpr int kScaleSets = 4;           // a tile's scales are read until its P is written
+constexpr int kListed = 4;              // stretches told of at a time
+constexpr int kStep = 64;               // keys of a warpgroup's step
+typedef Cut<kTilesUnit, true, kTilesStart> Units;
+
+template <int HD_, bool CODES_>
+struct Shape {
+  static constexpr int HD = HD_;
+  static constexpr bool CODES = CODES_;
+  static constexpr int kSlotBytes = kTile * HD * 2;
+  static constexpr int kQBytes = 128 * HD * 2;         // of 128 vectors
+  static constexpr int kScaleBytes = CODES ? kScaleSets * 3 * kTile * 4 : 0;
+  static constexpr int kSmem = 1024 + kSlots * kSlotBytes + 2 * kQBytes + kScaleBytes;
+};
+
+struct Ctl {
+  uint64_t full[kSlots], empty[kSlots];
+  uint64_t raw[2];           // V of an edge tile has landed, but is still to be looked over
+  uint64_t q_full;           // a stretch's vectors are there
+  uint64_t q_free[2];        // its last S is complete: every second stretch, so that who waits is never a phase late
+  uint64_t s_full[2][2];     // [warpgroup][buffer] S of a step is complete
+  uint64_t p_full[2][2];     // ... its P is written (4 warps)
+  uint64_t o_full[2][2];     // ... its P V is complete
+  uint64_t drain[2];
+  uint32_t tmem_base;
+  int abort_flag;
+  uint32_t bad[2][kTile / 32];        // keys of an edge tile whose values are not all finite
+  float q_down[4];                    // 1 / the power of two that a stretch's Q was taken by; the next one's Q may be
+                                      // there, and the one's after it begun, before this one's softmax reads its own
+  Plan plan;
+  uint64_t listed[kListed];           // a stretch's entry is there
+  Stretch list[kListed];              // (none: t0 == t1)
+};
+
+// 32 TMEM lanes x 32 consecutive columns, a lane per thread: load (and wait) ...
+__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, float* v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+// ... 64 columns ...
+__device__ __forceinline__ void tmem_ld_x64(uint32_t taddr, float* v) {
+  uint32_t r[64];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
+}
+// ... and store (tmem_st_wait completes it).
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {"
+      "%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor: fp32 sums, A and B both bf16 or both fp16.
+template <bool F16>
+constexpr uint32_t idesc(int m, int n) {
+  return make_idesc_bf16_f32(m, n) & ~(F16 ? (1u << 7) | (1u << 10) : 0u);
+}
+
+// The slot of tile t (of the CTA) of K or V, and how often it has been used before.
+__device__ __forceinline__ int slot_of(int t, int is_v) { return 2 * is_v + (t & 1); }
+__device__ __forceinline__ int use_of(int t) { return t >> 1; }
+
+struct TileMaps {   // of the caches of bf16
+  CUtensorMap k[2], v[2];
+};
+// 5-D box: 64 columns, 128 positions, hd / 64 halves of one head and sequence
+__device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, int pos, int head, int seq, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::"r"(smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(pos), "r"(head), "r"(seq), "r"(smem_addr(bar))
+      : "memory");
+}
+
+// Byte of element chunk c (16 bytes) of row r in an operand tile of 128 rows.
+__device__ __forceinline__ int chunk_at(int r, int c) { return (c >> 3) * (128 * 128) + r * 128 + (((c ^ r) & 7) << 4); }
+
+// The stretches of a CTA, as the roles go through them: one lane works them out (walk_role), and is
+// never so far ahead that an entry is written again before all have read it.
+struct Stretches {
+  Ctl& ctl;
+  int at = 0;
+  __device__ explicit Stretches(Ctl& c) : ctl(c) {}
+  __device__ __forceinline__ bool next(Stretch& u) {
+    const int i = at % kListed;
+    if (!__all_sync(~0u, mbar_wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, &ctl.abort_flag, nullptr)))
+      return false;
+    u = ctl.list[i];
+    ++at;
+    return u.t0 < u.t1;
+  }
+};
+__device__ __forceinline__ void walk_role(const ListArgs& a, Ctl& ctl) {
+  Walk<Units> walk(a, ctl.plan);
+  Stretch u;
+  bool more = true;
+#pragma unroll 1
+  for (int i = 0; more; ++i) {
+    more = walk.next(u);
+    if (!more) u.t0 = u.t1 = 0;
+    // the last S of the stretch before last is complete: so are the roles' steps of the one two before that
+    if (i >= 2 && !mbar_wait_bounded(&ctl.q_free[i & 1], static_cast<uint32_t>(i - 2 >> 1) & 1u, &ctl.abort_flag, nullptr)) return;
+    ctl.list[i % kListed] = u;
+    mbar_arrive(&ctl.listed[i % kListed]);
+  }
+}
+__device__ __forceinline__ bool is_pair(const Stretch& u) { return Units::weight(u.vecs, u.unit) == 2; }
+// ---------------------------------------------------------------- copies
+// A tile of V that not every vector sees all of: rows of the sequence's own, or rows past the keys' end.
+__device__ __forceinline__ bool own_rows(const Stretch& u, int t) { return u.own && (t + 1) * kTile > u.first; }
+__device__ __forceinline__ bool is_edge(const Stretch& u, int t) { return own_rows(u, t) || (t + 1) * kTile > u.end(); }
+
+// bf16: one lane for K, one for V.
+template <class S>
+__device__ __forceinline__ void tma_role(const ListArgs& a, const TileMaps& maps, Ctl& ctl, int is_v, uint8_t* ring) {
+  Stretches walk(ctl);
+  volatile int* abort_flag = &ctl.abort_flag;
+  int tile = 0;
+  uint64_t* last[2] = {nullptr, nullptr};   // what the last loads of the two slots complete, and its phase
+  uint32_t raws = 0, phase[2] = {0, 0};
+  bool ok = true;
+  Stretch u;
+#pragma unroll 1
+  while (ok && walk.next(u)) {
+    const int part = u.own ? 0 : 1;
+    const CUtensorMap* map = is_v ? &maps.v[part] : &maps.k[part];
+    const int seq = u.own && a.kv[0].seq != 0 ? u.b : 0, head = a.kv[part].head != 0 ? u.head : 0;
+#pragma unroll 1
+    for (int t = u.t0; t < u.t1; ++t, ++tile) {
+      const int s = slot_of(tile, is_v), i = s & 1;
+      if (use_of(tile) > 0 &&
+          !__all_sync(~0u, mbar_wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, abort_flag, nullptr))) {
+        ok = false;
+        break;
+      }
+      const bool edge = is_v && is_edge(u, t);
+      uint64_t* bar = edge ? &ctl.raw[i] : &ctl.full[s];
+      if (threadIdx.x % 32 == 0) {
+        mbar_arrive_expect_tx(bar, S::kSlotBytes);
+        tma_load_5d(ring + s * S::kSlotBytes, map, t * kTile, head, seq, bar);
+      }
+      last[i] = bar;
+      phase[i] = edge ? raws >> i & 1u : static_cast<uint32_t>(use_of(tile)) & 1u;
+      if (edge) raws ^= 1u << i;
+      __syncwarp();
+    }
+  }
+  if (!ok)   // no copy is in flight when the CTA leaves
+    for (int i = 0; i < 2; ++i)
+      if (last[i] != nullptr) mbar_wait_drain(last[i], phase[i]);
+}
+
+// bf16: the edge tiles of V, by kCopy threads: zeros where the keys have ended (a weight of 0 times
+// what lies there need not be 0), and for infinities and NaN of the rows' own, whose keys are noted.
+template <class S>
+__device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
+  constexpr int C = S::HD / 8;
+  const int tid = threadIdx.x % kCopy;
+  Stretches walk(ctl);
+  int tile = 0;
+  uint32_t raws = 0;
+  Stretch u;
+#pragma unroll 1
+  while (walk.next(u)) {
+#pragma unroll 1
+    for (int t = u.t0; t < u.t1; ++t, ++tile) {
+      if (!is_edge(u, t)) continue;
+      const int s = slot_of(tile, 1), i = s & 1, key0 = t * kTile;
+      if (!__all_sync(~0u, mbar_wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag, nullptr))) return;
+      raws ^= 1u << i;
+      if (tid < kTile / 32) ctl.bad[i][tid] = 0u;
+      named_bar_sync(2, kCopy);
+      const int live = min(u.end() - key0, kTile);
+      const int from = own_rows(u, t) ? static_cast<int>(max(u.first - key0, 0ll)) : live;
+#pragma unroll 1
+      for (int at = min(from, live) * C + tid; at < kTile * C; at += kCopy) {
+        const int r = at / C;
+        uint4* p = reinterpret_cast<uint4*>(ring + s * S::kSlotBytes + chunk_at(r, at % C));
+        bool odd = r >= live;
+        if (!odd) {
+          const uint32_t x[4] = {p->x, p->y, p->z, p->w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) odd |= (x[j] & 0x7f80u) == 0x7f80u || (x[j] & 0x7f800000u) == 0x7f800000u;
+          if (odd) atomicOr(&ctl.bad[i][r / 32], 1u << r % 32);
+        }
+        if (odd) *p = make_uint4(0u, 0u, 0u, 0u);
+      }
+      fence_proxy_async_smem();
+      named_bar_sync(2, kCopy);
+      if (tid == 0) mbar_arrive(&ctl.full[s]);
+    }
+  }
+}
+
+// Codes: kCopy threads for K, with the scales of both, and kCopy for V.  64 bytes of a row by four lanes: a
+// thread's 16 codes are two chunks of fp16.  The next tile is in registers while this one waits for its slot.
+template <class S>
+__device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v, uint8_t* ring, float* scales) {
+  constexpr int J = S::HD / 64, N = kTile * 4 / kCopy;   // parts of a row, rows
+  const int tid = threadIdx.x % kCopy, r0 = tid / 4, c = tid % 4;
+  Stretches walk(ctl);
+  int tile = 0;
+  Stretch u;
+#pragma unroll 1
+  while (walk.next(u)) {
+    const KvView& kv = a.kv[u.own ? 0 : 1];
+    const int seq = u.own ? u.b : 0, end = u.end();
+    const char* base = (is_v ? kv.v : kv.k) + seq * kv.seq + u.head * kv.head;
+    const float* ks = kv.k_scale + seq * kv.s_seq + u.head * kv.s_head;
+    const float* vs = kv.v_scale + seq * kv.s_seq + u.head * kv.s_head;
+    uint4 in[N * J];
+    float sc[4] = {0.f, 0.f, 0.f, 0.f};
+    auto fetch = [&](int t) {
+      int key = t * kTile + r0;
+      const char* src = base + key * kv.pos + c * 16;
+      const long long step = kv.pos * (kCopy / 4);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+          in[n * J + j] = key < end ? __ldcs(reinterpret_cast<const uint4*>(src + j * 64)) : make_uint4(0, 0, 0, 0);
+        key += kCopy / 4;
+        src += step;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        key = t * kTile + tid + i * kCopy;
+        if (!is_v) {
+          sc[i] = key < end ? ks[key * kv.s_pos] : 0.f;
+          sc[2 + i] = key < end ? vs[key * kv.s_pos] : 0.f;
+        }
+        if (key + 2 * kTile < end)   // a later tile's lines into L2
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(base + (key + 2 * kTile) * kv.pos));
+      }
+    };
+    fetch(u.t0);
+#pragma unroll 1
+    for (int t = u.t0; t < u.t1; ++t, ++tile) {
+      const int s = slot_of(tile, is_v);
+      if (use_of(tile) > 0 &&
+          !__all_sync(~0u, mbar_wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, &ctl.abort_flag, nullptr)))
+        return;
+      uint8_t* slot = ring + s * S::kSlotBytes;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const uint4 x = in[n * J + j];
+          const uint32_t w[4] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u, x.z ^ 0x80808080u, x.w ^ 0x80808080u};
+          const int r = r0 + n * (kCopy / 4), ch = j * 8 + c * 2;
+          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch)) = make_uint4(
+              codes_f16<0x4140>(w[0]), codes_f16<0x4342>(w[0]), codes_f16<0x4140>(w[1]), codes_f16<0x4342>(w[1]));
+          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch + 1)) = make_uint4(
+              codes_f16<0x4140>(w[2]), codes_f16<0x4342>(w[2]), codes_f16<0x4140>(w[3]), codes_f16<0x4342>(w[3]));
+        }
+      if (!is_v) {   // (S of two tiles before is complete, which followed the softmax of four before: its scales are free)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float* to = scales + (tile % kScaleSets) * 3 * kTile + tid + i * kCopy;
+          to[0] = sc[i] < kSmallestScale ? kSmallestScale : sc[i];   // a NaN stays
+          const float x = sc[2 + i] < kSmallestScale ? kSmallestScale : sc[2 + i], r = __frcp_rn(x);
+          to[kTile] = __log2f(x);
+          to[2 * kTile] = isnan(r) ? 0.f : r;   // the weight is a NaN already where it counts
+        }
+      }
+      if (t + 1 < u.t1) fetch(t + 1);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (threadIdx.x % 32 == 0) mbar_arrive(&ctl.full[s]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- query vectors
+template <class S>
+__device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem) {
+  constexpr int HD = S::HD, C = HD / 8;
+  const int tid = threadIdx.x % kQ;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  Stretches walk(ctl);
+  int stretch = 0;
+  Stretch u;
+#pragma unroll 1
+  while (walk.next(u)) {
+    const int vec0 = u.unit * kTilesUnit, here = min(u.vecs - vec0, kTilesUnit), chunks = here * C;
+    auto src = [&](int at) {
+      const int id = vec0 + at / C, row = vector_row(a, id);
+      return reinterpret_cast<const uint4*>(a.q + static_cast<long long>(u.row0 + row) * a.ldq +
+                                            (u.head * a.group + id - row * a.group) * HD + at % C * 8);
+    };
+    if (stretch > 0 &&
+        !__all_sync(~0u, mbar_wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag, nullptr)))
+      break;
+    auto dst = [&](int at) { return q_smem + (at / C >> 7) * S::kQBytes + chunk_at(at / C & 127, at % C); };
+    // as they are, all under way at once; then each thread goes over its own
+#pragma unroll 1
+    for (int at = tid; at < chunks; at += kQ) cp_async16(smem_addr(dst(at)), src(at), true);
+    cp_commit();
+    cp_wait<0>();
+    if constexpr (S::CODES) {
+      float top = 0.f;
+#pragma unroll 1
+      for (int at = tid; at < chunks; at += kQ) {
+        const uint4 x = *reinterpret_cast<const uint4*>(dst(at));
+        top_of(x.x, top);
+        top_of(x.y, top);
+        top_of(x.z, top);
+        top_of(x.w, top);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+      const float up = up_to_f16(top);
+      if (tid == 0) ctl.q_down[stretch & 3] = 1.f / up;
+#pragma unroll 1
+      for (int at = tid; at < chunks; at += kQ) {
+        uint4* p = reinterpret_cast<uint4*>(dst(at));
+        const uint4 x = *p;
+        *p = make_uint4(scaled_f16(x.x ^ flip, up), scaled_f16(x.y ^ flip, up), scaled_f16(x.z ^ flip, up),
+                        scaled_f16(x.w ^ flip, up));
+      }
+    } else if (flip != 0u) {
+#pragma unroll 1
+      for (int at = tid; at < chunks; at += kQ) {
+        uint4* p = reinterpret_cast<uint4*>(dst(at));
+        const uint4 x = *p;
+        *p = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+      }
+    }
+    fence_proxy_async_smem();
+    mbar_arrive(&ctl.q_full);
+    ++stretch;
+  }
+}
+
+// ---------------------------------------------------------------- softmax
+template <class S>
+__device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, const float* scales, uint32_t tmem) {
+  constexpr int HD = S::HD;
+  constexpr bool CODES = S::CODES;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, w = warp / 4, row = threadIdx.x % 128;
+  const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+  const uint32_t s_at = tmem + lanes + static_cast<uint32_t>(w * 128);
+  const uint32_t o_at = tmem + lanes + 256 + static_cast<uint32_t>(w * HD);
+  volatile int* abort_flag = &ctl.abort_flag;
+  Stretches walk(ctl);
+  bool ok = true;
+  int done = 0, tiles = 0, stretch = 0;      // steps of this warpgroup, tiles of the CTA, before this stretch
+  auto wait = [&](uint64_t* bar, int phase) {
+    ok = ok && __all_sync(~0u, mbar_wait_bounded(bar, static_cast<uint32_t>(phase) & 1u, abort_flag, nullptr));
+    return ok;
+  };
+  Stretch u;
+#pragma unroll 1
+  while (walk.next(u)) {
+    const bool pair = is_pair(u);
+    const int vec = u.unit * kTilesUnit + (pair ? w * 128 : 0) + row, end = u.end();
+    const bool live = vec < u.vecs, warp_live = __any_sync(~0u, live);
+    const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
+    float scale = fmaxf(fabsf(a.scale), 1e-30f);   // (not 0: it meets scores of -inf)
+    float m = kStart, l = 0.f;
+#pragma unroll 1
+    for (int t = u.t0; ok && t < u.t1; ++t)
+#pragma unroll 1
+      for (int half = pair ? 0 : w; half < (pair ? 2 : w + 1); ++half, ++done) {
+        const int buf = done & 1, key0 = t * kTile + half * kStep;
+        const bool begins = t == u.t0 && (half == 0 || !pair);
+        if (!wait(&ctl.s_full[w][buf], done >> 1)) break;
+        tc_fence_after();
+        if (warp_live) {
+          if (CODES && begins) scale = fmaxf(fabsf(a.scale), 1e-30f) * ctl.q_down[stretch & 3];
+          const uint32_t s_buf = s_at + buf * kStep;
+          float z[kStep];
+          tmem_ld_x64(s_buf, z);
+          const float* kf = scales + ((tiles + t - u.t0) % kScaleSets) * 3 * kTile + half * kStep;
+          if constexpr (CODES) {
+#pragma unroll
+            for (int e = 0; e < kStep; e += 4) {
+              const float4 k4 = *reinterpret_cast<const float4*>(kf + e);
+              const float4 v4 = *reinterpret_cast<const float4*>(kf + kTile + e);
+              z[e] = fmaf(z[e] * scale, k4.x, v4.x), z[e + 1] = fmaf(z[e + 1] * scale, k4.y, v4.y);
+              z[e + 2] = fmaf(z[e + 2] * scale, k4.z, v4.z), z[e + 3] = fmaf(z[e + 3] * scale, k4.w, v4.w);
+            }
+          }
+          if (key0 + kStep > end || key0 + kStep > u.first) {
+            // bit e: the vector sees key key0 + e
+            auto below = [](long long n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
+            const long long d = u.first - key0;
+            unsigned long long seen = below(static_cast<long long>(sight.limit) + 1 - key0);
+            seen |= d >= 64 || d <= -32 ? 0ull
+                    : d >= 0            ? static_cast<unsigned long long>(sight.bits) << d
+                                        : static_cast<unsigned long long>(sight.bits >> -d);
+            seen &= below(end - key0);
+#pragma unroll
+            for (int e = 0; e < kStep; ++e)
+              if (!(static_cast<uint32_t>(e < 32 ? seen : seen >> 32) >> (e & 31) & 1u)) z[e] = -INFINITY;
+            if constexpr (!CODES) {
+              if (own_rows(u, t)) {   // values that are not finite, to those that see them
+                const int tile = tiles + t - u.t0, s = slot_of(tile, 1);
+                if (!wait(&ctl.full[s], use_of(tile))) break;
+                const uint32_t* words = &ctl.bad[s & 1][half * 2];
+                const unsigned long long bad = words[0] | static_cast<unsigned long long>(words[1]) << 32;
+                if ((bad & seen) != 0ull) l = NAN;
+              }
+            }
+          }
+          float mx[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+          for (int e = 4; e < kStep; ++e) mx[e & 3] = fmaxf(mx[e & 3], z[e]);
+          float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          if constexpr (!CODES) top *= scale;
+          if (__any_sync(~0u, top - m > kAbove)) {
+            const float now = top - m > kAbove ? top - kBelow : m, by = ex2(m - now);
+            m = now;
+            l *= by;
+            if (!begins) {
+              if (!wait(&ctl.o_full[w][buf ^ 1], (done - 1) >> 1)) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < HD; c += 32) {
+                float o[32];
+                tmem_ld_x32(o_at + c, o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] *= by;
+                tmem_st_x32(o_at + c, reinterpret_cast<const uint32_t*>(o));
+              }
+            }
+          }
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          uint32_t p[kStep / 2];
+#pragma unroll
+          for (int e = 0; e < kStep; e += 4) {
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = ex2(CODES ? z[e + j] - m : fmaf(z[e + j], scale, -m));
+            if constexpr (CODES) {
+              const float4 r4 = *reinterpret_cast<const float4*>(kf + 2 * kTile + e);
+              sum[0] = fmaf(x[0], r4.x, sum[0]), sum[1] = fmaf(x[1], r4.y, sum[1]);
+              sum[2] = fmaf(x[2], r4.z, sum[2]), sum[3] = fmaf(x[3], r4.w, sum[3]);
+              p[e / 2] = pack_f16(x[0], x[1]), p[e / 2 + 1] = pack_f16(x[2], x[3]);
+            } else {
+              sum[0] += x[0], sum[1] += x[1], sum[2] += x[2], sum[3] += x[3];
+              p[e / 2] = pack_bf16(x[0], x[1]), p[e / 2 + 1] = pack_bf16(x[2], x[3]);
+            }
+          }
+          tmem_st_x32(s_buf, p);
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.p_full[w][buf]);
+      }
+    // ---- the record
+    wait(&ctl.o_full[w][(done - 1) & 1], (done - 1) >> 1);
+    if (!ok) m = kStart, l = NAN;
+    tc_fence_after();
+    if (warp_live) {
+      const int heads = a.group * a.kv_heads, vr = vector_row(a, vec);
+      const long long at = static_cast<long long>(u.row0 + vr) * heads + u.head * a.group + vec - vr * a.group;
+      // a pair's warpgroups have different vectors, others the same: two records of each.  Records lie side by
+      // side, [HD / 4][records][4]: a warp's stores are whole lines
+      const bool whole = u.whole();
+      const long long all = static_cast<long long>(a.rows) * heads;
+      const long long n = whole ? 2 * all : kTilesUnit, i = whole ? at + (pair ? 0 : w) * all : w * 128 + row;
+      float* rec = whole ? a.full[u.own ? 0 : 1] : a.slots + (2 * static_cast<long long>(blockIdx.x) + (u.t0 == 0)) *
+                                                                kTilesUnit * kRecord<HD>;
+      if (live) *reinterpret_cast<float2*>(rec + HD * n + 2 * i) = make_float2(m, l);
+      rec += 4 * i;
+#pragma unroll 1
+      for (int c = 0; c < HD; c += 32) {
+        float o[32];
+        tmem_ld_x32(o_at + c, o);
+        if (live) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            *reinterpret_cast<float4*>(rec) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            rec += 4 * n;
+          }
+        }
+      }
+    }
+    tc_fence_before();
+    tiles += u.t1 - u.t0;
+    ++stretch;
+  }
+}
+
+// ---------------------------------------------------------------- MMAs
+// A warp issues all MMAs of a warpgroup: its steps are both halves of every tile with the warpgroup's own
+// vectors (pair), or half w.  S of step n + 2 follows P V of step n, whose P lies where it goes: MMAs of
+// one thread run in order, so nothing waits for that between them.  (A tcgen05 fence after a wait holds a
+// thread until its own earlier MMAs have completed; those of the other warpgroup are another thread's.)
+// The warp stays converged, one lane issues.
+template <class S>
+__device__ __forceinline__ void mma_role(Ctl& ctl, int w, const uint8_t* ring, const uint8_t* q_smem, uint32_t tmem) {
+  constexpr uint32_t kIdS = idesc<S::CODES>(128, kStep), kIdO = idesc<S::CODES>(128, S::HD) | (1u << 16);   // V N-major
+  const uint64_t kdesc = make_smem_desc_sw128(smem_addr(ring));
+  // V tile, N-major: 64-element columns kTile x 128 bytes apart, 8-key groups 1024
+  const uint64_t vdesc = (kdesc & ~(0xFFFFull << 16)) | (static_cast<uint64_t>((kTile * 128) >> 4) << 16);
+  const bool lead = elect_one();
+  volatile int* abort_flag = &ctl.abort_flag;
+  Stretches walk(ctl);
+  bool ok = true;
+  auto wait = [&](uint64_t* bar, int phase) {
+    ok = ok && __all_sync(~0u, mbar_wait_bounded(bar, static_cast<uint32_t>(phase) & 1u, abort_flag, nullptr));
+    return ok;
+  };
+  int tiles = 0, stretch = 0, done = 0;   // before this stretch; done: steps
+  Stretch u;
+#pragma unroll 1
+  while (ok && walk.next(u)) {
+    const bool pair = is_pair(u);
+    const int per_tile = pair ? 2 : 1, steps = (u.t1 - u.t0) * per_tile;
+    const uint64_t qdesc = make_smem_desc_sw128(smem_addr(q_smem + (pair ? w * S::kQBytes : 0)));
+    if (!wait(&ctl.q_full, stretch)) break;
+    auto tile_of = [&](int n) { return tiles + (pair ? n >> 1 : n); };
+    auto first_key = [&](int n) { return (pair ? n & 1 : w) * kStep; };
+    // n = -2, -1: the first two S; then P V of step n, and S of step n + 2
+#pragma unroll 1
+    for (int n = -2; n < steps; ++n) {
+      if (n >= 0) {
+        const int g = done + n, buf = g & 1, s = slot_of(tile_of(n), 1);
+        if (!wait(&ctl.full[s], use_of(tile_of(n))) || !wait(&ctl.p_full[w][buf], g >> 1)) break;
+        tc_fence_after();
+        if (lead) {
+          const uint64_t vd = vdesc + static_cast<uint32_t>((s * S::kSlotBytes + first_key(n) * 128) >> 4);
+#pragma unroll
+          for (int ks = 0; ks < kStep / 16; ++ks)
+            mma_ts(tmem + 256 + w * S::HD, tmem + w * 128 + buf * kStep + ks * 8, vd + static_cast<uint32_t>((ks * 2048) >> 4),
+                   kIdO, n > 0 || ks > 0 ? 1u : 0u);
+          tc_commit(&ctl.o_full[w][buf]);
+          if (!pair || (n & 1)) tc_commit(&ctl.empty[s]);
+        }
+        __syncwarp();
+      }
+      if (n + 2 < steps) {
+        const int g = done + n + 2, buf = g & 1, s = slot_of(tile_of(n + 2), 0);
+        if (!wait(&ctl.full[s], use_of(tile_of(n + 2)))) break;
+        if (lead) {
+          const uint64_t kd = kdesc + static_cast<uint32_t>((s * S::kSlotBytes + first_key(n + 2) * 128) >> 4);
+#pragma unroll
+          for (int ks = 0; ks < S::HD / 16; ++ks) {
+            const uint32_t off = static_cast<uint32_t>(((ks >> 2) * kTile * 128 + (ks & 3) * 32) >> 4);
+            tc_mma_bf16(tmem + w * 128 + buf * kStep, qdesc + off, kd + off, kIdS, ks > 0 ? 1u : 0u);
+          }
+          tc_commit(&ctl.s_full[w][buf]);
+          if (!pair || (n & 1)) tc_commit(&ctl.empty[s]);
+          if (n + 3 == steps) tc_commit(&ctl.q_free[stretch & 1]);
+        }
+        __syncwarp();
+      }
+    }
+    done += steps;
+    tiles += u.t1 - u.t0;
+    ++stretch;
+  }
+  if (lead) {   // every MMA issued completes before the CTA leaves
+    tc_commit(&ctl.drain[w]);
+    mbar_wait_drain(&ctl.drain[w], 0);
+  }
+  __syncwarp();
+}
+
+template <class S>
+__global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constant__ ListArgs a, const __grid_constant__ TileMaps maps) {
+  __shared__ Ctl ctl;
+  extern __shared__ uint8_t dsmem_raw[];
+  uint8_t* ring = dsmem_raw + ((1024u - (smem_addr(dsmem_raw) & 1023u)) & 1023u);
+  uint8_t* q_smem = ring + kSlots * S::kSlotBytes;
+  float* scales = reinterpret_cast<float*>(q_smem + 2 * S::kQBytes);
+  const int warp = threadIdx.x / 32;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&ctl.full[s], S::CODES ? kCopy / 32 : 1);
+      mbar_init(&ctl.empty[s], 2);
+    }
+    mbar_init(&ctl.raw[0], 1);
+    mbar_init(&ctl.raw[1], 1);
+    mbar_init(&ctl.q_full, kQ);
+    mbar_init(&ctl.q_free[0], 2);
+    mbar_init(&ctl.q_free[1], 2);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&ctl.s_full[i >> 1][i & 1], 1);
+      mbar_init(&ctl.p_full[i >> 1][i & 1], 4);
+      mbar_init(&ctl.o_full[i >> 1][i & 1], 1);
+    }
+    mbar_init(&ctl.drain[0], 1);
+    mbar_init(&ctl.drain[1], 1);
+    for (int i = 0; i < kListed; ++i) mbar_init(&ctl.listed[i], 1);
+    ctl.abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 12) {
+    tmem_alloc(&ctl.tmem_base, 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  tc_fence_before();
+  make_plan<Units, kThreads>(a, ctl.plan);
+  tc_fence_after();
+  const uint32_t tmem = ctl.tmem_base;
+  if (warp < 8) {
+    soft_role<S>(a, ctl, scales, tmem);
+  } else if (warp < 12) {
+    if constexpr (S::CODES) {
+      codes_role<S>(a, ctl, (warp - 8) / 2, ring, scales);
+    } else if (warp < 10) {
+      tma_role<S>(a, maps, ctl, warp - 8, ring);
+    } else {
+      edge_role<S>(ctl, ring);
+    }
+  } else if (warp < 14) {
+    mma_role<S>(ctl, warp - 12, ring, q_smem, tmem);
+  } else if (warp == 14) {
+    q_role<S>(a, ctl, q_smem);
+  } else {
+    if (threadIdx.x % 32 == 0) walk_role(a, ctl);
+    __syncwarp();
+    if (blockIdx.x == 0)
+      for (int b = threadIdx.x % 32; b <= list_len(a); b += 32) a.bases[b] = ctl.plan.bases[b];
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <class S>
+cudaError_t launch(const ListArgs& a, cudaLaunchConfig_t cfg) {
+  static_assert(S::kSmem + sizeof(Ctl) <= 227 * 1024, "shared memory");
+  static std::atomic<bool> set[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev >= 64 || !set[dev].load(std::memory_order_relaxed))) {
+    e = cudaFuncSetAttribute(tiles_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e == cudaSuccess && dev < 64) set[dev].store(true, std::memory_order_relaxed);
+  }
+  if (e != cudaSuccess) return e;
+  TileMaps maps{};
+  if constexpr (!S::CODES)
+    for (int i = a.n_own > 0 ? 0 : 1; i < (a.prefix_len > 0 ? 2 : 1); ++i) {
+      const KvView& kv = a.kv[i];
+      if (!encode_cache(&maps.k[i], kv.k, S::HD, kv.max_pos, kv.n_heads, kv.n_seq, kv.pos, kv.head, kv.seq) ||
+          !encode_cache(&maps.v[i], kv.v, S::HD, kv.max_pos, kv.n_heads, kv.n_seq, kv.pos, kv.head, kv.seq))
+        return cudaErrorInvalidValue;
+    }
+  cfg.gridDim = dim3(kTilesCtas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = S::kSmem;
+  return cudaLaunchKernelEx(&cfg, tiles_kernel<S>, a, maps);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg) {
+  return hd == 64 ? (codes ? launch<Shape<64, true>>(a, cfg) : launch<Shape<64, false>>(a, cfg))
+                  : (codes ? launch<Shape<128, true>>(a, cfg) : launch<Shape<128, false>>(a, cfg));
+}
+
+}  // namespace memspec

@@ -300,16 +300,16 @@ const char* kv_problem(const memspec_kv* kv, bool write) {
   if (kv == nullptr || kv->k_dev == nullptr || kv->v_dev == nullptr) return "the cache's k or v is null";
   if ((kv->k_scale_dev == nullptr) != (kv->v_scale_dev == nullptr)) return "scales of both k and v, or of none";
   if (kv->head_dim != 64 && kv->head_dim != 128) return "head_dim must be 64 or 128";
-  if (kv->n_seq < 1 || kv->n_heads < 1 || kv->n_heads > 1024 || kv->max_pos < 1)
-    return "the cache needs at least one sequence and position and 1 to 1024 heads";
+  if (kv->n_seq < 1 || kv->n_heads < 1 || kv->n_heads > 1024 || kv->max_pos < 1 || kv->max_pos > 1 << 30)
+    return "the cache needs at least one sequence, 1 to 2^30 positions and 1 to 1024 heads";
   const bool codes = kv->k_scale_dev != nullptr;
   const int32_t n[3] = {kv->n_seq, kv->n_heads, kv->max_pos};
   const int64_t st[3] = {kv->seq_stride, kv->head_stride, kv->pos_stride};
   const int64_t ss[3] = {kv->scale_seq_stride, kv->scale_head_stride, kv->scale_pos_stride};
   for (int i = 0; i < 3; ++i) {
     if (n[i] == 1) continue;
-    if (st[i] < 0 || st[i] > INT64_C(1) << 40 || st[i] % (codes ? 16 : 8) != 0)
-      return "the cache's strides must be multiples of 16 bytes, 0 to 2^40 elements";
+    if (st[i] < (i == 2 ? kv->head_dim : 0) || st[i] > INT64_C(1) << 38 || st[i] % (codes ? 16 : 8) != 0)
+      return "the cache's strides must be multiples of 16 bytes, up to 2^38 elements, positions a vector apart";
     if (codes && (ss[i] < 0 || ss[i] > INT64_C(1) << 40)) return "the scales' strides must be 0 to 2^40";
   }
   if (misaligned(kv->k_dev, 16) || misaligned(kv->v_dev, 16) || misaligned(kv->k_scale_dev, 4) ||
@@ -328,12 +328,13 @@ KvView kv_view(const memspec_kv* kv) {
   v.v = static_cast<char*>(kv->v_dev);
   v.k_scale = kv->k_scale_dev;
   v.v_scale = kv->v_scale_dev;
-  v.seq = kv->seq_stride * size;
-  v.head = kv->head_stride * size;
-  v.pos = kv->pos_stride * size;
-  v.s_seq = kv->scale_seq_stride;
-  v.s_head = kv->scale_head_stride;
-  v.s_pos = kv->scale_pos_stride;
+  // of a dimension of one place the stride is not read
+  v.seq = kv->n_seq == 1 ? 0 : kv->seq_stride * size;
+  v.head = kv->n_heads == 1 ? 0 : kv->head_stride * size;
+  v.pos = kv->max_pos == 1 ? 0 : kv->pos_stride * size;
+  v.s_seq = kv->n_seq == 1 ? 0 : kv->scale_seq_stride;
+  v.s_head = kv->n_heads == 1 ? 0 : kv->scale_head_stride;
+  v.s_pos = kv->max_pos == 1 ? 0 : kv->scale_pos_stride;
   v.n_seq = kv->n_seq;
   v.n_heads = kv->n_heads;
   v.max_pos = kv->max_pos;
