@@ -30,7 +30,7 @@ namespace memspec {
 
 namespace {
 
-constexpr int kThreads = 512, kCopy = 64, kQ = 32;   // kCopy: for K, and as many for V
+constexpr int kThreads = 512, kSoft = 256, kCopy = 64;   // kCopy: for K, and as many for V
 constexpr int kSlots = 4;               // tiles in shared memory: K of two, V of two
 constexpr int kScaleSets = 4;           // a tile's scales are read until its P is written
 constexpr int kListed = 4;              // stretches told of at a time
@@ -61,6 +61,7 @@ struct Ctl {
   uint32_t bad[2][kTile / 32];        // keys of an edge tile whose values are not all finite
   float q_down[4];                    // 1 / the power of two that a stretch's Q was taken by; the next one's Q may be
                                       // there, and the one's after it begun, before this one's softmax reads its own
+  float tops[kSoft / 32];
   Plan plan;
   uint64_t listed[kListed];           // a stretch's entry is there
   Stretch list[kListed];              // (none: t0 == t1)
@@ -120,6 +121,30 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two floats at a time (half the issue slots, half the code).
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
 // D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
 __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
@@ -353,69 +378,82 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
 }
 
 // ---------------------------------------------------------------- query vectors
+// A stretch's vectors into shared memory by THREADS threads (`tid` of them; sync: their barrier), K-major; a
+// negative scale turns their signs.  Codes: to fp16, by a power of two that brings the largest to about 2^10.
+template <class S, int THREADS, class Sync>
+__device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretch& u, int stretch, int tid, uint8_t* q_smem, Sync sync) {
+  constexpr int HD = S::HD, C = HD / 8;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  const int vec0 = u.unit * kTilesUnit, chunks = min(u.vecs - vec0, kTilesUnit) * C;
+  auto dst = [&](int at) { return q_smem + (at / C >> 7) * S::kQBytes + chunk_at(at / C & 127, at % C); };
+  // as they are, all under way at once; then each thread goes over its own
+#pragma unroll 1
+  for (int at = tid; at < chunks; at += THREADS) {
+    const int id = vec0 + at / C, row = vector_row(a, id);
+    cp_async16(smem_addr(dst(at)), a.q + static_cast<long long>(u.row0 + row) * a.ldq +
+                                       (u.head * a.group + id - row * a.group) * HD + at % C * 8, true);
+  }
+  cp_commit();
+  cp_wait<0>();
+  if constexpr (S::CODES) {
+    float top = 0.f;
+#pragma unroll 1
+    for (int at = tid; at < chunks; at += THREADS) {
+      const uint4 x = *reinterpret_cast<const uint4*>(dst(at));
+      top_of(x.x, top);
+      top_of(x.y, top);
+      top_of(x.z, top);
+      top_of(x.w, top);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    if constexpr (THREADS > 32) {
+      if (tid % 32 == 0) ctl.tops[tid / 32] = top;
+      sync();
+#pragma unroll
+      for (int i = 0; i < THREADS / 32; ++i) top = fmaxf(top, ctl.tops[i]);
+    }
+    const float up = up_to_f16(top);
+    if (tid == 0) ctl.q_down[stretch & 3] = 1.f / up;
+#pragma unroll 1
+    for (int at = tid; at < chunks; at += THREADS) {
+      uint4* p = reinterpret_cast<uint4*>(dst(at));
+      const uint4 x = *p;
+      *p = make_uint4(scaled_f16(x.x ^ flip, up), scaled_f16(x.y ^ flip, up), scaled_f16(x.z ^ flip, up),
+                      scaled_f16(x.w ^ flip, up));
+    }
+  } else if (flip != 0u) {
+#pragma unroll 1
+    for (int at = tid; at < chunks; at += THREADS) {
+      uint4* p = reinterpret_cast<uint4*>(dst(at));
+      const uint4 x = *p;
+      *p = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
+    }
+  }
+  fence_proxy_async_smem();
+  sync();
+  if (tid == 0) mbar_arrive(&ctl.q_full);
+}
+
+// The smaller units' vectors, ahead of their stretch; those of a pair are many, and the softmax warps' own work.
 template <class S>
 __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem) {
-  constexpr int HD = S::HD, C = HD / 8;
-  const int tid = threadIdx.x % kQ;
-  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   Stretches walk(ctl);
   int stretch = 0;
   Stretch u;
 #pragma unroll 1
-  while (walk.next(u)) {
-    const int vec0 = u.unit * kTilesUnit, here = min(u.vecs - vec0, kTilesUnit), chunks = here * C;
-    auto src = [&](int at) {
-      const int id = vec0 + at / C, row = vector_row(a, id);
-      return reinterpret_cast<const uint4*>(a.q + static_cast<long long>(u.row0 + row) * a.ldq +
-                                            (u.head * a.group + id - row * a.group) * HD + at % C * 8);
-    };
+  for (; walk.next(u); ++stretch) {
+    if (is_pair(u)) continue;
     if (stretch > 0 &&
         !__all_sync(~0u, mbar_wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag, nullptr)))
       break;
-    auto dst = [&](int at) { return q_smem + (at / C >> 7) * S::kQBytes + chunk_at(at / C & 127, at % C); };
-    // as they are, all under way at once; then each thread goes over its own
-#pragma unroll 1
-    for (int at = tid; at < chunks; at += kQ) cp_async16(smem_addr(dst(at)), src(at), true);
-    cp_commit();
-    cp_wait<0>();
-    if constexpr (S::CODES) {
-      float top = 0.f;
-#pragma unroll 1
-      for (int at = tid; at < chunks; at += kQ) {
-        const uint4 x = *reinterpret_cast<const uint4*>(dst(at));
-        top_of(x.x, top);
-        top_of(x.y, top);
-        top_of(x.z, top);
-        top_of(x.w, top);
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-      const float up = up_to_f16(top);
-      if (tid == 0) ctl.q_down[stretch & 3] = 1.f / up;
-#pragma unroll 1
-      for (int at = tid; at < chunks; at += kQ) {
-        uint4* p = reinterpret_cast<uint4*>(dst(at));
-        const uint4 x = *p;
-        *p = make_uint4(scaled_f16(x.x ^ flip, up), scaled_f16(x.y ^ flip, up), scaled_f16(x.z ^ flip, up),
-                        scaled_f16(x.w ^ flip, up));
-      }
-    } else if (flip != 0u) {
-#pragma unroll 1
-      for (int at = tid; at < chunks; at += kQ) {
-        uint4* p = reinterpret_cast<uint4*>(dst(at));
-        const uint4 x = *p;
-        *p = make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip);
-      }
-    }
-    fence_proxy_async_smem();
-    mbar_arrive(&ctl.q_full);
-    ++stretch;
+    load_q<S, 32>(a, ctl, u, stretch, threadIdx.x % 32, q_smem, [] { __syncwarp(); });
   }
 }
 
 // ---------------------------------------------------------------- softmax
 template <class S>
-__device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, const float* scales, uint32_t tmem) {
+__device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem, const float* scales, uint32_t tmem) {
   constexpr int HD = S::HD;
   constexpr bool CODES = S::CODES;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, w = warp / 4, row = threadIdx.x % 128;
@@ -439,6 +477,10 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, const flo
     const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
     float scale = fmaxf(fabsf(a.scale), 1e-30f);   // (not 0: it meets scores of -inf)
     float m = kStart, l = 0.f;
+    if (pair) {
+      named_bar_sync(1, kSoft);   // both warpgroups have seen the last S of the stretch before: Q is free
+      load_q<S, kSoft>(a, ctl, u, stretch, threadIdx.x, q_smem, [] { named_bar_sync(1, kSoft); });
+    }
 #pragma unroll 1
     for (int t = u.t0; ok && t < u.t1; ++t)
 #pragma unroll 1
@@ -454,12 +496,13 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, const flo
           tmem_ld_x64(s_buf, z);
           const float* kf = scales + ((tiles + t - u.t0) % kScaleSets) * 3 * kTile + half * kStep;
           if constexpr (CODES) {
+            const f32x2 scale2 = pair_of(scale, scale);
 #pragma unroll
             for (int e = 0; e < kStep; e += 4) {
-              const float4 k4 = *reinterpret_cast<const float4*>(kf + e);
-              const float4 v4 = *reinterpret_cast<const float4*>(kf + kTile + e);
-              z[e] = fmaf(z[e] * scale, k4.x, v4.x), z[e + 1] = fmaf(z[e + 1] * scale, k4.y, v4.y);
-              z[e + 2] = fmaf(z[e + 2] * scale, k4.z, v4.z), z[e + 3] = fmaf(z[e + 3] * scale, k4.w, v4.w);
+              const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(kf + e);
+              const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(kf + kTile + e);
+              split(fma2(mul2(pair_of(z[e], z[e + 1]), scale2), k4.x, v4.x), z[e], z[e + 1]);
+              split(fma2(mul2(pair_of(z[e + 2], z[e + 3]), scale2), k4.y, v4.y), z[e + 2], z[e + 3]);
             }
           }
           if (key0 + kStep > end || key0 + kStep > u.first) {
@@ -489,8 +532,9 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, const flo
           for (int e = 4; e < kStep; ++e) mx[e & 3] = fmaxf(mx[e & 3], z[e]);
           float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           if constexpr (!CODES) top *= scale;
-          if (__any_sync(~0u, top - m > kAbove)) {
-            const float now = top - m > kAbove ? top - kBelow : m, by = ex2(m - now);
+          const bool above = live && top - m > kAbove;   // (rows without a vector have anything)
+          if (__any_sync(~0u, above)) {
+            const float now = above ? top - kBelow : m, by = ex2(m - now);
             m = now;
             l *= by;
             if (!begins) {
@@ -506,25 +550,31 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, const flo
               }
             }
           }
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          f32x2 sum[2] = {0ull, 0ull};
+          const f32x2 minus = pair_of(-m, -m), scale2 = pair_of(scale, scale);
           uint32_t p[kStep / 2];
 #pragma unroll
           for (int e = 0; e < kStep; e += 4) {
-            float x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = ex2(CODES ? z[e + j] - m : fmaf(z[e + j], scale, -m));
+            f32x2 r4[2] = {0ull, 0ull};
             if constexpr (CODES) {
-              const float4 r4 = *reinterpret_cast<const float4*>(kf + 2 * kTile + e);
-              sum[0] = fmaf(x[0], r4.x, sum[0]), sum[1] = fmaf(x[1], r4.y, sum[1]);
-              sum[2] = fmaf(x[2], r4.z, sum[2]), sum[3] = fmaf(x[3], r4.w, sum[3]);
-              p[e / 2] = pack_f16(x[0], x[1]), p[e / 2 + 1] = pack_f16(x[2], x[3]);
-            } else {
-              sum[0] += x[0], sum[1] += x[1], sum[2] += x[2], sum[3] += x[3];
-              p[e / 2] = pack_bf16(x[0], x[1]), p[e / 2 + 1] = pack_bf16(x[2], x[3]);
+              const ulonglong2 r = *reinterpret_cast<const ulonglong2*>(kf + 2 * kTile + e);
+              r4[0] = r.x, r4[1] = r.y;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const f32x2 zz = pair_of(z[e + 2 * j], z[e + 2 * j + 1]);
+              float x0, x1;
+              split(CODES ? add2(zz, minus) : fma2(zz, scale2, minus), x0, x1);
+              x0 = ex2(x0), x1 = ex2(x1);
+              const f32x2 x = pair_of(x0, x1);
+              sum[j] = CODES ? fma2(x, r4[j], sum[j]) : add2(sum[j], x);
+              p[e / 2 + j] = CODES ? pack_f16(x0, x1) : pack_bf16(x0, x1);
             }
           }
           tmem_st_x32(s_buf, p);
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          float l0, l1;
+          split(add2(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
           tmem_st_wait();
         }
         tc_fence_before();
@@ -657,7 +707,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     }
     mbar_init(&ctl.raw[0], 1);
     mbar_init(&ctl.raw[1], 1);
-    mbar_init(&ctl.q_full, kQ);
+    mbar_init(&ctl.q_full, 1);
     mbar_init(&ctl.q_free[0], 2);
     mbar_init(&ctl.q_free[1], 2);
     for (int i = 0; i < 4; ++i) {
@@ -682,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
   tc_fence_after();
   const uint32_t tmem = ctl.tmem_base;
   if (warp < 8) {
-    soft_role<S>(a, ctl, scales, tmem);
+    soft_role<S>(a, ctl, q_smem, scales, tmem);
   } else if (warp < 12) {
     if constexpr (S::CODES) {
       codes_role<S>(a, ctl, (warp - 8) / 2, ring, scales);
