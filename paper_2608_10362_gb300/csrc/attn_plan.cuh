@@ -100,14 +100,14 @@ struct Pieces {
 constexpr int kCached = 64;
 struct alignas(16) Plan {
   uint32_t bases[kMaxSeqs + 2];
-  uint32_t sums[16];
+  uint32_t sums[20];
   SeqRows rows[kCached];
 };
 
 // Made by all THREADS threads.
 template <class CUT, int THREADS>
 __device__ __forceinline__ void make_plan(const ListArgs& a, Plan& plan) {
-  static_assert(THREADS <= 512, "a word of sums per warp");
+  static_assert(THREADS <= 640, "a word of sums per warp");
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, n = list_len(a);
   uint32_t before = 0;
 #pragma unroll 1

@@ -13,13 +13,16 @@
 // of sums (two per vector for the smaller units) that attn_join.cu puts together.
 //
 // K and V pass through two slots each in shared memory, K-major and N-major alike [key][hd] with the
-// 128-byte swizzle.  bf16 comes by TMA; codes are turned into fp16 on the way, which
-// holds them exactly, by the warps that fetch them.  K's scales multiply the scores, V's are added as
-// logarithms: the weights are w' = p * scale_v, against a maximum of their own kind, and the sum of p
-// that of w' / scale_v; so no range of scales overflows fp16.  Q is taken to fp16 by a power of two.
+// 128-byte swizzle.  bf16 comes by TMA.  Codes are fetched by warps that write them as fp16, times their scale over
+// a power of two near the tile's largest: a value is off by 2^-10 of itself (its factor and the product are
+// rounded), or 2^-24 of the largest that its tile could hold.  K's power multiplies the tile's scores, V's is added to them as a logarithm: weights are
+// w' = p * power, against a maximum of their own kind, and the sum of p is that of w' / power; so no range of scales
+// overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu has them, are three numbers per
+// key for every thread out of shared memory, 128 bytes a clock: 0.7 us of a step's 1.5; now 0.6.)  Q is taken to fp16 by
+// a power of two.
 //
-// Roles (512 threads): warps 0-3, 4-7 softmax, 8-11 copies, 12 and 13 the MMAs of
-// each, 14 Q, 15 which units these are.  Every wait is bounded; after one that ran out the CTA's remaining records are NaN.
+// Roles (warps): 0-3, 4-7 softmax; copies, 4, or 8 of codes; two with the MMAs of a warpgroup each;
+// one for Q; one for which units these are.  Every wait is bounded; after one that ran out the CTA's remaining records are NaN.
 #include <algorithm>
 #include <atomic>
 
@@ -30,9 +33,9 @@ namespace memspec {
 
 namespace {
 
-constexpr int kThreads = 512, kSoft = 256, kCopy = 64;   // kCopy: for K, and as many for V
+constexpr int kSoft = 256;              // threads of the softmax
 constexpr int kSlots = 4;               // tiles in shared memory: K of two, V of two
-constexpr int kScaleSets = 4;           // a tile's scales are read until its P is written
+constexpr int kRefs = 4;                // a tile's references are read until its P is written
 constexpr int kListed = 4;              // stretches told of at a time
 constexpr int kStep = 64;               // keys of a warpgroup's step
 typedef Cut<kTilesUnit, true, kTilesStart> Units;
@@ -41,12 +44,18 @@ template <int HD_, bool CODES_>
 struct Shape {
   static constexpr int HD = HD_;
   static constexpr bool CODES = CODES_;
+  static constexpr int kCopy = CODES ? 128 : 64;       // threads for K, and as many for V
+  static constexpr int kThreads = kSoft + 2 * kCopy + 128;
+  static constexpr int kWidth = CODES ? 32 : 64;       // scores of a step in registers at a time (96 and 128 a thread)
   static constexpr int kSlotBytes = kTile * HD * 2;
   static constexpr int kQBytes = 128 * HD * 2;         // of 128 vectors
-  static constexpr int kScaleBytes = CODES ? kScaleSets * 3 * kTile * 4 : 0;
-  static constexpr int kSmem = 1024 + kSlots * kSlotBytes + 2 * kQBytes + kScaleBytes;
+  static constexpr int kSmem = 1024 + kSlots * kSlotBytes + 2 * kQBytes;
 };
 
+struct CodesSmem {   // of K's or V's threads, by the tile's parity: one barrier a tile
+  float scale[2][kTile];
+  float2 top[2][4];
+};
 struct Ctl {
   uint64_t full[kSlots], empty[kSlots];
   uint64_t raw[2];           // V of an edge tile has landed, but is still to be looked over
@@ -59,6 +68,8 @@ struct Ctl {
   uint32_t tmem_base;
   int abort_flag;
   uint32_t bad[2][kTile / 32];        // keys of an edge tile whose values are not all finite
+  float4 refs[kRefs];                 // codes: the power of two K's scales are taken against, V's logarithm, 1 / V's
+  CodesSmem codes[2];
   float q_down[4];                    // 1 / the power of two that a stretch's Q was taken by; the next one's Q may be
                                       // there, and the one's after it begun, before this one's softmax reads its own
   float tops[kSoft / 32];
@@ -120,6 +131,15 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {"
+      "%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Two floats at a time (half the issue slots, half the code).
@@ -133,11 +153,6 @@ __device__ __forceinline__ void split(f32x2 v, float& a, float& b) { asm("mov.b6
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
   f32x2 r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
@@ -261,6 +276,7 @@ __device__ __forceinline__ void tma_role(const ListArgs& a, const TileMaps& maps
 template <class S>
 __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
   constexpr int C = S::HD / 8;
+  constexpr int kCopy = S::kCopy;
   const int tid = threadIdx.x % kCopy;
   Stretches walk(ctl);
   int tile = 0;
@@ -298,10 +314,18 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
   }
 }
 
-// Codes: kCopy threads for K, with the scales of both, and kCopy for V.  64 bytes of a row by four lanes: a
-// thread's 16 codes are two chunks of fp16.  The next tile is in registers while this one waits for its slot.
+// Codes: kCopy threads for K and as many for V.  64 bytes of a row by four lanes: a thread's 16 codes are two
+// chunks of fp16.  The next tile is on its way to registers while this one is written.
+__device__ __forceinline__ float sane_scale(float s) { return s < kSmallestScale ? kSmallestScale : s; }   // a NaN stays
+__device__ __forceinline__ float finite_or_0(float s) { return s <= FLT_MAX ? s : 0.f; }
+// The exponent that a tile's scales are taken against (the largest finite one's), as a power of two and its inverse.
+__device__ __forceinline__ int reference(float top) { return min((__float_as_int(fmaxf(top, kSmallestScale)) >> 23) - 127, 126); }
+__device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
+
 template <class S>
-__device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v, uint8_t* ring, float* scales) {
+__device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v, uint8_t* ring, CodesSmem& sm) {
+  constexpr int kCopy = S::kCopy;
+  static_assert(kCopy == kTile, "a thread per scale");
   constexpr int J = S::HD / 64, N = kTile * 4 / kCopy;   // parts of a row, rows
   const int tid = threadIdx.x % kCopy, r0 = tid / 4, c = tid % 4;
   Stretches walk(ctl);
@@ -314,8 +338,8 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
     const char* base = (is_v ? kv.v : kv.k) + seq * kv.seq + u.head * kv.head;
     const float* ks = kv.k_scale + seq * kv.s_seq + u.head * kv.s_head;
     const float* vs = kv.v_scale + seq * kv.s_seq + u.head * kv.s_head;
-    uint4 in[N * J];
-    float sc[4] = {0.f, 0.f, 0.f, 0.f};
+    uint4 next[N * J];
+    float sc[2] = {0.f, 0.f};   // of V; of K (K's threads alone)
     auto fetch = [&](int t) {
       int key = t * kTile + r0;
       const char* src = base + key * kv.pos + c * 16;
@@ -324,52 +348,80 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
       for (int n = 0; n < N; ++n) {
 #pragma unroll
         for (int j = 0; j < J; ++j)
-          in[n * J + j] = key < end ? __ldcs(reinterpret_cast<const uint4*>(src + j * 64)) : make_uint4(0, 0, 0, 0);
+          next[n * J + j] = key < end ? __ldcs(reinterpret_cast<const uint4*>(src + j * 64)) : make_uint4(0, 0, 0, 0);
         key += kCopy / 4;
         src += step;
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        key = t * kTile + tid + i * kCopy;
-        if (!is_v) {
-          sc[i] = key < end ? ks[key * kv.s_pos] : 0.f;
-          sc[2 + i] = key < end ? vs[key * kv.s_pos] : 0.f;
-        }
-        if (key + 2 * kTile < end)   // a later tile's lines into L2
-          asm volatile("prefetch.global.L2 [%0];" ::"l"(base + (key + 2 * kTile) * kv.pos));
-      }
     };
+    auto fetch_scales = [&](int t) {
+      const int key = t * kTile + tid;
+      const long long at = key * kv.s_pos;
+      sc[0] = key < end ? vs[at] : 0.f;
+      if (!is_v) sc[1] = key < end ? ks[at] : 0.f;
+      if (key + 2 * kTile < end)   // a later tile's lines into L2
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(base + (key + 2 * kTile) * kv.pos));
+    };
+    fetch_scales(u.t0);
     fetch(u.t0);
 #pragma unroll 1
     for (int t = u.t0; t < u.t1; ++t, ++tile) {
-      const int s = slot_of(tile, is_v);
+      const int s = slot_of(tile, is_v), buf = tile & 1;
+      const float v_s = sane_scale(sc[0]), k_s = sane_scale(sc[1]);
+      sm.scale[buf][tid] = is_v ? v_s : k_s;
+      float2 top = make_float2(finite_or_0(v_s), finite_or_0(k_s));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        top.x = fmaxf(top.x, __shfl_xor_sync(~0u, top.x, o));
+        top.y = fmaxf(top.y, __shfl_xor_sync(~0u, top.y, o));
+      }
+      if (tid % 32 == 0) sm.top[buf][tid / 32] = top;
+      named_bar_sync(3 + is_v, kCopy);
+#pragma unroll
+      for (int i = 0; i < kCopy / 32; ++i) top.x = fmaxf(top.x, sm.top[buf][i].x), top.y = fmaxf(top.y, sm.top[buf][i].y);
+      const int ref_v = reference(top.x), ref_k = reference(top.y);
       if (use_of(tile) > 0 &&
           !__all_sync(~0u, mbar_wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, &ctl.abort_flag, nullptr)))
         return;
+      // V of a key whose scale is not finite: 0 where some vector does not see it, those that do are told
+      if (is_v) {
+        const uint32_t bad = __ballot_sync(~0u, !(sc[0] <= FLT_MAX));
+        if (tid % 32 == 0) ctl.bad[s & 1][tid / 32] = bad;
+      } else if (tid == 0) {   // (S of two tiles before is complete, after the softmax of four before: its entry is free)
+        ctl.refs[tile % kRefs] = make_float4(power(ref_k), static_cast<float>(ref_v), power(-ref_v), 0.f);
+      }
+      uint4 in[N * J];
+#pragma unroll
+      for (int i = 0; i < N * J; ++i) in[i] = next[i];
+      if (t + 1 < u.t1) {
+        fetch_scales(t + 1);
+        fetch(t + 1);
+      }
+      const float down = power(-(is_v ? ref_v : ref_k));
+      const bool hide = is_v && own_rows(u, t);
       uint8_t* slot = ring + s * S::kSlotBytes;
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+      for (int n = 0; n < N; ++n) {
+        const int r = r0 + n * (kCopy / 4);
+        float f = sm.scale[buf][r] * down;
+        if (hide && !(f <= FLT_MAX)) f = 0.f;
+        const __half2 f2 = __float2half2_rn(f);
+        auto value = [&](uint32_t codes) {
+          const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&codes), f2);
+          return *reinterpret_cast<const uint32_t*>(&y);
+        };
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const uint4 x = in[n * J + j];
           const uint32_t w[4] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u, x.z ^ 0x80808080u, x.w ^ 0x80808080u};
-          const int r = r0 + n * (kCopy / 4), ch = j * 8 + c * 2;
-          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch)) = make_uint4(
-              codes_f16<0x4140>(w[0]), codes_f16<0x4342>(w[0]), codes_f16<0x4140>(w[1]), codes_f16<0x4342>(w[1]));
-          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch + 1)) = make_uint4(
-              codes_f16<0x4140>(w[2]), codes_f16<0x4342>(w[2]), codes_f16<0x4140>(w[3]), codes_f16<0x4342>(w[3]));
-        }
-      if (!is_v) {   // (S of two tiles before is complete, which followed the softmax of four before: its scales are free)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float* to = scales + (tile % kScaleSets) * 3 * kTile + tid + i * kCopy;
-          to[0] = sc[i] < kSmallestScale ? kSmallestScale : sc[i];   // a NaN stays
-          const float x = sc[2 + i] < kSmallestScale ? kSmallestScale : sc[2 + i], r = __frcp_rn(x);
-          to[kTile] = __log2f(x);
-          to[2 * kTile] = isnan(r) ? 0.f : r;   // the weight is a NaN already where it counts
+          const int ch = j * 8 + c * 2;
+          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch)) =
+              make_uint4(value(codes_f16<0x4140>(w[0])), value(codes_f16<0x4342>(w[0])), value(codes_f16<0x4140>(w[1])),
+                         value(codes_f16<0x4342>(w[1])));
+          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch + 1)) =
+              make_uint4(value(codes_f16<0x4140>(w[2])), value(codes_f16<0x4342>(w[2])), value(codes_f16<0x4140>(w[3])),
+                         value(codes_f16<0x4342>(w[3])));
         }
       }
-      if (t + 1 < u.t1) fetch(t + 1);
       fence_proxy_async_smem();
       __syncwarp();
       if (threadIdx.x % 32 == 0) mbar_arrive(&ctl.full[s]);
@@ -453,7 +505,7 @@ __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_s
 
 // ---------------------------------------------------------------- softmax
 template <class S>
-__device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem, const float* scales, uint32_t tmem) {
+__device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem, uint32_t tmem) {
   constexpr int HD = S::HD;
   constexpr bool CODES = S::CODES;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, w = warp / 4, row = threadIdx.x % 128;
@@ -492,51 +544,57 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
         if (warp_live) {
           if (CODES && begins) scale = fmaxf(fabsf(a.scale), 1e-30f) * ctl.q_down[stretch & 3];
           const uint32_t s_buf = s_at + buf * kStep;
-          float z[kStep];
-          tmem_ld_x64(s_buf, z);
-          const float* kf = scales + ((tiles + t - u.t0) % kScaleSets) * 3 * kTile + half * kStep;
+          // z = by * S + plus: of codes with the tile's references
+          float by = scale, plus = 0.f, l_by = 1.f;
           if constexpr (CODES) {
-            const f32x2 scale2 = pair_of(scale, scale);
-#pragma unroll
-            for (int e = 0; e < kStep; e += 4) {
-              const ulonglong2 k4 = *reinterpret_cast<const ulonglong2*>(kf + e);
-              const ulonglong2 v4 = *reinterpret_cast<const ulonglong2*>(kf + kTile + e);
-              split(fma2(mul2(pair_of(z[e], z[e + 1]), scale2), k4.x, v4.x), z[e], z[e + 1]);
-              split(fma2(mul2(pair_of(z[e + 2], z[e + 3]), scale2), k4.y, v4.y), z[e + 2], z[e + 3]);
-            }
+            const float4 ref = ctl.refs[(tiles + t - u.t0) % kRefs];
+            by *= ref.x, plus = ref.y, l_by = ref.z;
           }
-          if (key0 + kStep > end || key0 + kStep > u.first) {
-            // bit e: the vector sees key key0 + e
+          const bool edge = key0 + kStep > end || key0 + kStep > u.first;
+          unsigned long long seen = ~0ull;   // bit e: the vector sees key key0 + e
+          if (edge) {
             auto below = [](long long n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; };
             const long long d = u.first - key0;
-            unsigned long long seen = below(static_cast<long long>(sight.limit) + 1 - key0);
+            seen = below(static_cast<long long>(sight.limit) + 1 - key0);
             seen |= d >= 64 || d <= -32 ? 0ull
                     : d >= 0            ? static_cast<unsigned long long>(sight.bits) << d
                                         : static_cast<unsigned long long>(sight.bits >> -d);
             seen &= below(end - key0);
-#pragma unroll
-            for (int e = 0; e < kStep; ++e)
-              if (!(static_cast<uint32_t>(e < 32 ? seen : seen >> 32) >> (e & 31) & 1u)) z[e] = -INFINITY;
-            if constexpr (!CODES) {
-              if (own_rows(u, t)) {   // values that are not finite, to those that see them
-                const int tile = tiles + t - u.t0, s = slot_of(tile, 1);
-                if (!wait(&ctl.full[s], use_of(tile))) break;
-                const uint32_t* words = &ctl.bad[s & 1][half * 2];
-                const unsigned long long bad = words[0] | static_cast<unsigned long long>(words[1]) << 32;
-                if ((bad & seen) != 0ull) l = NAN;
-              }
+            if (own_rows(u, t)) {   // values that are not finite, to those that see them
+              const int tile = tiles + t - u.t0, s = slot_of(tile, 1);
+              if (!wait(&ctl.full[s], use_of(tile))) break;
+              const uint32_t* words = &ctl.bad[s & 1][half * 2];
+              const unsigned long long bad = words[0] | static_cast<unsigned long long>(words[1]) << 32;
+              if ((bad & seen) != 0ull) l = NAN;
             }
           }
-          float mx[4] = {z[0], z[1], z[2], z[3]};
+          // scores c .. c + W - 1 of the step
+          constexpr int W = S::kWidth;
+          float z[W];
+          auto scores = [&](int c) {
+            if constexpr (W == 64) tmem_ld_x64(s_buf + c, z);
+            if constexpr (W == 32) tmem_ld_x32(s_buf + c, z);
+            if (edge) {
+              const unsigned long long here = seen >> c;
 #pragma unroll
-          for (int e = 4; e < kStep; ++e) mx[e & 3] = fmaxf(mx[e & 3], z[e]);
+              for (int e = 0; e < W; ++e)
+                if (!(static_cast<uint32_t>(e < 32 ? here : here >> 32) >> (e & 31) & 1u)) z[e] = -INFINITY;
+            }
+          };
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int c = 0; c < kStep; c += W) {
+            scores(c);
+#pragma unroll
+            for (int e = 0; e < W; ++e) mx[e & 3] = fmaxf(mx[e & 3], z[e]);
+          }
           float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-          if constexpr (!CODES) top *= scale;
+          top = fmaf(top, by, plus);
           const bool above = live && top - m > kAbove;   // (rows without a vector have anything)
           if (__any_sync(~0u, above)) {
-            const float now = above ? top - kBelow : m, by = ex2(m - now);
+            const float now = above ? top - kBelow : m, less = ex2(m - now);
             m = now;
-            l *= by;
+            l *= less;
             if (!begins) {
               if (!wait(&ctl.o_full[w][buf ^ 1], (done - 1) >> 1)) break;
               tc_fence_after();
@@ -545,36 +603,31 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
                 float o[32];
                 tmem_ld_x32(o_at + c, o);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] *= by;
+                for (int e = 0; e < 32; ++e) o[e] *= less;
                 tmem_st_x32(o_at + c, reinterpret_cast<const uint32_t*>(o));
               }
             }
           }
           f32x2 sum[2] = {0ull, 0ull};
-          const f32x2 minus = pair_of(-m, -m), scale2 = pair_of(scale, scale);
-          uint32_t p[kStep / 2];
+          const f32x2 by2 = pair_of(by, by), plus2 = pair_of(plus - m, plus - m);
+#pragma unroll 1
+          for (int c = 0; c < kStep; c += W) {
+            if constexpr (W < kStep) scores(c);
+            uint32_t p[W / 2];
 #pragma unroll
-          for (int e = 0; e < kStep; e += 4) {
-            f32x2 r4[2] = {0ull, 0ull};
-            if constexpr (CODES) {
-              const ulonglong2 r = *reinterpret_cast<const ulonglong2*>(kf + 2 * kTile + e);
-              r4[0] = r.x, r4[1] = r.y;
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const f32x2 zz = pair_of(z[e + 2 * j], z[e + 2 * j + 1]);
+            for (int e = 0; e < W; e += 2) {
               float x0, x1;
-              split(CODES ? add2(zz, minus) : fma2(zz, scale2, minus), x0, x1);
+              split(fma2(pair_of(z[e], z[e + 1]), by2, plus2), x0, x1);
               x0 = ex2(x0), x1 = ex2(x1);
-              const f32x2 x = pair_of(x0, x1);
-              sum[j] = CODES ? fma2(x, r4[j], sum[j]) : add2(sum[j], x);
-              p[e / 2 + j] = CODES ? pack_f16(x0, x1) : pack_bf16(x0, x1);
+              sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair_of(x0, x1));
+              p[e / 2] = CODES ? pack_f16(x0, x1) : pack_bf16(x0, x1);
             }
+            if constexpr (W == 64) tmem_st_x32(s_buf, p);
+            if constexpr (W == 32) tmem_st_x16(s_buf + c / 2, p);
           }
-          tmem_st_x32(s_buf, p);
           float l0, l1;
           split(add2(sum[0], sum[1]), l0, l1);
-          l += l0 + l1;
+          l = fmaf(l0 + l1, l_by, l);
           tmem_st_wait();
         }
         tc_fence_before();
@@ -693,16 +746,15 @@ __device__ __forceinline__ void mma_role(Ctl& ctl, int w, const uint8_t* ring, c
 }
 
 template <class S>
-__global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constant__ ListArgs a, const __grid_constant__ TileMaps maps) {
+__global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_constant__ ListArgs a, const __grid_constant__ TileMaps maps) {
   __shared__ Ctl ctl;
   extern __shared__ uint8_t dsmem_raw[];
   uint8_t* ring = dsmem_raw + ((1024u - (smem_addr(dsmem_raw) & 1023u)) & 1023u);
   uint8_t* q_smem = ring + kSlots * S::kSlotBytes;
-  float* scales = reinterpret_cast<float*>(q_smem + 2 * S::kQBytes);
   const int warp = threadIdx.x / 32;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&ctl.full[s], S::CODES ? kCopy / 32 : 1);
+      mbar_init(&ctl.full[s], S::CODES ? S::kCopy / 32 : 1);
       mbar_init(&ctl.empty[s], 2);
     }
     mbar_init(&ctl.raw[0], 1);
@@ -721,29 +773,31 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     ctl.abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 12) {
+  constexpr int kMma = (kSoft + 2 * S::kCopy) / 32;   // the first warp of the MMAs
+  if (warp == kMma) {
     tmem_alloc(&ctl.tmem_base, 512);
     tmem_relinquish();
   }
   pdl_wait();
   pdl_launch_dependents();
   tc_fence_before();
-  make_plan<Units, kThreads>(a, ctl.plan);
+  make_plan<Units, S::kThreads>(a, ctl.plan);
   tc_fence_after();
   const uint32_t tmem = ctl.tmem_base;
   if (warp < 8) {
-    soft_role<S>(a, ctl, q_smem, scales, tmem);
-  } else if (warp < 12) {
+    soft_role<S>(a, ctl, q_smem, tmem);
+  } else if (warp < kMma) {
+    const int w = warp - kSoft / 32;
     if constexpr (S::CODES) {
-      codes_role<S>(a, ctl, (warp - 8) / 2, ring, scales);
-    } else if (warp < 10) {
-      tma_role<S>(a, maps, ctl, warp - 8, ring);
+      codes_role<S>(a, ctl, w / (S::kCopy / 32), ring, ctl.codes[w / (S::kCopy / 32)]);
+    } else if (w < 2) {
+      tma_role<S>(a, maps, ctl, w, ring);
     } else {
       edge_role<S>(ctl, ring);
     }
-  } else if (warp < 14) {
-    mma_role<S>(ctl, warp - 12, ring, q_smem, tmem);
-  } else if (warp == 14) {
+  } else if (warp < kMma + 2) {
+    mma_role<S>(ctl, warp - kMma, ring, q_smem, tmem);
+  } else if (warp == kMma + 2) {
     q_role<S>(a, ctl, q_smem);
   } else {
     if (threadIdx.x % 32 == 0) walk_role(a, ctl);
@@ -753,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 12) {
+  if (warp == kMma) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -779,7 +833,7 @@ cudaError_t launch(const ListArgs& a, cudaLaunchConfig_t cfg) {
         return cudaErrorInvalidValue;
     }
   cfg.gridDim = dim3(kTilesCtas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(S::kThreads);
   cfg.dynamicSmemBytes = S::kSmem;
   return cudaLaunchKernelEx(&cfg, tiles_kernel<S>, a, maps);
 }

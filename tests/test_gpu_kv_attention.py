@@ -5,7 +5,9 @@ bits: off by 2^-8 (bf16 caches) or 2^-11 (codes) each, which moves a result by a
 A = sum w|v| / sum w.  A score is an fp32 sum of head_dim products of magnitude S = scale sum
 |q k| at most: off by (head_dim + 16) 2^-23 S (the tensor cores' sums may truncate: a whole
 step each), which moves its weight, and so the result, by as much of A, twice (numerator and
-denominator); sums of weights and exponentials add (keys 2^-23 at most, in practice their
+denominator).  Keys and values of codes of more than 16 vectors a head enter as fp16, off by 2^-10
+each, two roundings (their scales here lie within a factor of 7, so that nothing is near fp16's
+small end): a score by 2^-10 S more, a result by 2^-10 A more.  Sums of weights and exponentials add (keys 2^-23 at most, in practice their
 rounding averages out) 2^-18.
 """
 import math
@@ -49,7 +51,7 @@ def values(cache):
     return k, v
 
 
-def attention64(q, cache, starts, lens, tree=None, prefix=None, prefix_len=0, scale=None, codes_weights=None):
+def attention64(q, cache, starts, lens, tree=None, prefix=None, prefix_len=0, scale=None, max_rows=None):
     """(result, bound) of every row, NaN where the row is in no sequence."""
     rows, H, hd = q.shape
     G = H // cache.n_heads
@@ -93,8 +95,11 @@ def attention64(q, cache, starts, lens, tree=None, prefix=None, prefix_len=0, sc
             S = torch.where(s, torch.einsum("ngd,kd->ngk", x.abs(), k.nan_to_num(0, 0, 0).abs()) * abs(scale), 0.0)
             S = S.amax(2, keepdim=True) if S.shape[2] else S.sum(2, keepdim=True)
             weights = 2.0 ** -11 if cache.codes and (prefix is None or prefix.codes) else 2.0 ** -8
+            many = max((max_rows or rows) if cache.codes else 0, rows if prefix is not None and prefix.codes else 0) * G > 16
+            values16 = 2.0 ** -10 if many else 0.0
             bound[lo:hi, h * G:(h + 1) * G] = (2.0 ** -8 * (r.abs().nan_to_num(0) + weights * A)
-                                               + (weights + 2 * (hd + 16) * 2.0 ** -23 * S + 2.0 ** -18) * A + 1e-30)
+                                               + (weights + values16 + 2 * ((hd + 16) * 2.0 ** -23 + values16) * S
+                                                  + 2.0 ** -18) * A + 1e-30)
     return out, bound
 
 
@@ -138,10 +143,9 @@ def test_attention_follows_the_definition(shape, codes):
     cache = make_cache(codes, len(lens), Hk, max(lens) + 3, hd, seed=H + hd)
     q = 2 * torch.randn(starts[-1], H, hd, device=DEV, generator=_gen(5))
     q = q.bfloat16()
-    want, bound = attention64(q, cache, starts, lens)
     for max_rows in {max(rows_of), starts[-1]}:
         got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=max_rows)
-        check(got, want, bound)
+        check(got, *attention64(q, cache, starts, lens, max_rows=max_rows))
 
 
 @pytest.mark.parametrize("codes,pcodes", [(False, False), (True, True), (False, True), (True, False)])
@@ -156,4 +160,4 @@ def test_attention_behind_a_prefix(shape, codes, pcodes, prefix_len):
     q = (2 * torch.randn(starts[-1], H, hd, device=DEV, generator=_gen(6))).bfloat16()
     got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=max(rows_of), prefix=prefix,
                               prefix_len=prefix_len)
-    check(got, *attention64(q, cache, starts, lens, prefix=prefix, prefix_len=prefix_len))
+    check(got, *attention64(q, cache, starts, lens, prefix=prefix, prefix_len=prefix_len, max_rows=max(rows_of)))
