@@ -142,10 +142,13 @@ Layout lay_out(const memspec_batch* b, const memspec_kv* kv, const memspec_atten
   l.n = 1;
   if (two) {
     Launch x = launch(p->prefix, static_cast<long long>(b->rows) * group);
-    if (x.tiles && l.launch[0].tiles && x.codes == l.launch[0].codes) {
-      l.launch[0].prefix = true;
+    x.prefix = true;
+    if (x.tiles && x.codes == l.launch[0].codes) {
+      // one launch of attn_tiles.cu for both, whatever the sequences' own rows are (64 rows behind 32768 codes,
+      // up to 1024 codes of their own: 83.6 us, own keys by attn_rows.cu before it 87.2)
+      x.own = true;
+      l.launch[0] = x;
     } else {
-      x.prefix = true;
       l.launch[l.n++] = x;
     }
   }

@@ -302,7 +302,7 @@ int rows_ctas(bool codes, int nt);
 cudaError_t launch_attn_rows(int hd, bool codes, int nt, const ListArgs& a, cudaLaunchConfig_t cfg);
 constexpr int kTilesCtas = 152;
 cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg);   // InvalidValue: no tensor map
-constexpr int kTilesUnit = 256, kTilesStart = 2;   // vectors of a unit of attn_tiles.cu, its start's cost
+constexpr int kTilesUnit = 256, kTilesStart = 3;   // vectors of a unit of attn_tiles.cu, its start's cost
 constexpr int kRowsStart = 4;                      // of attn_rows.cu's
 
 }  // namespace memspec

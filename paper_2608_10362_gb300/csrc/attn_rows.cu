@@ -176,62 +176,48 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
       ahead += kTile;
       to = to + 1 == S::kDepth ? 0 : to + 1;
     };
+    // the unit's vectors first, a chunk a thread
+    constexpr int C = HD / 8;
+    static_assert(VT * C <= kThreads, "a thread per chunk");
+    const int q_vec = tid / C, q_c = tid % C, id = u.unit * VT + q_vec;
+    const uint32_t q_at = q_vec * HD * 2 + (q_c ^ (q_vec & 7)) * 16;
+    if (tid < VT * C) {
+      const int j = vector_row(a, id);
+      const bool on = id < u.vecs;
+      cp_async16(q_smem + q_at, on ? a.q + (u.row0 + j) * a.ldq + (u.head * a.group + id - j * a.group) * HD + q_c * 8 : a.q, on);
+    }
+    cp_commit();
 #pragma unroll 1
     for (int d = 0; d < S::kDepth - 1; ++d) fill_next();
-
-    // ---- the unit's vectors
-    {
-      constexpr int C = HD / 8, N = (VT * C + kThreads - 1) / kThreads;
-      uint4 in[N];
+    if (tid < VT) sm.sight[tid] = sight_of(a, u, u.unit * VT + tid);
+    cp_wait<S::kDepth - 1>();
+    if constexpr (CODES) {   // to fp16, and in the order of the fragments
+      uint4 in = make_uint4(0, 0, 0, 0);
+      if (tid < VT * C) in = *reinterpret_cast<const uint4*>(sm.q + q_at);
       float top = 0.f;
+      top_of(in.x, top);
+      top_of(in.y, top);
+      top_of(in.z, top);
+      top_of(in.w, top);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int at = i * kThreads + tid, vec = u.unit * VT + at / C;
-        in[i] = make_uint4(0, 0, 0, 0);
-        if (at < VT * C && vec < u.vecs) {
-          const int row = u.row0 + vec / a.group, head = u.head * a.group + vec % a.group;
-          in[i] = *reinterpret_cast<const uint4*>(a.q + row * a.ldq + head * HD + at % C * 8);
-        }
-        if constexpr (CODES) {
-          top_of(in[i].x, top);
-          top_of(in[i].y, top);
-          top_of(in[i].z, top);
-          top_of(in[i].w, top);
-        }
-      }
-      float up = 1.f;
-      if constexpr (CODES) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        if (lane == 0) sm.q_scale[warp] = top;
-        __syncthreads();
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm.q_scale[w]);
-        up = up_to_f16(top);
-        __syncthreads();
-        if (tid == 0) sm.q_scale[0] = 1.f / up;
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int at = i * kThreads + tid, vec = at / C, c = at % C;
-        if (at >= VT * C) continue;
-        if constexpr (CODES) {
-          const uint32_t w[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            // elements hd, hd + 1 go where the fragments' order wants them: a lane's word of four codes
-            // is one step's pairs k = 2t, 2t + 1 and 2t + 8, 2t + 9
-            const int hd = c * 8 + j * 2, to = hd / 64 * 64 + hd % 16 / 4 * 16 + hd % 64 / 16 * 2 + hd % 4 / 2 * 8;
-            const int chunk = to / 8 ^ (vec & 7);
-            *reinterpret_cast<uint32_t*>(sm.q + vec * HD * 2 + chunk * 16 + to % 8 * 2) =
-                scaled_f16(w[j], up);
-          }
-        } else {
-          *reinterpret_cast<uint4*>(sm.q + vec * HD * 2 + (c ^ (vec & 7)) * 16) = in[i];
-        }
-      }
-      if (tid < VT) sm.sight[tid] = sight_of(a, u, u.unit * VT + tid);
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+      if (lane == 0) sm.q_scale[warp] = top;
       __syncthreads();
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm.q_scale[w]);
+      const float up = up_to_f16(top);
+      if (tid < VT * C) {
+        const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          // a lane's word of four codes is one step's pairs k = 2t, 2t + 1 and 2t + 8, 2t + 9
+          const int hd = q_c * 8 + j * 2, to = hd / 64 * 64 + hd % 16 / 4 * 16 + hd % 64 / 16 * 2 + hd % 4 / 2 * 8;
+          *reinterpret_cast<uint32_t*>(sm.q + q_vec * HD * 2 + (to / 8 ^ (q_vec & 7)) * 16 + to % 8 * 2) = scaled_f16(w[j], up);
+        }
+      }
+      __syncthreads();
+      if (tid == 0) sm.q_scale[0] = 1.f / up;
     }
+    __syncthreads();
     const float scale = CODES ? a.scale * sm.q_scale[0] : a.scale;
     uint32_t qf[NT][KS][2];
 #pragma unroll

@@ -7,7 +7,7 @@ is not satisfied piece by piece for the error.
 from __future__ import annotations
 
 import ctypes as C
-import math
+import functools
 
 import torch
 
@@ -55,7 +55,8 @@ class KVCache:
         self.c = _lib.Kv(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if codes else None,
                          v_scale.data_ptr() if codes else None, *_strides(k),
                          *(_strides(k_scale) if codes else (0, 0, 0)), *k.shape)
-        self.ref = C.byref(self.c)
+        self.ref, self.pointer = C.byref(self.c), C.pointer(self.c)
+        self.sizes = (*k.shape, codes)
 
     @classmethod
     def zeros(cls, n_seq: int, n_heads: int, max_pos: int, head_dim: int, dtype=_BF16, device="cuda") -> "KVCache":
@@ -85,16 +86,14 @@ def op_rope_table(positions: int, head_dim: int, base: float = 10000.0, device="
 
 
 def _batch(starts: torch.Tensor, lens: torch.Tensor, cache: KVCache, rows: int) -> _lib.Batch:
-    if not isinstance(cache, KVCache):
+    if type(cache) is not KVCache:
         raise ValueError("cache must be a KVCache")
-    n = lens.shape[0] if lens.dim() == 1 else 0
-    if not (n > 0 and starts.shape == (n + 1,) and starts.dtype is _I32 and lens.dtype is _I32
-            and starts.get_device() == lens.get_device() == cache.dev and starts.is_contiguous()
-            and lens.is_contiguous()):
+    n, dev = lens.numel(), cache.dev
+    if not (starts.numel() == n + 1 and starts.dtype is _I32 and lens.dtype is _I32 and starts.get_device() == dev
+            and lens.get_device() == dev and starts.dim() == 1 and lens.dim() == 1 and starts.is_contiguous()
+            and lens.is_contiguous() and 0 < n <= cache.n_seq and 0 < rows < 1 << 31):
         _cuda_arg("lens", lens, _I32, (n,), cache.k)
         _cuda_arg("starts", starts, _I32, (n + 1,), cache.k)
-        raise ValueError("starts and lens must be 1-D, starts one longer than lens and lens not empty")
-    if n > cache.n_seq or rows >= 1 << 31:
         raise ValueError(f"{n} sequences of {rows} rows for a cache of {cache.n_seq}")
     return _lib.Batch(starts.data_ptr(), lens.data_ptr(), n, rows)
 
@@ -110,20 +109,25 @@ def op_kv_append(qkv: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: 
     op_rope_table's table (None: not) at position prefix_len + first own slot + offset (int32 [rows];
     None: the row's place), see memspec_op_kv_append."""
     lib = _lib.load()
-    if not isinstance(qkv, torch.Tensor) or qkv.dtype not in (_F32, _BF16):
+    if not isinstance(qkv, torch.Tensor) or qkv.dtype is not _F32 and qkv.dtype is not _BF16:
         raise ValueError("qkv must be a float32 or bfloat16 tensor")
-    ld = _rows_arg("qkv", qkv, qkv.dtype)
-    rows, width = qkv.shape
+    rows = qkv.shape[0] if qkv.dim() == 2 else 0
     b = _batch(starts, lens, cache, rows)
-    dev, hd = cache.dev, cache.head_dim
-    if qkv.get_device() != dev:
-        raise ValueError(f"qkv is on {qkv.device}, not on {cache.device}")
-    if n_heads < 1 or width != (n_heads + 2 * cache.n_heads) * hd:
-        raise ValueError(f"qkv must have {n_heads} + 2 * {cache.n_heads} heads of {hd}, not {width} columns")
+    dev, hd, width = cache.dev, cache.head_dim, (n_heads + 2 * cache.n_heads) * cache.head_dim
+    if qkv.is_contiguous() and qkv.get_device() == dev:
+        ld = width
+    else:
+        ld = _rows_arg("qkv", qkv, qkv.dtype, cache.k)
+    if n_heads < 1 or qkv.shape[1] != width:
+        raise ValueError(f"qkv must have {n_heads} + 2 * {cache.n_heads} heads of {hd}, not {qkv.shape[1]} columns")
+    positions = 0
     if rope is not None:
-        if rope.dim() != 3 or rope.shape[1] >= 1 << 31:
-            raise ValueError("rope must be op_rope_table's")
-        _cuda_arg("rope", rope, _F32, (2, rope.shape[1], hd // 2), qkv)
+        positions = rope.shape[1] if rope.dim() == 3 else 0
+        if not (0 < positions < 1 << 31 and rope.numel() == positions * hd and rope.shape[0] == 2 and rope.dtype is _F32
+                and rope.get_device() == dev and rope.is_contiguous()):
+            if not 0 < positions < 1 << 31:
+                raise ValueError("rope must be op_rope_table's")
+            _cuda_arg("rope", rope, _F32, (2, positions, hd // 2), qkv)
     if offsets is not None:
         _cuda_arg("offsets", offsets, _I32, (rows,), qkv)
     if (q_gain is None) != (k_gain is None):
@@ -134,13 +138,13 @@ def op_kv_append(qkv: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: 
     if not 0 <= prefix_len < 1 << 31:
         raise ValueError(f"prefix_len must be from 0 to 2^31 - 1, not {prefix_len!r}")
     if q is None:
-        q = _new_result(stream, rows, n_heads, hd, dtype=_BF16, device=qkv.device)
+        q = _new_result(stream, rows, n_heads, hd, dtype=_BF16, device=cache.device)
     else:
         _cuda_arg("q", q, _BF16, (rows, n_heads, hd), qkv)
     if stream is not None:
         _used_on(stream, qkv, *cache.tensors, starts, lens, rope, offsets, q_gain, k_gain, q)
     a = _lib.Append(qkv.data_ptr(), _lib.F32 if qkv.dtype is _F32 else _lib.BF16, n_heads, ld,
-                    None if rope is None else rope.data_ptr(), 0 if rope is None else rope.shape[1], prefix_len,
+                    None if rope is None else rope.data_ptr(), positions, prefix_len,
                     None if offsets is None else offsets.data_ptr(), None if q_gain is None else q_gain.data_ptr(),
                     None if k_gain is None else k_gain.data_ptr(), eps, q.data_ptr())
     st = _call_on(dev, stream, lib.memspec_op_kv_append, C.byref(b), cache.ref, C.byref(a))
@@ -174,6 +178,25 @@ def op_kv_read(cache: KVCache, starts: torch.Tensor, lens: torch.Tensor, rows: i
     return k, v
 
 
+def _of_sizes(sizes: tuple) -> _lib.Kv:
+    """A cache of these sizes, with addresses that only a size's check looks at."""
+    n_seq, n_heads, max_pos, hd, codes = sizes
+    at = 1 << 8
+    return _lib.Kv(at, at, at if codes else None, at if codes else None, 0, 0, hd, 0, 0, 1, n_seq, n_heads, max_pos, hd)
+
+
+@functools.lru_cache(maxsize=512)
+def _attention_scratch_bytes(sizes: tuple, n_seq: int, rows: int, n_heads: int, max_rows: int, prefix: tuple | None,
+                             prefix_len: int) -> int:
+    lib = _lib.load()
+    at, nb = 1 << 8, C.c_size_t()
+    kv, b = _of_sizes(sizes), _lib.Batch(at, at, n_seq, rows)
+    p = None if prefix is None else C.pointer(_of_sizes(prefix))
+    a = _lib.Attention(at, 0, at, 0, n_heads, 1.0, None, p, prefix_len, max_rows)
+    _check(lib, lib.memspec_op_attention_scratch_bytes(C.byref(b), C.byref(kv), C.byref(a), C.byref(nb)))
+    return nb.value
+
+
 def _heads_arg(name: str, t: torch.Tensor, like: torch.Tensor) -> int:
     """bf16 [rows][heads][head_dim] with whole rows without gaps; the row stride."""
     _cuda_arg(name, t, _BF16, like=like)
@@ -198,14 +221,17 @@ def op_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: to
     most rows that a sequence has (default: all rows; it chooses the kernel, nothing else).
     ``scratch`` (any content) of memspec_op_attention_scratch_bytes bytes saves an allocation."""
     lib = _lib.load()
-    if not isinstance(q, torch.Tensor):
-        raise ValueError("q must be a CUDA tensor")
-    b = _batch(starts, lens, cache, q.shape[0])
-    dev, hd = cache.dev, cache.head_dim
-    ldq = _heads_arg("q", q, cache.k)
-    rows, n_heads, _ = q.shape
-    if q.shape[2] != hd or n_heads % cache.n_heads:
-        raise ValueError(f"q's heads must be of {hd}, a multiple of {cache.n_heads}, not {list(q.shape)}")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a CUDA tensor [rows][heads][head_dim]")
+    rows, n_heads, hd = q.shape
+    b = _batch(starts, lens, cache, rows)
+    dev = cache.dev
+    if q.is_contiguous() and q.dtype is _BF16 and q.get_device() == dev:
+        ldq = n_heads * hd
+    else:
+        ldq = _heads_arg("q", q, cache.k)
+    if hd != cache.head_dim or n_heads < 1 or n_heads % cache.n_heads:
+        raise ValueError(f"q's heads must be of {cache.head_dim}, a multiple of {cache.n_heads}, not {list(q.shape)}")
     if max_rows is None:
         max_rows = rows
     if not 1 <= max_rows <= rows:
@@ -222,19 +248,19 @@ def op_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: to
     elif not 0 <= prefix_len <= prefix.max_pos:
         raise ValueError(f"prefix_len must be in 0..{prefix.max_pos}, not {prefix_len!r}")
     if out is None:
-        out = _new_result(stream, rows, n_heads, hd, dtype=_BF16, device=q.device)
+        out = _new_result(stream, rows, n_heads, hd, dtype=_BF16, device=cache.device)
         ldo = n_heads * hd
     else:
         ldo = _heads_arg("out", out, cache.k)
         if out.shape != q.shape:
             raise ValueError(f"out must be {list(q.shape)}, not {list(out.shape)}")
-    a = _lib.Attention(q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads, 1 / math.sqrt(hd) if scale is None else scale,
-                       None if tree is None else tree.data_ptr(), None if prefix is None else C.pointer(prefix.c),
+    a = _lib.Attention(q.data_ptr(), ldq, out.data_ptr(), ldo, n_heads, hd ** -0.5 if scale is None else scale,
+                       None if tree is None else tree.data_ptr(), None if prefix is None else prefix.pointer,
                        prefix_len or 0, max_rows)
     if scratch is None:
-        nb = C.c_size_t()
-        _check(lib, lib.memspec_op_attention_scratch_bytes(C.byref(b), cache.ref, C.byref(a), C.byref(nb)))
-        scratch = _new(stream, torch.empty, nb.value, dtype=torch.uint8, device=q.device)
+        nb = _attention_scratch_bytes(cache.sizes, b.n_seq, rows, n_heads, max_rows,
+                                      None if prefix is None else prefix.sizes, prefix_len or 0)
+        scratch = _new(stream, torch.empty, nb, dtype=torch.uint8, device=cache.device)
     elif scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be contiguous on {q.device}")
     if stream is not None:
