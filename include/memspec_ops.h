@@ -300,7 +300,8 @@ memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, co
  * A row that sees nothing gives 0.  All sequences share the prefix, which is read
  * once for all of them; it has the cache's heads and head_dim, its own strides and
  * type.  q . k and sums are fp32; the weights enter the product with v in 16 bits
- * (of bf16 caches bf16, of codes fp16), off by half a step of it each.  With more
+ * (of bf16 caches bf16, of codes fp16), off by half a step of it each, of codes
+ * also by 2^-31 of the largest weight times scale.  With more
  * than 16 query vectors (rows times heads of a group) a head of k and v, keys and
  * values of codes count as fp16: off by 2^-10 of themselves, or by 2^-23 of the
  * largest scale among their 128 positions.

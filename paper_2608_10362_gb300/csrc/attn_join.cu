@@ -21,20 +21,15 @@ constexpr int kRowsVectors = 16;
 template <int HD>
 __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ JoinArgs a) {
   constexpr int E = HD / 32;
-  __shared__ int found[4];
+  __shared__ int shared;
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32, heads = a.group * a.kv_heads;
   // (starts and lens were complete before the launch before this one began)
-  if (threadIdx.x == 0) found[0] = -1;
-  __syncthreads();
-  for (int b = threadIdx.x; b < a.n_seq; b += kThreads) {
-    const SeqRows s = seq_rows(a.starts, a.lens, b, a.rows);
-    if (row >= s.row0 && row < s.row0 + s.n) found[0] = b, found[1] = s.row0, found[2] = s.n, found[3] = s.len;
-  }
-  __syncthreads();
+  const int seq = find_sequence(a.starts, a.lens, a.n_seq, a.rows, row, &shared);
+  const SeqRows found = seq < 0 ? SeqRows{} : seq_rows(a.starts, a.lens, seq, a.rows);
   pdl_wait();
   pdl_launch_dependents();
   const int h = blockIdx.y * kWarps + warp;
-  if (found[0] < 0 || h >= heads) return;
+  if (seq < 0 || h >= heads) return;
   const int kv_head = h / a.group;
   float top = kStart, den = 0.f, sum[E] = {};
   bool any = false;
@@ -42,10 +37,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   for (int p = 0; p < a.parts; ++p) {
     const JoinPart& part = a.part[p];
     const bool own = part.at < 0;
-    const int b = own ? found[0] : part.at;
+    const int b = own ? seq : part.at;
     const uint32_t base = part.bases[b], total = part.bases[part.list];
-    const uint32_t vecs = (own ? found[2] : a.rows) * a.group, vec = (row - (own ? found[1] : 0)) * a.group + h - kv_head * a.group;
-    const uint32_t tiles = tiles_of(own ? min(max(found[3], 0), a.max_pos) : part.keys);
+    const uint32_t vecs = (own ? found.n : a.rows) * a.group, vec = (row - (own ? found.row0 : 0)) * a.group + h - kv_head * a.group;
+    const uint32_t tiles = tiles_of(own ? min(max(found.len, 0), a.max_pos) : part.keys);
     const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit, units = (vecs + part.unit - 1) / part.unit;
     const uint32_t per_tile = part.pairs ? (vecs + 127) / 128 : units, w = part.pairs && vecs - unit * part.unit > 128 ? 2 : 1;
     const bool pair = w == 2;

@@ -92,7 +92,7 @@ struct Pieces {
   }
   __device__ uint32_t owner(uint32_t x) const {
     const uint32_t at = longer * (each + 1);
-    return x < at ? x / (each + 1) : longer + (x - at) / max(each, 1u);
+    return min(x < at ? x / (each + 1) : longer + (x - at) / max(each, 1u), ctas - 1);
   }
 };
 
@@ -100,49 +100,45 @@ struct Pieces {
 constexpr int kCached = 64;
 struct alignas(16) Plan {
   uint32_t bases[kMaxSeqs + 2];
-  uint32_t sums[20];
+  uint64_t sums[20];
   SeqRows rows[kCached];
 };
 
-// Made by all THREADS threads.
+// Made by all THREADS threads.  Sequences whose rows overlap (starts that do not ascend) can make the line longer
+// than 32 bits count: it ends there, the rest is not worked on.
+constexpr uint64_t kLineEnd = 0xf0000000u;
 template <class CUT, int THREADS>
 __device__ __forceinline__ void make_plan(const ListArgs& a, Plan& plan) {
   static_assert(THREADS <= 640, "a word of sums per warp");
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, n = list_len(a);
-  uint32_t before = 0;
+  uint64_t before = 0;
 #pragma unroll 1
   for (int b0 = 0; b0 < n; b0 += THREADS) {
     const int b = b0 + tid;
-    uint32_t mine = 0;
+    uint64_t mine = 0;
     if (b < n) {
       const SeqRows s = list_rows(a, b);
       if (b < kCached) plan.rows[b] = s;
       mine = CUT::per_head(static_cast<uint32_t>(s.n) * a.group, tiles_of(list_keys(a, b, s))) * a.kv_heads;
     }
-    uint32_t incl = mine;
+    uint64_t incl = mine;
 #pragma unroll 1
     for (int o = 1; o < 32; o *= 2) {
-      const uint32_t up = __shfl_up_sync(~0u, incl, o);
+      const uint64_t up = __shfl_up_sync(~0u, incl, o);
       if (lane >= o) incl += up;
-    }
-    if (n <= 32) {   // the first warp has it all
-      if (tid < 32 && b <= n) plan.bases[b] = incl - mine;
-      if (b == 31 && n == 32) plan.bases[32] = incl;
-      break;
     }
     if (lane == 31) plan.sums[warp] = incl;
     __syncthreads();
-    uint32_t sum = before;
+    uint64_t sum = before;
 #pragma unroll 1
     for (int w = 0; w < THREADS / 32; ++w) {
       if (w < warp) sum += plan.sums[w];
       before += plan.sums[w];
     }
-    if (b < n) plan.bases[b] = sum + incl - mine;
-    if (b == n - 1) plan.bases[n] = sum + incl;
+    if (b < n) plan.bases[b] = static_cast<uint32_t>(min(sum + incl - mine, kLineEnd));
+    if (b == n - 1) plan.bases[n] = static_cast<uint32_t>(min(sum + incl, kLineEnd));
     __syncthreads();
   }
-  __syncthreads();
 }
 
 // A CTA's stretch of one unit.

@@ -37,6 +37,19 @@ __device__ __forceinline__ SeqRows seq_rows(const int* starts, const int* lens, 
   return {r0, r1 - r0, lens[b]};
 }
 
+// The sequence that a row belongs to (of several, where starts do not ascend, the first), -1: none.  All
+// threads call it.
+__device__ __forceinline__ int find_sequence(const int* starts, const int* lens, int n_seq, int rows, int row, int* shared) {
+  if (threadIdx.x == 0) *shared = n_seq;
+  __syncthreads();
+  for (int b = threadIdx.x; b < n_seq; b += blockDim.x) {
+    const SeqRows s = seq_rows(starts, lens, b, rows);
+    if (row >= s.row0 && row < s.row0 + s.n) atomicMin(shared, b);
+  }
+  __syncthreads();
+  return *shared < n_seq ? *shared : -1;
+}
+
 // Why `kv` cannot be used, or nullptr.
 const char* kv_problem(const memspec_kv* kv, bool write);
 KvView kv_view(const memspec_kv* kv);

@@ -49,16 +49,11 @@ struct ReadArgs {
 struct RowAt {
   int seq, j, n, len;
 };
-__device__ __forceinline__ RowAt find_row(const int* starts, const int* lens, int n_seq, int rows, int row,
-                                          RowAt* shared) {
-  if (threadIdx.x == 0) shared->seq = -1;
-  __syncthreads();
-  for (int b = threadIdx.x; b < n_seq; b += kThreads) {
-    const SeqRows s = seq_rows(starts, lens, b, rows);
-    if (row >= s.row0 && row < s.row0 + s.n) *shared = {b, row - s.row0, s.n, s.len};
-  }
-  __syncthreads();
-  return *shared;
+__device__ __forceinline__ RowAt find_row(const int* starts, const int* lens, int n_seq, int rows, int row, int* shared) {
+  const int b = find_sequence(starts, lens, n_seq, rows, row, shared);
+  if (b < 0) return {-1, 0, 0, 0};
+  const SeqRows s = seq_rows(starts, lens, b, rows);
+  return {b, row - s.row0, s.n, s.len};
 }
 
 template <int E>
@@ -146,7 +141,7 @@ __device__ __forceinline__ void store_codes(char* p, float* scale, const Vec<HD 
 template <int HD, class T>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a) {
   constexpr int E = HD / 64;
-  __shared__ RowAt shared;
+  __shared__ int shared;
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int heads = a.n_heads + 2 * a.kv.n_heads;
   const int h0 = blockIdx.y * kHeadsPerCta + warp * kHeadsPerWarp;
@@ -226,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant_
 template <int HD>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadArgs a) {
   constexpr int E = HD / 64;
-  __shared__ RowAt shared;
+  __shared__ int shared;
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   pdl_wait();
   pdl_launch_dependents();

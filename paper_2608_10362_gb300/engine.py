@@ -287,6 +287,18 @@ class Engine:
         self.verify_step(K)
         self.accept_commit(K, temperature, results)
 
+    def kv_cache(self, layer: int, draft_id: int | None = None):
+        """The keys and values of one layer of the target, or of a draft: a KVCache over the engine's own
+        memory ([requests][kv heads][max_seq][head_dim], bf16), for op_attention and op_kv_read.  What the
+        steps write there is ordered on `self.stream`."""
+        from .kv import KVCache
+        shape, kv = (self.shape, self.kv) if draft_id is None else (self.drafts[draft_id][0], self.drafts[draft_id][2])
+        if not 0 <= layer < shape.n_layers:
+            raise ValueError(f"layer must be in 0..{shape.n_layers - 1}, not {layer!r}")
+        layers = kv.view(torch.bfloat16).view(shape.n_layers, 2, self.max_batch, shape.n_kv_heads, self.max_seq,
+                                              shape.head_dim)
+        return KVCache(layers[layer, 0], layers[layer, 1])
+
     # -------------------------------------------------------------- inspection
     def info(self, what: int) -> int:
         v = C.c_int64()
