@@ -41,7 +41,7 @@ struct Shape {
   static constexpr int kDepth = std::min(8, kBudget / (kWarps * kStage));
   static constexpr int kRing = kWarps * kDepth * kStage;
   static constexpr int kSmem = kFixed + kRing;
-  static_assert(kFixed % 16 == 0 && kDepth >= 2 && kSmem <= (kPerSm == 2 ? 113 : 227) * 1024, "shared memory");
+  static_assert(kFixed % 128 == 0 && kDepth >= 2 && kSmem <= (kPerSm == 2 ? 113 : 227) * 1024, "shared memory");
   static_assert(kRing >= VT * (kWarps * (HD * 4 + 8) + 8), "the warps' sums lie where the ring was");
 };
 
