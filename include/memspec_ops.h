@@ -265,13 +265,15 @@ typedef struct memspec_append {
  * whose slot or position (where there is a table) is out of range leaves the cache
  * as it was, and its q is 0.  A vector with an infinity or a NaN is not finite when
  * it is read, others are not affected.  The cache's vectors must not overlap, nor
- * q any other argument; qkv is aligned to two elements.
+ * q any other argument.  qkv is aligned to two elements, the table to 16 bytes, q
+ * and gains to 8.
  * Allocates nothing.  Errors: INVALID_ARG, CUDA. */
 memspec_status memspec_op_kv_append(const memspec_batch* batch, const memspec_kv* kv,
                                     const memspec_append* args, void* stream);
 
 /* The rows' keys and values as the cache holds them: bf16 [rows][kv heads][head_dim]
- * each, codes times their scale rounded once; 0 at a slot out of range.  Allocates
+ * each, 8-byte aligned, codes times their scale rounded once; 0 at a slot out of
+ * range.  Allocates
  * nothing.  Errors: INVALID_ARG, CUDA. */
 memspec_status memspec_op_kv_read(const memspec_batch* batch, const memspec_kv* kv, void* k_out_dev,
                                   void* v_out_dev, void* stream);

@@ -6,8 +6,10 @@
 // turned by the position's angle, then bf16, or for a cache of codes rint(x' / s) with
 // s = max(max|x'|, 127 * 2^-64) / 127.  Every value is read once and written once, all of it
 // elementwise but two sums over a vector: the bound is memory, or at few rows the latency of
-// two dependent loads (which sequence, then the angles).  A warp takes whole vectors, so sums
-// are shuffles, and a lane holds both values of a pair, so a turn needs no exchange.
+// two dependent loads (which sequence, then the angles).  hd / 8 lanes take a vector, four
+// elements of each half a lane: a pair is in one lane, so that a turn needs no exchange, two or
+// four vectors share a warp's sums and every access is 8 or 16 bytes (a vector per warp, 4 bytes a
+// lane: 2047 rows of 96 heads 33 us, bound by issue; now @@).
 #include <algorithm>
 #include <string>
 
@@ -19,8 +21,13 @@ namespace memspec {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kHeadsPerWarp = 4;   // vectors of a warp, loaded together
-constexpr int kHeadsPerCta = kWarps * kHeadsPerWarp;
+constexpr int kSets = 2;           // vectors of a lane, loaded together
+
+template <int HD>
+struct Lanes {
+  static constexpr int kLanes = HD / 8, kVectors = 32 / kLanes;   // of a vector; vectors at a time
+  static constexpr int kHeads = kVectors * kSets * kWarps;        // of a CTA
+};
 
 struct AppendArgs {
   KvView kv;
@@ -28,6 +35,7 @@ struct AppendArgs {
   int n_seq, rows;
   const void* x;
   long long ldx;             // elements
+  bool wide;                 // x and its rows are aligned to four elements
   const float* rope;         // [2][positions][hd/2] or nullptr
   int positions;
   const int* offsets;        // [rows] or nullptr: the row's place
@@ -50,203 +58,172 @@ struct RowAt {
   int seq, j, n, len;
 };
 __device__ __forceinline__ RowAt find_row(const int* starts, const int* lens, int n_seq, int rows, int row, int* shared) {
-  const int b = find_sequence(starts, lens, n_seq, rows, row, shared);
+  const int b = n_seq == 1 ? 0 : find_sequence(starts, lens, n_seq, rows, row, shared);
   if (b < 0) return {-1, 0, 0, 0};
   const SeqRows s = seq_rows(starts, lens, b, rows);
+  if (row < s.row0 || row >= s.row0 + s.n) return {-1, 0, 0, 0};
   return {b, row - s.row0, s.n, s.len};
 }
 
-template <int E>
-struct Vec {
-  float lo[E], hi[E];   // elements E * lane .. and those half a vector further on
-};
-
-template <int HD, class T>
-__device__ __forceinline__ Vec<HD / 64> load_vec(const T* p, int lane) {
-  constexpr int E = HD / 64;
-  Vec<E> r;
+__device__ __forceinline__ float2 bf16_pair(uint32_t v) {
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ float4 two_pairs(uint32_t a, uint32_t b) {
+  const float2 x = bf16_pair(a), y = bf16_pair(b);
+  return make_float4(x.x, x.y, y.x, y.y);
+}
+// Four elements; p is aligned to four of them, or (wide: false) to two.
+template <class T>
+__device__ __forceinline__ float4 load4(const T* p, bool wide) {
   if constexpr (sizeof(T) == 4) {
-    if constexpr (E == 2) {
-      const float2 a = __ldcs(reinterpret_cast<const float2*>(p) + lane);
-      const float2 b = __ldcs(reinterpret_cast<const float2*>(p + HD / 2) + lane);
-      r.lo[0] = a.x, r.lo[1] = a.y, r.hi[0] = b.x, r.hi[1] = b.y;
-    } else {
-      r.lo[0] = __ldcs(p + lane);
-      r.hi[0] = __ldcs(p + HD / 2 + lane);
-    }
+    if (wide) return __ldcs(reinterpret_cast<const float4*>(p));
+    const float2 a = __ldcs(reinterpret_cast<const float2*>(p)), b = __ldcs(reinterpret_cast<const float2*>(p) + 1);
+    return make_float4(a.x, a.y, b.x, b.y);
   } else {
-    if constexpr (E == 2) {
-      const uint32_t a = __ldcs(reinterpret_cast<const uint32_t*>(p) + lane);
-      const uint32_t b = __ldcs(reinterpret_cast<const uint32_t*>(p + HD / 2) + lane);
-      r.lo[0] = __uint_as_float(a << 16), r.lo[1] = __uint_as_float(a & 0xffff0000u);
-      r.hi[0] = __uint_as_float(b << 16), r.hi[1] = __uint_as_float(b & 0xffff0000u);
-    } else {
-      r.lo[0] = __bfloat162float(p[lane]);
-      r.hi[0] = __bfloat162float(p[HD / 2 + lane]);
+    if (wide) {
+      const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
+      return two_pairs(v.x, v.y);
     }
-  }
-  return r;
-}
-
-template <int HD>
-__device__ __forceinline__ void store_bf16(bf16* p, const Vec<HD / 64>& v, int lane) {
-  if constexpr (HD == 128) {
-    reinterpret_cast<__nv_bfloat162*>(p)[lane] = __floats2bfloat162_rn(v.lo[0], v.lo[1]);
-    reinterpret_cast<__nv_bfloat162*>(p + HD / 2)[lane] = __floats2bfloat162_rn(v.hi[0], v.hi[1]);
-  } else {
-    p[lane] = __float2bfloat16_rn(v.lo[0]);
-    p[HD / 2 + lane] = __float2bfloat16_rn(v.hi[0]);
+    return two_pairs(__ldcs(reinterpret_cast<const uint32_t*>(p)), __ldcs(reinterpret_cast<const uint32_t*>(p) + 1));
   }
 }
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-  return v;
+__device__ __forceinline__ float4 gain4(const bf16* p) {
+  const uint2 v = *reinterpret_cast<const uint2*>(p);
+  return two_pairs(v.x, v.y);
 }
-// The largest; a NaN among them is the result, so that a vector with one is known by its scale.
+__device__ __forceinline__ void store4(bf16* p, const float4& v) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+__device__ __forceinline__ float4 mul(const float4& a, const float4& b) {
+  return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w);
+}
+__device__ __forceinline__ float4 mul(const float4& a, float b) { return make_float4(a.x * b, a.y * b, a.z * b, a.w * b); }
+__device__ __forceinline__ float dot(const float4& a) { return a.x * a.x + a.y * a.y + a.z * a.z + a.w * a.w; }
+
+// The larger; a NaN is the result, so that a vector with one is known by its scale.
 __device__ __forceinline__ float max_nan(float a, float b) { return a > b || isnan(a) ? a : b; }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(~0u, v, o));
-  return v;
+__device__ __forceinline__ float top4(const float4& a) {
+  return max_nan(max_nan(fabsf(a.x), fabsf(a.y)), max_nan(fabsf(a.z), fabsf(a.w)));
 }
-
-// Codes of a vector and its scale.  The division is as the definition has it: x / s is rounded
-// once, then to a whole number.
-template <int HD>
-__device__ __forceinline__ void store_codes(char* p, float* scale, const Vec<HD / 64>& v, int lane) {
-  constexpr int E = HD / 64;
-  float top = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) top = max_nan(max_nan(top, fabsf(v.lo[e])), fabsf(v.hi[e]));
-  top = warp_max(top);
-  const float s = (top < 127.f * kSmallestScale ? 127.f * kSmallestScale : top) / 127.f;   // a NaN stays
-  int8_t lo[E], hi[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    lo[e] = static_cast<int8_t>(__float2int_rn(fminf(fmaxf(v.lo[e] / s, -127.f), 127.f)));
-    hi[e] = static_cast<int8_t>(__float2int_rn(fminf(fmaxf(v.hi[e] / s, -127.f), 127.f)));
-  }
-  if constexpr (E == 2) {
-    reinterpret_cast<char2*>(p)[lane] = make_char2(lo[0], lo[1]);
-    reinterpret_cast<char2*>(p + HD / 2)[lane] = make_char2(hi[0], hi[1]);
-  } else {
-    p[lane] = lo[0];
-    p[HD / 2 + lane] = hi[0];
-  }
-  if (lane == 0) *scale = s;
+// Codes as the definition has them: x / s is rounded once, then to a whole number.
+__device__ __forceinline__ void store_codes4(char* p, const float4& v, float s) {
+  auto code = [s](float x) { return __float2int_rn(fminf(fmaxf(x / s, -127.f), 127.f)) & 255; };
+  *reinterpret_cast<int*>(p) = code(v.x) | code(v.y) << 8 | code(v.z) << 16 | code(v.w) << 24;
 }
 
 template <int HD, class T>
 __global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ AppendArgs a) {
-  constexpr int E = HD / 64;
+  typedef Lanes<HD> L;
   __shared__ int shared;
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int e = lane % L::kLanes * 4;    // the lane's elements: e .. e + 3 of each half
   const int heads = a.n_heads + 2 * a.kv.n_heads;
-  const int h0 = blockIdx.y * kHeadsPerCta + warp * kHeadsPerWarp;
+  const int h0 = blockIdx.y * L::kHeads + warp * L::kVectors * kSets + lane / L::kLanes;
   pdl_wait();
   pdl_launch_dependents();
-  Vec<E> v[kHeadsPerWarp];
-  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  float4 lo[kSets], hi[kSets];
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx + e;
 #pragma unroll
-  for (int i = 0; i < kHeadsPerWarp; ++i)
-    if (h0 + i < heads) v[i] = load_vec<HD>(x + (h0 + i) * HD, lane);
-  float gq[2 * E], gk[2 * E];
-  if (a.q_gain != nullptr) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      gq[e] = __bfloat162float(a.q_gain[lane * E + e]);
-      gq[E + e] = __bfloat162float(a.q_gain[HD / 2 + lane * E + e]);
-      gk[e] = __bfloat162float(a.k_gain[lane * E + e]);
-      gk[E + e] = __bfloat162float(a.k_gain[HD / 2 + lane * E + e]);
-    }
+  for (int i = 0; i < kSets; ++i) {
+    const int h = min(h0 + i * L::kVectors, heads - 1);
+    lo[i] = load4(x + h * HD, a.wide);
+    hi[i] = load4(x + h * HD + HD / 2, a.wide);
   }
   const RowAt at = find_row(a.starts, a.lens, a.n_seq, a.rows, row, &shared);
   if (at.seq < 0) return;
   const long long first = static_cast<long long>(at.len) - at.n, slot = first + at.j;
   const long long pos = a.prefix + first + (a.offsets != nullptr ? a.offsets[row] : at.j);
   const bool fits = slot >= 0 && slot < a.kv.max_pos && (a.rope == nullptr || (pos >= 0 && pos < a.positions));
-  float c[E], s[E];
+  float4 c = make_float4(1.f, 1.f, 1.f, 1.f), s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (fits && a.rope != nullptr) {
-    const float* cos_t = a.rope + pos * (HD / 2);
-    const float* sin_t = cos_t + static_cast<long long>(a.positions) * (HD / 2);
-#pragma unroll
-    for (int e = 0; e < E; ++e) c[e] = cos_t[lane * E + e], s[e] = sin_t[lane * E + e];
+    const float* cos_t = a.rope + pos * (HD / 2) + e;
+    c = *reinterpret_cast<const float4*>(cos_t);
+    s = *reinterpret_cast<const float4*>(cos_t + static_cast<long long>(a.positions) * (HD / 2));
   }
 #pragma unroll
-  for (int i = 0; i < kHeadsPerWarp; ++i) {
-    const int h = h0 + i;
-    if (h >= heads) return;
+  for (int i = 0; i < kSets; ++i) {   // every lane goes through the sums, whatever its vector is
+    const int h = h0 + i * L::kVectors;
     const bool is_q = h < a.n_heads, is_k = !is_q && h < a.n_heads + a.kv.n_heads;
-    if (!fits) {   // nothing is kept of the row
-      if (is_q) store_bf16<HD>(a.q + (static_cast<long long>(row) * a.n_heads + h) * HD, Vec<E>{}, lane);
-      continue;
-    }
-    if (is_q || is_k) {
-      if (a.q_gain != nullptr) {
-        float sum = 0.f;
+    if (a.q_gain != nullptr) {
+      float sum = dot(lo[i]) + dot(hi[i]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += v[i].lo[e] * v[i].lo[e] + v[i].hi[e] * v[i].hi[e];
-        const float r = rsqrtf(warp_sum(sum) * (1.f / HD) + a.eps);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          v[i].lo[e] = v[i].lo[e] * r * (is_q ? gq[e] : gk[e]);
-          v[i].hi[e] = v[i].hi[e] * r * (is_q ? gq[E + e] : gk[E + e]);
-        }
-      }
-      if (a.rope != nullptr) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float lo = v[i].lo[e], hi = v[i].hi[e];
-          v[i].lo[e] = lo * c[e] - hi * s[e];
-          v[i].hi[e] = lo * s[e] + hi * c[e];
-        }
+      for (int o = L::kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+      if (is_q || is_k) {
+        const bf16* g = (is_q ? a.q_gain : a.k_gain) + e;
+        const float r = rsqrtf(sum * (1.f / HD) + a.eps);
+        lo[i] = mul(mul(lo[i], r), gain4(g));
+        hi[i] = mul(mul(hi[i], r), gain4(g + HD / 2));
       }
     }
-    if (is_q) {
-      store_bf16<HD>(a.q + (static_cast<long long>(row) * a.n_heads + h) * HD, v[i], lane);
-      continue;
+    if (a.rope != nullptr && (is_q || is_k)) {
+      const float4 l = lo[i], u = hi[i];
+      lo[i] = make_float4(l.x * c.x - u.x * s.x, l.y * c.y - u.y * s.y, l.z * c.z - u.z * s.z, l.w * c.w - u.w * s.w);
+      hi[i] = make_float4(l.x * s.x + u.x * c.x, l.y * s.y + u.y * c.y, l.z * s.z + u.z * c.z, l.w * s.w + u.w * c.w);
     }
+    float scale = 0.f;
+    if (a.kv.k_scale != nullptr) {
+      float top = max_nan(top4(lo[i]), top4(hi[i]));
+#pragma unroll
+      for (int o = L::kLanes / 2; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(~0u, top, o));
+      scale = (top < 127.f * kSmallestScale ? 127.f * kSmallestScale : top) / 127.f;   // a NaN stays
+    }
+    if (h >= heads) continue;
     const int kh = h - a.n_heads - (is_k ? 0 : a.kv.n_heads);
     char* p = (is_k ? a.kv.k : a.kv.v) + at.seq * a.kv.seq + kh * a.kv.head + slot * a.kv.pos;
-    if (a.kv.k_scale == nullptr)
-      store_bf16<HD>(reinterpret_cast<bf16*>(p), v[i], lane);
-    else
-      store_codes<HD>(p, (is_k ? a.kv.k_scale : a.kv.v_scale) + at.seq * a.kv.s_seq + kh * a.kv.s_head +
-                             slot * a.kv.s_pos, v[i], lane);
+    if (is_q || a.kv.k_scale == nullptr) {
+      bf16* to = is_q ? a.q + (static_cast<long long>(row) * a.n_heads + h) * HD : reinterpret_cast<bf16*>(p);
+      if (!fits) {   // nothing is kept of the row
+        if (!is_q) continue;
+        lo[i] = hi[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      store4(to + e, lo[i]);
+      store4(to + e + HD / 2, hi[i]);
+    } else if (fits) {
+      store_codes4(p + e, lo[i], scale);
+      store_codes4(p + e + HD / 2, hi[i], scale);
+      if (e == 0)
+        (is_k ? a.kv.k_scale : a.kv.v_scale)[at.seq * a.kv.s_seq + kh * a.kv.s_head + slot * a.kv.s_pos] = scale;
+    }
   }
 }
 
 template <int HD>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadArgs a) {
-  constexpr int E = HD / 64;
+  typedef Lanes<HD> L;
   __shared__ int shared;
-  const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32, e = lane % L::kLanes * 4;
   pdl_wait();
   pdl_launch_dependents();
   const RowAt at = find_row(a.starts, a.lens, a.n_seq, a.rows, row, &shared);
   if (at.seq < 0) return;
   const long long slot = static_cast<long long>(at.len) - at.n + at.j;
   const bool fits = slot >= 0 && slot < a.kv.max_pos;
-  for (int i = blockIdx.y * kWarps + warp; i < 2 * a.kv.n_heads; i += gridDim.y * kWarps) {
-    const bool is_k = i < a.kv.n_heads;
-    const int h = is_k ? i : i - a.kv.n_heads;
-    Vec<E> v{};
+#pragma unroll
+  for (int i = 0; i < kSets; ++i) {
+    const int at_h = blockIdx.y * L::kHeads + (warp * kSets + i) * L::kVectors + lane / L::kLanes;
+    if (at_h >= 2 * a.kv.n_heads) return;
+    const bool is_k = at_h < a.kv.n_heads;
+    const int h = is_k ? at_h : at_h - a.kv.n_heads;
+    float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
     if (fits) {
       const char* p = (is_k ? a.kv.k : a.kv.v) + at.seq * a.kv.seq + h * a.kv.head + slot * a.kv.pos;
       if (a.kv.k_scale == nullptr) {
-        v = load_vec<HD>(reinterpret_cast<const bf16*>(p), lane);
+        lo = load4(reinterpret_cast<const bf16*>(p) + e, true);
+        hi = load4(reinterpret_cast<const bf16*>(p) + e + HD / 2, true);
       } else {
         const float s = (is_k ? a.kv.k_scale : a.kv.v_scale)[at.seq * a.kv.s_seq + h * a.kv.s_head + slot * a.kv.s_pos];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          v.lo[e] = s * static_cast<signed char>(p[lane * E + e]);
-          v.hi[e] = s * static_cast<signed char>(p[HD / 2 + lane * E + e]);
-        }
+        const char4 l = *reinterpret_cast<const char4*>(p + e), u = *reinterpret_cast<const char4*>(p + e + HD / 2);
+        auto value = [s](const char4& v) {
+          return make_float4(s * static_cast<signed char>(v.x), s * static_cast<signed char>(v.y),
+                             s * static_cast<signed char>(v.z), s * static_cast<signed char>(v.w));
+        };
+        lo = value(l), hi = value(u);
       }
     }
-    store_bf16<HD>((is_k ? a.k : a.v) + (static_cast<long long>(row) * a.kv.n_heads + h) * HD, v, lane);
+    bf16* to = (is_k ? a.k : a.v) + (static_cast<long long>(row) * a.kv.n_heads + h) * HD + e;
+    store4(to, lo);
+    store4(to + HD / 2, hi);
   }
 }
 
@@ -373,9 +350,9 @@ memspec_status memspec_op_kv_append(const memspec_batch* batch, const memspec_kv
   if (batch->rows > 1 && (p->ld < static_cast<int64_t>(p->n_heads + 2 * kv->n_heads) * hd || p->ld % 2 != 0 ||
                           p->ld > INT64_C(1) << 40))
     return refuse("qkv's row stride must be even, cover a row and be at most 2^40");
-  if (misaligned(p->qkv_dev, 2 * size) || misaligned(p->q_dev, 4) || misaligned(p->rope_dev, 4) ||
-      misaligned(p->offsets_dev, 4) || misaligned(p->q_gain_dev, 2) || misaligned(p->k_gain_dev, 2))
-    return refuse("qkv must be aligned to two elements, q, the table and offsets to 4 bytes, gains to 2");
+  if (misaligned(p->qkv_dev, 2 * size) || misaligned(p->q_dev, 8) || misaligned(p->rope_dev, 16) ||
+      misaligned(p->offsets_dev, 4) || misaligned(p->q_gain_dev, 8) || misaligned(p->k_gain_dev, 8))
+    return refuse("qkv must be aligned to two elements, the table to 16 bytes, q and gains to 8, offsets to 4");
   if (p->rope_dev != nullptr && p->rope_positions < 1) return refuse("the table has no positions");
   if (p->prefix_len < 0) return refuse("prefix_len must not be negative");
   if ((p->q_gain_dev == nullptr) != (p->k_gain_dev == nullptr)) return refuse("gains of both q and k, or of none");
@@ -388,6 +365,7 @@ memspec_status memspec_op_kv_append(const memspec_batch* batch, const memspec_kv
   a.rows = batch->rows;
   a.x = p->qkv_dev;
   a.ldx = batch->rows > 1 ? p->ld : 0;
+  a.wide = a.ldx % 4 == 0 && !misaligned(p->qkv_dev, 4 * size);
   a.rope = p->rope_dev;
   a.positions = p->rope_positions;
   a.offsets = p->offsets_dev;
@@ -397,7 +375,8 @@ memspec_status memspec_op_kv_append(const memspec_batch* batch, const memspec_kv
   a.eps = p->eps;
   a.q = static_cast<bf16*>(p->q_dev);
   a.n_heads = p->n_heads;
-  const dim3 grid(batch->rows, (p->n_heads + 2 * kv->n_heads + kHeadsPerCta - 1) / kHeadsPerCta);
+  const int at_once = hd == 64 ? Lanes<64>::kHeads : Lanes<128>::kHeads;
+  const dim3 grid(batch->rows, (p->n_heads + 2 * kv->n_heads + at_once - 1) / at_once);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   return launched("kv append", size == 4 ? (hd == 64 ? launch(append_kernel<64, float>, a, grid, s)
                                                      : launch(append_kernel<128, float>, a, grid, s))
@@ -409,8 +388,8 @@ memspec_status memspec_op_kv_read(const memspec_batch* batch, const memspec_kv* 
   using namespace memspec;
   if (const char* why = kv_problem(kv, false)) return refuse(why);
   if (const char* why = batch_problem(batch, kv)) return refuse(why);
-  if (k == nullptr || v == nullptr || misaligned(k, 4) || misaligned(v, 4))
-    return refuse("k and v must be 4-byte aligned and not null");
+  if (k == nullptr || v == nullptr || misaligned(k, 8) || misaligned(v, 8))
+    return refuse("k and v must be 8-byte aligned and not null");
   ReadArgs a{};
   a.kv = kv_view(kv);
   a.starts = batch->starts_dev;
@@ -419,7 +398,8 @@ memspec_status memspec_op_kv_read(const memspec_batch* batch, const memspec_kv* 
   a.rows = batch->rows;
   a.k = static_cast<bf16*>(k);
   a.v = static_cast<bf16*>(v);
-  const dim3 grid(batch->rows, (2 * kv->n_heads + 2 * kWarps - 1) / (2 * kWarps));
+  const int at_once = kv->head_dim == 64 ? Lanes<64>::kHeads : Lanes<128>::kHeads;
+  const dim3 grid(batch->rows, (2 * kv->n_heads + at_once - 1) / at_once);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   return launched("kv read", kv->head_dim == 64 ? launch(read_kernel<64>, a, grid, s)
                                                 : launch(read_kernel<128>, a, grid, s));
