@@ -305,7 +305,7 @@ memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, co
  * (of bf16 caches bf16, of codes fp16), off by half a step of it each, of codes
  * also by 2^-31 of the largest weight times scale.  With more
  * than 16 query vectors (rows times heads of a group) a head of k and v, keys and
- * values of codes count as fp16: off by 2^-10 of themselves, or by 2^-23 of the
+ * values of codes count as fp16: off by 2^-10 of themselves, or by 2^-16 of the
  * largest scale among their 128 positions.
  * Slots that a row does not see do not reach it, whatever they hold; an infinity
  * or a NaN in q, or in a key or value that it sees, makes that row and head

@@ -14,7 +14,7 @@ namespace memspec {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kTilesUnit = TileUnits::kUnit;
 // Up to so many vectors per head of k and v: attn_rows.cu, in units of so many; more: attn_tiles.cu
 constexpr int kRowsVectors = 16;
 
@@ -41,15 +41,26 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
     const uint32_t base = part.bases[b], total = part.bases[part.list];
     const uint32_t vecs = (own ? found.n : a.rows) * a.group, vec = (row - (own ? found.row0 : 0)) * a.group + h - kv_head * a.group;
     const uint32_t tiles = tiles_of(own ? min(max(found.len, 0), a.max_pos) : part.keys);
-    const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit, units = (vecs + part.unit - 1) / part.unit;
-    const uint32_t per_tile = part.pairs ? (vecs + 127) / 128 : units, w = part.pairs && vecs - unit * part.unit > 128 ? 2 : 1;
-    const bool pair = w == 2;
-    const uint32_t t0 = base + kv_head * (per_tile * tiles + units * part.start) +
-                        unit * ((part.pairs ? 2 : 1) * tiles + part.start);
-    const Pieces pieces(part.ctas, total, part.pairs ? 2 : 1);
-    // who has the first tile, the second and the last one: the CTAs between the first two have none
-    const int c0 = pieces.owner(t0), c1 = tiles > 1 ? pieces.owner(t0 + part.start + (tiles - 1) * w) : c0;
-    const int gap = tiles > 1 ? max(static_cast<int>(pieces.owner(t0 + part.start + w)) - c0 - 1, 0) : 0;
+    const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit;
+    // where the unit is, and who has its first tile, the second and the last one: the CTAs between the first two
+    // have none of it
+    int c0, c1, gap = 0;
+    bool pair;
+    auto find = [&](auto cut, uint32_t per_head, uint32_t per_unit) {
+      typedef decltype(cut) CUT;
+      const uint32_t w = CUT::weight(vecs, unit), t0 = base + kv_head * per_head + unit * per_unit;
+      const Pieces pieces(part.ctas, total, CUT::kGrain);
+      pair = w == 2;
+      c0 = pieces.owner(t0);
+      c1 = pieces.owner(t0 + CUT::place_of(tiles - 1, w));
+      if (tiles > 1) gap = max(static_cast<int>(pieces.owner(t0 + CUT::place_of(1, w))) - c0 - 1, 0);
+    };
+    if (part.pairs)
+      find(TileUnits{}, TileUnits::per_head(vecs, tiles), TileUnits::per_unit(tiles));
+    else if (part.unit == 8)
+      find(RowUnits<8>{}, RowUnits<8>::per_head(vecs, tiles), RowUnits<8>::per_unit(tiles));
+    else
+      find(RowUnits<16>{}, RowUnits<16>::per_head(vecs, tiles), RowUnits<16>::per_unit(tiles));
     if (c0 == c1 && part.full == nullptr) continue;   // written by that CTA
     any = true;
     // The vector's records: `copies` of each CTA, one of attn_rows.cu, of attn_tiles.cu's smaller units two.
@@ -183,10 +194,10 @@ const char* attention_problem(const memspec_batch* b, const memspec_kv* kv, cons
       return "the prefix must have the cache's heads and head_dim";
     if (p->prefix_len < 0 || p->prefix_len > p->prefix->max_pos) return "prefix_len must be in 0..the prefix's max_pos";
   }
-  // tiles are counted in 32 bits; every vector tile has at most this many
-  const double vts = static_cast<double>(b->rows) * (p->n_heads / kv->n_heads) / 8 + b->n_seq;
+  // the line is counted in 32 bits: at most a unit per 8 vectors, each of all tiles
+  const double units = static_cast<double>(b->rows) * (p->n_heads / kv->n_heads) / 8 + b->n_seq;
   const double keys = std::max(kv->max_pos, p->prefix != nullptr ? p->prefix_len : 0);
-  if (vts * kv->n_heads * (keys / kTile + 1 + kTilesStart) >= 4e9) return "too many rows for so many positions: split the call";
+  if (units * kv->n_heads * (keys / kTile + 9) >= 3.5e9) return "too many rows for so many positions: split the call";
   return nullptr;
 }
 
@@ -279,7 +290,7 @@ memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv
     for (int k = 0; k < 2; ++k)
       if (k == 0 ? x.own : x.prefix)
         j.part[j.parts++] = {a.bases, a.slots, a.full[k], x.ctas(), a.n_own + (x.prefix ? 1 : 0), k == 0 ? -1 : a.n_own,
-                             p->prefix_len, x.unit(), x.tiles ? kTilesStart : kRowsStart, x.tiles ? 1 : 0};
+                             p->prefix_len, x.unit(), x.tiles ? 1 : 0};
     e = x.tiles ? launch_attn_tiles(kv->head_dim, x.codes, a, cfg)
                 : launch_attn_rows(kv->head_dim, x.codes, x.nt, a, cfg);
   }

@@ -56,24 +56,28 @@ __device__ __forceinline__ int list_keys(const ListArgs& a, int b, const SeqRows
 // At least one, so that every row of a sequence is written.
 __host__ __device__ constexpr uint32_t tiles_of(int keys) { return keys == 0 ? 1 : (keys + kTile - 1u) / kTile; }
 
-// A unit of up to UNIT vectors costs `per tile` 1, or (PAIRS) 1 for each 128 vectors, and START to begin
-// with; its first tile stands at its beginning, tile t > 0 at START + t * per tile.
-template <int UNIT, bool PAIRS, int START>
+// A unit of up to UNIT vectors costs `per tile` 1, or (PAIRS) 2 where it has more than 128 of them, and START,
+// or START2, to begin with; its first tile stands at its beginning, tile t > 0 at its start's cost + t * per tile.
+template <int UNIT, bool PAIRS, int START, int START2>
 struct Cut {
-  static constexpr int kUnit = UNIT, kStart = START, kGrain = PAIRS ? 2 : 1;
+  static constexpr int kUnit = UNIT, kGrain = PAIRS ? 2 : 1;
   static constexpr bool kPairs = PAIRS;
-  __host__ __device__ static uint32_t units(uint32_t vecs) { return (vecs + UNIT - 1) / UNIT; }
-  __host__ __device__ static uint32_t per_tile(uint32_t vecs) {   // of all units of a head together
-    return PAIRS ? (vecs + 127) / 128 : units(vecs);
-  }
-  __device__ static uint32_t per_head(uint32_t vecs, uint32_t tiles) { return per_tile(vecs) * tiles + units(vecs) * START; }
-  __device__ static uint32_t per_unit(uint32_t tiles) { return kGrain * tiles + START; }   // of all but the last one
-  __device__ static uint32_t weight(uint32_t vecs, uint32_t unit) {
+  __host__ __device__ static uint32_t weight(uint32_t vecs, uint32_t unit) {   // of a tile
     return PAIRS && vecs - unit * UNIT > 128 ? 2 : 1;
   }
-  // the first tile at or after `at`, of a unit of weight w
+  __host__ __device__ static uint32_t start(uint32_t w) { return w == 2 ? START2 : START; }
+  // all units of a head together; one of them, but for the last one
+  __host__ __device__ static uint32_t per_head(uint32_t vecs, uint32_t tiles) {
+    const uint32_t units = (vecs + UNIT - 1) / UNIT;
+    if (units == 0) return 0;
+    const uint32_t w = weight(vecs, units - 1);
+    return (units - 1) * per_unit(tiles) + w * tiles + start(w);
+  }
+  __host__ __device__ static uint32_t per_unit(uint32_t tiles) { return kGrain * tiles + start(kGrain); }
+  // where tile t stands in a unit of weight w, and the first tile at or after place `at`
+  __host__ __device__ static uint32_t place_of(uint32_t t, uint32_t w) { return t == 0 ? 0 : start(w) + t * w; }
   __device__ static uint32_t tile_from(uint32_t at, uint32_t w) {
-    return at == 0 ? 0 : at <= START + w ? 1 : (at - START + w - 1) >> (w - 1);
+    return at == 0 ? 0 : at <= start(w) + w ? 1 : (at - start(w) + w - 1) >> (w - 1);
   }
 };
 
@@ -193,7 +197,7 @@ struct Walk {
       const uint32_t in_head = in - u.head * per_head;
       u.unit = in_head / per_unit;
       const uint32_t w = CUT::weight(u.vecs, u.unit), at = in_head - u.unit * per_unit,
-                     end = min(CUT::kStart + w * u.tiles, at + (x1 - x));
+                     end = min(CUT::start(w) + w * u.tiles, at + (x1 - x));
       u.t0 = min(CUT::tile_from(at, w), static_cast<uint32_t>(u.tiles));
       u.t1 = min(CUT::tile_from(end, w), static_cast<uint32_t>(u.tiles));
       x += end - at;
@@ -234,7 +238,7 @@ struct JoinPart {
   const float *slots, *full;   // full == nullptr: units within one CTA are written already
   int ctas, list, at;          // the launch's; `at`: the prefix's place in its list, or -1: the row's sequence
   int keys;                    // of the prefix
-  int unit, start;             // vectors of a unit, its cost to begin with
+  int unit;                    // vectors of a unit
   int pairs;                   // attn_tiles.cu's records
 };
 struct JoinArgs {
@@ -298,7 +302,10 @@ int rows_ctas(bool codes, int nt);
 cudaError_t launch_attn_rows(int hd, bool codes, int nt, const ListArgs& a, cudaLaunchConfig_t cfg);
 constexpr int kTilesCtas = 152;
 cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg);   // InvalidValue: no tensor map
-constexpr int kTilesUnit = 256, kTilesStart = 3;   // vectors of a unit of attn_tiles.cu, its start's cost
-constexpr int kRowsStart = 4;                      // of attn_rows.cu's
+// What a unit costs to begin with, in tiles of 128 vectors (us of a tile and a start: attn_rows.cu 0.5 and 4, a unit
+// of attn_tiles.cu with up to 128 vectors 1.0 and 2 to 3, with more 1.9 and 4 to 8).
+typedef Cut<256, true, 3, 4> TileUnits;
+template <int VT>
+using RowUnits = Cut<VT, false, 4, 4>;
 
 }  // namespace memspec

@@ -145,13 +145,13 @@ template <class S>
 __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_constant__ ListArgs a) {
   constexpr int HD = S::HD, NT = S::NT, VT = S::VT, KS = HD / 16, MT = HD / 16;
   constexpr bool CODES = S::CODES;
-  typedef Walk<Cut<VT, false, kRowsStart>> Stretches;
+  typedef Walk<RowUnits<VT>> Stretches;
   extern __shared__ __align__(128) char smem_raw[];
   const Smem<S> sm(smem_raw);
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane >> 2, t = lane & 3;
   pdl_wait();
   pdl_launch_dependents();
-  make_plan<Cut<VT, false, kRowsStart>, kThreads>(a, *sm.plan);
+  make_plan<RowUnits<VT>, kThreads>(a, *sm.plan);
   if (blockIdx.x == 0)
     for (int b = tid; b <= list_len(a); b += kThreads) a.bases[b] = sm.plan->bases[b];
   const uint32_t ring = smem_addr(sm.ring) + warp * S::kDepth * S::kStage, q_smem = smem_addr(sm.q);

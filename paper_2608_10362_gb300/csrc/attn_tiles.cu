@@ -15,7 +15,7 @@
 // K and V pass through two slots each in shared memory, K-major and N-major alike [key][hd] with the
 // 128-byte swizzle.  bf16 comes by TMA.  Codes are fetched by warps that write them as fp16, times their scale over
 // a power of two near the tile's largest: a value is off by 2^-10 of itself (its factor and the product are
-// rounded), or 2^-24 of the largest that its tile could hold.  K's power multiplies the tile's scores, V's is added to them as a logarithm: weights are
+// rounded), or by 2^-16 of the largest scale of its tile.  K's power multiplies the tile's scores, V's is added to them as a logarithm: weights are
 // w' = p * power, against a maximum of their own kind, and the sum of p is that of w' / power; so no range of scales
 // overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu has them, are three numbers per
 // key for every thread out of shared memory, 128 bytes a clock: 0.7 us of a step's 1.5; now 0.6.)  Q is taken to fp16 by
@@ -38,7 +38,8 @@ constexpr int kSlots = 4;               // tiles in shared memory: K of two, V o
 constexpr int kRefs = 4;                // a tile's references are read until its P is written
 constexpr int kListed = 4;              // stretches told of at a time
 constexpr int kStep = 64;               // keys of a warpgroup's step
-typedef Cut<kTilesUnit, true, kTilesStart> Units;
+typedef TileUnits Units;
+constexpr int kTilesUnit = Units::kUnit;
 
 template <int HD_, bool CODES_>
 struct Shape {
@@ -177,6 +178,32 @@ constexpr uint32_t idesc(int m, int n) {
   return make_idesc_bf16_f32(m, n) & ~(F16 ? (1u << 7) | (1u << 10) : 0u);
 }
 
+// ptx.cuh's mbar_wait_bounded, whose attempts may each sleep for 10 us.
+__device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  auto attempt = [&] {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_addr(bar)), "r"(parity), "r"(10000u)
+        : "memory");
+    return ok != 0;
+  };
+  if (attempt()) return true;
+  const long long t0 = clock64();
+#pragma unroll 1
+  while (!attempt()) {
+    if (*abort_flag) return false;
+    if (clock64() - t0 > kWaitBudgetCycles) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
 // The slot of tile t (of the CTA) of K or V, and how often it has been used before.
 __device__ __forceinline__ int slot_of(int t, int is_v) { return 2 * is_v + (t & 1); }
 __device__ __forceinline__ int use_of(int t) { return t >> 1; }
@@ -204,7 +231,7 @@ struct Stretches {
   __device__ explicit Stretches(Ctl& c) : ctl(c) {}
   __device__ __forceinline__ bool next(Stretch& u) {
     const int i = at % kListed;
-    if (!__all_sync(~0u, mbar_wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, &ctl.abort_flag, nullptr)))
+    if (!__all_sync(~0u, wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, &ctl.abort_flag)))
       return false;
     u = ctl.list[i];
     ++at;
@@ -220,7 +247,7 @@ __device__ __forceinline__ void walk_role(const ListArgs& a, Ctl& ctl) {
     more = walk.next(u);
     if (!more) u.t0 = u.t1 = 0;
     // the last S of the stretch before last is complete: so are the roles' steps of the one two before that
-    if (i >= 2 && !mbar_wait_bounded(&ctl.q_free[i & 1], static_cast<uint32_t>(i - 2 >> 1) & 1u, &ctl.abort_flag, nullptr)) return;
+    if (i >= 2 && !wait_bounded(&ctl.q_free[i & 1], static_cast<uint32_t>(i - 2 >> 1) & 1u, &ctl.abort_flag)) return;
     ctl.list[i % kListed] = u;
     mbar_arrive(&ctl.listed[i % kListed]);
   }
@@ -250,7 +277,7 @@ __device__ __forceinline__ void tma_role(const ListArgs& a, const TileMaps& maps
     for (int t = u.t0; t < u.t1; ++t, ++tile) {
       const int s = slot_of(tile, is_v), i = s & 1;
       if (use_of(tile) > 0 &&
-          !__all_sync(~0u, mbar_wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, abort_flag, nullptr))) {
+          !__all_sync(~0u, wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, abort_flag))) {
         ok = false;
         break;
       }
@@ -288,7 +315,7 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
     for (int t = u.t0; t < u.t1; ++t, ++tile) {
       if (!is_edge(u, t)) continue;
       const int s = slot_of(tile, 1), i = s & 1, key0 = t * kTile;
-      if (!__all_sync(~0u, mbar_wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag, nullptr))) return;
+      if (!__all_sync(~0u, wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag))) return;
       raws ^= 1u << i;
       if (tid < kTile / 32) ctl.bad[i][tid] = 0u;
       named_bar_sync(2, kCopy);
@@ -380,14 +407,14 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
       for (int i = 0; i < kCopy / 32; ++i) top.x = fmaxf(top.x, sm.top[buf][i].x), top.y = fmaxf(top.y, sm.top[buf][i].y);
       const int ref_v = reference(top.x), ref_k = reference(top.y);
       if (use_of(tile) > 0 &&
-          !__all_sync(~0u, mbar_wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, &ctl.abort_flag, nullptr)))
+          !__all_sync(~0u, wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, &ctl.abort_flag)))
         return;
       // V of a key whose scale is not finite: 0 where some vector does not see it, those that do are told
       if (is_v) {
         const uint32_t bad = __ballot_sync(~0u, !(sc[0] <= FLT_MAX));
         if (tid % 32 == 0) ctl.bad[s & 1][tid / 32] = bad;
       } else if (tid == 0) {   // (S of two tiles before is complete, after the softmax of four before: its entry is free)
-        ctl.refs[tile % kRefs] = make_float4(power(ref_k), static_cast<float>(ref_v), power(-ref_v), 0.f);
+        ctl.refs[tile % kRefs] = make_float4(512.f * power(ref_k), ref_v + 9.f, power(-ref_v) / 512.f, 0.f);
       }
       uint4 in[N * J];
 #pragma unroll
@@ -403,23 +430,24 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
       for (int n = 0; n < N; ++n) {
         const int r = r0 + n * (kCopy / 4);
         float f = sm.scale[buf][r] * down;
-        if (hide && !(f <= FLT_MAX)) f = 0.f;
-        const __half2 f2 = __float2half2_rn(f);
-        auto value = [&](uint32_t codes) {
-          const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&codes), f2);
+        if (!(f <= FLT_MAX)) f = hide ? 0.f : NAN;
+        // a byte u = code + 128 alone is the fp16 u 2^-24: times f 2^15, less f / 4, it is code f 2^-9, rounded once
+        // (f is below 2; of the last step below it 65504 is within a rounding)
+        const __half2 by = __float2half2_rn(f >= 1.999f ? 65504.f : f * 32768.f), less = __hmul2(by, __float2half2_rn(-0x1p-17f));
+        auto pair = [&](uint32_t bytes) {
+          const __half2 y = __hfma2(*reinterpret_cast<const __half2*>(&bytes), by, less);
           return *reinterpret_cast<const uint32_t*>(&y);
+        };
+        auto chunk = [&](uint32_t a, uint32_t b) {   // eight codes
+          return make_uint4(pair(__byte_perm(a, 0u, 0x4140)), pair(__byte_perm(a, 0u, 0x4342)), pair(__byte_perm(b, 0u, 0x4140)),
+                            pair(__byte_perm(b, 0u, 0x4342)));
         };
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const uint4 x = in[n * J + j];
-          const uint32_t w[4] = {x.x ^ 0x80808080u, x.y ^ 0x80808080u, x.z ^ 0x80808080u, x.w ^ 0x80808080u};
           const int ch = j * 8 + c * 2;
-          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch)) =
-              make_uint4(value(codes_f16<0x4140>(w[0])), value(codes_f16<0x4342>(w[0])), value(codes_f16<0x4140>(w[1])),
-                         value(codes_f16<0x4342>(w[1])));
-          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch + 1)) =
-              make_uint4(value(codes_f16<0x4140>(w[2])), value(codes_f16<0x4342>(w[2])), value(codes_f16<0x4140>(w[3])),
-                         value(codes_f16<0x4342>(w[3])));
+          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch)) = chunk(x.x ^ 0x80808080u, x.y ^ 0x80808080u);
+          *reinterpret_cast<uint4*>(slot + chunk_at(r, ch + 1)) = chunk(x.z ^ 0x80808080u, x.w ^ 0x80808080u);
         }
       }
       fence_proxy_async_smem();
@@ -487,7 +515,9 @@ __device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretc
   if (tid == 0) mbar_arrive(&ctl.q_full);
 }
 
-// The smaller units' vectors, ahead of their stretch; those of a pair are many, and the softmax warps' own work.
+// The smaller units' vectors, ahead of their stretch.  Those of a pair are many, and the first stretch's are waited
+// for by all: the softmax warps load them.
+__device__ __forceinline__ bool softmax_loads(const Stretch& u, int stretch) { return stretch == 0 || is_pair(u); }
 template <class S>
 __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem) {
   Stretches walk(ctl);
@@ -495,9 +525,9 @@ __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_s
   Stretch u;
 #pragma unroll 1
   for (; walk.next(u); ++stretch) {
-    if (is_pair(u)) continue;
+    if (softmax_loads(u, stretch)) continue;
     if (stretch > 0 &&
-        !__all_sync(~0u, mbar_wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag, nullptr)))
+        !__all_sync(~0u, wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag)))
       break;
     load_q<S, 32>(a, ctl, u, stretch, threadIdx.x % 32, q_smem, [] { __syncwarp(); });
   }
@@ -517,7 +547,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
   bool ok = true;
   int done = 0, tiles = 0, stretch = 0;      // steps of this warpgroup, tiles of the CTA, before this stretch
   auto wait = [&](uint64_t* bar, int phase) {
-    ok = ok && __all_sync(~0u, mbar_wait_bounded(bar, static_cast<uint32_t>(phase) & 1u, abort_flag, nullptr));
+    ok = ok && __all_sync(~0u, wait_bounded(bar, static_cast<uint32_t>(phase) & 1u, abort_flag));
     return ok;
   };
   Stretch u;
@@ -529,7 +559,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
     const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
     float scale = fmaxf(fabsf(a.scale), 1e-30f);   // (not 0: it meets scores of -inf)
     float m = kStart, l = 0.f;
-    if (pair) {
+    if (softmax_loads(u, stretch)) {
       named_bar_sync(1, kSoft);   // both warpgroups have seen the last S of the stretch before: Q is free
       load_q<S, kSoft>(a, ctl, u, stretch, threadIdx.x, q_smem, [] { named_bar_sync(1, kSoft); });
     }
@@ -686,7 +716,7 @@ __device__ __forceinline__ void mma_role(Ctl& ctl, int w, const uint8_t* ring, c
   Stretches walk(ctl);
   bool ok = true;
   auto wait = [&](uint64_t* bar, int phase) {
-    ok = ok && __all_sync(~0u, mbar_wait_bounded(bar, static_cast<uint32_t>(phase) & 1u, abort_flag, nullptr));
+    ok = ok && __all_sync(~0u, wait_bounded(bar, static_cast<uint32_t>(phase) & 1u, abort_flag));
     return ok;
   };
   int tiles = 0, stretch = 0, done = 0;   // before this stretch; done: steps

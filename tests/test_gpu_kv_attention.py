@@ -6,8 +6,8 @@ A = sum w|v| / sum w.  A score is an fp32 sum of head_dim products of magnitude 
 |q k| at most: off by (head_dim + 16) 2^-23 S (the tensor cores' sums may truncate: a whole
 step each), which moves its weight, and so the result, by as much of A, twice (numerator and
 denominator).  Keys and values of codes of more than 16 vectors a head enter as fp16, off by 2^-10
-each, two roundings (their scales here lie within a factor of 7, so that nothing is near fp16's
-small end): a score by 2^-10 S more, a result by 2^-10 A more.  Weights of codes are fp16 that carry v's
+each (two roundings) or, where fp16 runs out (2^-25 of what the tile's largest scale makes 2^-9), by 2^-16 of the
+largest scale: a score by 2^-10 S + 2^-16 scale sum|q| more, a result by 2^-10 A + 2^-16 scale more.  Weights of codes are fp16 that carry v's
 scale too, the largest at least 2^6 (the maximum is taken again when it is passed by 2^14, and then set
 2^6 below): what rounds at fp16's smallest step, 2^-24, is off by 2^-25, 2^-31 of the largest, so a
 result by 2^-31 of the largest |v| for each key.  Sums of weights and exponentials add (keys 2^-23 at most, in practice their
@@ -103,6 +103,13 @@ def attention64(q, cache, starts, lens, tree=None, prefix=None, prefix_len=0, sc
             bound[lo:hi, h * G:(h + 1) * G] = (2.0 ** -8 * (r.abs().nan_to_num(0) + weights * A)
                                                + (weights + values16 + 2 * ((hd + 16) * 2.0 ** -23 + values16) * S
                                                   + 2.0 ** -18) * A + 1e-30)
+            if many:
+                ends = [(c, e) for c, e in ((cache if cache.codes else None, end),
+                                            (prefix if prefix is not None and prefix.codes else None, prefix_len)) if c and e]
+                tops = [max(float(t[b if c is cache else 0, h, :e].nan_to_num(0, 0, 0).max()) for c, e in ends
+                            for t in (c.tensors[i],)) if ends else 0.0 for i in (2, 3)]
+                bound[lo:hi, h * G:(h + 1) * G] += 2.0 ** -16 * (
+                    2 * tops[0] * abs(scale) * x.abs().nan_to_num(0).sum(2, keepdim=True) * A + tops[1])
             if cache.codes or prefix is not None and prefix.codes:
                 bound[lo:hi, h * G:(h + 1) * G] += 2.0 ** -31 * clean.shape[0] * (clean.abs().max() if clean.numel() else 0.0)
     return out, bound
