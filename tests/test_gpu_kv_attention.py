@@ -669,3 +669,48 @@ def test_wrappers_refuse():
             pkg.KVCache(*bad)
     with pytest.raises(pkg.MemSpecError):      # k and v in one place are not written
         pkg.op_kv_append(x, pkg.KVCache(k, k), s, l, 4)
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("H,Hk,hd,prefix", [(2, 2, 64, 0), (8, 1, 128, 0), (32, 1, 64, 0), (20, 1, 128, 130)])
+def test_many_sequences_of_all_lengths(H, Hk, hd, prefix, codes):
+    """1024 sequences, more than any table of the kernels holds, most with a row or none."""
+    rng = np.random.default_rng(11)
+    rows_of = rng.choice([0, 1, 1, 1, 2, 5], 1024)
+    pasts = np.where(rng.random(1024) < 0.05, rng.integers(0, 900, 1024), rng.integers(0, 40, 1024))
+    starts, lens = batch(rows_of, pasts)
+    cache = make_cache(codes, 1024, Hk, max(lens), hd, seed=3)
+    pre = make_cache(codes, 1, Hk, prefix, hd, seed=4) if prefix else None
+    q = torch.randn(starts[-1], H, hd, device=DEV, generator=_gen(8)).bfloat16()
+    got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=5, prefix=pre)
+    some = list(range(0, 1024, 7)) + [1023]
+    for b in some:
+        rows = slice(starts[b], starts[b + 1])
+        if rows.stop > rows.start:
+            one = _pkg().KVCache(*[t[b:b + 1] for t in cache.tensors if t is not None])
+            check(got[rows], *attention64(q[rows], one, [0, rows.stop - rows.start], [lens[b]], prefix=pre, prefix_len=prefix,
+                                          max_rows=1 << 16))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_drawn_batches(seed):
+    """Shapes drawn from all that the calls take, each row against its definition."""
+    rng = np.random.default_rng(1000 + seed)
+    hd = int(rng.choice([64, 128]))
+    Hk = int(rng.choice([1, 2, 3, 8]))
+    H = Hk * int(rng.choice([1, 3, 4, 7, 16, 33, 64]))
+    B = int(rng.integers(1, 9))
+    rows_of = rng.integers(0, int(rng.choice([2, 10, 70])), B)
+    rows_of[rng.integers(0, B)] += 1
+    pasts = rng.integers(0, int(rng.choice([5, 300, 2500])), B)
+    starts, lens = batch(rows_of, pasts)
+    codes, pcodes = (bool(rng.integers(0, 2)) for _ in (0, 1))
+    plen = int(rng.choice([0, 0, 1, 128, 777]))
+    cache = make_cache(codes, B, Hk, max(lens) + 5, hd, seed=seed)
+    pre = make_cache(pcodes, 1, Hk, plen + 1, hd, seed=seed + 50) if plen else None
+    tree = torch.from_numpy(rng.integers(0, 1 << 32, starts[-1], dtype=np.uint32).view(np.int32)).to(DEV) \
+        if max(rows_of) <= 32 and rng.integers(0, 2) else None
+    q = (2 * torch.randn(starts[-1], H, hd, device=DEV, generator=_gen(seed))).bfloat16()
+    max_rows = int(rng.integers(1, starts[-1] + 1))
+    got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=max_rows, tree=tree, prefix=pre, prefix_len=plen)
+    check(got, *attention64(q, cache, starts, lens, tree=tree, prefix=pre, prefix_len=plen, max_rows=1 << 16))
