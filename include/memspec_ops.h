@@ -284,7 +284,7 @@ typedef struct memspec_attention {
   void* out_dev;                /* bf16 [rows][n_heads][head_dim], 16-byte aligned */
   int64_t ldo;                  /* as ldq (of a single row neither is read) */
   int32_t n_heads;              /* a multiple of the cache's, up to 64 times it */
-  float scale;                  /* of q . k, finite */
+  float scale;                  /* of q . k, up to 2e38 either way */
   const int32_t* tree_dev;      /* [rows] or NULL */
   const memspec_kv* prefix;     /* or NULL: its sequence 0 is before every sequence's positions */
   int32_t prefix_len;           /* 0..prefix->max_pos */
@@ -307,9 +307,10 @@ memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, co
  * than 16 query vectors (rows times heads of a group) a head of k and v, keys and
  * values of codes count as fp16: off by 2^-10 of themselves, or by 2^-16 of the
  * largest scale among their 128 positions.
- * Slots that a row does not see do not reach it, whatever they hold; an infinity
- * or a NaN in q, or in a key or value that it sees, makes that row and head
- * unspecified.  q may be out if ldq == ldo; else out overlaps no other argument.
+ * Slots that a row does not see do not reach it, whatever they hold (but for the
+ * scales among those 128 positions); an infinity
+ * or a NaN in q, in a key or value that it sees, or among its scores, makes that row
+ * and head unspecified.  out overlaps no other argument.
  * A sequence of more than max_rows rows gives the same, at another speed.
  * Deterministic.  scratch_dev: 16-byte aligned, any content; calls that may overlap
  * need scratches of their own.  Allocates nothing.  Errors: INVALID_ARG, CUDA. */

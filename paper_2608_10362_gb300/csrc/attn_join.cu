@@ -187,7 +187,7 @@ const char* attention_problem(const memspec_batch* b, const memspec_kv* kv, cons
   if (p->n_heads < 1 || p->n_heads % kv->n_heads != 0 || p->n_heads / kv->n_heads > 64)
     return "n_heads must be a multiple of the cache's heads, up to 64 times as many";
   if (p->max_rows < 1 || p->max_rows > b->rows) return "max_rows must be in 1..rows";
-  if (!(p->scale >= -3e38f && p->scale <= 3e38f)) return "scale must be finite";
+  if (!(fabsf(p->scale) <= 2e38f)) return "scale must be at most 2e38";   // (times log2(e) finite)
   if (p->prefix != nullptr) {
     if (const char* why = kv_problem(p->prefix, false)) return why;
     if (p->prefix->n_heads != kv->n_heads || p->prefix->head_dim != kv->head_dim)

@@ -271,17 +271,22 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
   const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&u), __half2half2(__ushort_as_half(0x6480)));
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// The power of two that brings bf16 values up to `top` near 2^10, where fp16 holds all their bits (what
-// falls off is below 2^-34 of the largest).
-__device__ __forceinline__ float up_to_f16(float top) {
-  const int e = top > 0.f ? min(max(ilogbf(top), -110), 127) : 0;
-  return __int_as_float((min(10 - e, 120) + 127) << 23);
+// Query vectors as fp16, for the products with codes: each times the power of two that brings its largest value
+// near 2^10, where fp16 holds all bits of bf16 (what falls off is below 2^-34 of the vector's largest).
+// Here of the vector of which each of LANES neighbours has eight values; the whole warp calls it.
+template <int LANES>
+__device__ __forceinline__ int exponent_of_lanes(const uint4& x) {
+  auto of = [](uint32_t pair) {
+    pair &= 0x7fff7fffu;
+    return *reinterpret_cast<const __nv_bfloat162*>(&pair);
+  };
+  __nv_bfloat162 top = __hmax2(__hmax2(of(x.x), of(x.y)), __hmax2(of(x.z), of(x.w)));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) top = __hmax2(top, __shfl_xor_sync(~0u, top, o));
+  const uint32_t bits = *reinterpret_cast<const uint32_t*>(&top);
+  return max(static_cast<int>(max(bits & 0xffffu, bits >> 16) >> 7) - 127, -110) - 10;
 }
-__device__ __forceinline__ void top_of(uint32_t pair, float& top) {   // of the finite ones
-  const float a = fabsf(__uint_as_float(pair << 16)), b = fabsf(__uint_as_float(pair & 0xffff0000u));
-  if (a <= FLT_MAX) top = fmaxf(top, a);
-  if (b <= FLT_MAX) top = fmaxf(top, b);
-}
+__device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 __device__ __forceinline__ uint32_t scaled_f16(uint32_t pair, float by) {
   return pack_f16(__uint_as_float(pair << 16) * by, __uint_as_float(pair & 0xffff0000u) * by);
 }

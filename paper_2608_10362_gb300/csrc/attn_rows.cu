@@ -91,7 +91,7 @@ struct Smem {
   Plan* plan;
   char* q;
   Sight* sight;     // [VT]
-  float* q_scale;
+  float* q_scale;   // [VT]
   char* ring;
   __device__ explicit Smem(char* p) {
     plan = reinterpret_cast<Plan*>(p);
@@ -192,33 +192,26 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
     if (tid < VT) sm.sight[tid] = sight_of(a, u, u.unit * VT + tid);
     cp_wait<S::kDepth - 1>();
     if constexpr (CODES) {   // to fp16, and in the order of the fragments
-      uint4 in = make_uint4(0, 0, 0, 0);
-      if (tid < VT * C) in = *reinterpret_cast<const uint4*>(sm.q + q_at);
-      float top = 0.f;
-      top_of(in.x, top);
-      top_of(in.y, top);
-      top_of(in.z, top);
-      top_of(in.w, top);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-      if (lane == 0) sm.q_scale[warp] = top;
-      __syncthreads();
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sm.q_scale[w]);
-      const float up = up_to_f16(top);
-      if (tid < VT * C) {
+      if (tid < VT * C) {    // (whole warps, and a vector's threads are of one)
+        const uint4 in = *reinterpret_cast<const uint4*>(sm.q + q_at);
         const uint32_t w[4] = {in.x, in.y, in.z, in.w};
+        const int e = exponent_of_lanes<C>(in);
+        const float up = power(-e);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           // a lane's word of four codes is one step's pairs k = 2t, 2t + 1 and 2t + 8, 2t + 9
           const int hd = q_c * 8 + j * 2, to = hd / 64 * 64 + hd % 16 / 4 * 16 + hd % 64 / 16 * 2 + hd % 4 / 2 * 8;
           *reinterpret_cast<uint32_t*>(sm.q + q_vec * HD * 2 + (to / 8 ^ (q_vec & 7)) * 16 + to % 8 * 2) = scaled_f16(w[j], up);
         }
+        if (q_c == 0) sm.q_scale[q_vec] = a.scale * power(e);
       }
-      __syncthreads();
-      if (tid == 0) sm.q_scale[0] = 1.f / up;
     }
     __syncthreads();
-    const float scale = CODES ? a.scale * sm.q_scale[0] : a.scale;
+    float scale[NT][2];   // of the lane's vectors
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) scale[nt][i] = CODES ? sm.q_scale[nt * 8 + 2 * t + i] : a.scale;
     uint32_t qf[NT][KS][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -289,21 +282,20 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
           float k_s = sc[g + 8 * i], v_s = sc[16 + g + 8 * i];
           if (k_s < kSmallestScale) k_s = kSmallestScale;   // a NaN stays
           if (v_s < kSmallestScale) v_s = kSmallestScale;
-          k_s *= scale;
           const float lv = __log2f(v_s);
           rv[i] = __frcp_rn(v_s);
           if (isnan(rv[i])) rv[i] = 0.f;   // the weight is a NaN already where it counts
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            z[nt][2 * i] = fmaf(z[nt][2 * i], k_s, lv);
-            z[nt][2 * i + 1] = fmaf(z[nt][2 * i + 1], k_s, lv);
+            z[nt][2 * i] = fmaf(z[nt][2 * i], k_s * scale[nt][0], lv);
+            z[nt][2 * i + 1] = fmaf(z[nt][2 * i + 1], k_s * scale[nt][1], lv);
           }
         }
       } else {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) z[nt][i] *= scale;
+          for (int i = 0; i < 4; ++i) z[nt][i] *= a.scale;
       }
       const bool edge = kb + 16 > end || kb + 15 >= u.first;
       if (edge) {

@@ -18,11 +18,12 @@
 // rounded), or by 2^-16 of the largest scale of its tile.  K's power multiplies the tile's scores, V's is added to them as a logarithm: weights are
 // w' = p * power, against a maximum of their own kind, and the sum of p is that of w' / power; so no range of scales
 // overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu has them, are three numbers per
-// key for every thread out of shared memory, 128 bytes a clock: 0.7 us of a step's 1.5; now 0.6.)  Q is taken to fp16 by
-// a power of two.
+// key for every thread out of shared memory, 128 bytes a clock: 0.7 us of a step's 1.5; now 0.6.)  A vector of Q is taken
+// to fp16 by a power of two of its own.
 //
 // Roles (warps): 0-3, 4-7 softmax; copies, 4, or 8 of codes; two with the MMAs of a warpgroup each;
-// one for Q; one for which units these are.  Every wait is bounded; after one that ran out the CTA's remaining records are NaN.
+// one for Q; one for which units these are.  Every wait is bounded; after one that ran out the CTA's records
+// are NaN or not written.
 #include <algorithm>
 #include <atomic>
 
@@ -71,9 +72,8 @@ struct Ctl {
   uint32_t bad[2][kTile / 32];        // keys of an edge tile whose values are not all finite
   float4 refs[kRefs];                 // codes: the power of two K's scales are taken against, V's logarithm, 1 / V's
   CodesSmem codes[2];
-  float q_down[4];                    // 1 / the power of two that a stretch's Q was taken by; the next one's Q may be
-                                      // there, and the one's after it begun, before this one's softmax reads its own
-  float tops[kSoft / 32];
+  float q_down[4][kTilesUnit];        // codes: 1 / the powers of two that a stretch's vectors were taken by; the next one's
+                                      // may be there, and the one's after it begun, before this one's softmax reads its own
   Plan plan;
   uint64_t listed[kListed];           // a stretch's entry is there
   Stretch list[kListed];              // (none: t0 == t1)
@@ -178,8 +178,11 @@ constexpr uint32_t idesc(int m, int n) {
   return make_idesc_bf16_f32(m, n) & ~(F16 ? (1u << 7) | (1u << 10) : 0u);
 }
 
-// ptx.cuh's mbar_wait_bounded, whose attempts may each sleep for 10 us.
-__device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+// ptx.cuh's mbar_wait_bounded, whose attempts may each sleep for 10 us.  A wait for a step or a tile is over when
+// the others are slower than any they can be; one for a stretch lasts as long as the stretch has tiles.
+constexpr long long kStretchBudgetCycles = 64 * kWaitBudgetCycles;
+__device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                             long long budget = kWaitBudgetCycles) {
   auto attempt = [&] {
     uint32_t ok;
     asm volatile(
@@ -196,7 +199,7 @@ __device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, vol
 #pragma unroll 1
   while (!attempt()) {
     if (*abort_flag) return false;
-    if (clock64() - t0 > kWaitBudgetCycles) {
+    if (clock64() - t0 > budget) {
       *abort_flag = 1;
       return false;
     }
@@ -231,7 +234,8 @@ struct Stretches {
   __device__ explicit Stretches(Ctl& c) : ctl(c) {}
   __device__ __forceinline__ bool next(Stretch& u) {
     const int i = at % kListed;
-    if (!__all_sync(~0u, wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, &ctl.abort_flag)))
+    if (!__all_sync(~0u, wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, &ctl.abort_flag,
+                                       kStretchBudgetCycles)))
       return false;
     u = ctl.list[i];
     ++at;
@@ -247,7 +251,9 @@ __device__ __forceinline__ void walk_role(const ListArgs& a, Ctl& ctl) {
     more = walk.next(u);
     if (!more) u.t0 = u.t1 = 0;
     // the last S of the stretch before last is complete: so are the roles' steps of the one two before that
-    if (i >= 2 && !wait_bounded(&ctl.q_free[i & 1], static_cast<uint32_t>(i - 2 >> 1) & 1u, &ctl.abort_flag)) return;
+    if (i >= 2 &&
+        !wait_bounded(&ctl.q_free[i & 1], static_cast<uint32_t>(i - 2 >> 1) & 1u, &ctl.abort_flag, kStretchBudgetCycles))
+      return;
     ctl.list[i % kListed] = u;
     mbar_arrive(&ctl.listed[i % kListed]);
   }
@@ -315,7 +321,7 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
     for (int t = u.t0; t < u.t1; ++t, ++tile) {
       if (!is_edge(u, t)) continue;
       const int s = slot_of(tile, 1), i = s & 1, key0 = t * kTile;
-      if (!__all_sync(~0u, wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag))) return;
+      if (!__all_sync(~0u, wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag, kStretchBudgetCycles))) return;
       raws ^= 1u << i;
       if (tid < kTile / 32) ctl.bad[i][tid] = 0u;
       named_bar_sync(2, kCopy);
@@ -347,7 +353,6 @@ __device__ __forceinline__ float sane_scale(float s) { return s < kSmallestScale
 __device__ __forceinline__ float finite_or_0(float s) { return s <= FLT_MAX ? s : 0.f; }
 // The exponent that a tile's scales are taken against (the largest finite one's), as a power of two and its inverse.
 __device__ __forceinline__ int reference(float top) { return min((__float_as_int(fmaxf(top, kSmallestScale)) >> 23) - 127, 126); }
-__device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 
 template <class S>
 __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v, uint8_t* ring, CodesSmem& sm) {
@@ -459,7 +464,7 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
 
 // ---------------------------------------------------------------- query vectors
 // A stretch's vectors into shared memory by THREADS threads (`tid` of them; sync: their barrier), K-major; a
-// negative scale turns their signs.  Codes: to fp16, by a power of two that brings the largest to about 2^10.
+// negative scale turns their signs.  Codes: to fp16.
 template <class S, int THREADS, class Sync>
 __device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretch& u, int stretch, int tid, uint8_t* q_smem, Sync sync) {
   constexpr int HD = S::HD, C = HD / 8;
@@ -476,31 +481,17 @@ __device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretc
   cp_commit();
   cp_wait<0>();
   if constexpr (S::CODES) {
-    float top = 0.f;
-#pragma unroll 1
-    for (int at = tid; at < chunks; at += THREADS) {
-      const uint4 x = *reinterpret_cast<const uint4*>(dst(at));
-      top_of(x.x, top);
-      top_of(x.y, top);
-      top_of(x.z, top);
-      top_of(x.w, top);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    if constexpr (THREADS > 32) {
-      if (tid % 32 == 0) ctl.tops[tid / 32] = top;
-      sync();
-#pragma unroll
-      for (int i = 0; i < THREADS / 32; ++i) top = fmaxf(top, ctl.tops[i]);
-    }
-    const float up = up_to_f16(top);
-    if (tid == 0) ctl.q_down[stretch & 3] = 1.f / up;
-#pragma unroll 1
-    for (int at = tid; at < chunks; at += THREADS) {
-      uint4* p = reinterpret_cast<uint4*>(dst(at));
+#pragma unroll 4
+    for (int at = tid; at - tid % 32 < chunks; at += THREADS) {   // (by whole warps; a vector's chunks are of one)
+      const bool on = at < chunks;
+      uint4* p = reinterpret_cast<uint4*>(dst(on ? at : tid));
       const uint4 x = *p;
+      const int e = exponent_of_lanes<C>(x);
+      const float up = power(-e);
+      if (!on) continue;
       *p = make_uint4(scaled_f16(x.x ^ flip, up), scaled_f16(x.y ^ flip, up), scaled_f16(x.z ^ flip, up),
                       scaled_f16(x.w ^ flip, up));
+      if (at % C == 0) ctl.q_down[stretch & 3][at / C] = power(e);
     }
   } else if (flip != 0u) {
 #pragma unroll 1
@@ -527,7 +518,8 @@ __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_s
   for (; walk.next(u); ++stretch) {
     if (softmax_loads(u, stretch)) continue;
     if (stretch > 0 &&
-        !__all_sync(~0u, wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag)))
+        !__all_sync(~0u, wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag,
+                                      kStretchBudgetCycles)))
       break;
     load_q<S, 32>(a, ctl, u, stretch, threadIdx.x % 32, q_smem, [] { __syncwarp(); });
   }
@@ -559,6 +551,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
     const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
     float scale = fmaxf(fabsf(a.scale), 1e-30f);   // (not 0: it meets scores of -inf)
     float m = kStart, l = 0.f;
+    bool huge = false;   // some m of the warp's
     if (softmax_loads(u, stretch)) {
       named_bar_sync(1, kSoft);   // both warpgroups have seen the last S of the stretch before: Q is free
       load_q<S, kSoft>(a, ctl, u, stretch, threadIdx.x, q_smem, [] { named_bar_sync(1, kSoft); });
@@ -572,7 +565,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
         if (!wait(&ctl.s_full[w][buf], done >> 1)) break;
         tc_fence_after();
         if (warp_live) {
-          if (CODES && begins) scale = fmaxf(fabsf(a.scale), 1e-30f) * ctl.q_down[stretch & 3];
+          if (CODES && begins) scale = fmaxf(fabsf(a.scale), 1e-30f) * ctl.q_down[stretch & 3][vec - u.unit * kTilesUnit];
           const uint32_t s_buf = s_at + buf * kStep;
           // z = by * S + plus: of codes with the tile's references
           float by = scale, plus = 0.f, l_by = 1.f;
@@ -625,6 +618,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
             const float now = above ? top - kBelow : m, less = ex2(m - now);
             m = now;
             l *= less;
+            huge = __any_sync(~0u, live && fabsf(m) > 0x1p20f && m != kStart);
             if (!begins) {
               if (!wait(&ctl.o_full[w][buf ^ 1], (done - 1) >> 1)) break;
               tc_fence_after();
@@ -639,6 +633,25 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
             }
           }
           f32x2 sum[2] = {0ull, 0ull};
+          if (huge) {
+            // scores so large that m's rounding shows: they are rounded as m was, else those next to the largest
+            // would be past fp16 or fp32
+            if constexpr (W == kStep) {
+#pragma unroll
+              for (int e = 0; e < W; ++e) z[e] = fmaf(z[e], by, plus);
+            } else {
+#pragma unroll 1
+              for (int c = 0; c < kStep; c += 32) {
+                float x[32];
+                tmem_ld_x32(s_buf + c, x);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = fmaf(x[e], by, plus);
+                tmem_st_x32(s_buf + c, reinterpret_cast<const uint32_t*>(x));
+              }
+              tmem_st_wait();
+            }
+            by = 1.f, plus = 0.f;
+          }
           const f32x2 by2 = pair_of(by, by), plus2 = pair_of(plus - m, plus - m);
 #pragma unroll 1
           for (int c = 0; c < kStep; c += W) {

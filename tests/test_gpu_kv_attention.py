@@ -714,3 +714,85 @@ def test_drawn_batches(seed):
     max_rows = int(rng.integers(1, starts[-1] + 1))
     got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=max_rows, tree=tree, prefix=pre, prefix_len=plen)
     check(got, *attention64(q, cache, starts, lens, tree=tree, prefix=pre, prefix_len=plen, max_rows=1 << 16))
+
+
+@pytest.mark.parametrize("codes", [True, False])
+@pytest.mark.parametrize("H,Hk", [(4, 4), (32, 8), (32, 4)])
+def test_a_vector_of_any_size_beside_others(H, Hk, codes):
+    """Rows of one sequence whose queries are powers of 2^40 apart, and rows of no sequence (of which a prefix's
+    units have the vectors too) with the largest values there are: each is as if it were alone."""
+    starts, lens = batch([3], [140])
+    cache = make_cache(codes, 1, Hk, 150, 128, seed=3)
+    prefix = make_cache(codes, 1, Hk, 200, 128, seed=4)
+    q = torch.randn(5, H, 128, device=DEV, generator=_gen(8))
+    q[0] *= 2.0 ** 40
+    q[2] *= 2.0 ** -40
+    q[3:] = 3e38
+    q = q.bfloat16()
+    for pre in (None, prefix):
+        got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=3, prefix=pre)
+        for r in range(3):   # (a bound over the row's own sizes)
+            want, bound = attention64(q, cache, starts, lens, prefix=pre, prefix_len=200, max_rows=3)
+            check(got[r:r + 1], want[r:r + 1], bound[r:r + 1])
+
+
+# ------------------------------------------------------------------ the ends of the ranges
+@pytest.mark.parametrize("codes", [False, True])
+def test_the_most_rows(codes):
+    """65535 rows: of 1024 sequences, and of a single one."""
+    pkg, hd = _pkg(), 64
+    for rows_of, H in (([64] * 1023 + [63], 2), ([65535], 1)):
+        starts, lens = batch(rows_of, [3] * len(rows_of))
+        cache = pkg.KVCache.zeros(len(rows_of), 1, lens[0], hd, dtype=torch.int8 if codes else torch.bfloat16)
+        x = torch.randn(65535, (H + 2) * hd, device=DEV, generator=_gen(3)).bfloat16()
+        s, l = _i32(*starts), _i32(*lens)
+        q = pkg.op_kv_append(x, cache, s, l, H)
+        k, v = pkg.op_kv_read(cache, s, l, 65535)
+        assert torch.equal(q, x.view(65535, H + 2, hd)[:, :H])
+        if not codes:
+            assert torch.equal(torch.cat([k, v], 1), x.view(65535, H + 2, hd)[:, H:])
+        got = pkg.op_attention(q, cache, s, l)
+        for row in (0, 1, 4097, 65471, 65533, 65534):
+            b = np.searchsorted(starts, row, "right") - 1
+            one = pkg.KVCache(*[t[b:b + 1] for t in cache.tensors if t is not None])
+            check(got[row:row + 1], *attention64(q[row:row + 1], one, [0, 1], [lens[b] - (starts[b + 1] - 1 - row)],
+                                                 max_rows=1 << 16))
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("H,Hk", [(1024, 1024), (4096, 64)])
+def test_the_most_heads(H, Hk, codes):
+    starts, lens = batch([1, 2], [40, 130])
+    cache = make_cache(codes, 2, Hk, 140, 64, seed=3)
+    q = torch.randn(3, H, 64, device=DEV, generator=_gen(8)).bfloat16()
+    got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens))
+    check(got, *attention64(q, cache, starts, lens))
+
+
+def test_a_layers_calls_on_a_side_stream_and_in_a_graph():
+    """Append, attention and read, one after another on another stream, and captured there: replayed with the
+    lengths of the next tokens they decode on."""
+    pkg, H, Hk, hd = _pkg(), 8, 2, 128
+    rope = pkg.op_rope_table(64, hd)
+    caches = [pkg.KVCache.zeros(2, Hk, 64, hd, dtype=torch.int8) for _ in range(2)]
+    s, l = _i32(0, 1, 2), _i32(5, 9)
+    x = torch.randn(2, (H + 2 * Hk) * hd, device=DEV, generator=_gen(3))
+
+    def layer(cache, stream=None):
+        q = pkg.op_kv_append(x, cache, s, l, H, rope=rope, stream=stream)
+        return pkg.op_attention(q, cache, s, l, max_rows=1, stream=stream), pkg.op_kv_read(cache, s, l, 2, stream=stream)[0]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for a, b in zip(layer(caches[0]), layer(caches[1], side)):
+        torch.cuda.synchronize()
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = layer(caches[0])
+    for _ in range(20):
+        l.add_(1)
+        x.normal_(generator=_gen(int(l[0])))
+        graph.replay()
+        for a, b in zip(outs, layer(caches[1])):
+            assert torch.equal(a, b)
+    assert all(torch.equal(a, b) for a, b in zip(caches[0].tensors, caches[1].tensors))

@@ -134,3 +134,57 @@ def test_wrappers_take_no_host_tensors():
         KVCache.zeros(1, 1, 1, 64, dtype=torch.float32)
     with pytest.raises(ValueError, match="CUDA"):
         op_rope_table(8, 64, device="cpu")
+
+
+# ------------------------------------------------------------------ memory, with a stream
+from test_wrapper_streams_cpu import BF, CURRENT, LOG, SIDE, _t, allocations  # noqa: E402,F401
+from paper_2608_10362_gb300 import kv as kv_module  # noqa: E402
+
+I32 = torch.int32
+
+
+def _cache(codes):
+    t = [_t(2, 1, 8, 64, dtype=torch.int8 if codes else BF) for _ in (0, 1)]
+    return KVCache(*t, *([_t(2, 1, 8), _t(2, 1, 8)] if codes else []))
+
+
+def _rows():
+    return [_t(3, dtype=I32), _t(2, dtype=I32)]
+
+
+CALLS = {   # name: (the caches, the call's tensors, the call)
+    "append": (lambda: [_cache(False)], lambda: [_t(3, 4 * 64), *_rows()],
+               lambda st, c, x, s, l: kv_module.op_kv_append(x, c, s, l, 2, stream=st)),
+    "append_codes": (lambda: [_cache(True)],
+                     lambda: [_t(3, 4 * 64, dtype=BF), *_rows(), _t(2, 9, 32), _t(3, dtype=I32), _t(64, dtype=BF), _t(64, dtype=BF)],
+                     lambda st, c, x, s, l, r, o, g, h: kv_module.op_kv_append(x, c, s, l, 2, r, o, 1, g, h, stream=st)),
+    "read": (lambda: [_cache(True)], _rows, lambda st, c, s, l: kv_module.op_kv_read(c, s, l, 3, stream=st)[0]),
+    "attention": (lambda: [_cache(False)], lambda: [_t(3, 4, 64, dtype=BF), *_rows()],
+                  lambda st, c, q, s, l: kv_module.op_attention(q, c, s, l, stream=st)),
+    "attention_prefix": (lambda: [_cache(False), _cache(True)], lambda: [_t(3, 4, 64, dtype=BF), *_rows(), _t(3, dtype=I32)],
+                         lambda st, c, p, q, s, l, t: kv_module.op_attention(q, c, s, l, tree=t, prefix=p, stream=st)),
+}
+
+
+@pytest.fixture
+def calls(allocations, monkeypatch):  # noqa: F811
+    monkeypatch.setattr(kv_module, "_call_on", lambda dev, stream, fn, *args: 0)
+    monkeypatch.setattr(kv_module, "_attention_scratch_bytes", lambda *a: 512)
+    return allocations
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_memory_and_tensors_of_a_call_on_another_stream(calls, name):
+    caches, tensors, call = CALLS[name]
+    caches, tensors = caches(), tensors()
+    calls.clear()
+    LOG.clear()
+    out = call(SIDE, *caches, *tensors)
+    assert calls and all(s is SIDE for _, s in calls)
+    assert ("record", out.data_ptr(), CURRENT) in LOG     # the caller goes on with it there
+    used = [p for what, p, s in LOG if s is SIDE]
+    assert all(t.data_ptr() in used for t in tensors + [t for c in caches for t in c.tensors if t is not None])
+    calls.clear()
+    LOG.clear()
+    call(None, *caches, *tensors)
+    assert calls and all(s is CURRENT for _, s in calls) and not LOG
