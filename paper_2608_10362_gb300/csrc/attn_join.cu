@@ -18,8 +18,66 @@ constexpr int kThreads = 256, kWarps = kThreads / 32, kTilesUnit = TileUnits::kU
 // Up to so many vectors per head of k and v: attn_rows.cu, in units of so many; more: attn_tiles.cu
 constexpr int kRowsVectors = 16;
 
+// Where a vector's records of a part are.
+struct Records {
+  int n;               // 0: the result is written already
+  const float *sums, *md;   // of the first one: 4 of its sums, its maximum and sum of weights
+  long long chunk;     // floats from 4 sums of it to the next 4
+  int copies;          // of each CTA, one after another
+  int copy, md_copy;   // floats from a CTA's copy to the next
+  int cta, second;     // floats from a CTA's to the next one's, and from the first CTA's to the second's
+  __device__ int at(int c) const { return c == 0 ? 0 : second + (c - 1) * cta; }
+};
 template <int HD>
-__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ JoinArgs a) {
+__device__ __forceinline__ Records records_of(const JoinArgs& a, const JoinPart& part, int seq, const SeqRows& found, int row,
+                                              int h, int kv_head) {
+  const bool own = part.at < 0;
+  const int b = own ? seq : part.at, heads = a.group * a.kv_heads;
+  const uint32_t base = part.bases[b], total = part.bases[part.list];
+  const uint32_t vecs = (own ? found.n : a.rows) * a.group, vec = (row - (own ? found.row0 : 0)) * a.group + h - kv_head * a.group;
+  const uint32_t tiles = tiles_of(own ? min(max(found.len, 0), a.max_pos) : part.keys);
+  const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit;
+  // where the unit is, and who has its first tile, the second and the last one: the CTAs between the first two
+  // have none of it
+  int c0, c1, gap = 0;
+  bool pair;
+  auto find = [&](auto cut, uint32_t per_head, uint32_t per_unit) {
+    typedef decltype(cut) CUT;
+    const uint32_t w = CUT::weight(vecs, unit), t0 = base + kv_head * per_head + unit * per_unit;
+    const Pieces pieces(part.ctas, total, CUT::kGrain);
+    pair = w == 2;
+    c0 = pieces.owner(t0);
+    c1 = pieces.owner(t0 + CUT::place_of(tiles - 1, w));
+    if (tiles > 1) gap = max(static_cast<int>(pieces.owner(t0 + CUT::place_of(1, w))) - c0 - 1, 0);
+  };
+  if (part.pairs)
+    find(TileUnits{}, TileUnits::per_head(vecs, tiles), TileUnits::per_unit(tiles));
+  else if (part.unit == 8)
+    find(RowUnits<8>{}, RowUnits<8>::per_head(vecs, tiles), RowUnits<8>::per_unit(tiles));
+  else
+    find(RowUnits<16>{}, RowUnits<16>::per_head(vecs, tiles), RowUnits<16>::per_unit(tiles));
+  // attn_rows.cu's records are one after another, one of a CTA; attn_tiles.cu's side by side, of its smaller units two
+  const bool whole = c0 == c1;
+  const long long all = static_cast<long long>(a.rows) * heads, i = whole ? static_cast<long long>(row) * heads + h : in_unit;
+  const long long side = whole ? 2 * all : part.unit;
+  const int record = part.unit * kRecord<HD>;
+  Records r;
+  r.copies = part.pairs && !pair ? 2 : 1;
+  r.n = whole && part.full == nullptr ? 0 : (c1 - c0 + 1 - gap) * r.copies;
+  const float* first = whole ? part.full : part.slots + (2ll * c0 + 1) * record;   // (of that CTA's two the one that begins a unit)
+  r.sums = first + i * (part.pairs ? 4 : kRecord<HD>);
+  r.md = part.pairs ? first + HD * side + 2 * i : r.sums + HD;
+  r.chunk = part.pairs ? 4 * side : 4;
+  r.copy = static_cast<int>(whole ? all : 128) * 4;
+  r.md_copy = r.copy / 2;
+  r.cta = 2 * record;
+  r.second = (1 + 2 * gap) * record;
+  return r;
+}
+
+// Records of attn_rows.cu alone: a warp to a row's head, its lanes the elements of a record, which are one after another.
+template <int HD>
+__global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_constant__ JoinArgs a) {
   constexpr int E = HD / 32;
   __shared__ int shared;
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32, heads = a.group * a.kv_heads;
@@ -30,60 +88,17 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   pdl_launch_dependents();
   const int h = blockIdx.y * kWarps + warp;
   if (seq < 0 || h >= heads) return;
-  const int kv_head = h / a.group;
   float top = kStart, den = 0.f, sum[E] = {};
   bool any = false;
 #pragma unroll 1
   for (int p = 0; p < a.parts; ++p) {
-    const JoinPart& part = a.part[p];
-    const bool own = part.at < 0;
-    const int b = own ? seq : part.at;
-    const uint32_t base = part.bases[b], total = part.bases[part.list];
-    const uint32_t vecs = (own ? found.n : a.rows) * a.group, vec = (row - (own ? found.row0 : 0)) * a.group + h - kv_head * a.group;
-    const uint32_t tiles = tiles_of(own ? min(max(found.len, 0), a.max_pos) : part.keys);
-    const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit;
-    // where the unit is, and who has its first tile, the second and the last one: the CTAs between the first two
-    // have none of it
-    int c0, c1, gap = 0;
-    bool pair;
-    auto find = [&](auto cut, uint32_t per_head, uint32_t per_unit) {
-      typedef decltype(cut) CUT;
-      const uint32_t w = CUT::weight(vecs, unit), t0 = base + kv_head * per_head + unit * per_unit;
-      const Pieces pieces(part.ctas, total, CUT::kGrain);
-      pair = w == 2;
-      c0 = pieces.owner(t0);
-      c1 = pieces.owner(t0 + CUT::place_of(tiles - 1, w));
-      if (tiles > 1) gap = max(static_cast<int>(pieces.owner(t0 + CUT::place_of(1, w))) - c0 - 1, 0);
-    };
-    if (part.pairs)
-      find(TileUnits{}, TileUnits::per_head(vecs, tiles), TileUnits::per_unit(tiles));
-    else if (part.unit == 8)
-      find(RowUnits<8>{}, RowUnits<8>::per_head(vecs, tiles), RowUnits<8>::per_unit(tiles));
-    else
-      find(RowUnits<16>{}, RowUnits<16>::per_head(vecs, tiles), RowUnits<16>::per_unit(tiles));
-    if (c0 == c1 && part.full == nullptr) continue;   // written by that CTA
-    any = true;
-    // The vector's records: `copies` of each CTA, one of attn_rows.cu, of attn_tiles.cu's smaller units two.
-    // attn_rows.cu's are one after another, attn_tiles.cu's side by side (chunks of 4 floats `chunk` apart)
-    const int copies = part.pairs && !pair ? 2 : 1, n = (c1 - c0 + 1 - gap) * copies;
-    const bool whole = c0 == c1;
-    const long long all = static_cast<long long>(a.rows) * heads, i = whole ? static_cast<long long>(row) * heads + h : in_unit;
-    const long long side = whole ? 2 * all : part.unit, chunk = part.pairs ? 4 * side : 4;
-    const float* first = (whole ? part.full : part.slots + 2 * c0 * static_cast<long long>(part.unit * kRecord<HD>)) +
-                         i * (part.pairs ? 4 : kRecord<HD>);
-    const long long to_md = part.pairs ? HD * side - 2 * i : HD;
-    // a stretch's records further on for each CTA, those of the one that begins the unit one further
-    auto record = [&](int r) {
-      const int c = copies == 2 ? r >> 1 : r, w = copies == 2 ? r & 1 : 0;
-      return first + (c > 0 ? 2 * (c + gap) : whole ? 0 : 1) * static_cast<long long>(part.unit * kRecord<HD>) +
-             w * (whole ? all : 128) * 4;
-    };
-    auto md_of = [&](int r) { return record(r) + to_md - (copies == 2 && (r & 1) ? 2 * (whole ? all : 128) : 0); };
+    const Records rec = records_of<HD>(a, a.part[p], seq, found, row, h, h / a.group);
+    any |= rec.n > 0;
 #pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += 32) {   // a lane has a record's maximum and sum of weights
-      const int here = min(n - i0, 32);
+    for (int i0 = 0; i0 < rec.n; i0 += 32) {   // a lane has a record's maximum and sum of weights
+      const int here = min(rec.n - i0, 32);
       float2 md = make_float2(kStart, 0.f);
-      if (lane < here) md = *reinterpret_cast<const float2*>(md_of(i0 + lane));
+      if (lane < here) md = *reinterpret_cast<const float2*>(rec.md + rec.at(i0 + lane));
       float now = fmaxf(top, md.x);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) now = fmaxf(now, __shfl_xor_sync(~0u, now, o));
@@ -97,13 +112,13 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
 #pragma unroll 4
       for (int r = 0; r < here; ++r) {
         const float f = __shfl_sync(~0u, by, r);
-        const float* rec = record(i0 + r) + (lane * E / 4) * chunk + lane * E % 4;
+        const float* at = rec.sums + rec.at(i0 + r) + lane * E;
         if constexpr (E == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(rec);
+          const float4 x = *reinterpret_cast<const float4*>(at);
           sum[0] = fmaf(x.x, f, sum[0]), sum[1] = fmaf(x.y, f, sum[1]);
           sum[2] = fmaf(x.z, f, sum[2]), sum[3] = fmaf(x.w, f, sum[3]);
         } else {
-          const float2 x = *reinterpret_cast<const float2*>(rec);
+          const float2 x = *reinterpret_cast<const float2*>(at);
           sum[0] = fmaf(x.x, f, sum[0]), sum[1] = fmaf(x.y, f, sum[1]);
         }
       }
@@ -115,6 +130,50 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * a.ldo + h * HD + lane * E);
 #pragma unroll
   for (int e = 0; e < E; e += 2) out[e / 2] = pack_bf16(sum[e] * by, sum[e + 1] * by);
+}
+
+// Where attn_tiles.cu's are among them: a lane to a vector, a warp to four elements of 32 vectors, so that its loads
+// are 512 bytes in a row.
+template <int HD>
+__global__ void __launch_bounds__(kThreads) join_tiles_kernel(const __grid_constant__ JoinArgs a) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, kv_head = blockIdx.y;
+  const uint32_t vec = blockIdx.x * 32 + lane;
+  const int row = min(a.group_magic == 0 ? vec : __umulhi(vec, a.group_magic), a.rows - 1u);
+  const int h = kv_head * a.group + vec - row * a.group, chunk = blockIdx.z * kWarps + warp;
+  int seq = 0;   // (starts and lens were complete before the launch before this one began)
+#pragma unroll 1
+  for (int end = a.n_seq; end - seq > 1;) {   // the last one that begins at or before the row
+    const int mid = (seq + end) / 2;
+    if (a.starts[mid] <= row)
+      seq = mid;
+    else
+      end = mid;
+  }
+  const SeqRows found = seq_rows(a.starts, a.lens, seq, a.rows);
+  pdl_wait();
+  pdl_launch_dependents();
+  if (row < found.row0 || row >= found.row0 + found.n || vec >= static_cast<uint32_t>(a.rows) * a.group || chunk >= HD / 4) return;
+  float top = kStart, den = 0.f, sum[4] = {};
+#pragma unroll 1
+  for (int p = 0; p < a.parts; ++p) {
+    const Records rec = records_of<HD>(a, a.part[p], seq, found, row, h, kv_head);
+    const float* const sums = rec.sums + chunk * rec.chunk;
+    const int twice = rec.copies - 1;
+#pragma unroll 4
+    for (int r = 0; r < rec.n; ++r) {
+      const int at = rec.at(r >> twice), copy = r & twice;
+      const float2 md = *reinterpret_cast<const float2*>(rec.md + at + copy * rec.md_copy);
+      const float now = fmaxf(top, md.x), was = ex2(top - now), by = ex2(md.x - now);
+      top = now;
+      den = fmaf(den, was, by * md.y);
+      const float4 x = *reinterpret_cast<const float4*>(sums + at + copy * rec.copy);
+      sum[0] = fmaf(x.x, by, sum[0] * was), sum[1] = fmaf(x.y, by, sum[1] * was);
+      sum[2] = fmaf(x.z, by, sum[2] * was), sum[3] = fmaf(x.w, by, sum[3] * was);
+    }
+  }
+  const float by = den == 0.f ? 0.f : 1.f / den;
+  *reinterpret_cast<uint2*>(a.out + row * a.ldo + h * HD + chunk * 4) =
+      make_uint2(pack_bf16(sum[0] * by, sum[1] * by), pack_bf16(sum[2] * by, sum[3] * by));
 }
 
 // ---------------------------------------------------------------- host
@@ -266,6 +325,7 @@ memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv
   j.rows = batch->rows;
   j.max_pos = kv->max_pos;
   j.group = a.group;
+  j.group_magic = a.group_magic;
   j.kv_heads = kv->n_heads;
   j.out = static_cast<bf16*>(p->out_dev);
   j.ldo = a.ldo;
@@ -296,8 +356,16 @@ memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv
   }
   if (e == cudaSuccess) {
     cfg.blockDim = dim3(kThreads);
-    cfg.gridDim = dim3(batch->rows, (p->n_heads + kWarps - 1) / kWarps);
-    e = kv->head_dim == 64 ? cudaLaunchKernelEx(&cfg, join_kernel<64>, j) : cudaLaunchKernelEx(&cfg, join_kernel<128>, j);
+    if (l.launch[0].tiles || l.launch[l.n - 1].tiles) {
+      constexpr int at_once = 4 * kWarps;   // elements
+      cfg.gridDim = dim3((batch->rows * a.group + 31) / 32, kv->n_heads, (kv->head_dim + at_once - 1) / at_once);
+      e = kv->head_dim == 64 ? cudaLaunchKernelEx(&cfg, join_tiles_kernel<64>, j)
+                             : cudaLaunchKernelEx(&cfg, join_tiles_kernel<128>, j);
+    } else {
+      cfg.gridDim = dim3(batch->rows, (p->n_heads + kWarps - 1) / kWarps);
+      e = kv->head_dim == 64 ? cudaLaunchKernelEx(&cfg, join_rows_kernel<64>, j)
+                             : cudaLaunchKernelEx(&cfg, join_rows_kernel<128>, j);
+    }
   }
   if (e != cudaSuccess) {
     set_op_error(std::string("attention launch: ") + cudaGetErrorString(e));

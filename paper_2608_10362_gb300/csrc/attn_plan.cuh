@@ -246,6 +246,7 @@ struct JoinArgs {
   int parts;
   const int *starts, *lens;
   int n_seq, rows, max_pos, group, kv_heads;
+  uint32_t group_magic;
   bf16* out;
   long long ldo;
 };
