@@ -25,8 +25,8 @@ struct Records {
   long long chunk;     // floats from 4 sums of it to the next 4
   int copies;          // of each CTA, one after another
   int copy, md_copy;   // floats from a CTA's copy to the next
-  int cta, second;     // floats from a CTA's to the next one's, and from the first CTA's to the second's
-  __device__ int at(int c) const { return c == 0 ? 0 : second + (c - 1) * cta; }
+  int record;          // floats of a unit's; the first CTA's is its second one, the others' their first
+  __device__ int at(int c) const { return c == 0 ? 0 : (2 * c - 1) * record; }
 };
 template <int HD>
 __device__ __forceinline__ Records records_of(const JoinArgs& a, const JoinPart& part, int seq, const SeqRows& found, int row,
@@ -37,18 +37,15 @@ __device__ __forceinline__ Records records_of(const JoinArgs& a, const JoinPart&
   const uint32_t vecs = (own ? found.n : a.rows) * a.group, vec = (row - (own ? found.row0 : 0)) * a.group + h - kv_head * a.group;
   const uint32_t tiles = tiles_of(own ? min(max(found.len, 0), a.max_pos) : part.keys);
   const uint32_t unit = vec / part.unit, in_unit = vec - unit * part.unit;
-  // where the unit is, and who has its first tile, the second and the last one: the CTAs between the first two
-  // have none of it
-  int c0, c1, gap = 0;
+  int c0, c1;   // who has the first tile, and the last one: all between them have some
   bool pair;
   auto find = [&](auto cut, uint32_t per_head, uint32_t per_unit) {
     typedef decltype(cut) CUT;
-    const uint32_t w = CUT::weight(vecs, unit), t0 = base + kv_head * per_head + unit * per_unit;
+    const uint32_t t0 = base + kv_head * per_head + unit * per_unit;
     const Pieces pieces(part.ctas, total, CUT::kGrain);
-    pair = w == 2;
-    c0 = pieces.owner(t0);
-    c1 = pieces.owner(t0 + CUT::place_of(tiles - 1, w));
-    if (tiles > 1) gap = max(static_cast<int>(pieces.owner(t0 + CUT::place_of(1, w))) - c0 - 1, 0);
+    pair = CUT::pair(vecs, unit);
+    c0 = pieces.owner(t0 + CUT::place_of(0, pair));
+    c1 = pieces.owner(t0 + CUT::place_of(tiles - 1, pair));
   };
   if (part.pairs)
     find(TileUnits{}, TileUnits::per_head(vecs, tiles), TileUnits::per_unit(tiles));
@@ -63,15 +60,14 @@ __device__ __forceinline__ Records records_of(const JoinArgs& a, const JoinPart&
   const int record = part.unit * kRecord<HD>;
   Records r;
   r.copies = part.pairs && !pair ? 2 : 1;
-  r.n = whole && part.full == nullptr ? 0 : (c1 - c0 + 1 - gap) * r.copies;
+  r.n = whole && part.full == nullptr ? 0 : (c1 - c0 + 1) * r.copies;
   const float* first = whole ? part.full : part.slots + (2ll * c0 + 1) * record;   // (of that CTA's two the one that begins a unit)
   r.sums = first + i * (part.pairs ? 4 : kRecord<HD>);
   r.md = part.pairs ? first + HD * side + 2 * i : r.sums + HD;
   r.chunk = part.pairs ? 4 * side : 4;
   r.copy = static_cast<int>(whole ? all : 128) * 4;
   r.md_copy = r.copy / 2;
-  r.cta = 2 * record;
-  r.second = (1 + 2 * gap) * record;
+  r.record = record;
   return r;
 }
 
@@ -253,10 +249,10 @@ const char* attention_problem(const memspec_batch* b, const memspec_kv* kv, cons
       return "the prefix must have the cache's heads and head_dim";
     if (p->prefix_len < 0 || p->prefix_len > p->prefix->max_pos) return "prefix_len must be in 0..the prefix's max_pos";
   }
-  // the line is counted in 32 bits: at most a unit per 8 vectors, each of all tiles
-  const double units = static_cast<double>(b->rows) * (p->n_heads / kv->n_heads) / 8 + b->n_seq;
+  // the line is counted in 32 bits: a unit per 8 vectors, each of all tiles, is more than there can be
+  const double units = static_cast<double>(b->rows) * (p->n_heads / kv->n_heads) / 8 + TileUnits::kGrain * (b->n_seq + 1);
   const double keys = std::max(kv->max_pos, p->prefix != nullptr ? p->prefix_len : 0);
-  if (units * kv->n_heads * (keys / kTile + 9) >= 3.5e9) return "too many rows for so many positions: split the call";
+  if (units * kv->n_heads * (keys / kTile + 16) >= 3.5e9) return "too many rows for so many positions: split the call";
   return nullptr;
 }
 

@@ -56,33 +56,29 @@ __device__ __forceinline__ int list_keys(const ListArgs& a, int b, const SeqRows
 // At least one, so that every row of a sequence is written.
 __host__ __device__ constexpr uint32_t tiles_of(int keys) { return keys == 0 ? 1 : (keys + kTile - 1u) / kTile; }
 
-// A unit of up to UNIT vectors costs `per tile` 1, or (PAIRS) 2 where it has more than 128 of them, and START,
-// or START2, to begin with; its first tile stands at its beginning, tile t > 0 at its start's cost + t * per tile.
-template <int UNIT, bool PAIRS, int START, int START2>
+// What a unit of up to UNIT vectors takes of the line: START to begin with, then TILE a tile; START2 and TILE2 (if not 0)
+// where it has more than 128 vectors.  A tile is whose its beginning is; a CTA whose piece ends within a start has
+// nothing of that unit, and who goes on in it does so as with its first: no CTA has more than its piece.
+template <int UNIT, int TILE, int START, int TILE2, int START2>
 struct Cut {
-  static constexpr int kUnit = UNIT, kGrain = PAIRS ? 2 : 1;
-  static constexpr bool kPairs = PAIRS;
-  __host__ __device__ static uint32_t weight(uint32_t vecs, uint32_t unit) {   // of a tile
-    return PAIRS && vecs - unit * UNIT > 128 ? 2 : 1;
-  }
-  __host__ __device__ static uint32_t start(uint32_t w) { return w == 2 ? START2 : START; }
-  // all units of a head together; one of them, but for the last one
+  static constexpr int kUnit = UNIT, kGrain = TILE2 > TILE ? TILE2 : TILE;
+  __host__ __device__ static bool pair(uint32_t vecs, uint32_t unit) { return TILE2 > 0 && vecs - unit * UNIT > 128; }
+  __host__ __device__ static uint32_t place_of(uint32_t t, bool pair) { return pair ? START2 + t * TILE2 : START + t * TILE; }
+  __host__ __device__ static uint32_t per_unit(uint32_t tiles) { return place_of(tiles, TILE2 > 0); }
+  // all units of a head together: one of them, but for the last one
   __host__ __device__ static uint32_t per_head(uint32_t vecs, uint32_t tiles) {
     const uint32_t units = (vecs + UNIT - 1) / UNIT;
-    if (units == 0) return 0;
-    const uint32_t w = weight(vecs, units - 1);
-    return (units - 1) * per_unit(tiles) + w * tiles + start(w);
+    return units == 0 ? 0 : (units - 1) * per_unit(tiles) + place_of(tiles, pair(vecs, units - 1));
   }
-  __host__ __device__ static uint32_t per_unit(uint32_t tiles) { return kGrain * tiles + start(kGrain); }
-  // where tile t stands in a unit of weight w, and the first tile at or after place `at`
-  __host__ __device__ static uint32_t place_of(uint32_t t, uint32_t w) { return t == 0 ? 0 : start(w) + t * w; }
-  __device__ static uint32_t tile_from(uint32_t at, uint32_t w) {
-    return at == 0 ? 0 : at <= start(w) + w ? 1 : (at - start(w) + w - 1) >> (w - 1);
+  // the first tile at or after place `at`
+  __device__ static uint32_t tile_from(uint32_t at, bool pair) {
+    const uint32_t start = pair ? START2 : START, in = at < start ? 0 : at - start;
+    return pair ? (in + TILE2 - 1) / (TILE2 > 0 ? TILE2 : 1) : (in + TILE - 1) / TILE;
   }
 };
 
-// Equal pieces of the line: the first total % ctas are one longer.  With fewer than `grain` places
-// each some CTAs have none; every other one that lies within a unit, past its start, has a tile of it.
+// Equal pieces of the line: the first total % ctas are one longer.  None is shorter than a tile: what lies within a
+// unit, past its start, has one of it.
 struct Pieces {
   uint32_t ctas, each, longer;
   __device__ Pieces(uint32_t ctas_, uint32_t total, int grain) {
@@ -196,12 +192,12 @@ struct Walk {
       u.head = in / per_head;
       const uint32_t in_head = in - u.head * per_head;
       u.unit = in_head / per_unit;
-      const uint32_t w = CUT::weight(u.vecs, u.unit), at = in_head - u.unit * per_unit,
-                     end = min(CUT::start(w) + w * u.tiles, at + (x1 - x));
-      u.t0 = min(CUT::tile_from(at, w), static_cast<uint32_t>(u.tiles));
-      u.t1 = min(CUT::tile_from(end, w), static_cast<uint32_t>(u.tiles));
+      const bool pair = CUT::pair(u.vecs, u.unit);
+      const uint32_t at = in_head - u.unit * per_unit, end = min(CUT::place_of(u.tiles, pair), at + (x1 - x));
+      u.t0 = min(CUT::tile_from(at, pair), static_cast<uint32_t>(u.tiles));
+      u.t1 = min(CUT::tile_from(end, pair), static_cast<uint32_t>(u.tiles));
       x += end - at;
-      found = u.t0 < u.t1;   // (pieces that lie within a unit's start, or a pair's tile, have nothing of it)
+      found = u.t0 < u.t1;   // (pieces that lie within a unit's start, or a tile, have nothing of it)
     }
     return found;
   }
@@ -310,8 +306,8 @@ constexpr int kTilesCtas = 152;
 cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg);   // InvalidValue: no tensor map
 // What a unit costs to begin with, in tiles of 128 vectors (us of a tile and a start: attn_rows.cu 0.5 and 4, a unit
 // of attn_tiles.cu with up to 128 vectors 1.0 and 2 to 3, with more 1.9 and 4 to 8).
-typedef Cut<256, true, 3, 4> TileUnits;
+typedef Cut<256, 3, 8, 5, 16> TileUnits;
 template <int VT>
-using RowUnits = Cut<VT, false, 4, 4>;
+using RowUnits = Cut<VT, 1, 2, 0, 0>;
 
 }  // namespace memspec

@@ -258,7 +258,7 @@ __device__ __forceinline__ void walk_role(const ListArgs& a, Ctl& ctl) {
     mbar_arrive(&ctl.listed[i % kListed]);
   }
 }
-__device__ __forceinline__ bool is_pair(const Stretch& u) { return Units::weight(u.vecs, u.unit) == 2; }
+__device__ __forceinline__ bool is_pair(const Stretch& u) { return Units::pair(u.vecs, u.unit); }
 // ---------------------------------------------------------------- copies
 // A tile of V that not every vector sees all of: rows of the sequence's own, or rows past the keys' end.
 __device__ __forceinline__ bool own_rows(const Stretch& u, int t) { return u.own && (t + 1) * kTile > u.first; }
