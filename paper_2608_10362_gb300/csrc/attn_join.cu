@@ -204,7 +204,7 @@ Layout lay_out(const memspec_batch* b, const memspec_kv* kv, const memspec_atten
   if (two) {
     Launch x = launch(p->prefix, static_cast<long long>(b->rows) * group);
     x.prefix = true;
-    if (x.tiles && x.codes == l.launch[0].codes) {
+    if (x.tiles && l.launch[0].tiles && x.codes == l.launch[0].codes) {
       // one launch of attn_tiles.cu for both, whatever the sequences' own rows are (64 rows behind 32768 codes,
       // up to 1024 codes of their own: 83.6 us, own keys by attn_rows.cu before it 87.2)
       x.own = true;
@@ -336,6 +336,7 @@ memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv
   for (int i = 0; i < l.n && e == cudaSuccess; ++i) {
     const Launch& x = l.launch[i];
     a.n_own = x.own ? batch->n_seq : 0;
+    a.beside = i > 0;
     a.prefix_len = x.prefix ? p->prefix_len : 0;
     a.tree = x.own ? p->tree_dev : nullptr;
     const bool direct = !two && !x.tiles;

@@ -39,6 +39,7 @@ struct ListArgs {
   float* full[2];            // records of the cache's and of the prefix's units: [rows][heads], of attn_tiles.cu two such
   float* slots;              // [ctas][2] units' records
   uint32_t* bases;           // [list + 1]: where each sequence's tiles begin on the line
+  int beside;                // the launch before this one is the same call's: what that one waited for is complete
 };
 
 // A record: HD sums, the maximum, the sum of weights (and two floats that align the next one).

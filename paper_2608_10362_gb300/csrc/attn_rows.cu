@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
   extern __shared__ __align__(128) char smem_raw[];
   const Smem<S> sm(smem_raw);
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane >> 2, t = lane & 3;
-  pdl_wait();
+  if (!a.beside) pdl_wait();
   pdl_launch_dependents();
   make_plan<RowUnits<VT>, kThreads>(a, *sm.plan);
   if (blockIdx.x == 0)
@@ -488,6 +488,7 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
     }
     __syncthreads();
   }
+  if (a.beside) pdl_wait();   // the launch after this one waits for both
 }
 
 template <class S>

@@ -821,7 +821,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     tmem_alloc(&ctl.tmem_base, 512);
     tmem_relinquish();
   }
-  pdl_wait();
+  if (!a.beside) pdl_wait();
   pdl_launch_dependents();
   tc_fence_before();
   make_plan<Units, S::kThreads>(a, ctl.plan);
@@ -848,6 +848,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     if (blockIdx.x == 0)
       for (int b = threadIdx.x % 32; b <= list_len(a); b += 32) a.bases[b] = ctl.plan.bases[b];
   }
+  if (a.beside) pdl_wait();   // the launch after this one waits for both
   tc_fence_before();
   __syncthreads();
   if (warp == kMma) {
