@@ -15,7 +15,10 @@ namespace memspec {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kTilesUnit = TileUnits::kUnit;
-// Up to so many vectors per head of k and v: attn_rows.cu, in units of so many; more: attn_tiles.cu
+// Up to so many vectors per head of k and v: attn_rows.cu, in units of 8 or 16; more: attn_tiles.cu.  16 sequences of 2048
+// positions, 8 heads of k and v, bf16 and codes, attn_rows.cu / attn_tiles.cu: 8 vectors 27.9 / 33.0 and 19.3 / 37.7 us, 16:
+// 29.5 / 33.4 and 28.8 / 37.8, 24: 44.2 / 34.2 and 46.0 / 38.0.  Units of 16 for 4 vectors: 64 sequences of 16384 codes
+// 590 us for 321 (what 8 vectors more cost is all lost).
 constexpr int kRowsVectors = 16;
 
 // Where a vector's records of a part are.
@@ -71,7 +74,9 @@ __device__ __forceinline__ Records records_of(const JoinArgs& a, const JoinPart&
   return r;
 }
 
-// Records of attn_rows.cu alone: a warp to a row's head, its lanes the elements of a record, which are one after another.
+// Records of attn_rows.cu alone, of one vector up to one per CTA (one row of 32 / 8 heads over 8192 codes: 38): a warp
+// to a row's head, kAtOnce of its records under way, its lanes the elements of a record, which are one after another.
+constexpr int kAtOnce = 8;   // (that case 14.2 us; 4: 17.7, 16: 13.5, and calls with few records 0.5 more than with 4)
 template <int HD>
 __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_constant__ JoinArgs a) {
   constexpr int E = HD / 32;
@@ -98,24 +103,32 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
       float now = fmaxf(top, md.x);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) now = fmaxf(now, __shfl_xor_sync(~0u, now, o));
-      const float was = ex2(top - now), by = ex2(md.x - now);
+      const float was = ex2(top - now), by = lane < here ? ex2(md.x - now) : 0.f;
       float d = by * md.y;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(~0u, d, o);
       den = fmaf(den, was, d);
 #pragma unroll
       for (int e = 0; e < E; ++e) sum[e] *= was;
-#pragma unroll 4
-      for (int r = 0; r < here; ++r) {
-        const float f = __shfl_sync(~0u, by, r);
-        const float* at = rec.sums + rec.at(i0 + r) + lane * E;
-        if constexpr (E == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(at);
-          sum[0] = fmaf(x.x, f, sum[0]), sum[1] = fmaf(x.y, f, sum[1]);
-          sum[2] = fmaf(x.z, f, sum[2]), sum[3] = fmaf(x.w, f, sum[3]);
-        } else {
-          const float2 x = *reinterpret_cast<const float2*>(at);
-          sum[0] = fmaf(x.x, f, sum[0]), sum[1] = fmaf(x.y, f, sum[1]);
+#pragma unroll 1
+      for (int r0 = 0; r0 < here; r0 += kAtOnce) {   // (past the last one: that one, times 0)
+        float2 x[kAtOnce][E / 2];
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) {
+          const float* at = rec.sums + rec.at(i0 + min(r0 + r, here - 1)) + lane * E;
+          if constexpr (E == 4) {
+            const float4 y = *reinterpret_cast<const float4*>(at);
+            x[r][0] = make_float2(y.x, y.y), x[r][E / 2 - 1] = make_float2(y.z, y.w);
+          } else {
+            x[r][0] = *reinterpret_cast<const float2*>(at);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < kAtOnce; ++r) {
+          const float f = __shfl_sync(~0u, by, r0 + r);
+#pragma unroll
+          for (int e = 0; e < E; e += 2)
+            sum[e] = fmaf(x[r][e / 2].x, f, sum[e]), sum[e + 1] = fmaf(x[r][e / 2].y, f, sum[e + 1]);
         }
       }
       top = now;
@@ -129,7 +142,7 @@ __global__ void __launch_bounds__(kThreads) join_rows_kernel(const __grid_consta
 }
 
 // Where attn_tiles.cu's are among them: a lane to a vector, a warp to four elements of 32 vectors, so that its loads
-// are 512 bytes in a row.
+// are 512 bytes in a row (a warp to a row's head, 16 bytes each from 32 places: 64 rows over 8192 positions 11 us more).
 template <int HD>
 __global__ void __launch_bounds__(kThreads) join_tiles_kernel(const __grid_constant__ JoinArgs a) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, kv_head = blockIdx.y;
@@ -205,8 +218,9 @@ Layout lay_out(const memspec_batch* b, const memspec_kv* kv, const memspec_atten
     Launch x = launch(p->prefix, static_cast<long long>(b->rows) * group);
     x.prefix = true;
     if (x.tiles && l.launch[0].tiles && x.codes == l.launch[0].codes) {
-      // one launch of attn_tiles.cu for both, whatever the sequences' own rows are (64 rows behind 32768 codes,
-      // up to 1024 codes of their own: 83.6 us, own keys by attn_rows.cu before it 87.2)
+      // one launch of attn_tiles.cu for both (16 x 9 rows behind 8192 positions, 300 of their own: 41.6 us, two launches
+      // 44.5).  Few own vectors stay attn_rows.cu's, and the prefix's launch does not wait for theirs (64 rows behind
+      // 32768 codes, up to 1024 of their own: 68.5, waiting 70.6, all in one launch 74.4)
       x.own = true;
       l.launch[0] = x;
     } else {

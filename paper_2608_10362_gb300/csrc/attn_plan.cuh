@@ -305,8 +305,11 @@ int rows_ctas(bool codes, int nt);
 cudaError_t launch_attn_rows(int hd, bool codes, int nt, const ListArgs& a, cudaLaunchConfig_t cfg);
 constexpr int kTilesCtas = 152;
 cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg);   // InvalidValue: no tensor map
-// What a unit costs to begin with, in tiles of 128 vectors (us of a tile and a start: attn_rows.cu 0.5 and 4, a unit
-// of attn_tiles.cu with up to 128 vectors 1.0 and 2 to 3, with more 1.9 and 4 to 8).
+// In attn_tiles.cu a tile of up to 128 vectors takes 1.1 us (codes 1.5), of more 1.9 (2.4); a further stretch in a CTA 2.6
+// us, where it is cut as well 5 (2.4, 4.2), of more vectors 5.3 (7.5).  16 x 9 rows over codes, 256 rows, 16 x 9 rows
+// behind 8192: with these weights 37.7, 41.2, 40.6 us; tiles 1 and 2, starts 3 and 5: 38.5, 42.3, 43.4; 2 and 4: 37.3, 42.6,
+// 46.9.  In attn_rows.cu a tile takes 0.5 us and a start of 2 of them measures best: one row of 32 heads 11.6 us (0: 13.2,
+// 4: 11.7), 5 rows over codes 12.7 (14.8, 12.9).
 typedef Cut<256, 3, 8, 5, 16> TileUnits;
 template <int VT>
 using RowUnits = Cut<VT, 1, 2, 0, 0>;

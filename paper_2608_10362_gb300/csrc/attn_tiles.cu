@@ -17,9 +17,15 @@
 // a power of two near the tile's largest: a value is off by 2^-10 of itself (its factor and the product are
 // rounded), or by 2^-16 of the largest scale of its tile.  K's power multiplies the tile's scores, V's is added to them as a logarithm: weights are
 // w' = p * power, against a maximum of their own kind, and the sum of p is that of w' / power; so no range of scales
-// overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu has them, are three numbers per
-// key for every thread out of shared memory, 128 bytes a clock: 0.7 us of a step's 1.5; now 0.6.)  A vector of Q is taken
-// to fp16 by a power of two of its own.
+// overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu has them, would be three numbers
+// per key for every thread out of shared memory, at 128 bytes a clock 0.7 us of a step.)  A vector of Q is taken to fp16
+// by a power of two of its own.
+//
+// What bounds it: a tile for 256 vectors takes 1.9 us of bf16, of which the MMAs' part is 1.3 (S in steps of 64 keys
+// reads its operands from shared memory for 48 clocks per 32 of arithmetic), and 2.4 of codes, where converting and the
+// softmax share the SM's issue.  64 rows of 32 heads, 8 of k and v, over 262144 positions: 221 us, 1.25 PFLOP/s, codes
+// 258.  At ordinary lengths it is what comes before and after: 6 us to the first S, 2 to write the records, 4 to 6 for
+// the join (the same rows over 8192 positions 24 us, of which 6.5 are tiles).
 //
 // Roles (warps): 0-3, 4-7 softmax; copies, 4, or 8 of codes; two with the MMAs of a warpgroup each;
 // one for Q; one for which units these are.  Every wait is bounded; after one that ran out the CTA's records
@@ -48,7 +54,7 @@ struct Shape {
   static constexpr bool CODES = CODES_;
   static constexpr int kCopy = CODES ? 128 : 64;       // threads for K, and as many for V
   static constexpr int kThreads = kSoft + 2 * kCopy + 128;
-  static constexpr int kWidth = CODES ? 32 : 64;       // scores of a step in registers at a time (96 and 128 a thread)
+  static constexpr int kWidth = CODES ? 32 : 64;       // scores of a step in registers at a time (a thread has 96 and 128)
   static constexpr int kSlotBytes = kTile * HD * 2;
   static constexpr int kQBytes = 128 * HD * 2;         // of 128 vectors
   static constexpr int kSmem = 1024 + kSlots * kSlotBytes + 2 * kQBytes;
