@@ -332,19 +332,29 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
       if (tid < kTile / 32) ctl.bad[i][tid] = 0u;
       named_bar_sync(2, kCopy);
       const int live = min(u.end() - key0, kTile);
-      const int from = own_rows(u, t) ? static_cast<int>(max(u.first - key0, 0ll)) : live;
+      const int from = own_rows(u, t) ? min(static_cast<int>(max(u.first - key0, 0ll)), live) : live;
+      auto chunk = [&](int at) {
+        return reinterpret_cast<uint4*>(ring + s * S::kSlotBytes + chunk_at(at / C, at % C));
+      };
 #pragma unroll 1
-      for (int at = min(from, live) * C + tid; at < kTile * C; at += kCopy) {
-        const int r = at / C;
-        uint4* p = reinterpret_cast<uint4*>(ring + s * S::kSlotBytes + chunk_at(r, at % C));
-        bool odd = r >= live;
-        if (!odd) {
-          const uint32_t x[4] = {p->x, p->y, p->z, p->w};
+      for (int at = live * C + tid; at < kTile * C; at += kCopy) *chunk(at) = make_uint4(0u, 0u, 0u, 0u);
+      constexpr int N = 8;   // under way
+#pragma unroll 1
+      for (int at = from * C + tid; at < live * C; at += N * kCopy) {
+        uint32_t odd = 0u;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) odd |= (x[j] & 0x7f80u) == 0x7f80u || (x[j] & 0x7f800000u) == 0x7f800000u;
-          if (odd) atomicOr(&ctl.bad[i][r / 32], 1u << r % 32);
+        for (int n = 0; n < N; ++n) {   // (past the last: that thread's first again)
+          const uint4 x = *chunk(at + n * kCopy < live * C ? at + n * kCopy : at);
+          // exponents of all ones carry into the sign's place
+          auto high = [](uint32_t v) { return (v & 0x7fff7fffu) + 0x00800080u; };
+          if ((high(x.x) | high(x.y) | high(x.z) | high(x.w)) & 0x80008000u) odd |= 1u << n;
         }
-        if (odd) *p = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+        for (; odd != 0u; odd &= odd - 1u) {
+          const int n = __ffs(odd) - 1, one = at + n * kCopy < live * C ? at + n * kCopy : at;
+          atomicOr(&ctl.bad[i][one / C / 32], 1u << one / C % 32);
+          *chunk(one) = make_uint4(0u, 0u, 0u, 0u);
+        }
       }
       fence_proxy_async_smem();
       named_bar_sync(2, kCopy);
