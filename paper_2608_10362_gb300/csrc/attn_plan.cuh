@@ -131,8 +131,9 @@ __device__ __forceinline__ void make_plan(const ListArgs& a, Plan& plan) {
     if (lane == 31) plan.sums[warp] = incl;
     __syncthreads();
     uint64_t sum = before;
+    const int warps = (min(n - b0, THREADS) + 31) / 32;   // those with a sequence
 #pragma unroll 1
-    for (int w = 0; w < THREADS / 32; ++w) {
+    for (int w = 0; w < warps; ++w) {
       if (w < warp) sum += plan.sums[w];
       before += plan.sums[w];
     }
