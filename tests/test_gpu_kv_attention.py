@@ -796,3 +796,37 @@ def test_a_layers_calls_on_a_side_stream_and_in_a_graph():
         for a, b in zip(outs, layer(caches[1])):
             assert torch.equal(a, b)
     assert all(torch.equal(a, b) for a, b in zip(caches[0].tensors, caches[1].tensors))
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("rows", [12, 64])
+def test_calls_back_to_back_behind_a_prefix(rows, codes):
+    """Rows by rows decoded behind a prefix: a call's launches may run beside one another, those of the next call
+    on the same scratch, with queries written just before it, after them; eager and in one graph."""
+    pkg, H, Hk, hd, P = _pkg(), 8, 4, 128, 700
+    starts, lens = batch([1] * rows, [(37 * i) % 300 for i in range(rows)])
+    cache = make_cache(codes, rows, Hk, 320, hd, seed=1)
+    prefix = make_cache(codes, 1, Hk, P, hd, seed=2)
+    s, l = _i32(*starts), _i32(*lens)
+    qs = [torch.randn(rows, H, hd, device=DEV, generator=_gen(i)).bfloat16() for i in range(6)]
+    scratch = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    q = torch.empty_like(qs[0])
+
+    def run():
+        outs = []
+        for x in qs:
+            q.copy_(x)
+            outs.append(pkg.op_attention(q, cache, s, l, max_rows=1, prefix=prefix, scratch=scratch))
+        return outs
+    want = []
+    for x in qs:
+        want.append(pkg.op_attention(x, cache, s, l, max_rows=1, prefix=prefix))
+        torch.cuda.synchronize()
+    check(want[0], *attention64(qs[0], cache, starts, lens, prefix=prefix, prefix_len=P, max_rows=1))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for _ in range(30):
+        graph.replay()
+        for a, b, c in zip(run(), captured, want):
+            assert torch.equal(a, c) and torch.equal(b, c)
