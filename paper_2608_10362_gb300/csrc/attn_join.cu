@@ -3,7 +3,7 @@
 //
 // A record is HD sums of weights times values, the maximum the weights were taken against and their
 // sum; records of one vector add up after each is scaled to the largest maximum, in the order of
-// the line.  A warp takes a row's head, its lanes the elements.
+// the line.  Two launches do it, for the two ways in which the kernels leave them.
 #include <algorithm>
 #include <string>
 

@@ -1,4 +1,4 @@
-// kv.cuh - what the cache and attention operators (kv_append.cu, attn_rows.cu) share: a
+// kv.cuh - what the cache and attention operators (kv_append.cu, attn_*.cu) share: a
 // layer's keys and values as the caller laid them out, which rows of a call belong to which
 // sequence, and their checks.
 #pragma once
