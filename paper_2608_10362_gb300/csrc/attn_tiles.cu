@@ -45,6 +45,9 @@ constexpr int kSlots = 4;               // tiles in shared memory: K of two, V o
 constexpr int kRefs = 4;                // a tile's references are read until its P is written
 constexpr int kListed = 4;              // stretches told of at a time
 constexpr int kStep = 64;               // keys of a warpgroup's step
+// What a step's products are multiplied by is at least this: it meets -inf where a vector does not see a key, which 0
+// would make a NaN (a vector of zeros over a tile of the smallest scales: the product of its factors is below fp32).
+constexpr float kLeastFactor = 0x1p-149f;
 typedef TileUnits Units;
 constexpr int kTilesUnit = Units::kUnit;
 
@@ -565,7 +568,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
     const int vec = u.unit * kTilesUnit + (pair ? w * 128 : 0) + row, end = u.end();
     const bool live = vec < u.vecs, warp_live = __any_sync(~0u, live);
     const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
-    float scale = fmaxf(fabsf(a.scale), 1e-30f);   // (not 0: it meets scores of -inf)
+    float scale = fmaxf(fabsf(a.scale), 1e-30f);
     float m = kStart, l = 0.f;
     bool huge = false;   // some m of the warp's
     if (softmax_loads(u, stretch)) {
@@ -589,6 +592,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
             const float4 ref = ctl.refs[(tiles + t - u.t0) % kRefs];
             by *= ref.x, plus = ref.y, l_by = ref.z;
           }
+          by = fmaxf(by, kLeastFactor);
           const bool edge = key0 + kStep > end || key0 + kStep > u.first;
           unsigned long long seen = ~0ull;   // bit e: the vector sees key key0 + e
           if (edge) {
