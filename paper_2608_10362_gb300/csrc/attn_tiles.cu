@@ -46,7 +46,8 @@ constexpr int kRefs = 4;                // a tile's references are read until it
 constexpr int kListed = 4;              // stretches told of at a time
 constexpr int kStep = 64;               // keys of a warpgroup's step
 // What a step's products are multiplied by is at least this: it meets -inf where a vector does not see a key, which 0
-// would make a NaN (a vector of zeros over a tile of the smallest scales: the product of its factors is below fp32).
+// would make a NaN (a call's scale of 0; a vector of zeros over a tile of the smallest scales: the product of its factors
+// is below fp32).  fp32's largest times it is 2^-21.
 constexpr float kLeastFactor = 0x1p-149f;
 typedef TileUnits Units;
 constexpr int kTilesUnit = Units::kUnit;
@@ -568,7 +569,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
     const int vec = u.unit * kTilesUnit + (pair ? w * 128 : 0) + row, end = u.end();
     const bool live = vec < u.vecs, warp_live = __any_sync(~0u, live);
     const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
-    float scale = fmaxf(fabsf(a.scale), 1e-30f);
+    float scale = fabsf(a.scale);
     float m = kStart, l = 0.f;
     bool huge = false;   // some m of the warp's
     if (softmax_loads(u, stretch)) {
@@ -584,7 +585,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
         if (!wait(&ctl.s_full[w][buf], done >> 1)) break;
         tc_fence_after();
         if (warp_live) {
-          if (CODES && begins) scale = fmaxf(fabsf(a.scale), 1e-30f) * ctl.q_down[stretch & 3][vec - u.unit * kTilesUnit];
+          if (CODES && begins) scale = fabsf(a.scale) * ctl.q_down[stretch & 3][vec - u.unit * kTilesUnit];
           const uint32_t s_buf = s_at + buf * kStep;
           // z = by * S + plus: of codes with the tile's references
           float by = scale, plus = 0.f, l_by = 1.f;

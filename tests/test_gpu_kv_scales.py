@@ -1,0 +1,48 @@
+"""op_attention where its scale, queries, keys or values are near the ends of their types: each
+product that stays in fp32 is right whatever its factors are, in both kernels.  Bounds as in
+test_gpu_kv_attention.py, which count relative to scale sum|q k| and to the values."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_kv_attention import DEV, _gen, _i32, _pkg, attention64, batch, check, make_cache
+
+pytestmark = pytest.mark.gpu
+HEADS = pytest.mark.parametrize("H,Hk", [(4, 4), (32, 4)], ids=["few", "many"])
+
+
+def _times(cache, k=0, v=0):
+    """The cache with its keys and values (of codes: their scales) times powers of two."""
+    for i, e in ((0, k), (1, v)):
+        (cache.tensors[2 + i] if cache.codes else cache.tensors[i]).mul_(2.0 ** e)
+    return cache
+
+
+def _attend(q, cache, starts, lens, **kw):
+    for max_rows in (3, 1):
+        got = _pkg().op_attention(q, cache, _i32(*starts), _i32(*lens), max_rows=max_rows, **kw)
+        check(got, *attention64(q, cache, starts, lens, max_rows=max_rows, **kw))
+
+
+@HEADS
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("q_e,k_e,scale_e", [(55, 55, -110), (100, 0, -100), (-100, 0, 100), (0, -50, 50), (60, 0, -60),
+                                             (0, 60, -60), (20, 100, -120), (-60, -55, 115)])
+def test_scales_that_make_up_for_sizes(H, Hk, codes, q_e, k_e, scale_e):
+    """Scores of size 1 from factors that are not."""
+    starts, lens = batch([3, 1], [140, 20])
+    cache = _times(make_cache(codes, 2, Hk, 150, 128, seed=3), k=k_e)
+    q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** q_e).bfloat16()
+    _attend(q, cache, starts, lens, scale=0.09 * 2.0 ** scale_e)
+
+
+@HEADS
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("scale", [0.0, 1e-38, -1e-32])
+def test_small_scales_of_large_products(H, Hk, codes, scale):
+    """q . k of 2^117 times 0 is 0, times 1e-38 is small: nothing stands in for the scale."""
+    starts, lens = batch([3, 1], [140, 20])
+    cache = _times(make_cache(codes, 2, Hk, 150, 128, seed=3), k=55)
+    q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** 55).bfloat16()
+    _attend(q, cache, starts, lens, scale=scale)
