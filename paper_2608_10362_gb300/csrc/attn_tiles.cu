@@ -45,10 +45,9 @@ constexpr int kSlots = 4;               // tiles in shared memory: K of two, V o
 constexpr int kRefs = 4;                // a tile's references are read until its P is written
 constexpr int kListed = 4;              // stretches told of at a time
 constexpr int kStep = 64;               // keys of a warpgroup's step
-// What a step's products are multiplied by is at least this: it meets -inf where a vector does not see a key, which 0
-// would make a NaN (a call's scale of 0; a vector of zeros over a tile of the smallest scales: the product of its factors
-// is below fp32).  fp32's largest times it is 2^-21.
-constexpr float kLeastFactor = 0x1p-149f;
+// What a scale of 0 counts as: it meets -inf where a vector does not see a key, which 0 would make a NaN.  fp32's largest
+// times it is 2^-21.
+constexpr float kLeastScale = 0x1p-149f;
 typedef TileUnits Units;
 constexpr int kTilesUnit = Units::kUnit;
 
@@ -80,9 +79,9 @@ struct Ctl {
   uint32_t tmem_base;
   int abort_flag;
   uint32_t bad[2][kTile / 32];        // keys of an edge tile whose values are not all finite
-  float4 refs[kRefs];                 // codes: the power of two K's scales are taken against, V's logarithm, 1 / V's
+  float4 refs[kRefs];                 // codes: the exponents K's and V's scales are taken against, 1 / V's power of two
   CodesSmem codes[2];
-  float q_down[4][kTilesUnit];        // codes: 1 / the powers of two that a stretch's vectors were taken by; the next one's
+  int q_exp[4][kTilesUnit];           // codes: the exponents that a stretch's vectors were taken down by; the next one's
                                       // may be there, and the one's after it begun, before this one's softmax reads its own
   Plan plan;
   uint64_t listed[kListed];           // a stretch's entry is there
@@ -439,7 +438,7 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
         const uint32_t bad = __ballot_sync(~0u, !(sc[0] <= FLT_MAX));
         if (tid % 32 == 0) ctl.bad[s & 1][tid / 32] = bad;
       } else if (tid == 0) {   // (S of two tiles before is complete, after the softmax of four before: its entry is free)
-        ctl.refs[tile % kRefs] = make_float4(512.f * power(ref_k), ref_v + 9.f, power(-ref_v) / 512.f, 0.f);
+        ctl.refs[tile % kRefs] = make_float4(__int_as_float(ref_k + 9), ref_v + 9.f, power(-ref_v) / 512.f, 0.f);
       }
       uint4 in[N * J];
 #pragma unroll
@@ -511,7 +510,7 @@ __device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretc
       if (!on) continue;
       *p = make_uint4(scaled_f16(x.x ^ flip, up), scaled_f16(x.y ^ flip, up), scaled_f16(x.z ^ flip, up),
                       scaled_f16(x.w ^ flip, up));
-      if (at % C == 0) ctl.q_down[stretch & 3][at / C] = power(e);
+      if (at % C == 0) ctl.q_exp[stretch & 3][at / C] = e;
     }
   } else if (flip != 0u) {
 #pragma unroll 1
@@ -569,7 +568,12 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
     const int vec = u.unit * kTilesUnit + (pair ? w * 128 : 0) + row, end = u.end();
     const bool live = vec < u.vecs, warp_live = __any_sync(~0u, live);
     const Sight sight = live ? sight_of(a, u, vec) : Sight{-1, 0u};
-    float scale = fabsf(a.scale);
+    int scale_e = 0;     // codes: the scale is scale * 2^scale_e, with the vector's power of two
+    float scale = fmaxf(fabsf(a.scale), kLeastScale);
+    if constexpr (CODES) {
+      scale = frexpf(scale, &scale_e);
+      if (a.scale == 0.f) scale_e = -1024;
+    }
     float m = kStart, l = 0.f;
     bool huge = false;   // some m of the warp's
     if (softmax_loads(u, stretch)) {
@@ -585,15 +589,15 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
         if (!wait(&ctl.s_full[w][buf], done >> 1)) break;
         tc_fence_after();
         if (warp_live) {
-          if (CODES && begins) scale = fabsf(a.scale) * ctl.q_down[stretch & 3][vec - u.unit * kTilesUnit];
+          if (CODES && begins) scale_e += ctl.q_exp[stretch & 3][vec - u.unit * kTilesUnit];
           const uint32_t s_buf = s_at + buf * kStep;
           // z = by * S + plus: of codes with the tile's references
           float by = scale, plus = 0.f, l_by = 1.f;
           if constexpr (CODES) {
+            // (products are 2^17 at most: below 2^-126 it does not matter what they are times)
             const float4 ref = ctl.refs[(tiles + t - u.t0) % kRefs];
-            by *= ref.x, plus = ref.y, l_by = ref.z;
+            by *= power(min(max(scale_e + __float_as_int(ref.x), -126), 127)), plus = ref.y, l_by = ref.z;
           }
-          by = fmaxf(by, kLeastFactor);
           const bool edge = key0 + kStep > end || key0 + kStep > u.first;
           unsigned long long seen = ~0ull;   // bit e: the vector sees key key0 + e
           if (edge) {

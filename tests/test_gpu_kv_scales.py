@@ -46,3 +46,25 @@ def test_small_scales_of_large_products(H, Hk, codes, scale):
     cache = _times(make_cache(codes, 2, Hk, 150, 128, seed=3), k=55)
     q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** 55).bfloat16()
     _attend(q, cache, starts, lens, scale=scale)
+
+
+@HEADS
+@pytest.mark.parametrize("prefix_len", [0, 130])
+@pytest.mark.parametrize("q_e,scale_e", [(-110, -15), (-20, -105), (0, -125), (-60, -65)])
+def test_keys_of_the_largest_scales(H, Hk, q_e, scale_e, prefix_len):
+    """Scales of K up to 2^120.2, keys up to 2^127.2: the largest that bf16 has too."""
+    starts, lens = batch([3, 1], [140, 20])
+    cache = _times(make_cache(True, 2, Hk, 150, 128, seed=3), k=125)
+    prefix = _times(make_cache(True, 1, Hk, 150, 128, seed=4), k=125) if prefix_len else None
+    assert cache.k_scale.max() > 2.0 ** 120
+    q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** q_e).bfloat16()
+    _attend(q, cache, starts, lens, scale=0.09 * 2.0 ** scale_e, prefix=prefix, prefix_len=prefix_len)
+
+
+@HEADS
+def test_a_scale_of_0_over_the_largest_keys(H, Hk):
+    """Codes never have q . k itself in fp32: 0 times 2^230 is 0."""
+    starts, lens = batch([3, 1], [140, 20])
+    cache = _times(make_cache(True, 2, Hk, 150, 128, seed=3), k=125)
+    q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** 100).bfloat16()
+    _attend(q, cache, starts, lens, scale=0.0)
