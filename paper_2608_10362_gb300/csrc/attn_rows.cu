@@ -95,12 +95,14 @@ struct Smem {
   char* q;
   Sight* sight;     // [VT]
   float* q_scale;   // [VT]
+  int* q_exp;       // [VT]
   char* ring;
   __device__ explicit Smem(char* p) {
     plan = reinterpret_cast<Plan*>(p);
     q = p + sizeof(Plan);
     sight = reinterpret_cast<Sight*>(q + S::kQBytes);
     q_scale = reinterpret_cast<float*>(sight + S::VT);
+    q_exp = reinterpret_cast<int*>(q_scale + S::VT);
     ring = q + S::kQBytes + S::VT * 16;
   }
 };
@@ -142,6 +144,14 @@ __device__ __forceinline__ void fill(const KvView& kv, const char* k, const char
     const bool on = s_key < end;
     cp_async4(stage + 32 * S::kRowBytes + lane * 4, (lane < 16 ? ks : vs) + (on ? s_key * kv.s_pos : 0), on);
   }
+}
+
+// scale * 2^e * k_s where scale * 2^e, which a vector is held with, is not a normal number: the product may be one.
+__device__ __noinline__ float far_factor(float scale, int e, float k_s) {
+  int scale_e;
+  const float fraction = frexpf(scale, &scale_e);
+  const float by = ldexpf(fraction * (k_s * 0x1p-32f), scale_e + e + 32);
+  return isinf(by) && k_s <= FLT_MAX ? copysignf(FLT_MAX, by) : by;   // (it meets products of 0)
 }
 
 template <class S>
@@ -206,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
           const int hd = q_c * 8 + j * 2, to = hd / 64 * 64 + hd % 16 / 4 * 16 + hd % 64 / 16 * 2 + hd % 4 / 2 * 8;
           *reinterpret_cast<uint32_t*>(sm.q + q_vec * HD * 2 + (to / 8 ^ (q_vec & 7)) * 16 + to % 8 * 2) = scaled_f16(w[j], up);
         }
-        if (q_c == 0) sm.q_scale[q_vec] = a.scale * power(e);
+        if (q_c == 0) sm.q_scale[q_vec] = a.scale * power(e), sm.q_exp[q_vec] = e;
       }
     }
     __syncthreads();
@@ -215,6 +225,14 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 2; ++i) scale[nt][i] = CODES ? sm.q_scale[nt * 8 + 2 * t + i] : a.scale;
+    bool far = false;
+    if (CODES && a.scale != 0.f) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) far |= !(fabsf(scale[nt][i]) >= FLT_MIN && fabsf(scale[nt][i]) <= FLT_MAX);
+      far = __any_sync(~0u, far);
+    }
     uint32_t qf[NT][KS][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -290,8 +308,13 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
           if (isnan(rv[i])) rv[i] = 0.f;   // the weight is a NaN already where it counts
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            z[nt][2 * i] = fmaf(z[nt][2 * i], k_s * scale[nt][0], lv);
-            z[nt][2 * i + 1] = fmaf(z[nt][2 * i + 1], k_s * scale[nt][1], lv);
+            float by[2] = {k_s * scale[nt][0], k_s * scale[nt][1]};
+            if (far) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j) by[j] = far_factor(a.scale, sm.q_exp[nt * 8 + 2 * t + j], k_s);
+            }
+            z[nt][2 * i] = fmaf(z[nt][2 * i], by[0], lv);
+            z[nt][2 * i + 1] = fmaf(z[nt][2 * i + 1], by[1], lv);
           }
         }
       } else {

@@ -68,3 +68,18 @@ def test_a_scale_of_0_over_the_largest_keys(H, Hk):
     cache = _times(make_cache(True, 2, Hk, 150, 128, seed=3), k=125)
     q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** 100).bfloat16()
     _attend(q, cache, starts, lens, scale=0.0)
+
+
+@HEADS
+def test_the_largest_scale_over_keys_of_zeros(H, Hk):
+    """2e38 q . 0 is 0, however large q is, and whatever the scale of a code of 0 is."""
+    starts, lens = batch([3, 1], [140, 20])
+    q = (torch.randn(4, H, 128, device=DEV, generator=_gen(8)) * 2.0 ** 20).bfloat16()
+    for codes in (False, True):
+        cache = make_cache(codes, 2, Hk, 150, 128, seed=3)
+        cache.k.zero_()
+        _attend(q, cache, starts, lens, scale=2e38)
+        _attend(q, cache, starts, lens, scale=-2e38)
+        if codes:
+            cache.k_scale.fill_(2.0 ** -64)
+            _attend(q, cache, starts, lens, scale=2e38)
