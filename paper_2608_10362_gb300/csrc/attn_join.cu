@@ -180,9 +180,12 @@ __global__ void __launch_bounds__(kThreads) join_tiles_kernel(const __grid_const
       sum[2] = fmaf(x.z, by, sum[2] * was), sum[3] = fmaf(x.w, by, sum[3] * was);
     }
   }
-  const float by = den == 0.f ? 0.f : 1.f / den;
+  // weights of codes carry V's scale, so that their sum is down to 2^-129: its reciprocal may be past fp32, the result is not
+  const float lift = den < 0x1p-60f ? 0x1p30f : 1.f, by = den == 0.f ? 0.f : 1.f / (den * lift);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum[e] = sum[e] * lift * by;
   *reinterpret_cast<uint2*>(a.out + row * a.ldo + h * HD + chunk * 4) =
-      make_uint2(pack_bf16(sum[0] * by, sum[1] * by), pack_bf16(sum[2] * by, sum[3] * by));
+      make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
 }
 
 // ---------------------------------------------------------------- host

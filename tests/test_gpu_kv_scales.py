@@ -15,7 +15,9 @@ HEADS = pytest.mark.parametrize("H,Hk", [(4, 4), (32, 4)], ids=["few", "many"])
 def _times(cache, k=0, v=0):
     """The cache with its keys and values (of codes: their scales) times powers of two."""
     for i, e in ((0, k), (1, v)):
-        (cache.tensors[2 + i] if cache.codes else cache.tensors[i]).mul_(2.0 ** e)
+        t = cache.tensors[2 + i] if cache.codes else cache.tensors[i]
+        t.mul_(2.0 ** (e // 2)).mul_(2.0 ** (e - e // 2))      # (2^e itself may be past fp32)
+        assert torch.isfinite(t).all()
     return cache
 
 
@@ -83,3 +85,18 @@ def test_the_largest_scale_over_keys_of_zeros(H, Hk):
         if codes:
             cache.k_scale.fill_(2.0 ** -64)
             _attend(q, cache, starts, lens, scale=2e38)
+
+
+@HEADS
+@pytest.mark.parametrize("prefix_len", [0, 130])
+@pytest.mark.parametrize("v_e,most", [(124, 127), (125, 127), (129, 2), (131, 1), (-58, 127)])
+def test_values_of_the_largest_scales(H, Hk, v_e, most, prefix_len):
+    """Scales of V up to 2^126.2 with codes that keep the values finite, and down to the smallest scale."""
+    starts, lens = batch([3, 1], [140, 0])     # (the second row sees one key: its sum of weights is the least)
+    cache = _times(make_cache(True, 2, Hk, 150, 128, seed=3), v=v_e)
+    prefix = _times(make_cache(True, 1, Hk, 150, 128, seed=4), v=v_e) if prefix_len else None
+    for c in (cache, prefix):
+        if c is not None:
+            c.v.clamp_(-most, most)
+    q = torch.randn(4, H, 128, device=DEV, generator=_gen(8)).bfloat16()
+    _attend(q, cache, starts, lens, prefix=prefix, prefix_len=prefix_len)
