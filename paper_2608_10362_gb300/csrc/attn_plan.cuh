@@ -18,10 +18,14 @@ namespace memspec {
 
 constexpr int kTile = 128;             // keys
 constexpr float kStart = -FLT_MAX;     // the maximum of nothing
-// Scores are kept in units of log2.  The maximum that weights are taken against is set kBelow under
-// the largest score, which keeps fp16 weights clear of the type's small end, and again only when
-// a score passes it by more than kAbove (fp16 holds 2^15), so that sums are rarely rescaled.
-constexpr float kAbove = 14.f, kBelow = 6.f;
+// Scores are kept in units of log2.  The maximum that weights are taken against is set kBelow under the largest score,
+// and again only when a score passes it by more than kAbove, so that sums are rarely rescaled.  Codes: weights are fp16,
+// which 2^6 keeps clear of the type's small end (it holds up to 2^15).  bf16: at most 2^-14, so that 2^14 of them
+// times the largest values of bf16 stay within fp32.
+template <bool CODES>
+struct Weights {
+  static constexpr float kAbove = CODES ? 14.f : -14.f, kBelow = CODES ? 6.f : -28.f;
+};
 
 struct ListArgs {
   KvView kv[2];              // the cache, the prefix

@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) above |= fmaxf(z[nt][i], z[nt][2 + i]) - m[nt][i] > kAbove;
+        for (int i = 0; i < 2; ++i) above |= fmaxf(z[nt][i], z[nt][2 + i]) - m[nt][i] > Weights<CODES>::kAbove;
       if (__any_sync(~0u, above)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, S::kPerSm) rows_kernel(const __grid_
             float top = fmaxf(z[nt][i], z[nt][2 + i]);
 #pragma unroll
             for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-            const float now = top - m[nt][i] > kAbove ? top - kBelow : m[nt][i], by = ex2(m[nt][i] - now);
+            const float now = top - m[nt][i] > Weights<CODES>::kAbove ? top - Weights<CODES>::kBelow : m[nt][i], by = ex2(m[nt][i] - now);
             m[nt][i] = now;
             l[nt][i] *= by;
 #pragma unroll

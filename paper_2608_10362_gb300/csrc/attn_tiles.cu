@@ -638,9 +638,9 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
           }
           float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           top = fmaf(top, by, plus);
-          const bool above = live && top - m > kAbove;   // (rows without a vector have anything)
+          const bool above = live && top - m > Weights<CODES>::kAbove;   // (rows without a vector have anything)
           if (__any_sync(~0u, above)) {
-            const float now = above ? top - kBelow : m, less = ex2(m - now);
+            const float now = above ? top - Weights<CODES>::kBelow : m, less = ex2(m - now);
             m = now;
             l *= less;
             huge = __any_sync(~0u, live && fabsf(m) > 0x1p20f && m != kStart);

@@ -100,3 +100,15 @@ def test_values_of_the_largest_scales(H, Hk, v_e, most, prefix_len):
             c.v.clamp_(-most, most)
     q = torch.randn(4, H, 128, device=DEV, generator=_gen(8)).bfloat16()
     _attend(q, cache, starts, lens, prefix=prefix, prefix_len=prefix_len)
+
+
+@HEADS
+@pytest.mark.parametrize("prefix_len", [0, 130])
+def test_values_at_the_end_of_bf16(H, Hk, prefix_len):
+    """A weighted mean of values up to 2^126 is no larger than they are."""
+    starts, lens = batch([3, 1], [140, 20])
+    cache = _times(make_cache(False, 2, Hk, 150, 128, seed=3), v=123)
+    prefix = _times(make_cache(False, 1, Hk, 150, 128, seed=4), v=123) if prefix_len else None
+    cache.v.clamp_(-2.0 ** 126, 2.0 ** 126)
+    q = (3 * torch.randn(4, H, 128, device=DEV, generator=_gen(8))).bfloat16()
+    _attend(q, cache, starts, lens, prefix=prefix, prefix_len=prefix_len)
