@@ -213,7 +213,8 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
         lo = load4(reinterpret_cast<const bf16*>(p) + e, true);
         hi = load4(reinterpret_cast<const bf16*>(p) + e + HD / 2, true);
       } else {
-        const float s = (is_k ? a.kv.k_scale : a.kv.v_scale)[at.seq * a.kv.s_seq + h * a.kv.s_head + slot * a.kv.s_pos];
+        float s = (is_k ? a.kv.k_scale : a.kv.v_scale)[at.seq * a.kv.s_seq + h * a.kv.s_head + slot * a.kv.s_pos];
+        if (s < kSmallestScale) s = kSmallestScale;   // a NaN stays
         const char4 l = *reinterpret_cast<const char4*>(p + e), u = *reinterpret_cast<const char4*>(p + e + HD / 2);
         auto value = [s](const char4& v) {
           return make_float4(s * static_cast<signed char>(v.x), s * static_cast<signed char>(v.y),

@@ -112,3 +112,20 @@ def test_values_at_the_end_of_bf16(H, Hk, prefix_len):
     cache.v.clamp_(-2.0 ** 126, 2.0 ** 126)
     q = (3 * torch.randn(4, H, 128, device=DEV, generator=_gen(8))).bfloat16()
     _attend(q, cache, starts, lens, prefix=prefix, prefix_len=prefix_len)
+
+
+def test_read_counts_small_scales_as_attention_does():
+    """A scale below 2^-64 counts as 2^-64, as the header has it."""
+    pkg = _pkg()
+    cache = make_cache(True, 1, 2, 8, 64, seed=3)
+    cache.k_scale[:] = torch.tensor([0.0, 2.0 ** -70, 2.0 ** -64, 2.0 ** -63, -1.0, 1e-40, 0.5, math.nan], device=DEV)
+    cache.v_scale[:] = cache.k_scale.flip(2)
+    k, v = pkg.op_kv_read(cache, _i32(0, 8), _i32(8), 8)
+    for got, codes, scale in ((k, cache.k, cache.k_scale), (v, cache.v, cache.v_scale)):
+        s = torch.where(scale < 2.0 ** -64, torch.tensor(2.0 ** -64, device=DEV), scale)
+        want = (codes.float() * s[..., None]).bfloat16()[0].transpose(0, 1)      # a product of 8 and 24 bits, rounded ...
+        exact = (codes.double() * s.double()[..., None])[0].transpose(0, 1)
+        ok = torch.isfinite(exact)
+        assert ((got.double() - exact).abs()[ok] <= (2.0 ** -8 + 2.0 ** -24) * exact.abs()[ok]).all()   # ... to fp32, then bf16
+        assert torch.equal(got[torch.isfinite(want)], want[torch.isfinite(want)])
+        assert torch.isnan(got[~ok]).all()
