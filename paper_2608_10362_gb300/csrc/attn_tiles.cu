@@ -28,8 +28,8 @@
 // the join (the same rows over 8192 positions 24 us, of which 6.5 are tiles).
 //
 // Roles (warps): 0-3, 4-7 softmax; copies, 4, or 8 of codes; two with the MMAs of a warpgroup each;
-// one for Q; one for which units these are.  Every wait is bounded; after one that ran out the CTA's records
-// are NaN or not written.
+// one for Q; one for which units these are.  Every wait is bounded, those of a role's warps for one another too (see
+// Stretches); after one that ran out the CTA's records are NaN or not written.
 #include <algorithm>
 #include <atomic>
 
@@ -43,7 +43,7 @@ namespace {
 constexpr int kSoft = 256;              // threads of the softmax
 constexpr int kSlots = 4;               // tiles in shared memory: K of two, V of two
 constexpr int kRefs = 4;                // a tile's references are read until its P is written
-constexpr int kListed = 4;              // stretches told of at a time
+constexpr int kListed = 8;              // stretches told of (as many again as are read behind one another at most)
 constexpr int kStep = 64;               // keys of a warpgroup's step
 // What a scale of 0 counts as: it meets -inf where a vector does not see a key, which 0 would make a NaN.  fp32's largest
 // times it is 2^-21.
@@ -207,9 +207,9 @@ __device__ __forceinline__ bool wait_bounded(uint64_t* bar, uint32_t parity, vol
   const long long t0 = clock64();
 #pragma unroll 1
   while (!attempt()) {
-    if (*abort_flag) return false;
+    if (abort_flag != nullptr && *abort_flag) return false;
     if (clock64() - t0 > budget) {
-      *abort_flag = 1;
+      if (abort_flag != nullptr) *abort_flag = 1;
       return false;
     }
   }
@@ -236,16 +236,20 @@ __device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, i
 __device__ __forceinline__ int chunk_at(int r, int c) { return (c >> 3) * (128 * 128) + r * 128 + (((c ^ r) & 7) << 4); }
 
 // The stretches of a CTA, as the roles go through them: one lane works them out (walk_role), and is
-// never so far ahead that an entry is written again before all have read it.
+// never so far ahead that an entry is written again before all have read it.  All warps see the same ones: once a wait
+// has run out that lane makes the next one the last.  So the warps of a role pass the same barriers whatever
+// becomes of their waits: after one that ran out a warp goes on to the end of what is listed.  (Leaving at each barrier by one decision: 16 x 9 rows over codes 38.9 us, at each stretch 38.0.)
 struct Stretches {
   Ctl& ctl;
   int at = 0;
   __device__ explicit Stretches(Ctl& c) : ctl(c) {}
   __device__ __forceinline__ bool next(Stretch& u) {
     const int i = at % kListed;
-    if (!__all_sync(~0u, wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, &ctl.abort_flag,
-                                       kStretchBudgetCycles)))
+    // (not given up for abort_flag: walk_role looks at that, and lists an end)
+    if (!__all_sync(~0u, wait_bounded(&ctl.listed[i], static_cast<uint32_t>(at / kListed) & 1u, nullptr, 2 * kStretchBudgetCycles))) {
+      ctl.abort_flag = 1;
       return false;
+    }
     u = ctl.list[i];
     ++at;
     return u.t0 < u.t1;
@@ -258,11 +262,11 @@ __device__ __forceinline__ void walk_role(const ListArgs& a, Ctl& ctl) {
 #pragma unroll 1
   for (int i = 0; more; ++i) {
     more = walk.next(u);
-    if (!more) u.t0 = u.t1 = 0;
     // the last S of the stretch before last is complete: so are the roles' steps of the one two before that
     if (i >= 2 &&
         !wait_bounded(&ctl.q_free[i & 1], static_cast<uint32_t>(i - 2 >> 1) & 1u, &ctl.abort_flag, kStretchBudgetCycles))
-      return;
+      more = false;
+    if (!more) u.t0 = u.t1 = 0;
     ctl.list[i % kListed] = u;
     mbar_arrive(&ctl.listed[i % kListed]);
   }
@@ -321,6 +325,7 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
   constexpr int kCopy = S::kCopy;
   const int tid = threadIdx.x % kCopy;
   Stretches walk(ctl);
+  bool ok = true;
   int tile = 0;
   uint32_t raws = 0;
   Stretch u;
@@ -330,7 +335,7 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
     for (int t = u.t0; t < u.t1; ++t, ++tile) {
       if (!is_edge(u, t)) continue;
       const int s = slot_of(tile, 1), i = s & 1, key0 = t * kTile;
-      if (!__all_sync(~0u, wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag, kStretchBudgetCycles))) return;
+      ok = ok && __all_sync(~0u, wait_bounded(&ctl.raw[i], raws >> i & 1u, &ctl.abort_flag, kStretchBudgetCycles));
       raws ^= 1u << i;
       if (tid < kTile / 32) ctl.bad[i][tid] = 0u;
       named_bar_sync(2, kCopy);
@@ -361,7 +366,7 @@ __device__ __forceinline__ void edge_role(Ctl& ctl, uint8_t* ring) {
       }
       fence_proxy_async_smem();
       named_bar_sync(2, kCopy);
-      if (tid == 0) mbar_arrive(&ctl.full[s]);
+      if (ok && tid == 0) mbar_arrive(&ctl.full[s]);
     }
   }
 }
@@ -430,9 +435,9 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
 #pragma unroll
       for (int i = 0; i < kCopy / 32; ++i) top.x = fmaxf(top.x, sm.top[buf][i].x), top.y = fmaxf(top.y, sm.top[buf][i].y);
       const int ref_v = reference(top.x), ref_k = reference(top.y);
-      if (use_of(tile) > 0 &&
-          !__all_sync(~0u, wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, &ctl.abort_flag)))
-        return;
+      // (where it runs out the tile is written and told of all the same: four arrivals a tile, whose barrier keeps them apart)
+      if (use_of(tile) > 0) wait_bounded(&ctl.empty[s], static_cast<uint32_t>(use_of(tile) - 1) & 1u, &ctl.abort_flag);
+      __syncwarp();
       // V of a key whose scale is not finite: 0 where some vector does not see it, those that do are told
       if (is_v) {
         const uint32_t bad = __ballot_sync(~0u, !(sc[0] <= FLT_MAX));
@@ -483,9 +488,10 @@ __device__ __forceinline__ void codes_role(const ListArgs& a, Ctl& ctl, int is_v
 
 // ---------------------------------------------------------------- query vectors
 // A stretch's vectors into shared memory by THREADS threads (`tid` of them; sync: their barrier), K-major; a
-// negative scale turns their signs.  Codes: to fp16.
+// negative scale turns their signs.  Codes: to fp16.  ok: no wait of the warp has run out.
 template <class S, int THREADS, class Sync>
-__device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretch& u, int stretch, int tid, uint8_t* q_smem, Sync sync) {
+__device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretch& u, int stretch, int tid, uint8_t* q_smem, bool ok,
+                                       Sync sync) {
   constexpr int HD = S::HD, C = HD / 8;
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   const int vec0 = u.unit * kTilesUnit, chunks = min(u.vecs - vec0, kTilesUnit) * C;
@@ -522,7 +528,7 @@ __device__ __forceinline__ void load_q(const ListArgs& a, Ctl& ctl, const Stretc
   }
   fence_proxy_async_smem();
   sync();
-  if (tid == 0) mbar_arrive(&ctl.q_full);
+  if (ok && tid == 0) mbar_arrive(&ctl.q_full);
 }
 
 // The smaller units' vectors, ahead of their stretch.  Those of a pair are many, and the first stretch's are waited
@@ -540,7 +546,7 @@ __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_s
         !__all_sync(~0u, wait_bounded(&ctl.q_free[(stretch - 1) & 1], static_cast<uint32_t>(stretch - 1 >> 1) & 1u, &ctl.abort_flag,
                                       kStretchBudgetCycles)))
       break;
-    load_q<S, 32>(a, ctl, u, stretch, threadIdx.x % 32, q_smem, [] { __syncwarp(); });
+    load_q<S, 32>(a, ctl, u, stretch, threadIdx.x % 32, q_smem, true, [] { __syncwarp(); });
   }
 }
 
@@ -578,7 +584,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
     bool huge = false;   // some m of the warp's
     if (softmax_loads(u, stretch)) {
       named_bar_sync(1, kSoft);   // both warpgroups have seen the last S of the stretch before: Q is free
-      load_q<S, kSoft>(a, ctl, u, stretch, threadIdx.x, q_smem, [] { named_bar_sync(1, kSoft); });
+      load_q<S, kSoft>(a, ctl, u, stretch, threadIdx.x, q_smem, ok, [] { named_bar_sync(1, kSoft); });
     }
 #pragma unroll 1
     for (int t = u.t0; ok && t < u.t1; ++t)
