@@ -313,7 +313,9 @@ memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, co
  * and head unspecified.  out overlaps no other argument.
  * A sequence of more than max_rows rows gives the same, at another speed.
  * Deterministic.  scratch_dev: 16-byte aligned, any content; calls that may overlap
- * need scratches of their own.  Allocates nothing.  Errors: INVALID_ARG, CUDA. */
+ * need scratches of their own.  Every wait on the device is bounded (a second or
+ * more; none takes so long): should one run out, the rows it concerns are NaN.
+ * Allocates nothing.  Errors: INVALID_ARG, CUDA. */
 memspec_status memspec_op_attention(const memspec_batch* batch, const memspec_kv* kv,
                                     const memspec_attention* args, void* scratch_dev, size_t scratch_bytes,
                                     void* stream);

@@ -29,7 +29,7 @@
 //
 // Roles (warps): 0-3, 4-7 softmax; copies, 4, or 8 of codes; two with the MMAs of a warpgroup each;
 // one for Q; one for which units these are.  Every wait is bounded, those of a role's warps for one another too (see
-// Stretches); after one that ran out the CTA's records are NaN or not written.
+// Stretches); after one that ran out the records of all the CTA's vectors are NaN, and so their results.
 #include <algorithm>
 #include <atomic>
 
@@ -238,7 +238,8 @@ __device__ __forceinline__ int chunk_at(int r, int c) { return (c >> 3) * (128 *
 // The stretches of a CTA, as the roles go through them: one lane works them out (walk_role), and is
 // never so far ahead that an entry is written again before all have read it.  All warps see the same ones: once a wait
 // has run out that lane makes the next one the last.  So the warps of a role pass the same barriers whatever
-// becomes of their waits: after one that ran out a warp goes on to the end of what is listed.  (Leaving at each barrier by one decision: 16 x 9 rows over codes 38.9 us, at each stretch 38.0.)
+// becomes of their waits: after one that ran out a warp goes on to the end of what is listed.  (That its results are lost is
+// seen to at the end.  Leaving at each barrier by one decision: 16 x 9 rows over codes 38.9 us, at each stretch 38.0.)
 struct Stretches {
   Ctl& ctl;
   int at = 0;
@@ -550,6 +551,39 @@ __device__ __forceinline__ void q_role(const ListArgs& a, Ctl& ctl, uint8_t* q_s
   }
 }
 
+// ---------------------------------------------------------------- records
+// Of vector v of a unit, copy c of it.  Records lie side by side, [HD / 4][records][4]: a warp's stores are whole lines.
+struct Record {
+  float* sums;        // 4 of its sums
+  long long chunk;    // floats to the next 4
+  float2* md;
+};
+template <int HD>
+__device__ __forceinline__ Record record_of(const ListArgs& a, const Stretch& u, bool pair, int v, int c) {
+  const int heads = a.group * a.kv_heads, vec = u.unit * kTilesUnit + v, vr = vector_row(a, vec);
+  const long long all = static_cast<long long>(a.rows) * heads;
+  const long long at = static_cast<long long>(u.row0 + vr) * heads + u.head * a.group + vec - vr * a.group;
+  const bool whole = u.whole();
+  const long long n = whole ? 2 * all : kTilesUnit, i = whole ? at + c * all : c * 128 + v;
+  float* rec = whole ? a.full[u.own ? 0 : 1]
+                     : a.slots + (2 * static_cast<long long>(blockIdx.x) + (u.t0 == 0)) * kTilesUnit * kRecord<HD>;
+  return {rec + 4 * i, 4 * n, reinterpret_cast<float2*>(rec + HD * n + 2 * i)};
+}
+// After a wait that ran out: whatever was written, the CTA's vectors are NaN (all threads).
+template <int HD>
+__device__ __noinline__ void lose_records(const ListArgs& a, const Plan& plan) {
+  Walk<Units> walk(a, plan);
+  Stretch u;
+#pragma unroll 1
+  while (walk.next(u)) {
+    const bool pair = is_pair(u);
+    const int vecs = min(u.vecs - u.unit * kTilesUnit, kTilesUnit);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < vecs * (pair ? 1 : 2); i += blockDim.x)
+      *record_of<HD>(a, u, pair, i % vecs, i / vecs).md = make_float2(kStart, NAN);
+  }
+}
+
 // ---------------------------------------------------------------- softmax
 template <class S>
 __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* q_smem, uint32_t tmem) {
@@ -710,20 +744,12 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
       }
     // ---- the record
     wait(&ctl.o_full[w][(done - 1) & 1], (done - 1) >> 1);
-    if (!ok) m = kStart, l = NAN;
     tc_fence_after();
-    if (warp_live) {
-      const int heads = a.group * a.kv_heads, vr = vector_row(a, vec);
-      const long long at = static_cast<long long>(u.row0 + vr) * heads + u.head * a.group + vec - vr * a.group;
-      // a pair's warpgroups have different vectors, others the same: two records of each.  Records lie side by
-      // side, [HD / 4][records][4]: a warp's stores are whole lines
-      const bool whole = u.whole();
-      const long long all = static_cast<long long>(a.rows) * heads;
-      const long long n = whole ? 2 * all : kTilesUnit, i = whole ? at + (pair ? 0 : w) * all : w * 128 + row;
-      float* rec = whole ? a.full[u.own ? 0 : 1] : a.slots + (2 * static_cast<long long>(blockIdx.x) + (u.t0 == 0)) *
-                                                                kTilesUnit * kRecord<HD>;
-      if (live) *reinterpret_cast<float2*>(rec + HD * n + 2 * i) = make_float2(m, l);
-      rec += 4 * i;
+    if (ok && warp_live) {
+      // a pair's warpgroups have different vectors, others the same: two records of each
+      const Record to = record_of<HD>(a, u, pair, vec - u.unit * kTilesUnit, pair ? 0 : w);
+      if (live) *to.md = make_float2(m, l);
+      float* rec = to.sums;
 #pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
         float o[32];
@@ -732,7 +758,7 @@ __device__ __forceinline__ void soft_role(const ListArgs& a, Ctl& ctl, uint8_t* 
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
             *reinterpret_cast<float4*>(rec) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-            rec += 4 * n;
+            rec += to.chunk;
           }
         }
       }
@@ -886,6 +912,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  if (ctl.abort_flag) lose_records<S::HD>(a, ctl.plan);
 }
 
 template <class S>

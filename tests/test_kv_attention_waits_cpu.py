@@ -1,5 +1,6 @@
 """What cannot be shown on a GPU without hanging it, read off the source: attn_tiles.cu's roles (warps
-that go different ways through a tile) hold no wait that lasts for ever once a wait of another has run out."""
+that go different ways through a tile) hold no wait that lasts for ever once a wait of another has run
+out, and results that were lost by one are told."""
 import os
 import re
 
@@ -41,7 +42,7 @@ def test_warps_that_meet_at_barriers_stay_to_the_end(role):
     assert "named_bar_sync" in body and len(re.findall(r"while \(walk\.next\(u\)\)", body)) == 1
     assert not re.search(r"\breturn;", body)
     if role == "soft_role":
-        tiles = body[body.index("ok && t < u.t1"):body.index("if (!ok) m = kStart")]
+        tiles = body[body.index("ok && t < u.t1"):body.index("const Record to")]
         assert "named_bar_sync" not in tiles and body.count("break;") == tiles.count("break;")
         # what tells a stretch's loads of Q, and so their barriers, is counted whatever became of the stretch
         assert re.search(r"tiles \+= u\.t1 - u\.t0;\s+\+\+stretch;\s+\}\s*$", body)
@@ -58,3 +59,11 @@ def test_the_list_of_stretches_always_ends():
     assert re.search(r"wait_bounded\(&ctl\.q_free.*?\)\s+more = false;", loop, re.S)
     assert loop.index("more = false") < loop.index("if (!more) u.t0 = u.t1 = 0;") < loop.index("mbar_arrive(&ctl.listed")
     assert re.search(r"wait_bounded\(&ctl\.listed\[i\],[^;]*nullptr", _body("next"))
+
+
+def test_a_wait_that_ran_out_is_seen_in_the_result():
+    """Records that were not written would be an earlier call's: after the roles they are all made NaN."""
+    kernel = _body("tiles_kernel")
+    end = kernel[kernel.index("__syncthreads"):]
+    assert kernel.index("walk_role(") < kernel.index("__syncthreads") and "if (ctl.abort_flag) lose_records" in end
+    assert "make_float2(kStart, NAN)" in _body("lose_records")
