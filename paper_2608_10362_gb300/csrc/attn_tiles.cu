@@ -313,9 +313,8 @@ __device__ __forceinline__ void tma_role(const ListArgs& a, const TileMaps& maps
       __syncwarp();
     }
   }
-  if (!ok)   // no copy is in flight when the CTA leaves
-    for (int i = 0; i < 2; ++i)
-      if (last[i] != nullptr) mbar_wait_drain(last[i], phase[i]);
+  for (int i = 0; i < 2; ++i)   // no copy is in flight when the CTA leaves, whoever gave up
+    if (last[i] != nullptr) mbar_wait_drain(last[i], phase[i]);
 }
 
 // bf16: the edge tiles of V, by kCopy threads: zeros where the keys have ended (a weight of 0 times

@@ -67,3 +67,9 @@ def test_a_wait_that_ran_out_is_seen_in_the_result():
     end = kernel[kernel.index("__syncthreads"):]
     assert kernel.index("walk_role(") < kernel.index("__syncthreads") and "if (ctl.abort_flag) lose_records" in end
     assert "make_float2(kStart, NAN)" in _body("lose_records")
+
+
+def test_copies_under_way_are_waited_for_however_a_role_ends():
+    role = _body("tma_role")
+    drain = role[role.rindex("\n  }\n"):]
+    assert "mbar_wait_drain" in drain and "ok" not in drain
