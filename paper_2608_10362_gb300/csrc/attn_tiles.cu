@@ -904,7 +904,6 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     if (blockIdx.x == 0)
       for (int b = threadIdx.x % 32; b <= list_len(a); b += 32) a.bases[b] = ctl.plan.bases[b];
   }
-  if (a.beside) pdl_wait();   // the launch after this one waits for both
   tc_fence_before();
   __syncthreads();
   if (warp == kMma) {
@@ -912,6 +911,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     tmem_dealloc(tmem, 512);
   }
   if (ctl.abort_flag) lose_records<S::HD>(a, ctl.plan);
+  // The launch after this one waits for both.  (By now the tensor memory is free: a CTA of the launch before this one may
+  // still be waiting for it.)
+  if (a.beside) pdl_wait();
 }
 
 template <class S>

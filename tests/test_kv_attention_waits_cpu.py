@@ -73,3 +73,10 @@ def test_copies_under_way_are_waited_for_however_a_role_ends():
     role = _body("tma_role")
     drain = role[role.rindex("\n  }\n"):]
     assert "mbar_wait_drain" in drain and "ok" not in drain
+
+
+def test_tensor_memory_is_free_before_a_launch_waits_for_another():
+    """A CTA of a launch beside another would hold all of it while it waits for CTAs that may still be asking for it."""
+    kernel = _body("tiles_kernel")
+    assert 0 < kernel.index("tmem_dealloc(") < kernel.index("if (a.beside) pdl_wait();")
+    assert kernel.count("pdl_wait()") == 2 and "if (!a.beside) pdl_wait();" in kernel
