@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmemspec.so")
 SOURCES = ["gemm.cu", "gemm_pair.cu", "gemm_finish.cu", "gemm_small.cu", "attention.cu", "attn_tc.cu", "embed.cu", "sampling.cu", "api.cu", "noalloc.cu", "pass.cu", "pack.cu", "tree.cu",
-           "draft_fused.cu", "sched.cpp", "int4.cu", "filter.cu", "lora.cu", "kv_append.cu", "attn_rows.cu", "attn_tiles.cu", "attn_join.cu"]
+           "draft_fused.cu", "sched.cpp", "int4.cu", "filter.cu", "lora.cu", "kv_append.cu", "attn_rows.cu", "attn_tiles.cu", "attn_join.cu", "cache_map.cu"]
 HEADERS = ["ptx.cuh", "internal.h", "gemm_epi.cuh", "attn_body.cuh", "sample_body.cuh", "embed_body.cuh", "pass.h",
            "first_use.h", "expfix.cuh", "kv.cuh", "attn_plan.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

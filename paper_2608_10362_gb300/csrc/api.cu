@@ -97,22 +97,6 @@ bool encode_kv(CUtensorMap* map, const void* base, long long rows, int hd) {
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A bf16 cache of any strides (bytes; 0: one place), in boxes of 128 positions by all of hd, as encode_kv's.
-bool encode_cache_impl(CUtensorMap* map, const void* base, int hd, int positions, int heads, int seqs, long long pos,
-                       long long head, long long seq) {
-  EncodeTiledFn fn = get_encode_fn();
-  if (fn == nullptr) return false;
-  auto dim = [](int n, long long stride) { return static_cast<cuuint64_t>(stride == 0 ? 1 : n); };
-  auto bytes = [](long long stride) { return static_cast<cuuint64_t>(stride == 0 ? 128 : stride); };
-  cuuint64_t dims[5] = {64, dim(positions, pos), static_cast<cuuint64_t>(hd / 64), dim(heads, head), dim(seqs, seq)};
-  cuuint64_t strides[4] = {bytes(pos), 128, bytes(head), bytes(seq)};
-  cuuint32_t box[5] = {64, 128, static_cast<cuuint32_t>(hd / 64), 1, 1};
-  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // Packed tiles (16 KB each, contiguous) as rows of 256 bf16, box {256, 32}: one tile
 // per box, copied as stored.
 bool encode_packed(CUtensorMap* map, const void* base, long long tiles) {
@@ -2370,10 +2354,6 @@ const char* memspec_op_last_error(void) { return g_op_error.c_str(); }
 }  // extern "C"
 
 void memspec::set_op_error(const char* msg) { g_op_error = msg; }
-bool memspec::encode_cache(CUtensorMap* map, const void* base, int hd, int positions, int heads, int seqs, long long pos,
-                           long long head, long long seq) {
-  return encode_cache_impl(map, base, hd, positions, heads, seqs, pos, head, seq);
-}
 
 extern "C" {
 

@@ -418,10 +418,6 @@ __device__ __forceinline__ void store_split_bf16(bf16* hi_p, bf16* lo_p, float x
 void set_op_error(const char* msg);
 inline void set_op_error(const std::string& msg) { set_op_error(msg.c_str()); }
 
-// Tensor map of a bf16 cache of a caller's strides (api.cu).
-bool encode_cache(CUtensorMap* map, const void* base, int hd, int positions, int heads, int seqs, long long pos,
-                  long long head, long long seq);
-
 // Philox4x32-10 (Salmon et al., SC'11), device side.
 __host__ __device__ inline uint32_t philox_u01_bits(uint32_t c0, uint32_t c1, uint32_t c2,
                                                     uint32_t c3, uint32_t k0, uint32_t k1) {

@@ -2,6 +2,7 @@
 // layer's keys and values as the caller laid them out, which rows of a call belong to which
 // sequence, and their checks.
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -54,5 +55,10 @@ __device__ __forceinline__ int find_sequence(const int* starts, const int* lens,
 const char* kv_problem(const memspec_kv* kv, bool write);
 KvView kv_view(const memspec_kv* kv);
 const char* batch_problem(const memspec_batch* b, const memspec_kv* kv);
+
+// Tensor map of a bf16 cache of a caller's strides (bytes; 0: one place), in boxes of 128 positions by all of hd: 64 column
+// halves one after the other, each with the 128-byte swizzle (cache_map.cu).
+bool encode_cache(CUtensorMap* map, const void* base, int hd, int positions, int heads, int seqs, long long pos,
+                  long long head, long long seq);
 
 }  // namespace memspec
