@@ -86,7 +86,7 @@ def op_rope_table(positions: int, head_dim: int, base: float = 10000.0, device="
 
 
 def _batch(starts: torch.Tensor, lens: torch.Tensor, cache: KVCache, rows: int) -> _lib.Batch:
-    if type(cache) is not KVCache:
+    if not isinstance(cache, KVCache):
         raise ValueError("cache must be a KVCache")
     n, dev = lens.numel(), cache.dev
     if not (starts.numel() == n + 1 and starts.dtype is _I32 and lens.dtype is _I32 and starts.get_device() == dev
