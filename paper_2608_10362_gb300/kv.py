@@ -88,10 +88,10 @@ def op_rope_table(positions: int, head_dim: int, base: float = 10000.0, device="
 def _batch(starts: torch.Tensor, lens: torch.Tensor, cache: KVCache, rows: int) -> _lib.Batch:
     if not isinstance(cache, KVCache):
         raise ValueError("cache must be a KVCache")
-    n, dev = lens.numel(), cache.dev
-    if not (starts.numel() == n + 1 and starts.dtype is _I32 and lens.dtype is _I32 and starts.get_device() == dev
-            and lens.get_device() == dev and starts.dim() == 1 and lens.dim() == 1 and starts.is_contiguous()
-            and lens.is_contiguous() and 0 < n <= cache.n_seq and 0 < rows < 1 << 31):
+    n, dev = lens.numel() if isinstance(lens, torch.Tensor) else 0, cache.dev
+    if not (isinstance(starts, torch.Tensor) and 0 < n <= cache.n_seq and starts.numel() == n + 1 and starts.dtype is _I32
+            and lens.dtype is _I32 and starts.get_device() == dev and lens.get_device() == dev and starts.dim() == 1
+            and lens.dim() == 1 and starts.is_contiguous() and lens.is_contiguous() and 0 < rows < 1 << 31):
         _cuda_arg("lens", lens, _I32, (n,), cache.k)
         _cuda_arg("starts", starts, _I32, (n + 1,), cache.k)
         raise ValueError(f"{n} sequences of {rows} rows for a cache of {cache.n_seq}")
@@ -122,7 +122,7 @@ def op_kv_append(qkv: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: 
         raise ValueError(f"qkv must have {n_heads} + 2 * {cache.n_heads} heads of {hd}, not {qkv.shape[1]} columns")
     positions = 0
     if rope is not None:
-        positions = rope.shape[1] if rope.dim() == 3 else 0
+        positions = rope.shape[1] if isinstance(rope, torch.Tensor) and rope.dim() == 3 else 0
         if not (0 < positions < 1 << 31 and rope.numel() == positions * hd and rope.shape[0] == 2 and rope.dtype is _F32
                 and rope.get_device() == dev and rope.is_contiguous()):
             if not 0 < positions < 1 << 31:
@@ -261,7 +261,7 @@ def op_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: to
         nb = _attention_scratch_bytes(cache.sizes, b.n_seq, rows, n_heads, max_rows,
                                       None if prefix is None else prefix.sizes, prefix_len or 0)
         scratch = _new(stream, torch.empty, nb, dtype=torch.uint8, device=cache.device)
-    elif scratch.get_device() != dev or not scratch.is_contiguous():
+    elif not isinstance(scratch, torch.Tensor) or scratch.get_device() != dev or not scratch.is_contiguous():
         raise ValueError(f"scratch must be contiguous on {q.device}")
     if stream is not None:
         _used_on(stream, q, *cache.tensors, starts, lens, tree, *(() if prefix is None else prefix.tensors), out, scratch)

@@ -21,3 +21,26 @@ def test_a_subclass_is_a_cache(calls):  # noqa: F811
     assert kv_module.op_kv_read(cache, s, l, 3)[0].shape == (3, 1, 64)
     with pytest.raises(ValueError, match="KVCache"):
         kv_module.op_attention(q, cache.k, s, l)
+
+
+def test_what_is_no_tensor_is_refused(calls):  # noqa: F811
+    """With the wrappers' own error, as an argument of the wrong kind is elsewhere."""
+    cache, q, (s, l) = _cache(False), _t(3, 4, 64, dtype=BF), _rows()
+    x = _t(3, 4 * 64)
+    for bad in ([0, 1, 3], None, 7):
+        for call in (lambda: kv_module.op_attention(q, cache, bad, l), lambda: kv_module.op_attention(q, cache, s, bad),
+                     lambda: kv_module.op_kv_append(x, cache, bad, l, 2), lambda: kv_module.op_kv_append(x, cache, s, bad, 2),
+                     lambda: kv_module.op_kv_read(cache, bad, l, 3), lambda: kv_module.op_kv_read(cache, s, bad, 3)):
+            with pytest.raises(ValueError):
+                call()
+        if bad is not None:
+            for kw in (dict(scratch=bad), dict(tree=bad), dict(out=bad), dict(prefix=bad)):
+                with pytest.raises(ValueError):
+                    kv_module.op_attention(q, cache, s, l, **kw)
+            for kw in (dict(rope=bad), dict(offsets=bad), dict(q_gain=bad, k_gain=bad), dict(q=bad)):
+                with pytest.raises(ValueError):
+                    kv_module.op_kv_append(x, cache, s, l, 2, **kw)
+            with pytest.raises(ValueError):
+                kv_module.op_kv_read(cache, s, l, 3, k=bad)
+            with pytest.raises(ValueError):
+                KVCache(cache.k, bad)
