@@ -149,7 +149,10 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 // of them started 6 us late although SMs were free by then (verify pass of the 1.1B
 // target 0.866 -> 0.821 ms, 7B 2.755 -> 2.715, batched 8B 7.25 -> 7.12).  One launch's
 // time is still enough for the next one's set-up and first copies.  It also means that
-// when a kernel starts, the one before its predecessor has completed.
+// when a kernel starts, the one before its predecessor has completed.  One exception: the
+// second of op_attention's launches that run beside each other (ListArgs::beside) calls it
+// at its start and waits at its end.  The launch after it may start while both run, and
+// before its own wait reads only what was complete when the first one began.
 __device__ __forceinline__ void pdl_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
