@@ -292,8 +292,10 @@ class Engine:
         memory ([requests][kv heads][max_seq][head_dim], bf16), for op_attention and op_kv_read.  What the
         steps write there is ordered on `self.stream`."""
         from .kv import KVCache
+        if draft_id is not None and draft_id not in self.drafts:
+            raise ValueError(f"no draft {draft_id!r} is registered")
         shape, kv = (self.shape, self.kv) if draft_id is None else (self.drafts[draft_id][0], self.drafts[draft_id][2])
-        if not 0 <= layer < shape.n_layers:
+        if not hasattr(layer, "__index__") or not 0 <= layer < shape.n_layers:
             raise ValueError(f"layer must be in 0..{shape.n_layers - 1}, not {layer!r}")
         layers = kv.view(torch.bfloat16).view(shape.n_layers, 2, self.max_batch, shape.n_kv_heads, self.max_seq,
                                               shape.head_dim)

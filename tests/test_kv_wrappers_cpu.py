@@ -44,3 +44,16 @@ def test_what_is_no_tensor_is_refused(calls):  # noqa: F811
                 kv_module.op_kv_read(cache, s, l, 3, k=bad)
             with pytest.raises(ValueError):
                 KVCache(cache.k, bad)
+
+
+def test_the_engines_cache_of_a_draft_that_is_none():
+    """The wrapper's own error again, before anything is looked up."""
+    import types
+
+    from paper_2608_10362_gb300 import Engine
+    engine = Engine.__new__(Engine)
+    engine.ctx, engine.drafts, engine.kv = None, {}, None
+    engine.shape = types.SimpleNamespace(n_layers=2, n_kv_heads=1, head_dim=64)
+    for args in ((0, 3), (0, -1), (2,), (-1,), (0.5,), (None,)):
+        with pytest.raises(ValueError):
+            engine.kv_cache(*args)
