@@ -194,7 +194,7 @@ struct Launch {
   bool tiles, own, prefix, codes;
   int nt;                       // attn_rows.cu: units of 8 nt vectors
   size_t bases, slots;          // in the scratch
-  int ctas() const { return tiles ? kTilesCtas : rows_ctas(codes, nt); }
+  int ctas() const { return tiles ? kTilesCtas : rows_ctas(codes); }
   int unit() const { return tiles ? kTilesUnit : 8 * nt; }
 };
 struct Layout {

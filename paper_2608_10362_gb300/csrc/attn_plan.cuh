@@ -305,8 +305,9 @@ __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Launches (attn_rows.cu, attn_tiles.cu): records in `slots` are [ctas][2] x rows_records or tile_records.
-int rows_ctas(bool codes, int nt);
+// Launches (attn_rows.cu, attn_tiles.cu): `slots` holds two units' records for each CTA, of the unit's 8 nt or 256 vectors
+// (attn_tiles.cu's smaller units: two copies of 128) by HD + 4 floats.
+int rows_ctas(bool codes);
 cudaError_t launch_attn_rows(int hd, bool codes, int nt, const ListArgs& a, cudaLaunchConfig_t cfg);
 constexpr int kTilesCtas = 152;
 cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg);   // InvalidValue: no tensor map

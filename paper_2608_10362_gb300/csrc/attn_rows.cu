@@ -539,7 +539,7 @@ cudaError_t launch_nt(int nt, const ListArgs& a, const cudaLaunchConfig_t& cfg) 
 
 }  // namespace
 
-int rows_ctas(bool codes, int) { return 152 * (codes ? Shape<128, true, 2>::kPerSm : Shape<128, false, 2>::kPerSm); }
+int rows_ctas(bool codes) { return 152 * (codes ? Shape<128, true, 2>::kPerSm : Shape<128, false, 2>::kPerSm); }
 
 cudaError_t launch_attn_rows(int hd, bool codes, int nt, const ListArgs& a, cudaLaunchConfig_t cfg) {
   return hd == 64 ? (codes ? launch_nt<64, true>(nt, a, cfg) : launch_nt<64, false>(nt, a, cfg))
