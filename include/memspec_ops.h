@@ -303,9 +303,9 @@ memspec_status memspec_op_attention_scratch_bytes(const memspec_batch* batch, co
  * once for all of them; it has the cache's heads and head_dim, its own strides and
  * type.  q . k and sums are fp32; the weights enter the product with v in 16 bits
  * (of bf16 caches bf16, of codes fp16), off by half a step of it each, of codes
- * also by 2^-31 of the largest weight times scale.  With more
- * than 16 query vectors (rows times heads of a group) a head of k and v, keys and
- * values of codes count as fp16: off by 2^-10 of themselves, or by 2^-16 of the
+ * also by 2^-31 of the largest weight times scale.  With more than 16 query vectors
+ * a head of k and v (max_rows, of a prefix rows, times heads of a group), keys and
+ * values of codes count as fp16: off by 2^-10 of themselves, or by 2^-15 of the
  * largest scale among their 128 positions.
  * Slots that a row does not see do not reach it, whatever they hold (but for the
  * scales among those 128 positions); an infinity

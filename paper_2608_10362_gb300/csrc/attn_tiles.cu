@@ -15,10 +15,12 @@
 // K and V pass through two slots each in shared memory, K-major and N-major alike [key][hd] with the
 // 128-byte swizzle.  bf16 comes by TMA.  Codes are fetched by warps that write them as fp16, times their scale over
 // a power of two near the tile's largest: a value is off by 2^-10 of itself (its factor and the product are
-// rounded), or by 2^-16 of the largest scale of its tile.  K's power multiplies the tile's scores, V's is added to
+// rounded), or by 2^-15 of the largest scale of its tile (the product and what is taken from it round at fp16's smallest
+// step, 2^-24, by half of it each, of what that scale makes 2^-9).  K's power multiplies the tile's scores, V's is added to
 // them as a logarithm: weights are w' = p * power, against a maximum of their own kind, and the sum of p is that of
-// w' / power; so no range of scales overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu has them, would be three numbers
-// per key for every thread out of shared memory, at 128 bytes a clock 0.7 us of a step.)  A vector of Q is taken to fp16
+// w' / power; so no range of scales overflows fp16.  (Exact codes with a scale per key in the softmax, as attn_rows.cu
+// has them, would be three numbers per key for every thread out of shared memory, at 128 bytes a clock 0.7 us of a
+// step.)  A vector of Q is taken to fp16
 // by a power of two of its own.
 //
 // What bounds it: a tile for 256 vectors takes 1.9 us of bf16, of which the MMAs' part is 1.3 (S in steps of 64 keys

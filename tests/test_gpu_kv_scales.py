@@ -129,3 +129,30 @@ def test_read_counts_small_scales_as_attention_does():
         assert ((got.double() - exact).abs()[ok] <= (2.0 ** -8 + 2.0 ** -24) * exact.abs()[ok]).all()   # ... to fp32, then bf16
         assert torch.equal(got[torch.isfinite(want)], want[torch.isfinite(want)])
         assert torch.isnan(got[~ok]).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_of_small_scales_beside_large_ones(hd):
+    """Codes of many vectors a head enter as fp16: off by 2^-10 of themselves or, where fp16 runs out of bits, by what the
+    header gives of the tile's largest scale.  A key's product and the subtrahend that takes 128 from its codes round at
+    fp16's smallest step, 2^-24, each by half of it, of what the largest scale makes 2^-9: 2^-15 of that scale."""
+    import os
+    import re
+
+    pkg = _pkg()
+    header = os.path.join(os.path.dirname(os.path.dirname(pkg.__file__)), "include", "memspec_ops.h")
+    with open(header) as fh:
+        stated = 2.0 ** -int(re.search(r"themselves, or by 2\^-(\d+) of the", fh.read()).group(1))
+    scales = torch.linspace(0, 1, 400, device=DEV).double().mul(6).sub(18).exp2().float()      # 2^-18 to 2^-12 of the largest
+    n = len(scales)
+    v = torch.zeros(n, 1, 2, hd, dtype=torch.int8, device=DEV)
+    v[:, 0, 0] = torch.randint(-127, 128, (n, hd), device=DEV, generator=_gen(4), dtype=torch.int8)
+    v_scale = torch.ones(n, 1, 2, device=DEV)
+    v_scale[:, 0, 0] = scales
+    cache = pkg.KVCache(torch.zeros_like(v), v, torch.ones_like(v_scale), v_scale)
+    # 17 heads a row, one row a sequence, which weighs both keys alike: half of the first's value
+    starts, lens = _i32(*range(n + 1)), _i32(*[2] * n)
+    got = pkg.op_attention(torch.zeros(n, 17, hd, device=DEV, dtype=torch.bfloat16), cache, starts, lens, max_rows=1)
+    want = 0.5 * v[:, :, 0].double() * scales.double()[:, None, None]
+    bound = (2.0 ** -8 + 2.0 ** -10) * want.abs() + 0.5 * stated
+    assert ((got.double() - want).abs() <= bound).all(), f"{((got.double() - want).abs() / bound).max():.2f} of the bound"
