@@ -288,7 +288,8 @@ typedef struct memspec_attention {
   const int32_t* tree_dev;      /* [rows] or NULL */
   const memspec_kv* prefix;     /* or NULL: its sequence 0 is before every sequence's positions */
   int32_t prefix_len;           /* 0..prefix->max_pos */
-  int32_t max_rows;             /* of one sequence: what the call is laid out for (1..rows) */
+  int32_t max_rows;             /* of one sequence: what the call is laid out for (1..rows; rows of many
+                                   short sequences take up to twice the time if it is rows) */
 } memspec_attention;
 
 /* Scratch bytes of memspec_op_attention.  Errors: INVALID_ARG. */

@@ -15,10 +15,15 @@ namespace memspec {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kTilesUnit = TileUnits::kUnit;
-// Up to so many vectors per head of k and v: attn_rows.cu, in units of 8 or 16; more: attn_tiles.cu.  16 sequences of 2048
-// positions, 8 heads of k and v, bf16 and codes, attn_rows.cu / attn_tiles.cu: 8 vectors 27.9 / 33.0 and 19.3 / 37.7 us, 16:
-// 29.5 / 33.4 and 28.8 / 37.8, 24: 44.2 / 34.2 and 46.0 / 38.0.  Units of 16 for 4 vectors: 64 sequences of 16384 codes
-// 590 us for 321 (what 8 vectors more cost is all lost).
+// Up to so many vectors per head of k and v: attn_rows.cu, in units of 8 or 16; more: attn_tiles.cu.  bf16 and codes, caches
+// cold, attn_rows.cu / attn_tiles.cu, us:
+//                                           8 vectors                16                       24
+//   16 sequences of 2048, 8 heads of 128    28.0 / 33.3, 21.4 / 39.2  29.3 / 33.2, 33.9 / 39.0  44.8 / 34.4, 50.6 / 39.6
+//   64 of 512, 8 heads of 128               32.8 / 36.0, 24.6 / 42.2  38.4 / 40.2, 39.0 / 46.9  54.8 / 44.0, 61.2 / 52.2
+//   one of 16384, 8 heads of 128            21.2 / 30.5, 18.5 / 32.5  23.0 / 27.7, 25.6 / 31.0  24.4 / 31.0, 31.9 / 33.9
+//   16 of 2048, 4 heads of 64               13.5 / 19.3, 12.6 / 21.2  14.7 / 18.5, 14.1 / 20.9  18.7 / 19.3, 18.9 / 21.7
+// At 24 it is the keys that decide (two units read them twice), which the host does not know; attn_tiles.cu loses
+// the least there.  Units of 16 for 4 vectors: 64 sequences of 16384 codes 590 us for 315 (what 8 vectors more cost is all lost).
 constexpr int kRowsVectors = 16;
 
 // Where a vector's records of a part are.
@@ -221,9 +226,9 @@ Layout lay_out(const memspec_batch* b, const memspec_kv* kv, const memspec_atten
     Launch x = launch(p->prefix, static_cast<long long>(b->rows) * group);
     x.prefix = true;
     if (x.tiles && l.launch[0].tiles && x.codes == l.launch[0].codes) {
-      // one launch of attn_tiles.cu for both (16 x 9 rows behind 8192 positions, 300 of their own: 41.6 us, two launches
-      // 44.5).  Few own vectors stay attn_rows.cu's, and the prefix's launch does not wait for theirs (64 rows behind
-      // 32768 codes, up to 1024 of their own: 68.5, waiting 70.6, all in one launch 74.4)
+      // one launch of attn_tiles.cu for both (16 x 9 rows behind 8192 positions, 300 of their own: 40.0 us, two launches
+      // 44.8).  Few own vectors stay attn_rows.cu's, and the prefix's launch does not wait for theirs (64 rows behind
+      // 32768 codes, up to 1024 of their own: 73.1, waiting 75.2, all in one launch 83.7)
       x.own = true;
       l.launch[0] = x;
     } else {

@@ -275,7 +275,8 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t w) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 // Query vectors as fp16, for the products with codes: each times the power of two that brings its largest value
-// near 2^10, where fp16 holds all bits of bf16 (what falls off is below 2^-34 of the vector's largest).
+// near 2^10, where fp16 holds all bits of bf16 (what falls off is below 2^-34 of the vector's largest; of one below 2^-110,
+// which is left smaller, below 2^-144).
 // Here of the vector of which each of LANES neighbours has eight values; the whole warp calls it.
 template <int LANES>
 __device__ __forceinline__ int exponent_of_lanes(const uint4& x) {
@@ -312,10 +313,11 @@ cudaError_t launch_attn_rows(int hd, bool codes, int nt, const ListArgs& a, cuda
 constexpr int kTilesCtas = 152;
 cudaError_t launch_attn_tiles(int hd, bool codes, const ListArgs& a, cudaLaunchConfig_t cfg);   // InvalidValue: no tensor map
 // In attn_tiles.cu a tile of up to 128 vectors takes 1.1 us (codes 1.5), of more 1.9 (2.4); a further stretch in a CTA 2.6
-// us, where it is cut as well 5 (2.4, 4.2), of more vectors 5.3 (7.5).  16 x 9 rows over codes, 256 rows, 16 x 9 rows
-// behind 8192: with these weights 37.7, 41.2, 40.6 us; tiles 1 and 2, starts 3 and 5: 38.5, 42.3, 43.4; 2 and 4: 37.3, 42.6,
-// 46.9.  In attn_rows.cu a tile takes 0.5 us and a start of 2 of them measures best: one row of 32 heads 11.6 us (0: 13.2,
-// 4: 11.7), 5 rows over codes 12.7 (14.8, 12.9).
+// us, where it is cut as well 5 (2.4, 4.2), of more vectors 5.3 (7.5).  One set of weights serves both types: 256 rows over
+// 4355 positions, 16 x 9 rows behind 8192, 16 x 9 rows over codes, caches cold, 35.0, 40.0, 41.9 us; tiles of 1 and 2 with starts of
+// 3 and 5: 36.1, 40.1, 41.7; starts of 2 and 4: 36.4, 44.1, 41.5.  In attn_rows.cu a tile takes 0.5 us; with a start of 2 of
+// them one row of 32 heads over 2048 takes 12.9 us (0: 14.1, 4: 12.8), 5 rows over codes 13.4 (15.0, 13.1), 16 rows over codes 20.9
+// (21.5, 21.9).
 typedef Cut<256, 3, 8, 5, 16> TileUnits;
 template <int VT>
 using RowUnits = Cut<VT, 1, 2, 0, 0>;

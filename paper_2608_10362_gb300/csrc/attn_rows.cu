@@ -7,12 +7,12 @@
 // tiles of 128 keys, one after another, are split evenly over the CTAs (whatever the lengths
 // are; every CTA works its share out from the lengths itself), a warp takes 16 keys at a time
 // through a cp.async ring of its own.  What a unit's CTAs found is joined by a second launch.
-// 64 sequences of up to 32768 positions, 8 heads of codes: 270 us, 6.7 TB/s (the measured copy's 6.8); one row of
-// 32 heads over 2048 positions 11.7 us of which 5 are reading, the others two launches' beginnings and the join.
+// 64 sequences of up to 32768 positions, 8 heads of codes: 267 us, 6.8 TB/s (the measured copy's 6.8); one row of
+// 32 heads over 2048 positions 12.7 us of which 5 are reading, the others two launches' beginnings and the join.  The form for
+// 16 vectors of 128 over codes spills 88 bytes a thread at two CTAs an SM.
 //
 // Scores are kept in units of log2: z = log2(e) scale q.k.  The running maximum m of a vector is
-// taken again only when a score passes it by more than 2^14, so that O is rarely rescaled; it
-// is set 2^6 below the largest, so that weights in fp16 stay clear of its small end.
+// taken again only when a score passes what Weights allows, so that O is rarely rescaled.
 // Codes: exact in fp16 (1024 + 128 + code by one byte permutation, less 1152).  K's scale
 // multiplies the score, V's is added to it as a logarithm: weights are w' = p * scale_v with a
 // maximum of their own kind, and the sum of p is that of w' / scale_v; so no range of scales

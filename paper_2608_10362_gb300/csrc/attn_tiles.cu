@@ -25,9 +25,10 @@
 //
 // What bounds it: a tile for 256 vectors takes 1.9 us of bf16, of which the MMAs' part is 1.3 (S in steps of 64 keys
 // reads its operands from shared memory for 48 clocks per 32 of arithmetic), and 2.4 of codes, where converting and the
-// softmax share the SM's issue.  64 rows of 32 heads, 8 of k and v, over 262144 positions: 221 us, 1.25 PFLOP/s, codes
-// 258.  At ordinary lengths it is what comes before and after: 6 us to the first S, 2 to write the records, 4 to 6 for
-// the join (the same rows over 8192 positions 24 us, of which 6.5 are tiles).
+// softmax share the SM's issue.  64 rows of 32 heads, 8 of k and v, over 262144 positions: 219 us, 1.26 PFLOP/s, codes
+// 256.  At ordinary lengths it is what comes before and after: 6 us to the first S, 2 to write the records, 4 to 6 for
+// the join (the same rows over 8192 positions, caches cold, 26.5 us, of which 6.5 are tiles).  Registers are full: three of
+// the four forms spill 12 to 32 bytes a thread.
 //
 // Roles (warps): 0-3, 4-7 softmax; copies, 4, or 8 of codes; two with the MMAs of a warpgroup each;
 // one for Q; one for which units these are.  Every wait is bounded, those of a role's warps for one another too (see

@@ -218,7 +218,8 @@ def op_attention(q: torch.Tensor, cache: KVCache, starts: torch.Tensor, lens: to
     those before the sequence's rows and, of the rows', those whose bit is set.  `prefix` is a cache
     whose first sequence, up to prefix_len (default: all of it), is before every sequence's slots; it is
     read once for the whole batch.  scale: of q . k, 1 / sqrt(head_dim) by default; max_rows: the
-    most rows that a sequence has (default: all rows; it chooses the kernel, nothing else).
+    most rows that a sequence has (default: all rows).  It chooses the kernel, and with it roundings; name it for a batch
+    of short sequences, which the kernel for many rows serves at up to twice the time.
     ``scratch`` (any content) of memspec_op_attention_scratch_bytes bytes saves an allocation."""
     lib = _lib.load()
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
