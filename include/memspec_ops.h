@@ -261,7 +261,8 @@ typedef struct memspec_append {
  * x / sqrt(mean(x^2) + eps) * gain, then the pairs (i, i + head_dim/2) are turned by
  * the angles of position prefix_len + lens[b] - n + offset (a draft tree's row: its
  * depth).  q is rounded to bf16; k and v to bf16, or to codes rint(x / s) with
- * s = max(max|x|, 127 * 2^-64) / 127 over the vector.  Arithmetic is fp32.  A row
+ * s = max(max|x|, 127 * 2^-64) / 127 over the vector.  Arithmetic is fp32,
+ * a norm's squares and their mean too.  A row
  * whose slot or position (where there is a table) is out of range leaves the cache
  * as it was, and its q is 0.  A vector with an infinity or a NaN is not finite when
  * it is read, others are not affected.  The cache's vectors must not overlap, nor
